@@ -18,7 +18,8 @@ The keys of a case:
   rec:     gate (the output gate is there), packed (v, f and o are column
            blocks of one projection's output [n, L, 2C or 3C]), state (an
            initial state comes in, and in the backward pass a gradient of the
-           last state)
+           last state), keep (a forward pass in training, which also returns
+           the states before the steps 0, 128, 256, ... for the backward pass)
   drop:    p, residual (y = residual + dropout(x)), call (the call's number,
            which may pass 32 bits)
 
@@ -27,7 +28,8 @@ Group norm over a series of T steps, group g of C / groups channels:
     (x - m)^2 there, r = 1 / sqrt(s + eps)
     z = (x - m) r w_c + b_c,   y = act(z);   m = r = 0 where T = 0
 Recurrence, with S the logistic function:
-    h_t = S(f_t) h_{t-1} + (1 - S(f_t)) v_t,   y_t = S(o_t) h_t or h_t
+    h_t = S(f_t) h_{t-1} + (1 - S(f_t)) v_t,   y_t = S(o_t) h_t or h_t;
+    steps past a series' length leave h as it is
 Dropout: Philox4x32-10 (Salmon, Moraes, Dror and Shaw 2011) with the key
 (seed low, seed high) and the counter (i / 8 low, i / 8 high, call low, call
 high) gives eight 16-bit numbers for the elements 8 (i / 8) + 0..7, low halves
@@ -43,6 +45,7 @@ import torch
 own = False
 
 EPS = 1e-5
+EVERY = 128        # steps between the states that training keeps
 LARGEST = 1.54e9   # bytes of the largest listed case
 TYPES = {"float32": torch.float32, "bfloat16": torch.bfloat16, "float16": torch.float16}
 
@@ -51,8 +54,8 @@ def _norm(op, n, L, C, groups, dtype, act, ragged=False):
     return dict(op=op, n=n, L=L, C=C, groups=groups, dtype=dtype, act=act, ragged=ragged)
 
 
-def _rec(op, n, L, C, dtype, gate, packed=False, state=False, ragged=False):
-    return dict(op=op, n=n, L=L, C=C, dtype=dtype, gate=gate, packed=packed, state=state, ragged=ragged)
+def _rec(op, n, L, C, dtype, gate, packed=False, state=False, ragged=False, keep=False):
+    return dict(op=op, n=n, L=L, C=C, dtype=dtype, gate=gate, packed=packed, state=state, ragged=ragged, keep=keep)
 
 
 def _drop(op, n, L, C, dtype, p, residual=False, call=0):
@@ -71,8 +74,8 @@ def listed():
         dict(_norm("norm_back", 1000, 1000, 256, 16, "bfloat16", "silu"), name="norm_back"),
         # one new step for every stream of a service
         dict(_rec("rec_step", 64, 1, 512, "bfloat16", gate=True, packed=True, state=True), name="rec_step"),
-        # ragged series through an odd number of channels
-        dict(_rec("rec", 777, 129, 331, "float16", gate=True, ragged=True), name="rec_ragged"),
+        # ragged series through an odd number of channels, in training
+        dict(_rec("rec", 777, 129, 331, "float16", gate=True, ragged=True, keep=True), name="rec_ragged"),
         # few long recordings: the time axis is all there is to split
         dict(_rec("rec", 4, 16384, 256, "bfloat16", gate=False, state=True), name="rec_few_long"),
         # an ordinary training batch, the gates from one projection
@@ -108,7 +111,8 @@ def draw(rng):
         elif op == "rec_step":
             case = _rec(op, log_int(1, 4000), 1, C, dtype, rng.random() < 0.5, rng.random() < 0.5, True)
         elif op in ("rec", "rec_back"):
-            case = _rec(op, n, L, C, dtype, rng.random() < 0.5, rng.random() < 0.5, rng.random() < 0.5, ragged)
+            case = _rec(op, n, L, C, dtype, rng.random() < 0.5, rng.random() < 0.5, rng.random() < 0.5, ragged,
+                        op == "rec" and rng.random() < 0.5)
         else:
             case = _drop(op, n, L, C, dtype, round(rng.uniform(0.01, 0.9), 4),
                          op == "drop" and rng.random() < 0.5, rng.randrange(1 << 36))
@@ -176,6 +180,8 @@ def prepare(case, seed):
             o = _blank(normal(n, L, C), s["lengths"]) if case["gate"] else None
         s.update(v=v, f=f, o=o, h0=normal(n, C, dtype=torch.float32) if case["state"] else None)
         if op == "rec_back":
+            # the states that the forward pass kept
+            s.update(states=_plain_rec(dict(s, case=dict(case, keep=True)))["states"])
             s.update(dy=_blank(normal(n, L, C), s["lengths"]),
                      dh_last=normal(n, C, dtype=torch.float32) if case["state"] else None, out=None)
             if case["packed"]:   # the gradients go where the projection's gradient is wanted
@@ -304,7 +310,11 @@ def _plain_rec(s):
     live, a, keep, v, so = _gates(s)
     h = _plain_states(a, keep * v, s["h0"])
     y = h if so is None else h * so
-    return dict(y=_own_steps(y, live).to(s["v"].dtype), h_last=h[:, -1].clone())
+    out = dict(y=_own_steps(y, live).to(s["v"].dtype), h_last=h[:, -1].clone())
+    if s["case"]["keep"]:
+        first = torch.zeros_like(h[:, :1]) if s["h0"] is None else s["h0"][:, None]
+        out["states"] = torch.cat([first, h[:, EVERY - 1:-1:EVERY]], dim=1)
+    return out
 
 
 def _plain_rec_back(s):
@@ -389,10 +399,11 @@ def run(s):
             activation=case["act"], lengths=s["lengths"])
         return dict(dx=dx, dweight=dweight, dbias=dbias)
     if op == "rec":
-        y, h_last = sequence.recurrence(s["v"], s["f"], s["o"], h0=s["h0"], lengths=s["lengths"])
-        return dict(y=y, h_last=h_last)
+        y, h_last, states = sequence.recurrence(s["v"], s["f"], s["o"], h0=s["h0"], lengths=s["lengths"],
+                                                keep_states=case["keep"])
+        return dict(y=y, h_last=h_last, states=states) if case["keep"] else dict(y=y, h_last=h_last)
     if op == "rec_back":
-        dv, df, do, dh0 = sequence.recurrence_backward(s["dy"], s["v"], s["f"], s["o"], h0=s["h0"],
+        dv, df, do, dh0 = sequence.recurrence_backward(s["dy"], s["v"], s["f"], s["states"], s["o"],
                                                        dh_last=s["dh_last"], lengths=s["lengths"], out=s["out"])
         out = dict(dv=dv, df=df, dh0=dh0)
         return out if do is None else dict(out, do=do)
@@ -419,10 +430,10 @@ def work(case):
         small = (8 if op == "norm" else 16) * C + 8 * n * case["groups"]
     elif op in ("rec", "rec_step"):
         reads, writes, flops = (3, 1, 10) if case["gate"] else (2, 1, 7)
-        small = 4 * (2 if case["state"] else 1) * n * C
+        small = 4 * ((2 if case["state"] else 1) + (-(-L // EVERY) if case["keep"] else 0)) * n * C
     elif op == "rec_back":
         reads, writes, flops = (4, 3, 26) if case["gate"] else (3, 2, 18)
-        small = 4 * (3 if case["state"] else 1) * n * C
+        small = 4 * ((2 if case["state"] else 1) + -(-L // EVERY)) * n * C
     else:
         reads, writes, flops, small = (2 if case["residual"] else 1), 1, 15, 0
     return dict(bytes=int((reads * live + writes * whole) * size + small), flops=int(flops * live))
@@ -520,7 +531,10 @@ def _exact_rec(s):
         y = y * _logistic(s["o"])
     if s["lengths"] is not None:
         y = y.masked_fill((torch.arange(L, device=y.device)[None, :] >= s["lengths"][:, None])[:, :, None], 0.0)
-    return dict(y=y, h_last=states[L].clone())
+    out = dict(y=y, h_last=states[L].clone())
+    if s["case"]["keep"]:
+        out["states"] = states[0:L:EVERY].transpose(0, 1).contiguous()
+    return out
 
 
 def _exact_rec_back(s):
