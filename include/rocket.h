@@ -527,6 +527,183 @@ void rocket_minirocket_free(rocket_minirocket_params *p);
 rocket_status rocket_minirocket_plan_create(const rocket_minirocket_params *m, uint32_t flags,
                                             rocket_plan **out);
 
+/*
+ * Sequence operators: what a trained head over ROCKET features runs.  The
+ * transform gives a feature row for every window of a series, so a long
+ * series is a sequence of steps (windows, or samples) with channels
+ * (features), channels last: [n, steps, channels].
+ *
+ * Rules for the operators below, beside those at the top of this file:
+ *   - Sequences are caller-owned DEVICE memory on the current HIP device, of
+ *     one type per call (rocket_dtype).  Channels are contiguous; series and
+ *     steps have strides of their own, so a block of columns of a wider matrix
+ *     is a sequence as it stands.  Addresses need the alignment of an element
+ *     only.  Sums, statistics, weights, states and their gradients are fp32;
+ *     results of 16-bit types are rounded once, to nearest even.
+ *   - lengths (DEVICE, int32 [n], or NULL: every series has all its steps):
+ *     the steps of each series, taken into [0, steps].  Steps past a series'
+ *     length are not read (they may hold anything), and results there are 0.
+ *   - Values may be infinite or NaN; they give what the formulas give.
+ *   - n, steps and the series' lengths may be 0.
+ *   - An output may be one of the inputs of its own shape, type and strides;
+ *     operands must not overlap otherwise.
+ *   - Results do not change from call to call, nor with the alignment.
+ *   - No device memory is allocated.  A workspace is caller-owned DEVICE memory
+ *     of the size the query gives for the same shape, 8-byte aligned, and free
+ *     again when the call's work on hip_stream is done; nothing in it needs
+ *     clearing.  Calls may be captured into HIP graphs.
+ */
+typedef enum {
+    ROCKET_FLOAT32 = 0,
+    ROCKET_BFLOAT16 = 1,
+    ROCKET_FLOAT16 = 2
+} rocket_dtype;
+
+typedef enum {
+    ROCKET_ACT_NONE = 0,
+    ROCKET_ACT_RELU = 1, /* max(z, 0); slope 0 at 0 */
+    ROCKET_ACT_SILU = 2, /* z S(z), S the logistic function */
+    ROCKET_ACT_GELU = 3  /* z (1 + erf(z / sqrt 2)) / 2 */
+} rocket_activation;
+
+/* The shape of a call's sequences: n and steps in [0, 2^31), channels in
+ * [1, 2^24], n * steps * channels at most 2^56. */
+typedef struct {
+    int64_t n;
+    int64_t steps;
+    int64_t channels;
+    int32_t dtype;          /* rocket_dtype */
+    const int32_t *lengths; /* DEVICE [n], or NULL */
+} rocket_sequence_shape;
+
+/* One sequence: element (i, t, c) is data[i * series_stride + t * step_stride + c].
+ * Strides count elements and are >= 0; an input may repeat rows (stride 0), the
+ * rows of an output must not overlap. */
+typedef struct {
+    void *data;
+    int64_t series_stride;
+    int64_t step_stride;
+} rocket_sequence;
+
+/*
+ * Group norm with an activation.  Channels form `groups` groups of
+ * channels / groups neighbours; over the T steps of series i and the channels
+ * of group g (N = T channels / groups elements):
+ *     m = sum x / N,  s = sum (x - m)^2 / N,  r = 1 / sqrt(s + eps)
+ *     y = act((x - m) r weight_c + bias_c)
+ *   weight, bias  DEVICE fp32 [channels], or NULL: 1 and 0
+ *   eps           finite, >= 0
+ *   activation    rocket_activation
+ *   mean, rstd    DEVICE fp32 [n, groups]: m and r, 0 and 0 for a series of no
+ *                 steps; the backward pass reads them
+ * The variance is the mean of squares about the mean (two passes over values
+ * on the chip, merged over chunks), so a level far above the spread costs no
+ * more digits than m itself loses.
+ * Errors: ROCKET_ERR_INVALID_ARG (a NULL pointer, a shape, view, stride, type,
+ *         activation or eps outside the above, groups that do not divide
+ *         channels, a workspace too small); ROCKET_ERR_HIP.
+ */
+rocket_status rocket_group_norm_forward(const rocket_sequence_shape *shape, int32_t groups,
+                                        const rocket_sequence *x, const float *weight, const float *bias,
+                                        float eps, int32_t activation, const rocket_sequence *y, float *mean,
+                                        float *rstd, void *workspace, int64_t workspace_bytes,
+                                        void *hip_stream);
+
+/*
+ * Its gradient: from dy, x and the forward pass's mean and rstd,
+ *     xh = (x - m) r,  dz = dy act'(xh weight_c + bias_c),  g = dz weight_c
+ *     dx = r (g - mean(g) - xh mean(g xh)),  means over the group's N elements
+ *     dweight_c = sum dz xh,  dbias_c = sum dz, over all series and steps
+ *   dweight, dbias  DEVICE fp32 [channels], or NULL: not wanted
+ * dx may be dy or x.  Errors as rocket_group_norm_forward.
+ */
+rocket_status rocket_group_norm_backward(const rocket_sequence_shape *shape, int32_t groups,
+                                         const rocket_sequence *dy, const rocket_sequence *x,
+                                         const float *weight, const float *bias, int32_t activation,
+                                         const float *mean, const float *rstd, const rocket_sequence *dx,
+                                         float *dweight, float *dbias, void *workspace,
+                                         int64_t workspace_bytes, void *hip_stream);
+
+/* Workspace of the forward (backward = 0) or backward pass for this shape
+ * (its lengths and the data are not looked at).  Host only.
+ * Errors: ROCKET_ERR_INVALID_ARG (bytes NULL, a shape or groups as above). */
+rocket_status rocket_group_norm_workspace(const rocket_sequence_shape *shape, int32_t groups, int32_t backward,
+                                          int64_t *bytes);
+
+/*
+ * Gated linear recurrence along the steps, channel by channel; S is the
+ * logistic function:
+ *     h_t = S(f_t) h_{t-1} + (1 - S(f_t)) v_t,   y_t = S(o_t) h_t
+ * (the pooling of quasi-recurrent networks: Bradbury, Merity, Xiong and
+ * Socher 2017).  Steps past a series' length leave h as it is.
+ *   o       output gate, or NULL: y_t = h_t
+ *   h0      DEVICE fp32 [n, channels], the state before step 0, or NULL: 0
+ *   h_last  DEVICE fp32 [n, channels]: the state after the last step; may be
+ *           h0
+ *   states  DEVICE fp32 [n, ceil(steps / ROCKET_RECURRENCE_EVERY), channels],
+ *           or NULL: the states before the steps 0, 128, 256, ..., which the
+ *           backward pass starts from
+ * States and inputs that are infinite may give NaN where the step-by-step
+ * formula gives an infinity (0 times an infinity in a product of gates).
+ * Errors: ROCKET_ERR_INVALID_ARG (as above); ROCKET_ERR_HIP.
+ */
+#define ROCKET_RECURRENCE_EVERY 128
+rocket_status rocket_recurrence_forward(const rocket_sequence_shape *shape, const rocket_sequence *v,
+                                        const rocket_sequence *f, const rocket_sequence *o, const float *h0,
+                                        const rocket_sequence *y, float *h_last, float *states,
+                                        void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Its gradient: from dy, the inputs, the kept states and the gradient of the
+ * last state (dh_last, DEVICE fp32 [n, channels], or NULL: 0), with a = S(f):
+ *     dh_t = dy_t S(o_t) + a_{t+1} dh_{t+1}   (dh_last after the last step)
+ *     dv = dh (1 - a),  df = dh (h_{t-1} - v) a (1 - a),  dO = dy h S(o) (1 - S(o))
+ *   dO    given where o is, NULL where o is NULL
+ *   dh0   DEVICE fp32 [n, channels]: the gradient of the first state
+ *         (dh_last for a series of no steps); may be dh_last
+ * dv, df and dO may be blocks of one matrix, the gradient of a projection.
+ * Errors as rocket_recurrence_forward.
+ */
+rocket_status rocket_recurrence_backward(const rocket_sequence_shape *shape, const rocket_sequence *dy,
+                                         const rocket_sequence *v, const rocket_sequence *f,
+                                         const rocket_sequence *o, const float *states, const float *dh_last,
+                                         const rocket_sequence *dv, const rocket_sequence *df,
+                                         const rocket_sequence *dO, float *dh0, void *workspace,
+                                         int64_t workspace_bytes, void *hip_stream);
+
+/* Workspace of either pass for this shape.  Host only.
+ * Errors: ROCKET_ERR_INVALID_ARG (bytes NULL, a shape outside the above). */
+rocket_status rocket_recurrence_workspace(const rocket_sequence_shape *shape, int64_t *bytes);
+
+/*
+ * One step of every series, for serving: v, f, o (or NULL) and y are
+ * [n, channels] with row strides in elements, h_in and h_out DEVICE fp32
+ * [n, channels] (h_out may be h_in).  No workspace.
+ * Errors as rocket_recurrence_forward.
+ */
+rocket_status rocket_recurrence_step(int64_t n, int64_t channels, int32_t dtype, const void *v,
+                                     int64_t v_stride, const void *f, int64_t f_stride, const void *o,
+                                     int64_t o_stride, const float *h_in, float *h_out, void *y,
+                                     int64_t y_stride, void *hip_stream);
+
+/*
+ * Dropout whose mask is never stored.  x, residual (or NULL) and y are
+ * [rows, cols] with row strides in elements; element i = row * cols + col:
+ *     y = residual + (u_i < D ? 0 : x 65536 / (65536 - D)),   D = floor(65536 p + 1/2)
+ * u_i: the 128 bits of block i / 8 of Philox4x32-10 (Salmon, Moraes, Dror and
+ * Shaw 2011), key (low, high half of seed), counter (low, high half of i / 8,
+ * low, high half of call), are the numbers u of elements 8 (i / 8) + 0 .. 7, two
+ * in each word, the low half first.  p in [0, 1]; p = 1 drops everything.
+ * A dropped element does not pass on what x holds there, NaN and infinities
+ * included.  Calls with another seed or call number draw other masks.
+ * The gradient is the same call on dy with residual NULL (residual's own
+ * gradient is dy).  y may be x or residual.  rows * cols at most 2^41.
+ * Errors: ROCKET_ERR_INVALID_ARG; ROCKET_ERR_HIP.
+ */
+rocket_status rocket_dropout(const void *x, const void *residual, void *y, int64_t rows, int64_t cols,
+                             int64_t x_stride, int64_t residual_stride, int64_t y_stride, int32_t dtype,
+                             double p, uint64_t seed, uint64_t call, void *hip_stream);
+
 /* Static, human-readable name of a status code ("unknown status" otherwise). */
 const char *rocket_status_string(rocket_status s);
 

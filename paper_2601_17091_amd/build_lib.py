@@ -18,7 +18,11 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "librocket.so")
 CHECKED_LIB = os.path.join(HERE, "librocket_checked.so")
-SOURCES = ["transform.hip", "split.hip", "plan.cpp", "plan_split.cpp", "generate.cpp", "minirocket.cpp"]
+SOURCES = ["transform.hip", "split.hip", "plan.cpp", "plan_split.cpp", "generate.cpp", "minirocket.cpp",
+           "group_norm.hip", "recurrence.hip", "dropout.hip"]
+# sources whose device code keeps IEEE NaN semantics: their operands may hold
+# NaN (the transform's series are finite)
+NAN_SOURCES = ("group_norm.hip", "recurrence.hip", "dropout.hip")
 ARCH = "gfx950"
 
 
@@ -32,7 +36,7 @@ def hipcc() -> str:
     return found
 
 
-def compile_flags() -> list[str]:
+def compile_flags(src: str = "transform.hip") -> list[str]:
     return [
         "--offload-arch=" + ARCH,
         "-O3",
@@ -44,13 +48,14 @@ def compile_flags() -> list[str]:
         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
         # host arithmetic (the generator) exactly as written
         "-ffp-contract=off",
-        # device code only: inputs are finite, so fmaxf is a plain v_max_f32
-        # without NaN canonicalisation; host code (generator, planner,
-        # MINIROCKET fit) keeps IEEE NaN semantics
+    ] + ([] if src in NAN_SOURCES else [
+        # device code of the transform only: inputs are finite, so fmaxf is a
+        # plain v_max_f32 without NaN canonicalisation; host code (generator,
+        # planner, MINIROCKET fit) keeps IEEE NaN semantics
         "-Xarch_device", "-fno-honor-nans",
         # MFMA results straight into VGPRs (no accumulator-register copies)
         "-mllvm", "-amdgpu-mfma-vgpr-form",
-    ]
+    ])
 
 
 def build(verbose: bool = False) -> str:
@@ -67,7 +72,7 @@ def build(verbose: bool = False) -> str:
                 objs[True].append(os.path.join(HERE, "_build", src + ".o"))
                 continue
             obj = os.path.join(HERE, "_build", src + (".checked.o" if checked else ".o"))
-            cmd = [hipcc()] + compile_flags() + (["-DROCKET_CHECKED=1"] if checked else []) + \
+            cmd = [hipcc()] + compile_flags(src) + (["-DROCKET_CHECKED=1"] if checked else []) + \
                 ["-c", os.path.join(CSRC, src), "-o", obj]
             jobs.append(cmd)
             objs[checked].append(obj)

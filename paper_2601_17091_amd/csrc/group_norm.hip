@@ -1,0 +1,709 @@
+// Group norm with an activation over sequences [n, L, C], channels last.
+//
+// A series of T steps, a group of C / G channels, N = T C / G elements:
+//   m = sum x / N,  s = sum (x - m)^2 / N,  r = 1 / sqrt(s + eps)
+//   xh = (x - m) r,  z = xh w_c + b_c,  y = act(z)
+// and backwards, with dz = dy act'(z) and g = dz w_c,
+//   db_c = sum dz,  dw_c = sum dz xh  (over series and steps)
+//   dx = r (g - mean(g) - xh mean(g xh))  (means over the group's N elements)
+//
+// A workgroup takes a slab: all steps of a few whole groups, at least 128
+// bytes of channels wide.  Where the slab fits its registers it is read once:
+// the sum, then the squares about the mean, then the output come from there
+// (held).  Longer series are cut into chunks of steps: one launch leaves each
+// chunk's mean and squares (or, backwards, its channel sums), a second one
+// merges them in a fixed order and writes the output.  Groups wider than a
+// workgroup's columns are cut along the channels in the same way.  There are
+// no atomics: results do not change from call to call.
+//
+// A thread owns one column of 16 bytes of channels in every `rows`-th step.
+// The last column of a slab is moved back so that it ends with the slab; the
+// channels it shares with its neighbour are computed twice and counted once.
+#include <climits>
+
+#include "sequence.h"
+
+namespace {
+
+using rocket::Elem;
+
+enum Mode { kHeld, kStats, kApply };
+
+struct View {
+    char *p;
+    int64_t ss, ts;  // bytes
+};
+
+struct NormArgs {
+    View x, dy, out;   // out: y, or dx
+    int64_t n, L;
+    int32_t C, G, width;       // width: channels of a group
+    int32_t slabs, parts;      // slabs per series; parts > 1: slabs per group
+    int32_t cols, rows;        // columns of a slab; steps a workgroup passes at once
+    int32_t chunks;            // of steps
+    int32_t act;
+    float eps;
+    const float *w, *b;        // or null
+    const int32_t *lengths;
+    float *mean, *rstd;        // [n, G]: written forward, read backward
+    float2 *stats;             // forward: [n, G, chunks * parts] (mean, squares)
+    float *sums;               // backward: [rows of sums, 2, C] sums of dz and dz xh
+    int32_t series;            // backward, held: workgroups along the series
+};
+
+// A column's elements: 16 bytes, or one element where a row has fewer.
+template <int DT, bool WIDE>
+struct Pack {
+    typedef uint32_t vec __attribute__((ext_vector_type(4)));
+    static constexpr int kN = 4 * Elem<DT>::kPerWord;
+    vec v;
+    __device__ void load(const char *p) { v = rocket::load_at<vec>(p); }
+    __device__ float get(int e) const { return Elem<DT>::get(v[e / Elem<DT>::kPerWord], e % Elem<DT>::kPerWord); }
+    __device__ static void store(char *p, const float *f) {
+        vec o;
+#pragma unroll
+        for (int k = 0; k < 4; k++) o[k] = Elem<DT>::put(f + k * Elem<DT>::kPerWord);
+        rocket::store_at(p, o);
+    }
+    __device__ void clear() { v = vec{0, 0, 0, 0}; }
+};
+
+template <int DT>
+struct Pack<DT, false> {
+    using raw = typename Elem<DT>::raw;
+    static constexpr int kN = 1;
+    raw v;
+    __device__ void load(const char *p) { v = *(const raw *)p; }
+    __device__ float get(int) const { return Elem<DT>::one(v); }
+    __device__ static void store(char *p, const float *f) { *(raw *)p = Elem<DT>::round(f[0]); }
+    __device__ void clear() { v = 0; }
+};
+
+__device__ inline float activate(float z, int act) {
+    switch (act) {
+    case ROCKET_ACT_RELU: return z < 0.0f ? 0.0f : z;
+    case ROCKET_ACT_SILU: {
+        float s, rest;
+        rocket::logistic(z, s, rest);
+        return z * s;
+    }
+    case ROCKET_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    default: return z;
+    }
+}
+
+__device__ inline float slope(float z, int act) {
+    switch (act) {
+    case ROCKET_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
+    case ROCKET_ACT_SILU: {
+        float s, rest;
+        rocket::logistic(z, s, rest);
+        return s * (1.0f + z * rest);
+    }
+    case ROCKET_ACT_GELU: {
+        float e = rocket::exp_neg_abs(0.5f * z * z);
+        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * e * 0.39894228040143268f;
+    }
+    default: return 1.0f;
+    }
+}
+
+// Where a workgroup and a thread work.
+struct Place {
+    int64_t i;            // series
+    int slab, chunk;
+    int c0, c1, g0, ng;   // the slab's channels and groups
+    int row, col;         // the thread's first step in a pass, its column
+    int c, skip;          // its first channel; leading channels that its neighbour counts
+    bool active;
+};
+
+template <int NT, int VEC>
+__device__ inline void place_thread(const NormArgs &a, Place &p) {
+    if (a.parts == 1) {
+        p.g0 = (int)((int64_t)a.G * p.slab / a.slabs);
+        p.ng = (int)((int64_t)a.G * (p.slab + 1) / a.slabs) - p.g0;
+        p.c0 = p.g0 * a.width;
+        p.c1 = p.c0 + p.ng * a.width;
+    } else {
+        p.g0 = p.slab / a.parts;
+        p.ng = 1;
+        const int part = p.slab % a.parts, base = p.g0 * a.width;
+        p.c0 = base + (int)((int64_t)a.width * part / a.parts);
+        p.c1 = base + (int)((int64_t)a.width * (part + 1) / a.parts);
+    }
+    p.row = threadIdx.x / a.cols;
+    p.col = threadIdx.x - p.row * a.cols;
+    const int nominal = p.c0 + p.col * VEC;
+    p.active = p.row < a.rows && nominal < p.c1;
+    p.c = nominal + VEC <= p.c1 ? nominal : p.c1 - VEC;
+    p.skip = nominal - p.c;
+    if (!p.active) p.c = p.c0, p.skip = 0;
+}
+
+// Shared memory of the sums of a slab.
+template <int NT, int VEC>
+struct Scratch {
+    static constexpr int kMost = (NT < 256 ? NT : 256) * VEC;   // channels of a slab
+    float rows[NT * VEC];                                       // all rows' columns
+    float chan[NT > kMost ? NT : kMost];
+    float group[kMost];
+    float group2[kMost];
+};
+
+// Sums acc over the workgroup's rows: s.chan[part * W + channel], `parts`
+// parts of every channel of the slab.
+template <int NT, int VEC>
+__device__ inline int sum_rows(const NormArgs &a, const Place &p, const float (&acc)[VEC], Scratch<NT, VEC> &s) {
+    const int W = p.c1 - p.c0;
+    __syncthreads();   // rows and chan are free
+    if (p.active) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++)
+            if (e >= p.skip) s.rows[p.row * W + p.c - p.c0 + e] = acc[e];
+    }
+    __syncthreads();
+    const int parts = W < NT ? min(NT / W, a.rows) : 1;
+    const int per = W < NT ? W : NT;
+    const int part = threadIdx.x / per;
+    if (part < parts)
+        for (int ch = threadIdx.x - part * per; ch < W; ch += NT) {
+            float t = 0.0f;
+            for (int r = part; r < a.rows; r += parts) t += s.rows[r * W + ch];
+            s.chan[part * W + ch] = t;
+        }
+    __syncthreads();
+    return parts;
+}
+
+// group[k] = the sum over the slab's channels of group k of scale_c times the
+// channel's parts (scale may be null).
+template <int NT, int VEC>
+__device__ inline void sum_groups(const Place &p, int parts, const float *scale, Scratch<NT, VEC> &s, float *group) {
+    const int W = p.c1 - p.c0, each = W / p.ng;
+    if (each * parts <= 32) {
+        for (int k = threadIdx.x; k < p.ng; k += NT) {
+            float t = 0.0f;
+            for (int ch = k * each; ch < (k + 1) * each; ch++) {
+                float u = 0.0f;
+                for (int q = 0; q < parts; q++) u += s.chan[q * W + ch];
+                t += scale ? scale[p.c0 + ch] * u : u;
+            }
+            group[k] = t;
+        }
+    } else {
+        for (int k = threadIdx.x >> 6; k < p.ng; k += NT >> 6) {
+            float t = 0.0f;
+            for (int ch = k * each + (threadIdx.x & 63); ch < (k + 1) * each; ch += 64) {
+                float u = 0.0f;
+                for (int q = 0; q < parts; q++) u += s.chan[q * W + ch];
+                t += scale ? scale[p.c0 + ch] * u : u;
+            }
+#pragma unroll
+            for (int off = 32; off; off /= 2) t += __shfl_xor(t, off);
+            if ((threadIdx.x & 63) == 0) group[k] = t;
+        }
+    }
+    __syncthreads();
+}
+
+// The steps of chunk k, and how many of them are the series' own.
+__device__ inline int chunk_rows(const NormArgs &a, int64_t T, int chunk, int64_t per, int64_t &first) {
+    first = chunk * per;
+    int64_t left = T - first;
+    return (int)(left < 0 ? 0 : left < per ? left : per);
+}
+
+// Forward.  R: passes over the rows that a thread holds.
+template <int DT, bool WIDE, int NT, int R, int MODE>
+__global__ __launch_bounds__(NT) void norm_kernel(NormArgs a) {
+    using P = Pack<DT, WIDE>;
+    constexpr int VEC = P::kN;
+    __shared__ Scratch<NT, VEC> s;
+    Place p;
+    const int64_t b = blockIdx.x;
+    p.slab = (int)(b % a.slabs);
+    p.chunk = (int)(b / a.slabs % a.chunks);
+    p.i = b / a.slabs / a.chunks;
+    place_thread<NT, VEC>(a, p);
+    const int64_t T = rocket::steps_of(a.lengths, p.i, a.L), per = (int64_t)R * a.rows;
+    int64_t first;
+    const int own = chunk_rows(a, T, p.chunk, per, first);
+
+    P held[R];
+    const char *x = a.x.p + p.i * a.x.ss + first * a.x.ts + (int64_t)p.c * Elem<DT>::kSize;
+#pragma unroll
+    for (int j = 0; j < R; j++) {
+        if (j * a.rows < own) {
+            const int r = p.row + j * a.rows;
+            held[j].load(x + (int64_t)(r < own ? r : own - 1) * a.x.ts);
+        } else {
+            held[j].clear();
+        }
+    }
+    int group_of[VEC];   // within the slab
+#pragma unroll
+    for (int e = 0; e < VEC; e++) group_of[e] = a.parts == 1 ? (p.c + e - p.c0) / a.width : 0;
+
+    const int W = p.c1 - p.c0, each = W / p.ng;
+    if (MODE != kApply) {
+        float acc[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; e++) acc[e] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < R; j++)
+            if (p.row + j * a.rows < own) {
+#pragma unroll
+                for (int e = 0; e < VEC; e++) acc[e] += held[j].get(e);
+            }
+        int parts = sum_rows<NT, VEC>(a, p, acc, s);
+        sum_groups<NT, VEC>(p, parts, nullptr, s, s.group);
+        const float count = (float)own * (float)each;
+        const float inv = own ? 1.0f / count : 0.0f;
+        float m[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; e++) m[e] = s.group[group_of[e]] * inv, acc[e] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < R; j++)
+            if (p.row + j * a.rows < own) {
+#pragma unroll
+                for (int e = 0; e < VEC; e++) {
+                    float d = held[j].get(e) - m[e];
+                    acc[e] = __builtin_fmaf(d, d, acc[e]);
+                }
+            }
+        parts = sum_rows<NT, VEC>(a, p, acc, s);
+        sum_groups<NT, VEC>(p, parts, nullptr, s, s.group2);
+        if (MODE == kStats) {
+            const int K = a.chunks * a.parts, k = p.chunk * a.parts + (a.parts > 1 ? p.slab % a.parts : 0);
+            for (int g = threadIdx.x; g < p.ng; g += NT)
+                a.stats[(p.i * a.G + p.g0 + g) * K + k] = make_float2(s.group[g] * inv, s.group2[g]);
+            return;
+        }
+        for (int g = threadIdx.x; g < p.ng; g += NT) {
+            const float mean = s.group[g] * inv, rstd = own ? 1.0f / sqrtf(s.group2[g] * inv + a.eps) : 0.0f;
+            s.group[g] = mean, s.group2[g] = rstd;
+            a.mean[p.i * a.G + p.g0 + g] = mean;
+            a.rstd[p.i * a.G + p.g0 + g] = rstd;
+        }
+        __syncthreads();
+    } else {
+        // merge the chunks' statistics: N = sum n_k, m = sum n_k m_k / N,
+        // squares = sum (squares_k + n_k (m_k - m)^2)
+        const int K = a.chunks * a.parts;
+        const float inv = T ? 1.0f / ((float)T * (float)a.width) : 0.0f;
+        for (int g = threadIdx.x >> 6; g < p.ng; g += NT >> 6) {
+            const float2 *st = a.stats + (p.i * a.G + p.g0 + g) * K;
+            float mean = 0.0f, sq = 0.0f;
+            for (int pass = 0; pass < 2; pass++) {
+                float t = 0.0f;
+                for (int k = threadIdx.x & 63; k < K; k += 64) {
+                    const int part = k % a.parts;
+                    int64_t f0;
+                    const float rows = (float)chunk_rows(a, T, k / a.parts, per, f0);
+                    const int wide = (int)((int64_t)a.width * (part + 1) / a.parts) -
+                                     (int)((int64_t)a.width * part / a.parts);
+                    const float nk = rows * (float)wide, d = st[k].x - mean;
+                    t += pass ? __builtin_fmaf(nk * d, d, st[k].y) : nk * inv * st[k].x;
+                }
+#pragma unroll
+                for (int off = 32; off; off /= 2) t += __shfl_xor(t, off);
+                if (pass)
+                    sq = t;
+                else
+                    mean = t;
+            }
+            if ((threadIdx.x & 63) == 0) {
+                const float rstd = T ? 1.0f / sqrtf(sq * inv + a.eps) : 0.0f;
+                s.group[g] = mean, s.group2[g] = rstd;
+                if (p.chunk == 0 && (a.parts == 1 || p.slab % a.parts == 0)) {
+                    a.mean[p.i * a.G + p.g0 + g] = mean;
+                    a.rstd[p.i * a.G + p.g0 + g] = rstd;
+                }
+            }
+        }
+        __syncthreads();
+    }
+
+    if (!p.active) return;
+    float m[VEC], sc[VEC], sh[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; e++) {
+        m[e] = s.group[group_of[e]];
+        sc[e] = s.group2[group_of[e]] * (a.w ? a.w[p.c + e] : 1.0f);
+        sh[e] = a.b ? a.b[p.c + e] : 0.0f;
+    }
+    char *out = a.out.p + p.i * a.out.ss + first * a.out.ts + (int64_t)p.c * Elem<DT>::kSize;
+    const int64_t rest = a.L - first;
+#pragma unroll
+    for (int j = 0; j < R; j++) {
+        const int r = p.row + j * a.rows;
+        if (r >= rest) break;
+        float y[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; e++)
+            y[e] = r < own ? activate(__builtin_fmaf(held[j].get(e) - m[e], sc[e], sh[e]), a.act) : 0.0f;
+        P::store(out + (int64_t)r * a.out.ts, y);
+    }
+}
+
+// Backward.  Held: a workgroup goes through the series b, b + a.series, ... and
+// keeps the channel sums over them; kStats leaves the channel sums of a chunk.
+template <int DT, bool WIDE, int NT, int R, int MODE>
+__global__ __launch_bounds__(NT) void norm_back_kernel(NormArgs a) {
+    using P = Pack<DT, WIDE>;
+    constexpr int VEC = P::kN;
+    __shared__ Scratch<NT, VEC> s;
+    __shared__ float total[2][MODE == kHeld ? Scratch<NT, VEC>::kMost : 1];
+    Place p;
+    const int64_t b = blockIdx.x;
+    p.slab = (int)(b % a.slabs);
+    p.chunk = MODE == kHeld ? 0 : (int)(b / a.slabs % a.chunks);
+    const int64_t begin = MODE == kHeld ? b / a.slabs : b / a.slabs / a.chunks;
+    place_thread<NT, VEC>(a, p);
+    const int W = p.c1 - p.c0;
+    const int64_t per = (int64_t)R * a.rows;
+    int group_of[VEC];
+    float w[VEC], bias[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; e++) {
+        group_of[e] = a.parts == 1 ? (p.c + e - p.c0) / a.width : 0;
+        w[e] = a.w ? a.w[p.c + e] : 1.0f;
+        bias[e] = a.b ? a.b[p.c + e] : 0.0f;
+    }
+    if (MODE == kHeld)
+        for (int ch = threadIdx.x; ch < W; ch += NT) total[0][ch] = 0.0f, total[1][ch] = 0.0f;
+
+    for (p.i = begin; p.i < a.n; p.i += MODE == kHeld ? a.series : a.n) {
+        const int64_t T = rocket::steps_of(a.lengths, p.i, a.L);
+        int64_t first;
+        const int own = chunk_rows(a, T, p.chunk, per, first);
+        P hx[R], hg[R];
+        const char *x = a.x.p + p.i * a.x.ss + first * a.x.ts + (int64_t)p.c * Elem<DT>::kSize;
+        const char *dy = a.dy.p + p.i * a.dy.ss + first * a.dy.ts + (int64_t)p.c * Elem<DT>::kSize;
+#pragma unroll
+        for (int j = 0; j < R; j++) {
+            if (j * a.rows < own) {
+                const int r = p.row + j * a.rows, rr = r < own ? r : own - 1;
+                hx[j].load(x + (int64_t)rr * a.x.ts);
+                hg[j].load(dy + (int64_t)rr * a.dy.ts);
+            } else {
+                hx[j].clear();
+                hg[j].clear();
+            }
+        }
+        float m[VEC], rs[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+            m[e] = a.mean[p.i * a.G + p.g0 + group_of[e]];
+            rs[e] = a.rstd[p.i * a.G + p.g0 + group_of[e]];
+        }
+        if (MODE != kApply) {
+            float sd[VEC], sx[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; e++) sd[e] = 0.0f, sx[e] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < R; j++)
+                if (p.row + j * a.rows < own) {
+#pragma unroll
+                    for (int e = 0; e < VEC; e++) {
+                        const float xh = (hx[j].get(e) - m[e]) * rs[e];
+                        const float dz = hg[j].get(e) * slope(xh * w[e] + bias[e], a.act);
+                        sd[e] += dz;
+                        sx[e] = __builtin_fmaf(dz, xh, sx[e]);
+                    }
+                }
+            for (int q = 0; q < 2; q++) {
+                const int parts = q ? sum_rows<NT, VEC>(a, p, sx, s) : sum_rows<NT, VEC>(a, p, sd, s);
+                for (int ch = threadIdx.x; ch < W; ch += NT) {
+                    float t = 0.0f;
+                    for (int k = 0; k < parts; k++) t += s.chan[k * W + ch];
+                    if (MODE == kHeld)
+                        total[q][ch] += t;
+                    else
+                        a.sums[((p.i * a.chunks + p.chunk) * 2 + q) * a.C + p.c0 + ch] = t;
+                }
+                if (MODE == kHeld) sum_groups<NT, VEC>(p, parts, a.w, s, q ? s.group2 : s.group);
+            }
+            if (MODE == kStats) return;
+        } else {
+            // the groups' sums from the chunks' channel sums
+            for (int k = threadIdx.x >> 6; k < 2 * p.ng; k += NT >> 6) {
+                const int q = k & 1, g = k >> 1;
+                float t = 0.0f;
+                for (int ch = threadIdx.x & 63; ch < a.width; ch += 64) {
+                    const int c = (p.g0 + g) * a.width + ch;
+                    float u = 0.0f;
+                    for (int chunk = 0; chunk < a.chunks; chunk++)
+                        u += a.sums[((p.i * a.chunks + chunk) * 2 + q) * a.C + c];
+                    t += a.w ? a.w[c] * u : u;
+                }
+#pragma unroll
+                for (int off = 32; off; off /= 2) t += __shfl_xor(t, off);
+                if ((threadIdx.x & 63) == 0) (q ? s.group2 : s.group)[g] = t;
+            }
+            __syncthreads();
+        }
+        if (p.active) {
+            const float inv = T ? 1.0f / ((float)T * (float)a.width) : 0.0f;
+            float mg[VEC], mx[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; e++) mg[e] = s.group[group_of[e]] * inv, mx[e] = s.group2[group_of[e]] * inv;
+            char *out = a.out.p + p.i * a.out.ss + first * a.out.ts + (int64_t)p.c * Elem<DT>::kSize;
+            const int64_t rest = a.L - first;
+#pragma unroll
+            for (int j = 0; j < R; j++) {
+                const int r = p.row + j * a.rows;
+                if (r >= rest) break;
+                float dx[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; e++) {
+                    const float xh = (hx[j].get(e) - m[e]) * rs[e];
+                    const float g = hg[j].get(e) * slope(xh * w[e] + bias[e], a.act) * w[e];
+                    dx[e] = r < own ? rs[e] * (g - mg[e] - xh * mx[e]) : 0.0f;
+                }
+                P::store(out + (int64_t)r * a.out.ts, dx);
+            }
+        }
+        if (MODE == kHeld) __syncthreads();   // group and group2 are free again
+    }
+    if (MODE == kHeld)
+        for (int q = 0; q < 2; q++)
+            for (int ch = threadIdx.x; ch < W; ch += NT)
+                a.sums[(begin * 2 + q) * a.C + p.c0 + ch] = total[q][ch];
+}
+
+// Rows of channel sums to fewer rows: out[o, q, c] = the sum of in[r, q, c]
+// over rows r of block o.  16 rows of 64 channels at a time.
+__global__ __launch_bounds__(1024) void fold_kernel(const float *in, int64_t rows, int64_t per, int C, float *out0,
+                                                    float *out1, int64_t out_stride) {
+    __shared__ float part[16][64];
+    const int blocks = (C + 63) / 64;
+    const int cb = blockIdx.x % blocks, q = blockIdx.x / blocks & 1;
+    const int64_t o = blockIdx.x / blocks / 2;
+    const int c = cb * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
+    const int64_t end = (o + 1) * per < rows ? (o + 1) * per : rows;
+    float t = 0.0f;
+    if (c < C)
+        for (int64_t r = o * per + k; r < end; r += 16) t += in[(r * 2 + q) * C + c];
+    part[k][threadIdx.x & 63] = t;
+    __syncthreads();
+    if (k == 0 && c < C) {
+        for (int j = 1; j < 16; j++) t += part[j][threadIdx.x & 63];
+        float *out = q ? out1 : out0;
+        if (out) out[o * out_stride + c] = t;
+    }
+}
+
+// How a call is cut.
+struct Cut {
+    bool wide, held;
+    int32_t width, slabs, parts, cols, rows, threads, run, chunks;
+    int32_t series;     // backward, held
+    int64_t grid;
+    int64_t sum_rows;   // backward: rows of channel sums
+    int64_t folded;     // rows after the first fold, 0: one fold is enough
+};
+
+constexpr int kFold = 128;
+
+bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut) {
+    const int size = rocket::elem_size(s->dtype), vec_wide = 16 / size;
+    const int64_t C = s->channels, width = C / groups, L = s->steps > 0 ? s->steps : 1;
+    cut->wide = C >= vec_wide;
+    cut->width = (int32_t)width;
+    const int vec = cut->wide ? vec_wide : 1;
+    const int64_t most = 256 * (int64_t)vec;   // channels of a slab
+    // A slab is at least 128 bytes wide, and wider while that leaves
+    // workgroups for the whole chip and the slab is small.
+    int64_t per = 1;
+    cut->parts = 1;
+    if (width > most) {
+        cut->parts = (int32_t)((width + most - 1) / most);
+        cut->slabs = (int32_t)(groups * cut->parts);
+        int64_t part = (width + cut->parts - 1) / cut->parts;
+        cut->cols = (int32_t)((part + vec - 1) / vec);
+    } else {
+        while (per < groups && per * width * size < 128) per++;
+        while (per * 2 <= groups && per * 2 * width <= most && per * width * size * L < (16 << 10) &&
+               s->n * ((groups + 2 * per - 1) / (2 * per)) >= 1024)
+            per *= 2;
+        cut->slabs = (int32_t)((groups + per - 1) / per);
+        per = (groups + cut->slabs - 1) / cut->slabs;   // the most groups a slab gets
+        cut->cols = (int32_t)((per * width + vec - 1) / vec);
+    }
+    // Held where the slab fits: the smallest workgroup that holds it.
+    static const int kSizes[5][2] = {{64, 4}, {256, 4}, {256, 16}, {512, 16}, {1024, 16}};
+    static const int kBackSizes[5][2] = {{64, 4}, {256, 4}, {256, 8}, {512, 8}, {512, 8}};
+    const int(*sizes)[2] = back ? kBackSizes : kSizes;
+    cut->held = false;
+    for (int k = 0; k < 5 && cut->parts == 1; k++) {
+        if (!cut->wide && k != 2) continue;
+        const int rows = sizes[k][0] / cut->cols;
+        if (rows >= 1 && (int64_t)rows * sizes[k][1] >= L) {
+            cut->held = true, cut->threads = sizes[k][0], cut->run = sizes[k][1], cut->rows = rows;
+            break;
+        }
+    }
+    cut->chunks = 1;
+    cut->folded = 0;
+    if (!cut->held) {
+        cut->threads = 256, cut->run = sizes[2][1], cut->rows = 256 / cut->cols;
+        const int64_t step = (int64_t)cut->rows * cut->run, chunks = (L + step - 1) / step;
+        if (chunks > INT_MAX) return false;
+        cut->chunks = (int32_t)chunks;
+        if (__builtin_mul_overflow(s->n * chunks, (int64_t)cut->slabs, &cut->grid)) return false;
+        cut->sum_rows = s->n * chunks;
+    } else if (back) {
+        int64_t series = (2048 + cut->slabs - 1) / cut->slabs;
+        if (series > s->n) series = s->n;
+        cut->series = (int32_t)(series > 0 ? series : 1);
+        cut->grid = (int64_t)cut->series * cut->slabs;
+        cut->sum_rows = cut->series;
+    } else {
+        cut->grid = s->n * cut->slabs;
+    }
+    if (back && cut->sum_rows > 4 * kFold) cut->folded = (cut->sum_rows + kFold - 1) / kFold;
+    const int64_t fold_grid = (cut->folded ? cut->folded : 1) * 2 * ((C + 63) / 64);
+    return cut->grid <= INT_MAX && (!back || fold_grid <= INT_MAX);
+}
+
+int64_t workspace_of(const rocket_sequence_shape *s, int32_t groups, bool back, const Cut &c) {
+    if (back) return (c.sum_rows + c.folded) * 2 * s->channels * (int64_t)sizeof(float);
+    return c.held ? 0 : s->n * groups * (int64_t)c.chunks * c.parts * (int64_t)sizeof(float2);
+}
+
+template <int DT, bool BACK, bool WIDE, int NT, int R, int MODE>
+void go(const NormArgs &a, const Cut &c, hipStream_t s) {
+    if (BACK)
+        norm_back_kernel<DT, WIDE, NT, R, MODE><<<(uint32_t)c.grid, NT, 0, s>>>(a);
+    else
+        norm_kernel<DT, WIDE, NT, R, MODE><<<(uint32_t)c.grid, NT, 0, s>>>(a);
+}
+
+template <int DT, bool BACK>
+void run(const NormArgs &a, const Cut &c, hipStream_t s) {
+    constexpr int kLong = BACK ? 8 : 16;   // passes of the larger sizes
+    if (!c.held) {
+        if (c.wide) {
+            go<DT, BACK, true, 256, kLong, kStats>(a, c, s);
+            go<DT, BACK, true, 256, kLong, kApply>(a, c, s);
+        } else {
+            go<DT, BACK, false, 256, kLong, kStats>(a, c, s);
+            go<DT, BACK, false, 256, kLong, kApply>(a, c, s);
+        }
+    } else if (!c.wide) {
+        go<DT, BACK, false, 256, kLong, kHeld>(a, c, s);
+    } else if (c.threads == 64) {
+        go<DT, BACK, true, 64, 4, kHeld>(a, c, s);
+    } else if (c.threads == 256 && c.run == 4) {
+        go<DT, BACK, true, 256, 4, kHeld>(a, c, s);
+    } else if (c.threads == 256) {
+        go<DT, BACK, true, 256, kLong, kHeld>(a, c, s);
+    } else if (c.threads == 512) {
+        go<DT, BACK, true, 512, kLong, kHeld>(a, c, s);
+    } else if constexpr (!BACK) {
+        go<DT, BACK, true, 1024, kLong, kHeld>(a, c, s);
+    }
+}
+
+template <bool BACK>
+void run_type(int32_t dtype, const NormArgs &a, const Cut &c, hipStream_t s) {
+    if (dtype == ROCKET_FLOAT32)
+        run<ROCKET_FLOAT32, BACK>(a, c, s);
+    else if (dtype == ROCKET_BFLOAT16)
+        run<ROCKET_BFLOAT16, BACK>(a, c, s);
+    else
+        run<ROCKET_FLOAT16, BACK>(a, c, s);
+}
+
+View view(const rocket_sequence *q, int size) {
+    return View{(char *)q->data, q->series_stride * size, q->step_stride * size};
+}
+
+bool aligned(const void *p, uintptr_t to) { return (uintptr_t)p % to == 0; }
+
+bool args_ok(const rocket_sequence_shape *shape, int32_t groups, int32_t act, const float *w, const float *b) {
+    return rocket::shape_ok(shape) && groups >= 1 && groups <= shape->channels && shape->channels % groups == 0 &&
+           (int64_t)groups * shape->n <= ((int64_t)1 << 40) && act >= ROCKET_ACT_NONE && act <= ROCKET_ACT_GELU &&
+           aligned(w, 4) && aligned(b, 4) && aligned(shape->lengths, 4);
+}
+
+NormArgs args_of(const rocket_sequence_shape *shape, int32_t groups, int32_t act, const float *w, const float *b,
+                 const Cut &cut) {
+    NormArgs a = {};
+    a.n = shape->n, a.L = shape->steps, a.C = (int32_t)shape->channels, a.G = groups, a.width = cut.width;
+    a.slabs = cut.slabs, a.parts = cut.parts, a.cols = cut.cols, a.rows = cut.rows, a.chunks = cut.chunks;
+    a.act = act, a.w = w, a.b = b, a.lengths = shape->lengths, a.series = cut.series;
+    return a;
+}
+
+}  // namespace
+
+extern "C" rocket_status rocket_group_norm_workspace(const rocket_sequence_shape *shape, int32_t groups,
+                                                     int32_t backward, int64_t *bytes) {
+    Cut cut = {};
+    if (!bytes || !args_ok(shape, groups, ROCKET_ACT_NONE, nullptr, nullptr) ||
+        !cut_of(shape, groups, backward != 0, &cut))
+        return ROCKET_ERR_INVALID_ARG;
+    *bytes = workspace_of(shape, groups, backward != 0, cut);
+    return ROCKET_OK;
+}
+
+extern "C" rocket_status rocket_group_norm_forward(const rocket_sequence_shape *shape, int32_t groups,
+                                                   const rocket_sequence *x, const float *weight, const float *bias,
+                                                   float eps, int32_t activation, const rocket_sequence *y,
+                                                   float *mean, float *rstd, void *workspace,
+                                                   int64_t workspace_bytes, void *hip_stream) {
+    Cut cut = {};
+    if (!args_ok(shape, groups, activation, weight, bias) || !cut_of(shape, groups, false, &cut) ||
+        !rocket::view_ok(x, shape) || !rocket::out_ok(y, shape) || !(eps >= 0.0f) || !(eps <= 3.0e38f) ||
+        (shape->n > 0 && (!mean || !rstd)) || !aligned(mean, 4) || !aligned(rstd, 4))
+        return ROCKET_ERR_INVALID_ARG;
+    const int64_t need = workspace_of(shape, groups, false, cut);
+    if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 8)))) return ROCKET_ERR_INVALID_ARG;
+    if (shape->n == 0) return ROCKET_OK;
+    const int size = rocket::elem_size(shape->dtype);
+    NormArgs a = args_of(shape, groups, activation, weight, bias, cut);
+    a.x = view(x, size), a.out = view(y, size);
+    a.eps = eps, a.mean = mean, a.rstd = rstd, a.stats = (float2 *)workspace;
+    run_type<false>(shape->dtype, a, cut, (hipStream_t)hip_stream);
+    return rocket::launched();
+}
+
+extern "C" rocket_status rocket_group_norm_backward(const rocket_sequence_shape *shape, int32_t groups,
+                                                    const rocket_sequence *dy, const rocket_sequence *x,
+                                                    const float *weight, const float *bias, int32_t activation,
+                                                    const float *mean, const float *rstd, const rocket_sequence *dx,
+                                                    float *dweight, float *dbias, void *workspace,
+                                                    int64_t workspace_bytes, void *hip_stream) {
+    Cut cut = {};
+    if (!args_ok(shape, groups, activation, weight, bias) || !cut_of(shape, groups, true, &cut) ||
+        !rocket::view_ok(dy, shape) || !rocket::view_ok(x, shape) || !rocket::out_ok(dx, shape) ||
+        (shape->n > 0 && (!mean || !rstd)) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dweight, 4) ||
+        !aligned(dbias, 4))
+        return ROCKET_ERR_INVALID_ARG;
+    const int64_t need = workspace_of(shape, groups, true, cut);
+    if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 4)))) return ROCKET_ERR_INVALID_ARG;
+    hipStream_t s = (hipStream_t)hip_stream;
+    const int size = rocket::elem_size(shape->dtype), C = (int)shape->channels;
+    float *sums = (float *)workspace;
+    int64_t rows = 0;
+    if (!rocket::empty(shape)) {
+        NormArgs a = args_of(shape, groups, activation, weight, bias, cut);
+        a.x = view(x, size), a.dy = view(dy, size), a.out = view(dx, size);
+        a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd), a.sums = sums;
+        run_type<true>(shape->dtype, a, cut, s);
+        rows = cut.sum_rows;
+    }
+    if (!dweight && !dbias) return rocket::launched();
+    const uint32_t blocks = (uint32_t)((C + 63) / 64);
+    if (rows && cut.folded) {
+        float *next = sums + rows * 2 * C;
+        fold_kernel<<<(uint32_t)cut.folded * 2 * blocks, 1024, 0, s>>>(sums, rows, kFold, C, next, next + C,
+                                                                       2 * (int64_t)C);
+        sums = next, rows = cut.folded;
+    }
+    fold_kernel<<<2 * blocks, 1024, 0, s>>>(sums, rows, rows ? rows : 1, C, dbias, dweight, 0);
+    return rocket::launched();
+}

@@ -57,6 +57,14 @@ EXPORTED = (
     "rocket_minirocket_plan_create",
     "rocket_checked_build",
     "rocket_check_flags",
+    "rocket_group_norm_forward",
+    "rocket_group_norm_backward",
+    "rocket_group_norm_workspace",
+    "rocket_recurrence_forward",
+    "rocket_recurrence_backward",
+    "rocket_recurrence_workspace",
+    "rocket_recurrence_step",
+    "rocket_dropout",
 )
 
 
@@ -120,6 +128,17 @@ class CPlanTables(ctypes.Structure):
     ]
 
 
+class CSequenceShape(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int64), ("steps", ctypes.c_int64), ("channels", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("lengths", ctypes.c_void_p),
+    ]
+
+
+class CSequence(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("series_stride", ctypes.c_int64), ("step_stride", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -129,6 +148,8 @@ def _signatures() -> dict:
     kp = ctypes.POINTER(CKernels)
     mp = ctypes.POINTER(CMiniRocketParams)
     st = ctypes.c_int
+    f32, f64, u64 = ctypes.c_float, ctypes.c_double, ctypes.c_uint64
+    shp, seq, out64 = ctypes.POINTER(CSequenceShape), ctypes.POINTER(CSequence), ctypes.POINTER(i64)
     return {
         "rocket_generate_kernels": ([ctypes.c_uint64, i32, i32, kp], st),
         "rocket_generate_kernels_multi": ([ctypes.c_uint64, i32, i32, i32, kp], st),
@@ -150,6 +171,14 @@ def _signatures() -> dict:
         "rocket_minirocket_fit": ([vp, i64, i32, i32, ctypes.c_uint64, mp], st),
         "rocket_minirocket_free": ([mp], None),
         "rocket_minirocket_plan_create": ([mp, ctypes.c_uint32, ctypes.POINTER(vp)], st),
+        "rocket_group_norm_forward": ([shp, i32, seq, vp, vp, f32, i32, seq, vp, vp, vp, i64, vp], st),
+        "rocket_group_norm_backward": ([shp, i32, seq, seq, vp, vp, i32, vp, vp, seq, vp, vp, vp, i64, vp], st),
+        "rocket_group_norm_workspace": ([shp, i32, i32, out64], st),
+        "rocket_recurrence_forward": ([shp, seq, seq, seq, vp, seq, vp, vp, vp, i64, vp], st),
+        "rocket_recurrence_backward": ([shp, seq, seq, seq, seq, vp, vp, seq, seq, seq, vp, vp, i64, vp], st),
+        "rocket_recurrence_workspace": ([shp, out64], st),
+        "rocket_recurrence_step": ([i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp], st),
+        "rocket_dropout": ([vp, vp, vp, i64, i64, i64, i64, i64, i32, f64, u64, u64, vp], st),
     }
 
 
