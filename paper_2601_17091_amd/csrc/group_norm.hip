@@ -79,12 +79,13 @@ struct Pack<DT, false> {
     __device__ void clear() { v = 0; }
 };
 
+template <int DT>
 __device__ inline float activate(float z, int act) {
     switch (act) {
     case ROCKET_ACT_RELU: return z < 0.0f ? 0.0f : z;
     case ROCKET_ACT_SILU: {
         float s, rest;
-        rocket::logistic(z, s, rest);
+        rocket::logistic<DT>(z, s, rest);
         return z * s;
     }
     case ROCKET_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
@@ -92,16 +93,17 @@ __device__ inline float activate(float z, int act) {
     }
 }
 
+template <int DT>
 __device__ inline float slope(float z, int act) {
     switch (act) {
     case ROCKET_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
     case ROCKET_ACT_SILU: {
         float s, rest;
-        rocket::logistic(z, s, rest);
+        rocket::logistic<DT>(z, s, rest);
         return s * (1.0f + z * rest);
     }
     case ROCKET_ACT_GELU: {
-        float e = rocket::exp_neg_abs(0.5f * z * z);
+        float e = rocket::exp_neg_abs<DT>(0.5f * z * z);
         return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * e * 0.39894228040143268f;
     }
     default: return 1.0f;
@@ -342,7 +344,7 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs a) {
         float y[VEC];
 #pragma unroll
         for (int e = 0; e < VEC; e++)
-            y[e] = r < own ? activate(__builtin_fmaf(held[j].get(e) - m[e], sc[e], sh[e]), a.act) : 0.0f;
+            y[e] = r < own ? activate<DT>(__builtin_fmaf(held[j].get(e) - m[e], sc[e], sh[e]), a.act) : 0.0f;
         P::store(out + (int64_t)r * a.out.ts, y);
     }
 }
@@ -408,7 +410,7 @@ __global__ __launch_bounds__(NT) void norm_back_kernel(NormArgs a) {
 #pragma unroll
                     for (int e = 0; e < VEC; e++) {
                         const float xh = (hx[j].get(e) - m[e]) * rs[e];
-                        const float dz = hg[j].get(e) * slope(xh * w[e] + bias[e], a.act);
+                        const float dz = hg[j].get(e) * slope<DT>(xh * w[e] + bias[e], a.act);
                         sd[e] += dz;
                         sx[e] = __builtin_fmaf(dz, xh, sx[e]);
                     }
@@ -459,7 +461,7 @@ __global__ __launch_bounds__(NT) void norm_back_kernel(NormArgs a) {
 #pragma unroll
                 for (int e = 0; e < VEC; e++) {
                     const float xh = (hx[j].get(e) - m[e]) * rs[e];
-                    const float g = hg[j].get(e) * slope(xh * w[e] + bias[e], a.act) * w[e];
+                    const float g = hg[j].get(e) * slope<DT>(xh * w[e] + bias[e], a.act) * w[e];
                     dx[e] = r < own ? rs[e] * (g - mg[e] - xh * mx[e]) : 0.0f;
                 }
                 P::store(out + (int64_t)r * a.out.ts, dx);

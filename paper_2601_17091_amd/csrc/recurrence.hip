@@ -4,21 +4,28 @@
 //
 // Any run of steps is an affine map of the state before it, h -> A h + B, and
 // maps compose: (A2, B2) after (A1, B1) is (A2 A1, A2 B1 + B2).  So the time
-// axis splits: a thread composes its own 16 steps, the lanes and wavefronts of
-// a workgroup combine theirs into the map of a tile, and the tiles of a series
-// combine over the grid.  Every combination runs in a fixed order, so results
-// do not change from call to call.  The gradient is the same scan from the
-// other end: with g_t = dy_t S(o_t), the gradient that reaches h_{t-1} is
+// axis splits: a thread composes its own run of steps, and the lanes and
+// wavefronts of a workgroup combine theirs into the states at the runs' starts.
+// The gradient is the same scan from the other end: with g_t = dy_t S(o_t), the
+// gradient that reaches h_{t-1} is
 //   e_t = S(f_t) (g_t + e_{t+1}),   e_L = the gradient of the last state,
 // and with dh_t = g_t + e_{t+1}
 //   dv = dh (1 - a),  df = dh (h_{t-1} - v) a (1 - a),  do = dy h S(o) (1 - S(o)).
-// The states are held in fp32 throughout; y and the gradients are rounded once.
+// Every combination runs in a fixed order, so results do not change from call
+// to call.  States, gates and gradients of states are held in fp32 throughout;
+// y and the gradients are rounded once.
 //
-// Layout: a lane takes one 32-bit word of channels (one fp32, two 16-bit), so
-// that a wavefront's load of one step is 256 contiguous bytes; where a series
-// has fewer than 64 words of channels, the lanes left over take further runs
-// of steps.  Steps past a series' length act as h -> h and are not read.
+// Layout: a lane takes one 32-bit word of channels (one fp32, two 16-bit) of
+// 16 elements' worth of steps; 32 lanes side by side take 128 contiguous bytes
+// of a step, and the lanes left over take further runs.  A workgroup covers a
+// tile of 128 steps (more where few channels leave lanes over) and goes through
+// the tiles of a segment of one series, the state carried from tile to tile.
+// Where series and channels alone do not fill the chip, a series is cut into
+// segments: a first launch leaves each segment's map, and the second starts
+// each segment from the maps before it.  The backward pass starts each tile
+// from the state that the forward pass kept there.
 #include <climits>
+#include <type_traits>
 
 #include "sequence.h"
 
@@ -26,11 +33,12 @@ namespace {
 
 using rocket::Elem;
 
-constexpr int kWaves = 8;
-constexpr int kThreads = 64 * kWaves;
-constexpr int kRun = 16;                       // steps of one thread
 constexpr int kEvery = ROCKET_RECURRENCE_EVERY;  // steps between kept states
-static_assert(kEvery % kRun == 0 && (kWaves * kRun) % kEvery == 0, "kept states fall on the starts of runs and tiles");
+constexpr int kElems = 16;                       // elements of a thread in a tile
+constexpr int kMostLanes = 32;                   // lanes over channels
+constexpr int kMostWaves = 8;
+constexpr int kMostChannels = 64;                // of a workgroup: 32 lanes x 2
+constexpr int64_t kFill = 1024;                  // workgroups that fill the chip
 
 struct View {
     char *p;
@@ -47,17 +55,26 @@ struct RecArgs {
     float *states;          // kept states [n, ceil(L / kEvery), C]: written (or null) forward, read backward
     const float *dh_last;   // backward, or null
     float *dh0;             // backward
-    float2 *maps;           // [n, tiles, C], tiles > 1
-    int32_t tiles, lanes;   // lanes over channels, a power of two
+    float2 *maps;           // [n, segments, C], segments > 1
     int32_t blocks;         // channel blocks
+    int32_t lanes;          // lanes over channels, a power of two
+    int32_t waves;          // wavefronts of a workgroup
+    int32_t segments, tiles;  // segments of a series, tiles of a segment
 };
+
+template <int DT>
+constexpr int kRun = kElems / Elem<DT>::kPerWord;  // steps of one thread in a tile
+
+// A gate that keeps the state: S = 1 and 1 - S = 0 to the bit.
+template <int DT>
+constexpr uint32_t kKeep = DT == ROCKET_FLOAT32 ? 0x7f800000u : DT == ROCKET_BFLOAT16 ? 0x7f807f80u : 0x7c007c00u;
 
 // Where a thread works.
 struct Place {
     int64_t i, len;   // series, its steps
-    int64_t t0;       // first step of the thread's run
-    int64_t c, c_ld;  // its first channel, and the channel it loads from
-    int tile, wave, lane, lanes;
+    int64_t c, c_ld;  // first channel, and the channel it loads from
+    int64_t tile;     // steps of a tile
+    int segment, wave, lane, cl, run;
     int count;        // channels it owns: 0, 1 or 2
     bool high;        // its one channel is the high half of the word at c_ld
     bool single;      // C == 1 and 16-bit elements: no whole word to load
@@ -70,321 +87,353 @@ __device__ inline Place place_of(const RecArgs &a) {
     const int64_t b = blockIdx.x;
     const int64_t cb = b % a.blocks, rest = b / a.blocks;
     p.i = rest % a.n;
-    p.tile = (int)(rest / a.n);
+    p.segment = (int)(rest / a.n);
     p.wave = threadIdx.x >> 6;
     p.lane = threadIdx.x & 63;
-    p.lanes = a.lanes;
     const int runs = 64 / a.lanes;
-    const int cl = p.lane & (a.lanes - 1), q = p.lane / a.lanes;
-    p.c = (cb * a.lanes + cl) * P;
+    p.cl = p.lane & (a.lanes - 1);
+    p.run = p.wave * runs + p.lane / a.lanes;
+    p.tile = (int64_t)a.waves * runs * kRun<DT>;
+    p.c = (cb * a.lanes + p.cl) * P;
     int64_t left = a.C - p.c;
     p.count = left <= 0 ? 0 : left < P ? 1 : P;
     p.high = P == 2 && p.count == 1 && a.C > 1;
     p.single = P == 2 && a.C == 1;
     p.c_ld = p.c + P <= a.C ? p.c : a.C > P ? a.C - P : 0;
     p.len = rocket::steps_of(a.lengths, p.i, a.L);
-    p.t0 = (((int64_t)p.tile * kWaves + p.wave) * runs + q) * kRun;
     return p;
 }
 
-// The words of a run; steps past the series' length repeat its last one (they
-// are masked later), and a series of no steps loads nothing.
+// The words of a run from step t0; steps past the series' length get `fill`.
 template <int DT>
-__device__ inline void load_run(const View &x, const Place &p, uint32_t (&w)[kRun]) {
-    if (p.len == 0) {
+__device__ inline void load_run(const View &x, const Place &p, int64_t t0, uint32_t fill, uint32_t (&w)[kRun<DT>]) {
+    using raw = typename Elem<DT>::raw;
+    const char *at = x.p + p.i * x.ss + t0 * x.ts + p.c_ld * Elem<DT>::kSize;
+    if (p.single) {
 #pragma unroll
-        for (int s = 0; s < kRun; s++) w[s] = 0;
-        return;
-    }
-    const char *base = x.p + p.i * x.ss + p.c_ld * Elem<DT>::kSize;
+        for (int s = 0; s < kRun<DT>; s++) w[s] = t0 + s < p.len ? (uint32_t)*(const raw *)(at + s * x.ts) : fill;
+    } else if (t0 + kRun<DT> <= p.len) {
 #pragma unroll
-    for (int s = 0; s < kRun; s++) {
-        int64_t t = p.t0 + s < p.len ? p.t0 + s : p.len - 1;
-        if (p.single)
-            w[s] = *(const typename Elem<DT>::raw *)(base + t * x.ts);
-        else
-            w[s] = rocket::load_at<uint32_t>(base + t * x.ts);
+        for (int s = 0; s < kRun<DT>; s++) w[s] = rocket::load_at<uint32_t>(at + s * x.ts);
+    } else {
+#pragma unroll
+        for (int s = 0; s < kRun<DT>; s++) w[s] = t0 + s < p.len ? rocket::load_at<uint32_t>(at + s * x.ts) : fill;
     }
     if (p.high) {
 #pragma unroll
-        for (int s = 0; s < kRun; s++) w[s] >>= 16;
+        for (int s = 0; s < kRun<DT>; s++) w[s] = t0 + s < p.len ? w[s] >> 16 : fill;
     }
+}
+
+// Whether a run's stores need no checks: whole words, all steps inside.
+template <int DT>
+__device__ inline bool whole_run(const Place &p, int64_t t0, int64_t L) {
+    return p.count == Elem<DT>::kPerWord && t0 + kRun<DT> <= L;
+}
+
+// Makes the compiler take the words as new, so that it unpacks them (and
+// computes gates of them) again instead of holding the results in registers.
+template <int N>
+__device__ inline void renew(uint32_t (&w)[N]) {
+#pragma unroll
+    for (int s = 0; s < N; s++) asm("" : "+v"(w[s]));
+}
+
+// Writes the packed word of step t of a run that starts at `at`, checked
+// unless the run is whole.
+template <int DT, bool WHOLE>
+__device__ inline void store_step(char *at, int64_t stride, const Place &p, int s, int64_t left, uint32_t w) {
+    using raw = typename Elem<DT>::raw;
+    if (WHOLE)
+        rocket::store_at(at + s * stride, w);
+    else if (s < left && p.count == Elem<DT>::kPerWord)
+        rocket::store_at(at + s * stride, w);
+    else if (s < left && p.count == 1)
+        *(raw *)(at + s * stride) = (raw)w;
 }
 
 template <int DT>
-__device__ inline void store_step(const View &x, const Place &p, int64_t t, const float *val) {
-    char *q = x.p + p.i * x.ss + t * x.ts + p.c * Elem<DT>::kSize;
-    if (p.count == Elem<DT>::kPerWord)
-        rocket::store_at(q, Elem<DT>::put(val));
-    else if (p.count == 1)
-        *(typename Elem<DT>::raw *)q = Elem<DT>::round(val[0]);
+__device__ inline char *run_at(const View &x, const Place &p, int64_t t0) {
+    return x.p + p.i * x.ss + t0 * x.ts + p.c * Elem<DT>::kSize;
 }
 
-// Composes the maps of the runs before a thread's own inside its tile:
-// (eA, eB), applied to the state at the tile's start, gives the state at the
-// run's start.  tA, tB: the whole tile's map.  REVERSE: from the last run to
-// the first.
+// Shared memory of one scan over the wavefronts of a workgroup.
+struct Scan {
+    float2 map[kMostWaves][kMostChannels];
+    float start[kMostWaves][kMostChannels];
+};
+
+// Inclusive scan of the runs' maps over the lanes of a wavefront, then
+// (A, B) becomes the map of the runs before the thread's own (REVERSE: after
+// it), and the wavefront's whole map goes to shared memory.
 template <int P, bool REVERSE>
-__device__ inline void compose_tile(const Place &p, const float *A, const float *B, float *eA, float *eB, float *tA,
-                                    float *tB, float2 (*maps)[64 * 2]) {
-    float sA[P], sB[P];
-#pragma unroll
-    for (int j = 0; j < P; j++) sA[j] = A[j], sB[j] = B[j];
-    for (int off = p.lanes; off < 64; off *= 2) {
-        bool on = REVERSE ? p.lane + off < 64 : p.lane >= off;
+__device__ inline void scan_lanes(const RecArgs &a, const Place &p, float *A, float *B, Scan &s) {
+    for (int off = a.lanes; off < 64; off *= 2) {
+        const bool on = REVERSE ? p.lane + off < 64 : p.lane >= off;
 #pragma unroll
         for (int j = 0; j < P; j++) {
-            float pa = REVERSE ? __shfl_down(sA[j], off) : __shfl_up(sA[j], off);
-            float pb = REVERSE ? __shfl_down(sB[j], off) : __shfl_up(sB[j], off);
-            if (on) {
-                sB[j] = __builtin_fmaf(sA[j], pb, sB[j]);
-                sA[j] *= pa;
-            }
+            const float pa = REVERSE ? __shfl_down(A[j], off) : __shfl_up(A[j], off);
+            const float pb = REVERSE ? __shfl_down(B[j], off) : __shfl_up(B[j], off);
+            B[j] = on ? __builtin_fmaf(A[j], pb, B[j]) : B[j];
+            A[j] = on ? A[j] * pa : A[j];
         }
     }
-    const int cl = p.lane & (p.lanes - 1);
-    const bool first = REVERSE ? p.lane + p.lanes >= 64 : p.lane < p.lanes;   // nothing before it in its wavefront
-    const bool last = REVERSE ? p.lane < p.lanes : p.lane + p.lanes >= 64;
+    const bool first = REVERSE ? p.lane + a.lanes >= 64 : p.lane < a.lanes;   // nothing before it in its wavefront
+    const bool last = REVERSE ? p.lane < a.lanes : p.lane + a.lanes >= 64;
     if (last) {
 #pragma unroll
-        for (int j = 0; j < P; j++) maps[p.wave][cl * P + j] = make_float2(sA[j], sB[j]);
+        for (int j = 0; j < P; j++) s.map[p.wave][p.cl * P + j] = make_float2(A[j], B[j]);
     }
 #pragma unroll
     for (int j = 0; j < P; j++) {
-        float xa = sA[j], xb = sB[j];
-        if (p.lanes < 64) {
-            xa = REVERSE ? __shfl_down(sA[j], p.lanes) : __shfl_up(sA[j], p.lanes);
-            xb = REVERSE ? __shfl_down(sB[j], p.lanes) : __shfl_up(sB[j], p.lanes);
+        float xa = A[j], xb = B[j];
+        if (a.lanes < 64) {
+            xa = REVERSE ? __shfl_down(A[j], a.lanes) : __shfl_up(A[j], a.lanes);
+            xb = REVERSE ? __shfl_down(B[j], a.lanes) : __shfl_up(B[j], a.lanes);
         }
-        eA[j] = first ? 1.0f : xa;
-        eB[j] = first ? 0.0f : xb;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < P; j++) {
-        float wA = 1.0f, wB = 0.0f;   // the wavefronts before this one
-        float aA = 1.0f, aB = 0.0f;   // all of them
-#pragma unroll
-        for (int k = 0; k < kWaves; k++) {
-            const int w = REVERSE ? kWaves - 1 - k : k;
-            if (w == p.wave) wA = aA, wB = aB;
-            float2 m = maps[w][cl * P + j];
-            aB = __builtin_fmaf(m.x, aB, m.y);
-            aA *= m.x;
-        }
-        eB[j] = __builtin_fmaf(eA[j], wB, eB[j]);
-        eA[j] *= wA;
-        tA[j] = aA, tB[j] = aB;
+        A[j] = first ? 1.0f : xa;
+        B[j] = first ? 0.0f : xb;
     }
 }
 
-// The state at a tile's start: the maps of the tiles before it (REVERSE:
-// after it) applied to `h` in order.  Each wavefront composes a range of them,
-// then the ranges are applied in turn.
-template <int P, bool REVERSE>
-__device__ inline void apply_tiles(const RecArgs &a, const Place &p, float *h, float2 (*maps)[64 * 2]) {
-    const int before = REVERSE ? a.tiles - 1 - p.tile : p.tile;
-    if (before == 0) return;   // the same for the whole workgroup
-    const int cl = p.lane & (p.lanes - 1);
-    __syncthreads();           // maps is free again
-    if (p.lane < p.lanes) {
-        float A[P], B[P];
+// One thread per channel goes through the wavefronts' maps: the state at each
+// wavefront's start, and in `carry` the state past the tile.
+template <bool REVERSE>
+__device__ inline void scan_waves(int waves, int ch, float &carry, Scan &s) {
+    for (int k = 0; k < waves; k++) {
+        const int w = REVERSE ? waves - 1 - k : k;
+        const float2 m = s.map[w][ch];
+        s.start[w][ch] = carry;
+        carry = __builtin_fmaf(m.x, carry, m.y);
+    }
+}
+
+// The state at a segment's start: the maps of the segments before it (REVERSE:
+// after it), applied in order.
+template <bool REVERSE>
+__device__ inline float scan_segments(const RecArgs &a, const Place &p, int64_t c, float h) {
+    const int before = REVERSE ? a.segments - 1 - p.segment : p.segment;
+    const float2 *m = a.maps + (p.i * a.segments + (REVERSE ? a.segments - 1 : 0)) * a.C + c;
+    const int64_t step = REVERSE ? -a.C : a.C;
+#pragma unroll 8
+    for (int k = 0; k < before; k++) {
+        const float2 x = m[k * step];
+        h = __builtin_fmaf(x.x, h, x.y);
+    }
+    return h;
+}
+
+// The forward pass over a segment.  MAPS: only its map.
+template <int DT, bool MAPS, bool GATE>
+__global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) {
+    constexpr int P = Elem<DT>::kPerWord, S = kRun<DT>;
+    __shared__ Scan scan;
+    const Place p = place_of<DT>(a);
+    const bool scans = threadIdx.x < a.lanes * P;   // the threads that go through the wavefronts, one a channel
+    const int64_t ch = (p.c - p.cl * P) + threadIdx.x;
+    float carry = 0.0f, carry_a = 1.0f;
+    if (scans && ch < a.C && !MAPS) {
+        if (a.h0) carry = a.h0[p.i * a.C + ch];
+        if (a.segments > 1) carry = scan_segments<false>(a, p, ch, carry);
+    }
+    const int64_t first = (int64_t)p.segment * a.tiles * p.tile, per = (a.L + kEvery - 1) / kEvery;
+    uint32_t wv[S], wf[S], wo[S];
+    load_run<DT>(a.v, p, first + p.run * S, 0, wv);
+    load_run<DT>(a.f, p, first + p.run * S, kKeep<DT>, wf);
+    if (GATE && !MAPS) load_run<DT>(a.o, p, first + p.run * S, 0, wo);
+
+    for (int k = 0; k < a.tiles; k++) {
+        const int64_t tile0 = first + k * p.tile, t0 = tile0 + p.run * S;
+        if (k > 0 && tile0 >= a.L) break;
+        float fa[S][P], fb[S][P], A[P], B[P];
 #pragma unroll
         for (int j = 0; j < P; j++) A[j] = 1.0f, B[j] = 0.0f;
-        const int from = (int)((int64_t)before * p.wave / kWaves), to = (int)((int64_t)before * (p.wave + 1) / kWaves);
-        for (int k = from; k < to; k++) {
-            const int tile = REVERSE ? a.tiles - 1 - k : k;
-            const float2 *m = a.maps + (p.i * a.tiles + tile) * a.C + p.c;
 #pragma unroll
-            for (int j = 0; j < P; j++)
-                if (j < p.count) {
-                    float2 x = m[j];
-                    B[j] = __builtin_fmaf(x.x, B[j], x.y);
-                    A[j] *= x.x;
+        for (int s = 0; s < S; s++)
+#pragma unroll
+            for (int j = 0; j < P; j++) {
+                float in;
+                rocket::logistic<DT>(Elem<DT>::get(wf[s], j), fa[s][j], in);
+                fb[s][j] = in * Elem<DT>::get(wv[s], j);
+                B[j] = __builtin_fmaf(fa[s][j], B[j], fb[s][j]);
+                A[j] *= fa[s][j];
+            }
+        uint32_t go[S];   // the next tile's words go over these
+        if (GATE && !MAPS) {
+#pragma unroll
+            for (int s = 0; s < S; s++) go[s] = wo[s];
+        }
+        const int64_t next = t0 + p.tile;
+        if (k + 1 < a.tiles && tile0 + p.tile < a.L) {   // on their way during the scan
+            load_run<DT>(a.v, p, next, 0, wv);
+            load_run<DT>(a.f, p, next, kKeep<DT>, wf);
+            if (GATE && !MAPS) load_run<DT>(a.o, p, next, 0, wo);
+        }
+        scan_lanes<P, false>(a, p, A, B, scan);
+        __syncthreads();
+        if (scans) {
+            if (MAPS) {
+                for (int w = 0; w < a.waves; w++) {
+                    const float2 m = scan.map[w][threadIdx.x];
+                    carry = __builtin_fmaf(m.x, carry, m.y);
+                    carry_a *= m.x;
                 }
-        }
-#pragma unroll
-        for (int j = 0; j < P; j++) maps[p.wave][cl * P + j] = make_float2(A[j], B[j]);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < P; j++)
-#pragma unroll
-        for (int w = 0; w < kWaves; w++) {
-            float2 m = maps[w][cl * P + j];
-            h[j] = __builtin_fmaf(m.x, h[j], m.y);
-        }
-}
-
-// The forward pass over a tile.  MAPS: only the tile's map, for the tiles that
-// follow; else everything.
-template <int DT, bool MAPS, bool GATE>
-__global__ __launch_bounds__(kThreads, 4) void forward_kernel(RecArgs a) {
-    constexpr int P = Elem<DT>::kPerWord;
-    __shared__ float2 maps[kWaves][64 * 2];
-    const Place p = place_of<DT>(a);
-    uint32_t wv[kRun], wf[kRun], wo[kRun];
-    load_run<DT>(a.v, p, wv);
-    load_run<DT>(a.f, p, wf);
-    if (GATE && !MAPS) load_run<DT>(a.o, p, wo);
-
-    float fa[kRun][P], fb[kRun][P], A[P], B[P];
-#pragma unroll
-    for (int j = 0; j < P; j++) A[j] = 1.0f, B[j] = 0.0f;
-#pragma unroll
-    for (int s = 0; s < kRun; s++)
-#pragma unroll
-        for (int j = 0; j < P; j++) {
-            float keep, in;
-            rocket::logistic(Elem<DT>::get(wf[s], j), keep, in);
-            float b = in * Elem<DT>::get(wv[s], j);
-            const bool live = p.t0 + s < p.len;
-            fa[s][j] = live ? keep : 1.0f;
-            fb[s][j] = live ? b : 0.0f;
-            B[j] = __builtin_fmaf(fa[s][j], B[j], fb[s][j]);
-            A[j] *= fa[s][j];
-        }
-
-    float eA[P], eB[P], tA[P], tB[P];
-    compose_tile<P, false>(p, A, B, eA, eB, tA, tB, maps);
-    if (MAPS) {
-        if (p.wave == 0 && p.lane < p.lanes)
-#pragma unroll
-            for (int j = 0; j < P; j++)
-                if (j < p.count) a.maps[(p.i * a.tiles + p.tile) * a.C + p.c + j] = make_float2(tA[j], tB[j]);
-        return;
-    }
-
-    float h[P];
-#pragma unroll
-    for (int j = 0; j < P; j++) h[j] = a.h0 && j < p.count ? a.h0[p.i * a.C + p.c + j] : 0.0f;
-    apply_tiles<P, false>(a, p, h, maps);
-#pragma unroll
-    for (int j = 0; j < P; j++) h[j] = __builtin_fmaf(eA[j], h[j], eB[j]);
-
-    if (a.states && p.t0 % kEvery == 0 && p.t0 < a.L) {
-        const int64_t per = (a.L + kEvery - 1) / kEvery;
-#pragma unroll
-        for (int j = 0; j < P; j++)
-            if (j < p.count) a.states[(p.i * per + p.t0 / kEvery) * a.C + p.c + j] = h[j];
-    }
-#pragma unroll
-    for (int s = 0; s < kRun; s++) {
-        float y[P];
-#pragma unroll
-        for (int j = 0; j < P; j++) {
-            h[j] = __builtin_fmaf(fa[s][j], h[j], fb[s][j]);
-            y[j] = h[j];
-            if (GATE) {
-                float so, rest;
-                rocket::logistic(Elem<DT>::get(wo[s], j), so, rest);
-                y[j] *= so;
-            }
-            if (!(p.t0 + s < p.len)) y[j] = 0.0f;
-        }
-        if (p.t0 + s < a.L) store_step<DT>(a.y, p, p.t0 + s, y);
-    }
-    const int64_t end = a.L > 0 ? a.L - 1 : 0;
-    if (p.t0 <= end && end < p.t0 + kRun)
-#pragma unroll
-        for (int j = 0; j < P; j++)
-            if (j < p.count) a.h_last[p.i * a.C + p.c + j] = h[j];
-}
-
-// The backward pass over a tile.  MAPS: only the tile's map of the gradient
-// that runs towards its start; else everything, from the kept state.
-template <int DT, bool MAPS, bool GATE>
-__global__ __launch_bounds__(kThreads, 4) void backward_kernel(RecArgs a) {
-    constexpr int P = Elem<DT>::kPerWord;
-    __shared__ float2 maps[kWaves][64 * 2];
-    const Place p = place_of<DT>(a);
-    uint32_t wv[kRun], wf[kRun], wo[kRun], wg[kRun];
-    load_run<DT>(a.f, p, wf);
-    load_run<DT>(a.dy, p, wg);
-    if (GATE) load_run<DT>(a.o, p, wo);
-    if (!MAPS) load_run<DT>(a.v, p, wv);
-
-    float h[kRun][P];   // the state before each step
-    float A[P], R[P], B[P];
-#pragma unroll
-    for (int j = 0; j < P; j++) A[j] = 1.0f, R[j] = 0.0f, B[j] = 0.0f;
-#pragma unroll
-    for (int s = kRun - 1; s >= 0; s--)
-#pragma unroll
-        for (int j = 0; j < P; j++) {
-            float keep, in, so = 1.0f, rest;
-            rocket::logistic(Elem<DT>::get(wf[s], j), keep, in);
-            if (GATE) rocket::logistic(Elem<DT>::get(wo[s], j), so, rest);
-            const float g = Elem<DT>::get(wg[s], j) * so;
-            if (p.t0 + s < p.len) {
-                R[j] = keep * (R[j] + g);
-                if (!MAPS) B[j] = __builtin_fmaf(A[j], in * Elem<DT>::get(wv[s], j), B[j]);
-                A[j] *= keep;
+            } else {
+                scan_waves<false>(a.waves, threadIdx.x, carry, scan);
             }
         }
-
-    float eA[P], eR[P], tA[P], tR[P];
-    compose_tile<P, true>(p, A, R, eA, eR, tA, tR, maps);
-    if (MAPS) {
-        if (p.wave == 0 && p.lane < p.lanes)
+        __syncthreads();
+        if (MAPS) continue;
+        float h[P];
+#pragma unroll
+        for (int j = 0; j < P; j++) h[j] = __builtin_fmaf(A[j], scan.start[p.wave][p.cl * P + j], B[j]);
+        if (a.states && t0 % kEvery == 0 && t0 < a.L)
 #pragma unroll
             for (int j = 0; j < P; j++)
-                if (j < p.count) a.maps[(p.i * a.tiles + p.tile) * a.C + p.c + j] = make_float2(tA[j], tR[j]);
-        return;
+                if (j < p.count) a.states[(p.i * per + t0 / kEvery) * a.C + p.c + j] = h[j];
+        char *at = run_at<DT>(a.y, p, t0);
+        auto steps = [&](auto whole) {
+#pragma unroll
+            for (int s = 0; s < S; s++) {
+                float out[P];
+#pragma unroll
+                for (int j = 0; j < P; j++) {
+                    h[j] = __builtin_fmaf(fa[s][j], h[j], fb[s][j]);
+                    out[j] = h[j];
+                    if (GATE) {
+                        float so, rest;
+                        rocket::logistic<DT>(Elem<DT>::get(go[s], j), so, rest);
+                        out[j] *= so;
+                    }
+                }
+                store_step<DT, whole.value>(at, a.y.ts, p, s, a.L - t0, t0 + s < p.len ? Elem<DT>::put(out) : 0);
+            }
+        };
+        if (whole_run<DT>(p, t0, a.L))
+            steps(std::true_type());
+        else
+            steps(std::false_type());
     }
-    float e[P];
-#pragma unroll
-    for (int j = 0; j < P; j++) e[j] = a.dh_last && j < p.count ? a.dh_last[p.i * a.C + p.c + j] : 0.0f;
-    apply_tiles<P, true>(a, p, e, maps);
-#pragma unroll
-    for (int j = 0; j < P; j++) e[j] = __builtin_fmaf(eA[j], e[j], eR[j]);
+    if (scans && ch < a.C) {
+        if (MAPS)
+            a.maps[(p.i * a.segments + p.segment) * a.C + ch] = make_float2(carry_a, carry);
+        else if (p.segment == a.segments - 1)
+            a.h_last[p.i * a.C + ch] = carry;
+    }
+}
 
-    float fA[P], fB[P];
-    __syncthreads();
-    compose_tile<P, false>(p, A, B, fA, fB, tA, tR, maps);
-    const int64_t start = p.tile * (int64_t)(kWaves * kRun) * (64 / p.lanes);   // the tile's first step
-    const int64_t per = (a.L + kEvery - 1) / kEvery;
-    float state[P];
-#pragma unroll
-    for (int j = 0; j < P; j++) {
-        float s0 = start < a.L && j < p.count ? a.states[(p.i * per + start / kEvery) * a.C + p.c + j] : 0.0f;
-        state[j] = __builtin_fmaf(fA[j], s0, fB[j]);
+// The backward pass over a segment, from its last tile to its first.  MAPS:
+// only the map of the gradient that runs towards its start.
+template <int DT, bool MAPS, bool GATE>
+__global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a) {
+    constexpr int P = Elem<DT>::kPerWord, S = kRun<DT>;
+    __shared__ Scan scan, fscan;
+    const Place p = place_of<DT>(a);
+    const int channels = a.lanes * P;
+    const bool scans = threadIdx.x < channels;                    // the threads that go through the gradients' maps
+    const int other = a.waves > 1 ? 64 : 0;                       // and those that go through the states'
+    const bool fscans = (int)threadIdx.x >= other && (int)threadIdx.x < other + channels;
+    const int64_t c0 = p.c - p.cl * P, ch = c0 + threadIdx.x, fch = c0 + threadIdx.x - other;
+    float carry = 0.0f, carry_a = 1.0f;
+    if (scans && ch < a.C && !MAPS) {
+        if (a.dh_last) carry = a.dh_last[p.i * a.C + ch];
+        if (a.segments > 1) carry = scan_segments<true>(a, p, ch, carry);
     }
+    const int64_t first = (int64_t)p.segment * a.tiles * p.tile, per = (a.L + kEvery - 1) / kEvery;
+    for (int k = a.tiles - 1; k >= 0; k--) {
+        const int64_t tile0 = first + k * p.tile, t0 = tile0 + p.run * S;
+        if (k > 0 && tile0 >= a.L) continue;
+        uint32_t wv[S], wf[S], wo[S], wg[S];
+        load_run<DT>(a.f, p, t0, kKeep<DT>, wf);
+        load_run<DT>(a.dy, p, t0, 0, wg);
+        if (GATE) load_run<DT>(a.o, p, t0, 0, wo);
+        if (!MAPS) load_run<DT>(a.v, p, t0, 0, wv);
+        float state = 0.0f;
+        if (!MAPS && fscans && tile0 < a.L && fch < a.C) state = a.states[(p.i * per + tile0 / kEvery) * a.C + fch];
+
+        float fa[S][P], in[S][P], A[P], R[P], FA[P], B[P];
 #pragma unroll
-    for (int s = 0; s < kRun; s++)
+        for (int j = 0; j < P; j++) A[j] = 1.0f, R[j] = 0.0f, B[j] = 0.0f;
+#pragma unroll
+        for (int s = S - 1; s >= 0; s--)
+#pragma unroll
+            for (int j = 0; j < P; j++) {
+                float so = 1.0f, rest;
+                rocket::logistic<DT>(Elem<DT>::get(wf[s], j), fa[s][j], in[s][j]);
+                if (GATE) rocket::logistic<DT>(Elem<DT>::get(wo[s], j), so, rest);
+                const float g = GATE ? Elem<DT>::get(wg[s], j) * so : Elem<DT>::get(wg[s], j);
+                R[j] = fa[s][j] * (R[j] + g);
+                if (!MAPS) B[j] = __builtin_fmaf(A[j], in[s][j] * Elem<DT>::get(wv[s], j), B[j]);
+                A[j] *= fa[s][j];
+            }
+#pragma unroll
+        for (int j = 0; j < P; j++) FA[j] = A[j];
+        scan_lanes<P, true>(a, p, A, R, scan);
+        if (!MAPS) scan_lanes<P, false>(a, p, FA, B, fscan);
+        __syncthreads();
+        if (MAPS) {
+            if (scans)
+                for (int w = a.waves - 1; w >= 0; w--) {
+                    const float2 m = scan.map[w][threadIdx.x];
+                    carry = __builtin_fmaf(m.x, carry, m.y);
+                    carry_a *= m.x;
+                }
+            __syncthreads();
+            continue;
+        }
+        if (scans) scan_waves<true>(a.waves, threadIdx.x, carry, scan);
+        if (fscans) scan_waves<false>(a.waves, (int)threadIdx.x - other, state, fscan);
+        __syncthreads();
+
+        renew(wv);
+        renew(wg);
+        if (GATE) renew(wo);
+        float h[S][P], e[P];   // the state before each step
 #pragma unroll
         for (int j = 0; j < P; j++) {
-            float keep, in;
-            rocket::logistic(Elem<DT>::get(wf[s], j), keep, in);
-            h[s][j] = state[j];
-            state[j] = __builtin_fmaf(keep, state[j], in * Elem<DT>::get(wv[s], j));
+            const int at = p.cl * P + j;
+            e[j] = __builtin_fmaf(A[j], scan.start[p.wave][at], R[j]);
+            h[0][j] = __builtin_fmaf(FA[j], fscan.start[p.wave][at], B[j]);
         }
 #pragma unroll
-    for (int s = kRun - 1; s >= 0; s--) {
-        const bool live = p.t0 + s < p.len;
-        float gv[P], gf[P], go[P];
+        for (int s = 0; s + 1 < S; s++)
 #pragma unroll
-        for (int j = 0; j < P; j++) {
-            float keep, in, so = 1.0f, rest = 0.0f;
-            rocket::logistic(Elem<DT>::get(wf[s], j), keep, in);
-            if (GATE) rocket::logistic(Elem<DT>::get(wo[s], j), so, rest);
-            const float v = Elem<DT>::get(wv[s], j), dy = Elem<DT>::get(wg[s], j);
-            const float dh = __builtin_fmaf(dy, so, e[j]);
-            gv[j] = live ? dh * in : 0.0f;
-            gf[j] = live ? gv[j] * (h[s][j] - v) * keep : 0.0f;
-            if (GATE) go[j] = live ? dy * __builtin_fmaf(keep, h[s][j], in * v) * so * rest : 0.0f;
-            e[j] = live ? keep * dh : e[j];
-        }
-        if (p.t0 + s < a.L) {
-            store_step<DT>(a.dv, p, p.t0 + s, gv);
-            store_step<DT>(a.df, p, p.t0 + s, gf);
-            if (GATE) store_step<DT>(a.dO, p, p.t0 + s, go);
-        }
+            for (int j = 0; j < P; j++)
+                h[s + 1][j] = __builtin_fmaf(fa[s][j], h[s][j], in[s][j] * Elem<DT>::get(wv[s], j));
+        char *at_v = run_at<DT>(a.dv, p, t0), *at_f = run_at<DT>(a.df, p, t0);
+        char *at_o = GATE ? run_at<DT>(a.dO, p, t0) : nullptr;
+        auto steps = [&](auto whole) {
+#pragma unroll
+            for (int s = S - 1; s >= 0; s--) {
+                float xv[P], xf[P], xo[P];
+#pragma unroll
+                for (int j = 0; j < P; j++) {
+                    float so = 1.0f, rest = 0.0f;
+                    if (GATE) rocket::logistic<DT>(Elem<DT>::get(wo[s], j), so, rest);
+                    const float v = Elem<DT>::get(wv[s], j), dy = Elem<DT>::get(wg[s], j);
+                    const float dh = GATE ? __builtin_fmaf(dy, so, e[j]) : dy + e[j];
+                    xv[j] = dh * in[s][j];
+                    xf[j] = xv[j] * (h[s][j] - v) * fa[s][j];
+                    if (GATE) xo[j] = dy * __builtin_fmaf(fa[s][j], h[s][j], in[s][j] * v) * so * rest;
+                    e[j] = fa[s][j] * dh;
+                }
+                const bool live = t0 + s < p.len;
+                store_step<DT, whole.value>(at_v, a.dv.ts, p, s, a.L - t0, live ? Elem<DT>::put(xv) : 0);
+                store_step<DT, whole.value>(at_f, a.df.ts, p, s, a.L - t0, live ? Elem<DT>::put(xf) : 0);
+                if (GATE) store_step<DT, whole.value>(at_o, a.dO.ts, p, s, a.L - t0, live ? Elem<DT>::put(xo) : 0);
+            }
+        };
+        if (whole_run<DT>(p, t0, a.L))
+            steps(std::true_type());
+        else
+            steps(std::false_type());
     }
-    if (p.t0 == 0)
-#pragma unroll
-        for (int j = 0; j < P; j++)
-            if (j < p.count) a.dh0[p.i * a.C + p.c + j] = e[j];
+    if (scans && ch < a.C) {
+        if (MAPS)
+            a.maps[(p.i * a.segments + p.segment) * a.C + ch] = make_float2(carry_a, carry);
+        else if (p.segment == 0)
+            a.dh0[p.i * a.C + ch] = carry;
+    }
 }
 
 // One step of every series: a word of channels per thread.
@@ -422,12 +471,12 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
 #pragma unroll
     for (int j = 0; j < P; j++) {
         float keep, in;
-        rocket::logistic(Elem<DT>::get(wf, j), keep, in);
+        rocket::logistic<DT>(Elem<DT>::get(wf, j), keep, in);
         h[j] = __builtin_fmaf(keep, h[j], in * Elem<DT>::get(wv, j));
         y[j] = h[j];
         if (GATE) {
             float so, rest;
-            rocket::logistic(Elem<DT>::get(wo, j), so, rest);
+            rocket::logistic<DT>(Elem<DT>::get(wo, j), so, rest);
             y[j] *= so;
         }
     }
@@ -442,26 +491,33 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
 
 // How a call is cut.
 struct Cut {
-    int32_t lanes, blocks, tiles;
+    int32_t lanes, waves, blocks, segments, tiles;
     int64_t grid;
 };
 
-// Lanes over channels: the power of two that covers the words of channels, 64
+// Lanes over channels: the power of two that covers the words of channels, 32
 // at most; the wavefront's other lanes take further runs of steps, so that
-// few channels do not leave lanes idle.
+// few channels do not leave lanes idle.  Segments: as many as fill the chip
+// beside series and channel blocks, one where those do so alone.
 bool cut_of(const rocket_sequence_shape *s, Cut *cut) {
     const int64_t per_word = rocket::elem_size(s->dtype) == 4 ? 1 : 2;
     const int64_t words = (s->channels + per_word - 1) / per_word;
     cut->lanes = 1;
-    while (cut->lanes < 64 && cut->lanes < words) cut->lanes *= 2;
-    const int64_t steps = (int64_t)kWaves * kRun * (64 / cut->lanes);
+    while (cut->lanes < kMostLanes && cut->lanes < words) cut->lanes *= 2;
+    const int64_t in_wave = (64 / cut->lanes) * (kElems / per_word);   // steps of a wavefront
+    cut->waves = (int32_t)(in_wave < kEvery ? kEvery / in_wave : 1);
+    const int64_t tile = cut->waves * in_wave, tiles = s->steps > tile ? (s->steps + tile - 1) / tile : 1;
     cut->blocks = (int32_t)((words + cut->lanes - 1) / cut->lanes);
-    cut->tiles = (int32_t)(s->steps > steps ? (s->steps + steps - 1) / steps : 1);
-    return !__builtin_mul_overflow(s->n * cut->blocks, (int64_t)cut->tiles, &cut->grid) && cut->grid <= INT_MAX;
+    const int64_t rows = s->n * cut->blocks;
+    int64_t segments = rows > 0 ? (kFill + rows - 1) / rows : 1;
+    if (segments > tiles) segments = tiles;
+    cut->tiles = (int32_t)((tiles + segments - 1) / segments);
+    cut->segments = (int32_t)((tiles + cut->tiles - 1) / cut->tiles);
+    return !__builtin_mul_overflow(rows, (int64_t)cut->segments, &cut->grid) && cut->grid <= INT_MAX;
 }
 
 int64_t workspace_of(const rocket_sequence_shape *s, const Cut &cut) {
-    return cut.tiles > 1 ? s->n * cut.tiles * s->channels * (int64_t)sizeof(float2) : 0;
+    return cut.segments > 1 ? s->n * cut.segments * s->channels * (int64_t)sizeof(float2) : 0;
 }
 
 View view(const rocket_sequence *q, int size) {
@@ -472,14 +528,14 @@ bool aligned(const void *p, uintptr_t to) { return (uintptr_t)p % to == 0; }
 
 template <int DT, bool GATE>
 void run_forward(const RecArgs &a, const Cut &cut, hipStream_t s) {
-    if (cut.tiles > 1) forward_kernel<DT, true, GATE><<<(uint32_t)cut.grid, kThreads, 0, s>>>(a);
-    forward_kernel<DT, false, GATE><<<(uint32_t)cut.grid, kThreads, 0, s>>>(a);
+    if (cut.segments > 1) forward_kernel<DT, true, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+    forward_kernel<DT, false, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
 }
 
 template <int DT, bool GATE>
 void run_backward(const RecArgs &a, const Cut &cut, hipStream_t s) {
-    if (cut.tiles > 1) backward_kernel<DT, true, GATE><<<(uint32_t)cut.grid, kThreads, 0, s>>>(a);
-    backward_kernel<DT, false, GATE><<<(uint32_t)cut.grid, kThreads, 0, s>>>(a);
+    if (cut.segments > 1) backward_kernel<DT, true, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+    backward_kernel<DT, false, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
 }
 
 template <int DT, bool GATE>
@@ -525,7 +581,8 @@ extern "C" rocket_status rocket_recurrence_forward(const rocket_sequence_shape *
     a.v = view(v, size), a.f = view(f, size), a.o = view(o, size), a.y = view(y, size);
     a.n = shape->n, a.L = shape->steps, a.C = shape->channels, a.lengths = shape->lengths;
     a.h0 = h0, a.h_last = h_last, a.states = states, a.maps = (float2 *)workspace;
-    a.tiles = cut.tiles, a.lanes = cut.lanes, a.blocks = cut.blocks;
+    a.blocks = cut.blocks, a.lanes = cut.lanes, a.waves = cut.waves;
+    a.segments = cut.segments, a.tiles = cut.tiles;
     BY_TYPE(run_forward, shape->dtype, o != nullptr, a, cut, (hipStream_t)hip_stream);
     return rocket::launched();
 }
@@ -553,7 +610,8 @@ extern "C" rocket_status rocket_recurrence_backward(const rocket_sequence_shape 
     a.dy = view(dy, size), a.dv = view(dv, size), a.df = view(df, size), a.dO = view(dO, size);
     a.n = shape->n, a.L = shape->steps, a.C = shape->channels, a.lengths = shape->lengths;
     a.states = const_cast<float *>(states), a.dh_last = dh_last, a.dh0 = dh0, a.maps = (float2 *)workspace;
-    a.tiles = cut.tiles, a.lanes = cut.lanes, a.blocks = cut.blocks;
+    a.blocks = cut.blocks, a.lanes = cut.lanes, a.waves = cut.waves;
+    a.segments = cut.segments, a.tiles = cut.tiles;
     BY_TYPE(run_backward, shape->dtype, o != nullptr, a, cut, (hipStream_t)hip_stream);
     return rocket::launched();
 }
