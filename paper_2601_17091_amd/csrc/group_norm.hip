@@ -20,6 +20,7 @@
 // The last column of a slab is moved back so that it ends with the slab; the
 // channels it shares with its neighbour are computed twice and counted once.
 #include <climits>
+#include <type_traits>
 
 #include "sequence.h"
 
@@ -41,6 +42,7 @@ struct NormArgs {
     int32_t slabs, parts;      // slabs per series; parts > 1: slabs per group
     int32_t cols, rows;        // columns of a slab; steps a workgroup passes at once
     int32_t chunks;            // of steps
+    int32_t most_groups;       // groups of a slab, at most
     int32_t act;
     float eps;
     const float *w, *b;        // or null
@@ -66,6 +68,11 @@ struct Pack {
         rocket::store_at(p, o);
     }
     __device__ void clear() { v = vec{0, 0, 0, 0}; }
+    __device__ void renew() {
+        uint32_t w[4] = {v[0], v[1], v[2], v[3]};
+        rocket::renew(w);
+        v = vec{w[0], w[1], w[2], w[3]};
+    }
 };
 
 template <int DT>
@@ -77,37 +84,60 @@ struct Pack<DT, false> {
     __device__ float get(int) const { return Elem<DT>::one(v); }
     __device__ static void store(char *p, const float *f) { *(raw *)p = Elem<DT>::round(f[0]); }
     __device__ void clear() { v = 0; }
+    __device__ void renew() {}
 };
 
+// The normal distribution function and e = exp(-z^2 / 2).  fp32 elements: the
+// library's erf.  16-bit elements: formula 7.1.26 of Abramowitz and Stegun
+// (1964), erf to 1.5e-7, far below the elements' own rounding; its tail is a
+// product, so that small values of z < 0 keep their digits.
 template <int DT>
-__device__ inline float activate(float z, int act) {
-    switch (act) {
-    case ROCKET_ACT_RELU: return z < 0.0f ? 0.0f : z;
-    case ROCKET_ACT_SILU: {
+__device__ inline float normal_cdf(float z, float &e) {
+    e = rocket::exp_neg_abs<DT>(0.5f * z * z);
+    if (DT == ROCKET_FLOAT32) return 0.5f + 0.5f * erff(z * 0.70710678118654752f);
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(z), 0.3275911f * 0.70710678f, 1.0f));
+    float q = __builtin_fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+    q = __builtin_fmaf(t, q, 0.5f * 1.421413741f);
+    q = __builtin_fmaf(t, q, 0.5f * -0.284496736f);
+    q = __builtin_fmaf(t, q, 0.5f * 0.254829592f);
+    const float tail = q * t * e;
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+
+template <int DT, int ACT>
+__device__ inline float activate(float z) {
+    if (ACT == ROCKET_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if (ACT == ROCKET_ACT_SILU) {
         float s, rest;
         rocket::logistic<DT>(z, s, rest);
         return z * s;
     }
-    case ROCKET_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    default: return z;
+    if (ACT == ROCKET_ACT_GELU) {
+        float e;
+        return z * normal_cdf<DT>(z, e);
     }
+    return z;
 }
 
-template <int DT>
-__device__ inline float slope(float z, int act) {
-    switch (act) {
-    case ROCKET_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-    case ROCKET_ACT_SILU: {
-        float s, rest;
-        rocket::logistic<DT>(z, s, rest);
-        return s * (1.0f + z * rest);
+template <int DT, int ACT>
+__device__ inline float slope(float z) {
+    if (ACT == ROCKET_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (ACT == ROCKET_ACT_SILU) {
+        float s;
+        if (DT == ROCKET_FLOAT32) {
+            float rest;
+            rocket::logistic<DT>(z, s, rest);
+            return s * __builtin_fmaf(z, rest, 1.0f);
+        }
+        s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+        return s * (1.0f + __builtin_fmaf(-s, z, z));
     }
-    case ROCKET_ACT_GELU: {
-        float e = rocket::exp_neg_abs<DT>(0.5f * z * z);
-        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * e * 0.39894228040143268f;
+    if (ACT == ROCKET_ACT_GELU) {
+        float e;
+        const float c = normal_cdf<DT>(z, e);
+        return __builtin_fmaf(z * 0.39894228040143268f, e, c);
     }
-    default: return 1.0f;
-    }
+    return 1.0f;
 }
 
 // Where a workgroup and a thread work.
@@ -143,26 +173,68 @@ __device__ inline void place_thread(const NormArgs &a, Place &p) {
     if (!p.active) p.c = p.c0, p.skip = 0;
 }
 
-// Shared memory of the sums of a slab.
-template <int NT, int VEC>
+// Shared memory of a slab, sized by the launch.  Arrays of W start on 16 bytes.
 struct Scratch {
-    static constexpr int kMost = (NT < 256 ? NT : 256) * VEC;   // channels of a slab
-    float rows[NT * VEC];                                       // all rows' columns
-    float chan[NT > kMost ? NT : kMost];
-    float group[kMost];
-    float group2[kMost];
+    float *rows;             // [rows][W]: the threads' sums
+    float *chan;             // parts of the channels' sums
+    float *group, *group2;   // [groups of a slab]
+    float *of[4];            // [4][W]: what the elements of a channel are scaled by
+    float *first;            // [W], backward
+    float *total;            // [2][W], backward, held
 };
+
+__host__ __device__ inline int64_t scratch_floats(int threads, int vec, int cols, int rows, int groups, bool back) {
+    const int W = cols * vec;
+    return (int64_t)rows * W + ((threads > W ? threads : W) + 3) / 4 * 4 + 2 * ((groups + 3) / 4 * 4) +
+           (back ? 7 : 4) * W;
+}
+
+template <int NT, int VEC>
+__device__ inline Scratch scratch_of(const NormArgs &a) {
+    extern __shared__ __attribute__((aligned(16))) float shared[];
+    const int W = a.cols * VEC, groups = (a.most_groups + 3) / 4 * 4;
+    Scratch s;
+    s.of[0] = shared;
+    for (int k = 1; k < 4; k++) s.of[k] = s.of[k - 1] + W;
+    s.rows = s.of[3] + W;
+    s.chan = s.rows + a.rows * W;
+    s.group = s.chan + ((NT > W ? NT : W) + 3) / 4 * 4;
+    s.group2 = s.group + groups;
+    s.first = s.group2 + groups;
+    s.total = s.first + W;
+    return s;
+}
+
+// The values of an array of channels for a thread's column.
+template <int VEC>
+__device__ inline void of_column(const float *of, const Place &p, float (&v)[VEC]) {
+    const float *at = of + (p.c - p.c0);
+#pragma unroll
+    for (int e = 0; e < VEC; e++) v[e] = at[e];
+}
+
+// fn(channel of the slab, its group of the slab), a thread a channel.
+template <int NT, class Fn>
+__device__ inline void for_channels(const NormArgs &a, const Place &p, Fn fn) {
+    for (int ch = threadIdx.x; ch < p.c1 - p.c0; ch += NT) fn(ch, a.parts == 1 ? ch / a.width : 0);
+}
 
 // Sums acc over the workgroup's rows: s.chan[part * W + channel], `parts`
 // parts of every channel of the slab.
 template <int NT, int VEC>
-__device__ inline int sum_rows(const NormArgs &a, const Place &p, const float (&acc)[VEC], Scratch<NT, VEC> &s) {
+__device__ inline int sum_rows(const NormArgs &a, const Place &p, const float (&acc)[VEC], const Scratch &s) {
     const int W = p.c1 - p.c0;
     __syncthreads();   // rows and chan are free
     if (p.active) {
+        float *at = s.rows + p.row * W + p.c - p.c0;
+        if (p.skip == 0) {
 #pragma unroll
-        for (int e = 0; e < VEC; e++)
-            if (e >= p.skip) s.rows[p.row * W + p.c - p.c0 + e] = acc[e];
+            for (int e = 0; e < VEC; e++) at[e] = acc[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; e++)
+                if (e >= p.skip) at[e] = acc[e];
+        }
     }
     __syncthreads();
     const int parts = W < NT ? min(NT / W, a.rows) : 1;
@@ -179,28 +251,25 @@ __device__ inline int sum_rows(const NormArgs &a, const Place &p, const float (&
 }
 
 // group[k] = the sum over the slab's channels of group k of scale_c times the
-// channel's parts (scale may be null).
-template <int NT, int VEC>
-__device__ inline void sum_groups(const Place &p, int parts, const float *scale, Scratch<NT, VEC> &s, float *group) {
+// channel's `parts` values in `of` (scale may be null).
+template <int NT>
+__device__ inline void sum_groups(const Place &p, const float *of, int parts, const float *scale, float *group) {
     const int W = p.c1 - p.c0, each = W / p.ng;
+    auto channel = [&](int ch) {
+        float u = 0.0f;
+        for (int q = 0; q < parts; q++) u += of[q * W + ch];
+        return scale ? scale[p.c0 + ch] * u : u;
+    };
     if (each * parts <= 32) {
         for (int k = threadIdx.x; k < p.ng; k += NT) {
             float t = 0.0f;
-            for (int ch = k * each; ch < (k + 1) * each; ch++) {
-                float u = 0.0f;
-                for (int q = 0; q < parts; q++) u += s.chan[q * W + ch];
-                t += scale ? scale[p.c0 + ch] * u : u;
-            }
+            for (int ch = k * each; ch < (k + 1) * each; ch++) t += channel(ch);
             group[k] = t;
         }
     } else {
         for (int k = threadIdx.x >> 6; k < p.ng; k += NT >> 6) {
             float t = 0.0f;
-            for (int ch = k * each + (threadIdx.x & 63); ch < (k + 1) * each; ch += 64) {
-                float u = 0.0f;
-                for (int q = 0; q < parts; q++) u += s.chan[q * W + ch];
-                t += scale ? scale[p.c0 + ch] * u : u;
-            }
+            for (int ch = k * each + (threadIdx.x & 63); ch < (k + 1) * each; ch += 64) t += channel(ch);
 #pragma unroll
             for (int off = 32; off; off /= 2) t += __shfl_xor(t, off);
             if ((threadIdx.x & 63) == 0) group[k] = t;
@@ -216,14 +285,31 @@ __device__ inline int chunk_rows(const NormArgs &a, int64_t T, int chunk, int64_
     return (int)(left < 0 ? 0 : left < per ? left : per);
 }
 
+// The column of step `pass` + row of a workgroup's pass over `rows` steps, 0
+// past the series' own steps.
+template <class P>
+__device__ inline void load_row(P &v, const char *at, int pass, int rows, int row, int own, int64_t stride) {
+    if (pass + rows <= own) {   // the same for the whole workgroup
+        v.load(at + pass * stride);
+    } else {
+        v.clear();
+        if (pass + row < own) v.load(at + pass * stride);
+    }
+}
+
+template <int DT>
+__device__ inline char *column_at(const View &x, const Place &p, int64_t first) {
+    return x.p + p.i * x.ss + (first + p.row) * x.ts + (int64_t)p.c * Elem<DT>::kSize;
+}
+
 // Forward.  R: passes over the rows that a thread holds.
 template <int DT, bool WIDE, int NT, int R, int MODE>
-__global__ __launch_bounds__(NT) void norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a) {
     using P = Pack<DT, WIDE>;
     constexpr int VEC = P::kN;
-    __shared__ Scratch<NT, VEC> s;
+    const Scratch s = scratch_of<NT, VEC>(a);
     Place p;
-    const int64_t b = blockIdx.x;
+    const int64_t b = rocket::item_of_block();
     p.slab = (int)(b % a.slabs);
     p.chunk = (int)(b / a.slabs % a.chunks);
     p.i = b / a.slabs / a.chunks;
@@ -232,23 +318,18 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs a) {
     int64_t first;
     const int own = chunk_rows(a, T, p.chunk, per, first);
 
-    P held[R];
-    const char *x = a.x.p + p.i * a.x.ss + first * a.x.ts + (int64_t)p.c * Elem<DT>::kSize;
+    // Columns at a time: all that the thread holds, or four in a second launch.
+    constexpr int H = MODE == kApply && R > 4 ? 4 : R;
+    P held[H];
+    const char *x = column_at<DT>(a.x, p, first);
+    auto load = [&](int j0) {
 #pragma unroll
-    for (int j = 0; j < R; j++) {
-        if (j * a.rows < own) {
-            const int r = p.row + j * a.rows;
-            held[j].load(x + (int64_t)(r < own ? r : own - 1) * a.x.ts);
-        } else {
-            held[j].clear();
-        }
-    }
-    int group_of[VEC];   // within the slab
-#pragma unroll
-    for (int e = 0; e < VEC; e++) group_of[e] = a.parts == 1 ? (p.c + e - p.c0) / a.width : 0;
+        for (int j = 0; j < H; j++) load_row<P>(held[j], x, (j0 + j) * a.rows, a.rows, p.row, own, a.x.ts);
+    };
 
     const int W = p.c1 - p.c0, each = W / p.ng;
     if (MODE != kApply) {
+        load(0);
         float acc[VEC];
 #pragma unroll
         for (int e = 0; e < VEC; e++) acc[e] = 0.0f;
@@ -259,12 +340,16 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs a) {
                 for (int e = 0; e < VEC; e++) acc[e] += held[j].get(e);
             }
         int parts = sum_rows<NT, VEC>(a, p, acc, s);
-        sum_groups<NT, VEC>(p, parts, nullptr, s, s.group);
-        const float count = (float)own * (float)each;
-        const float inv = own ? 1.0f / count : 0.0f;
+        sum_groups<NT>(p, s.chan, parts, nullptr, s.group);
+        const float inv = own ? 1.0f / ((float)own * (float)each) : 0.0f;
+        for_channels<NT>(a, p, [&](int ch, int g) { s.of[0][ch] = s.group[g] * inv; });
+        __syncthreads();
         float m[VEC];
+        of_column<VEC>(s.of[0], p, m);
 #pragma unroll
-        for (int e = 0; e < VEC; e++) m[e] = s.group[group_of[e]] * inv, acc[e] = 0.0f;
+        for (int e = 0; e < VEC; e++) acc[e] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < H; j++) held[j].renew();
 #pragma unroll
         for (int j = 0; j < R; j++)
             if (p.row + j * a.rows < own) {
@@ -275,7 +360,7 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs a) {
                 }
             }
         parts = sum_rows<NT, VEC>(a, p, acc, s);
-        sum_groups<NT, VEC>(p, parts, nullptr, s, s.group2);
+        sum_groups<NT>(p, s.chan, parts, nullptr, s.group2);
         if (MODE == kStats) {
             const int K = a.chunks * a.parts, k = p.chunk * a.parts + (a.parts > 1 ? p.slab % a.parts : 0);
             for (int g = threadIdx.x; g < p.ng; g += NT)
@@ -288,7 +373,6 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs a) {
             a.mean[p.i * a.G + p.g0 + g] = mean;
             a.rstd[p.i * a.G + p.g0 + g] = rstd;
         }
-        __syncthreads();
     } else {
         // merge the chunks' statistics: N = sum n_k, m = sum n_k m_k / N,
         // squares = sum (squares_k + n_k (m_k - m)^2)
@@ -324,83 +408,124 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs a) {
                 }
             }
         }
-        __syncthreads();
     }
+    __syncthreads();
+    for_channels<NT>(a, p, [&](int ch, int g) {
+        s.of[0][ch] = s.group[g];
+        s.of[1][ch] = s.group2[g] * (a.w ? a.w[p.c0 + ch] : 1.0f);
+        s.of[2][ch] = a.b ? a.b[p.c0 + ch] : 0.0f;
+    });
+    __syncthreads();
 
     if (!p.active) return;
     float m[VEC], sc[VEC], sh[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; e++) {
-        m[e] = s.group[group_of[e]];
-        sc[e] = s.group2[group_of[e]] * (a.w ? a.w[p.c + e] : 1.0f);
-        sh[e] = a.b ? a.b[p.c + e] : 0.0f;
-    }
-    char *out = a.out.p + p.i * a.out.ss + first * a.out.ts + (int64_t)p.c * Elem<DT>::kSize;
+    of_column<VEC>(s.of[0], p, m);
+    of_column<VEC>(s.of[1], p, sc);
+    of_column<VEC>(s.of[2], p, sh);
+    char *out = column_at<DT>(a.out, p, first);
     const int64_t rest = a.L - first;
+    auto write = [&](int j0, auto act) {
 #pragma unroll
-    for (int j = 0; j < R; j++) {
-        const int r = p.row + j * a.rows;
-        if (r >= rest) break;
-        float y[VEC];
+        for (int j = 0; j < H; j++) {
+            const int pass = (j0 + j) * a.rows, r = p.row + pass;
+            float y[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; e++)
-            y[e] = r < own ? activate<DT>(__builtin_fmaf(held[j].get(e) - m[e], sc[e], sh[e]), a.act) : 0.0f;
-        P::store(out + (int64_t)r * a.out.ts, y);
+            for (int e = 0; e < VEC; e++) y[e] = 0.0f;
+            if (r < own) {
+#pragma unroll
+                for (int e = 0; e < VEC; e++)
+                    y[e] = activate<DT, act.value>(__builtin_fmaf(held[j].get(e) - m[e], sc[e], sh[e]));
+            }
+            if (r < rest) P::store(out + pass * a.out.ts, y);
+        }
+    };
+    for (int j0 = 0; j0 < R && j0 * a.rows < rest; j0 += H) {
+        if (MODE == kApply) load(j0);
+#pragma unroll
+        for (int j = 0; j < H; j++) held[j].renew();
+        switch (a.act) {
+        case ROCKET_ACT_RELU: write(j0, std::integral_constant<int, ROCKET_ACT_RELU>()); break;
+        case ROCKET_ACT_SILU: write(j0, std::integral_constant<int, ROCKET_ACT_SILU>()); break;
+        case ROCKET_ACT_GELU: write(j0, std::integral_constant<int, ROCKET_ACT_GELU>()); break;
+        default: write(j0, std::integral_constant<int, ROCKET_ACT_NONE>());
+        }
     }
 }
 
+// What the backward pass keeps of an element's channel.  z is the fused
+// x A + B with A = r w and B = b - m A, but for ReLU: there z is rounded step by
+// step as the formula is written, since the slope jumps with z's sign.
+template <int VEC, int ACT>
+struct Channel {
+    static constexpr bool kSteps = ACT == ROCKET_ACT_RELU;
+    float A[VEC], B[VEC];                                // x A + B; in steps: w and b
+    float m[kSteps ? VEC : 1], r[kSteps ? VEC : 1];
+    __device__ float z(float x, int e) const {
+        if (kSteps) return (x - m[kSteps ? e : 0]) * r[kSteps ? e : 0] * A[e] + B[e];
+        return __builtin_fmaf(x, A[e], B[e]);
+    }
+    __device__ float scale(int e) const { return kSteps ? A[e] * r[kSteps ? e : 0] : A[e]; }
+    __device__ void take(const Scratch &s, const Place &p) {
+        of_column<VEC>(s.of[0], p, A);
+        of_column<VEC>(s.of[1], p, B);
+        if constexpr (kSteps) {
+            of_column<VEC>(s.of[2], p, m);
+            of_column<VEC>(s.of[3], p, r);
+        }
+    }
+};
+
 // Backward.  Held: a workgroup goes through the series b, b + a.series, ... and
 // keeps the channel sums over them; kStats leaves the channel sums of a chunk.
-template <int DT, bool WIDE, int NT, int R, int MODE>
-__global__ __launch_bounds__(NT) void norm_back_kernel(NormArgs a) {
+// sum dz xh is gathered as sum dz (x - k), k the mean of the slab's first
+// group, and completed once a channel: r (sum dz (x - k) - (m - k) sum dz).
+template <int DT, bool WIDE, int NT, int R, int MODE, int ACT>
+__global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
     using P = Pack<DT, WIDE>;
     constexpr int VEC = P::kN;
-    __shared__ Scratch<NT, VEC> s;
-    __shared__ float total[2][MODE == kHeld ? Scratch<NT, VEC>::kMost : 1];
+    const Scratch s = scratch_of<NT, VEC>(a);
     Place p;
-    const int64_t b = blockIdx.x;
+    const int64_t b = rocket::item_of_block();
     p.slab = (int)(b % a.slabs);
     p.chunk = MODE == kHeld ? 0 : (int)(b / a.slabs % a.chunks);
     const int64_t begin = MODE == kHeld ? b / a.slabs : b / a.slabs / a.chunks;
     place_thread<NT, VEC>(a, p);
     const int W = p.c1 - p.c0;
     const int64_t per = (int64_t)R * a.rows;
-    int group_of[VEC];
-    float w[VEC], bias[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; e++) {
-        group_of[e] = a.parts == 1 ? (p.c + e - p.c0) / a.width : 0;
-        w[e] = a.w ? a.w[p.c + e] : 1.0f;
-        bias[e] = a.b ? a.b[p.c + e] : 0.0f;
-    }
     if (MODE == kHeld)
-        for (int ch = threadIdx.x; ch < W; ch += NT) total[0][ch] = 0.0f, total[1][ch] = 0.0f;
+        for (int ch = threadIdx.x; ch < W; ch += NT) s.total[ch] = 0.0f, s.total[W + ch] = 0.0f;
+    constexpr int H = MODE == kApply && R > 2 ? 2 : R;
 
     for (p.i = begin; p.i < a.n; p.i += MODE == kHeld ? a.series : a.n) {
+        // as if new: what follows from them is not kept across series
+        asm("" : "+v"(p.row), "+v"(p.c), "+s"(a.x.ts), "+s"(a.dy.ts), "+s"(a.out.ts));
         const int64_t T = rocket::steps_of(a.lengths, p.i, a.L);
         int64_t first;
         const int own = chunk_rows(a, T, p.chunk, per, first);
-        P hx[R], hg[R];
-        const char *x = a.x.p + p.i * a.x.ss + first * a.x.ts + (int64_t)p.c * Elem<DT>::kSize;
-        const char *dy = a.dy.p + p.i * a.dy.ss + first * a.dy.ts + (int64_t)p.c * Elem<DT>::kSize;
+        P hx[H], hg[H];
+        const char *x = column_at<DT>(a.x, p, first), *dy = column_at<DT>(a.dy, p, first);
+        auto load = [&](int j0) {
 #pragma unroll
-        for (int j = 0; j < R; j++) {
-            if (j * a.rows < own) {
-                const int r = p.row + j * a.rows, rr = r < own ? r : own - 1;
-                hx[j].load(x + (int64_t)rr * a.x.ts);
-                hg[j].load(dy + (int64_t)rr * a.dy.ts);
-            } else {
-                hx[j].clear();
-                hg[j].clear();
+            for (int j = 0; j < H; j++) {
+                load_row<P>(hx[j], x, (j0 + j) * a.rows, a.rows, p.row, own, a.x.ts);
+                load_row<P>(hg[j], dy, (j0 + j) * a.rows, a.rows, p.row, own, a.dy.ts);
             }
-        }
-        float m[VEC], rs[VEC];
-#pragma unroll
-        for (int e = 0; e < VEC; e++) {
-            m[e] = a.mean[p.i * a.G + p.g0 + group_of[e]];
-            rs[e] = a.rstd[p.i * a.G + p.g0 + group_of[e]];
-        }
+        };
+        if (MODE != kApply) load(0);
+        const float *mean = a.mean + p.i * a.G + p.g0, *rstd = a.rstd + p.i * a.G + p.g0;
+        for_channels<NT>(a, p, [&](int ch, int g) {
+            const float m = mean[g], r = rstd[g], w = a.w ? a.w[p.c0 + ch] : 1.0f, bias = a.b ? a.b[p.c0 + ch] : 0.0f;
+            if (ACT == ROCKET_ACT_RELU) {
+                s.of[0][ch] = w, s.of[1][ch] = bias, s.of[2][ch] = m, s.of[3][ch] = r;
+            } else {
+                s.of[0][ch] = r * w, s.of[1][ch] = __builtin_fmaf(-m, r * w, bias);
+            }
+        });
+        __syncthreads();
         if (MODE != kApply) {
+            Channel<VEC, ACT> of;
+            of.take(s, p);
+            const float k = mean[0];
             float sd[VEC], sx[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; e++) sd[e] = 0.0f, sx[e] = 0.0f;
@@ -409,25 +534,36 @@ __global__ __launch_bounds__(NT) void norm_back_kernel(NormArgs a) {
                 if (p.row + j * a.rows < own) {
 #pragma unroll
                     for (int e = 0; e < VEC; e++) {
-                        const float xh = (hx[j].get(e) - m[e]) * rs[e];
-                        const float dz = hg[j].get(e) * slope<DT>(xh * w[e] + bias[e], a.act);
+                        const float v = hx[j].get(e);
+                        const float dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
                         sd[e] += dz;
-                        sx[e] = __builtin_fmaf(dz, xh, sx[e]);
+                        sx[e] = __builtin_fmaf(dz, v - k, sx[e]);
                     }
                 }
-            for (int q = 0; q < 2; q++) {
-                const int parts = q ? sum_rows<NT, VEC>(a, p, sx, s) : sum_rows<NT, VEC>(a, p, sd, s);
-                for (int ch = threadIdx.x; ch < W; ch += NT) {
-                    float t = 0.0f;
-                    for (int k = 0; k < parts; k++) t += s.chan[k * W + ch];
-                    if (MODE == kHeld)
-                        total[q][ch] += t;
-                    else
-                        a.sums[((p.i * a.chunks + p.chunk) * 2 + q) * a.C + p.c0 + ch] = t;
-                }
-                if (MODE == kHeld) sum_groups<NT, VEC>(p, parts, a.w, s, q ? s.group2 : s.group);
+            int parts = sum_rows<NT, VEC>(a, p, sd, s);
+            for (int ch = threadIdx.x; ch < W; ch += NT) {
+                float t = 0.0f;
+                for (int q = 0; q < parts; q++) t += s.chan[q * W + ch];
+                s.first[ch] = t;
             }
+            if (MODE == kHeld) sum_groups<NT>(p, s.chan, parts, a.w, s.group);
+            parts = sum_rows<NT, VEC>(a, p, sx, s);
+            for_channels<NT>(a, p, [&](int ch, int g) {
+                const float d = s.first[ch];
+                float t = 0.0f;
+                for (int q = 0; q < parts; q++) t += s.chan[q * W + ch];
+                t = rstd[g] * __builtin_fmaf(k - mean[g], d, t);
+                if (MODE == kHeld) {
+                    s.total[ch] += d, s.total[W + ch] += t;
+                } else {
+                    float *sum = a.sums + (p.i * a.chunks + p.chunk) * 2 * a.C + p.c0 + ch;
+                    sum[0] = d, sum[a.C] = t;
+                }
+                s.first[ch] = t;
+            });
             if (MODE == kStats) return;
+            __syncthreads();
+            sum_groups<NT>(p, s.first, 1, a.w, s.group2);
         } else {
             // the groups' sums from the chunks' channel sums
             for (int k = threadIdx.x >> 6; k < 2 * p.ng; k += NT >> 6) {
@@ -435,9 +571,9 @@ __global__ __launch_bounds__(NT) void norm_back_kernel(NormArgs a) {
                 float t = 0.0f;
                 for (int ch = threadIdx.x & 63; ch < a.width; ch += 64) {
                     const int c = (p.g0 + g) * a.width + ch;
+                    const float *sum = a.sums + (p.i * a.chunks * 2 + q) * a.C + c;
                     float u = 0.0f;
-                    for (int chunk = 0; chunk < a.chunks; chunk++)
-                        u += a.sums[((p.i * a.chunks + chunk) * 2 + q) * a.C + c];
+                    for (int chunk = 0; chunk < a.chunks; chunk++) u += sum[(int64_t)chunk * 2 * a.C];
                     t += a.w ? a.w[c] * u : u;
                 }
 #pragma unroll
@@ -446,33 +582,48 @@ __global__ __launch_bounds__(NT) void norm_back_kernel(NormArgs a) {
             }
             __syncthreads();
         }
+        // dx = r (dz w - mean(g) - xh mean(g xh)) = dz r w - (x D + E)
+        const float inv = T ? 1.0f / ((float)T * (float)a.width) : 0.0f;
+        for_channels<NT>(a, p, [&](int ch, int g) {
+            const float m = mean[g], r = rstd[g], D = r * r * (s.group2[g] * inv);
+            s.chan[ch] = D;
+            s.first[ch] = __builtin_fmaf(-m, D, r * (s.group[g] * inv));
+        });
+        __syncthreads();
         if (p.active) {
-            const float inv = T ? 1.0f / ((float)T * (float)a.width) : 0.0f;
-            float mg[VEC], mx[VEC];
-#pragma unroll
-            for (int e = 0; e < VEC; e++) mg[e] = s.group[group_of[e]] * inv, mx[e] = s.group2[group_of[e]] * inv;
-            char *out = a.out.p + p.i * a.out.ss + first * a.out.ts + (int64_t)p.c * Elem<DT>::kSize;
+            Channel<VEC, ACT> of;
+            float D[VEC], E[VEC];
+            of.take(s, p);
+            of_column<VEC>(s.chan, p, D);
+            of_column<VEC>(s.first, p, E);
+            char *out = column_at<DT>(a.out, p, first);
             const int64_t rest = a.L - first;
+            for (int j0 = 0; j0 < R && j0 * a.rows < rest; j0 += H) {
+                if (MODE == kApply) load(j0);
 #pragma unroll
-            for (int j = 0; j < R; j++) {
-                const int r = p.row + j * a.rows;
-                if (r >= rest) break;
-                float dx[VEC];
+                for (int j = 0; j < H; j++) {
+                    const int pass = (j0 + j) * a.rows, r = p.row + pass;
+                    float dx[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; e++) {
-                    const float xh = (hx[j].get(e) - m[e]) * rs[e];
-                    const float g = hg[j].get(e) * slope<DT>(xh * w[e] + bias[e], a.act) * w[e];
-                    dx[e] = r < own ? rs[e] * (g - mg[e] - xh * mx[e]) : 0.0f;
+                    for (int e = 0; e < VEC; e++) dx[e] = 0.0f;
+                    if (r < own) {
+                        hx[j].renew(), hg[j].renew();
+#pragma unroll
+                        for (int e = 0; e < VEC; e++) {
+                            const float v = hx[j].get(e), dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
+                            dx[e] = __builtin_fmaf(dz, of.scale(e), -__builtin_fmaf(v, D[e], E[e]));
+                        }
+                    }
+                    if (r < rest) P::store(out + pass * a.out.ts, dx);
                 }
-                P::store(out + (int64_t)r * a.out.ts, dx);
             }
         }
-        if (MODE == kHeld) __syncthreads();   // group and group2 are free again
+        if (MODE == kHeld) __syncthreads();   // the shared arrays are free again
     }
     if (MODE == kHeld)
         for (int q = 0; q < 2; q++)
             for (int ch = threadIdx.x; ch < W; ch += NT)
-                a.sums[(begin * 2 + q) * a.C + p.c0 + ch] = total[q][ch];
+                a.sums[(begin * 2 + q) * a.C + p.c0 + ch] = s.total[q * W + ch];
 }
 
 // Rows of channel sums to fewer rows: out[o, q, c] = the sum of in[r, q, c]
@@ -502,12 +653,35 @@ struct Cut {
     bool wide, held;
     int32_t width, slabs, parts, cols, rows, threads, run, chunks;
     int32_t series;     // backward, held
+    int32_t groups;     // of a slab, at most
     int64_t grid;
     int64_t sum_rows;   // backward: rows of channel sums
     int64_t folded;     // rows after the first fold, 0: one fold is enough
 };
 
 constexpr int kFold = 128;
+// Workgroups that hold a slab: threads, and 16-byte columns of a thread (of
+// each operand); the last is also the size of a chunk's workgroup.
+constexpr int kSizes[4][2] = {{64, 4}, {256, 4}, {256, 16}, {512, 16}};
+constexpr int kBackSizes[4][2] = {{64, 4}, {256, 4}, {256, 8}, {512, 8}};
+
+// The slabs for `per` groups each, and the smallest workgroup that holds one.
+bool hold(const rocket_sequence_shape *s, int32_t groups, int64_t per, int vec, bool back, Cut *cut) {
+    const int64_t L = s->steps > 0 ? s->steps : 1;
+    cut->slabs = (int32_t)((groups + per - 1) / per);
+    const int64_t most = (groups + cut->slabs - 1) / cut->slabs;   // the most groups a slab gets
+    cut->cols = (int32_t)((most * cut->width + vec - 1) / vec);
+    cut->groups = (int32_t)most;
+    const int(*sizes)[2] = back ? kBackSizes : kSizes;
+    for (int k = cut->wide ? 0 : 2; k < (cut->wide ? 4 : 3); k++) {
+        const int rows = sizes[k][0] / cut->cols;
+        if (rows >= 1 && (int64_t)rows * sizes[k][1] >= L) {
+            cut->threads = sizes[k][0], cut->run = sizes[k][1], cut->rows = rows;
+            return true;
+        }
+    }
+    return false;
+}
 
 bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut) {
     const int size = rocket::elem_size(s->dtype), vec_wide = 16 / size;
@@ -516,48 +690,39 @@ bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut)
     cut->width = (int32_t)width;
     const int vec = cut->wide ? vec_wide : 1;
     const int64_t most = 256 * (int64_t)vec;   // channels of a slab
-    // A slab is at least 128 bytes wide, and wider while that leaves
-    // workgroups for the whole chip and the slab is small.
-    int64_t per = 1;
     cut->parts = 1;
+    cut->held = false;
     if (width > most) {
         cut->parts = (int32_t)((width + most - 1) / most);
         cut->slabs = (int32_t)(groups * cut->parts);
+        cut->groups = 1;
         int64_t part = (width + cut->parts - 1) / cut->parts;
         cut->cols = (int32_t)((part + vec - 1) / vec);
     } else {
+        // A slab is at least 128 bytes wide (a cache line), and wider while
+        // that leaves workgroups for the whole chip and the slab is small.
+        // 64 bytes where only that is held.
+        int64_t per = 1, half = 1;
+        while (half < groups && half * width * size < 64) half++;
         while (per < groups && per * width * size < 128) per++;
         while (per * 2 <= groups && per * 2 * width <= most && per * width * size * L < (16 << 10) &&
                s->n * ((groups + 2 * per - 1) / (2 * per)) >= 1024)
             per *= 2;
-        cut->slabs = (int32_t)((groups + per - 1) / per);
-        per = (groups + cut->slabs - 1) / cut->slabs;   // the most groups a slab gets
-        cut->cols = (int32_t)((per * width + vec - 1) / vec);
-    }
-    // Held where the slab fits: the smallest workgroup that holds it.
-    static const int kSizes[5][2] = {{64, 4}, {256, 4}, {256, 16}, {512, 16}, {1024, 16}};
-    static const int kBackSizes[5][2] = {{64, 4}, {256, 4}, {256, 8}, {512, 8}, {512, 8}};
-    const int(*sizes)[2] = back ? kBackSizes : kSizes;
-    cut->held = false;
-    for (int k = 0; k < 5 && cut->parts == 1; k++) {
-        if (!cut->wide && k != 2) continue;
-        const int rows = sizes[k][0] / cut->cols;
-        if (rows >= 1 && (int64_t)rows * sizes[k][1] >= L) {
-            cut->held = true, cut->threads = sizes[k][0], cut->run = sizes[k][1], cut->rows = rows;
-            break;
-        }
+        cut->held = hold(s, groups, per, vec, back, cut) ||
+                    (half < per && hold(s, groups, half, vec, back, cut));
+        if (!cut->held) hold(s, groups, per, vec, back, cut);
     }
     cut->chunks = 1;
     cut->folded = 0;
     if (!cut->held) {
-        cut->threads = 256, cut->run = sizes[2][1], cut->rows = 256 / cut->cols;
+        cut->threads = 256, cut->run = back ? kBackSizes[2][1] : kSizes[2][1], cut->rows = 256 / cut->cols;
         const int64_t step = (int64_t)cut->rows * cut->run, chunks = (L + step - 1) / step;
         if (chunks > INT_MAX) return false;
         cut->chunks = (int32_t)chunks;
         if (__builtin_mul_overflow(s->n * chunks, (int64_t)cut->slabs, &cut->grid)) return false;
         cut->sum_rows = s->n * chunks;
     } else if (back) {
-        int64_t series = (2048 + cut->slabs - 1) / cut->slabs;
+        int64_t series = (1024 + cut->slabs - 1) / cut->slabs;
         if (series > s->n) series = s->n;
         cut->series = (int32_t)(series > 0 ? series : 1);
         cut->grid = (int64_t)cut->series * cut->slabs;
@@ -577,15 +742,23 @@ int64_t workspace_of(const rocket_sequence_shape *s, int32_t groups, bool back, 
 
 template <int DT, bool BACK, bool WIDE, int NT, int R, int MODE>
 void go(const NormArgs &a, const Cut &c, hipStream_t s) {
-    if (BACK)
-        norm_back_kernel<DT, WIDE, NT, R, MODE><<<(uint32_t)c.grid, NT, 0, s>>>(a);
-    else
-        norm_kernel<DT, WIDE, NT, R, MODE><<<(uint32_t)c.grid, NT, 0, s>>>(a);
+    const uint32_t grid = (uint32_t)c.grid;
+    const int lds = (int)scratch_floats(NT, Pack<DT, WIDE>::kN, c.cols, c.rows, c.groups, BACK) * 4;
+    if constexpr (!BACK) {
+        norm_kernel<DT, WIDE, NT, R, MODE><<<grid, NT, lds, s>>>(a);
+    } else {
+        switch (a.act) {
+        case ROCKET_ACT_RELU: norm_back_kernel<DT, WIDE, NT, R, MODE, ROCKET_ACT_RELU><<<grid, NT, lds, s>>>(a); break;
+        case ROCKET_ACT_SILU: norm_back_kernel<DT, WIDE, NT, R, MODE, ROCKET_ACT_SILU><<<grid, NT, lds, s>>>(a); break;
+        case ROCKET_ACT_GELU: norm_back_kernel<DT, WIDE, NT, R, MODE, ROCKET_ACT_GELU><<<grid, NT, lds, s>>>(a); break;
+        default: norm_back_kernel<DT, WIDE, NT, R, MODE, ROCKET_ACT_NONE><<<grid, NT, lds, s>>>(a);
+        }
+    }
 }
 
 template <int DT, bool BACK>
 void run(const NormArgs &a, const Cut &c, hipStream_t s) {
-    constexpr int kLong = BACK ? 8 : 16;   // passes of the larger sizes
+    constexpr int kLong = BACK ? kBackSizes[2][1] : kSizes[2][1];   // columns of a thread in the larger sizes
     if (!c.held) {
         if (c.wide) {
             go<DT, BACK, true, 256, kLong, kStats>(a, c, s);
@@ -602,10 +775,8 @@ void run(const NormArgs &a, const Cut &c, hipStream_t s) {
         go<DT, BACK, true, 256, 4, kHeld>(a, c, s);
     } else if (c.threads == 256) {
         go<DT, BACK, true, 256, kLong, kHeld>(a, c, s);
-    } else if (c.threads == 512) {
+    } else {
         go<DT, BACK, true, 512, kLong, kHeld>(a, c, s);
-    } else if constexpr (!BACK) {
-        go<DT, BACK, true, 1024, kLong, kHeld>(a, c, s);
     }
 }
 
@@ -636,7 +807,7 @@ NormArgs args_of(const rocket_sequence_shape *shape, int32_t groups, int32_t act
     NormArgs a = {};
     a.n = shape->n, a.L = shape->steps, a.C = (int32_t)shape->channels, a.G = groups, a.width = cut.width;
     a.slabs = cut.slabs, a.parts = cut.parts, a.cols = cut.cols, a.rows = cut.rows, a.chunks = cut.chunks;
-    a.act = act, a.w = w, a.b = b, a.lengths = shape->lengths, a.series = cut.series;
+    a.most_groups = cut.groups, a.act = act, a.w = w, a.b = b, a.lengths = shape->lengths, a.series = cut.series;
     return a;
 }
 

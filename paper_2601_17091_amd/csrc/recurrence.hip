@@ -84,7 +84,7 @@ template <int DT>
 __device__ inline Place place_of(const RecArgs &a) {
     constexpr int P = Elem<DT>::kPerWord;
     Place p;
-    const int64_t b = blockIdx.x;
+    const int64_t b = rocket::item_of_block();
     const int64_t cb = b % a.blocks, rest = b / a.blocks;
     p.i = rest % a.n;
     p.segment = (int)(rest / a.n);
@@ -129,14 +129,6 @@ __device__ inline void load_run(const View &x, const Place &p, int64_t t0, uint3
 template <int DT>
 __device__ inline bool whole_run(const Place &p, int64_t t0, int64_t L) {
     return p.count == Elem<DT>::kPerWord && t0 + kRun<DT> <= L;
-}
-
-// Makes the compiler take the words as new, so that it unpacks them (and
-// computes gates of them) again instead of holding the results in registers.
-template <int N>
-__device__ inline void renew(uint32_t (&w)[N]) {
-#pragma unroll
-    for (int s = 0; s < N; s++) asm("" : "+v"(w[s]));
 }
 
 // Writes the packed word of step t of a run that starts at `at`, checked
@@ -385,9 +377,9 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a)
         if (fscans) scan_waves<false>(a.waves, (int)threadIdx.x - other, state, fscan);
         __syncthreads();
 
-        renew(wv);
-        renew(wg);
-        if (GATE) renew(wo);
+        rocket::renew(wv);
+        rocket::renew(wg);
+        if (GATE) rocket::renew(wo);
         float h[S][P], e[P];   // the state before each step
 #pragma unroll
         for (int j = 0; j < P; j++) {

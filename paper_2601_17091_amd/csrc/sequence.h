@@ -104,6 +104,22 @@ __device__ inline void logistic(float x, float &s, float &rest) {
     rest = pos ? small : big;
 }
 
+// Makes the compiler take the words as new, so that what it computed of them
+// is computed again instead of being held in registers across a barrier.
+template <int N>
+__device__ inline void renew(uint32_t (&w)[N]) {
+#pragma unroll
+    for (int s = 0; s < N; s++) asm("" : "+v"(w[s]));
+}
+
+// The work item of a workgroup: workgroups go to the 8 XCDs in turn, and each
+// XCD has an L2 of its own, so that items in a row (which share cache lines at
+// their borders) are given to workgroups of one XCD.
+__device__ inline int64_t item_of_block() {
+    const uint32_t b = blockIdx.x, x = b & 7, each = gridDim.x >> 3, more = gridDim.x & 7;
+    return (int64_t)x * each + (x < more ? x : more) + (b >> 3);
+}
+
 // Steps of series i: its length, clamped into [0, L].
 __device__ inline int64_t steps_of(const int32_t *lengths, int64_t i, int64_t L) {
     if (!lengths) return L;
