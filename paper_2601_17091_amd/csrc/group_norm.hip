@@ -479,7 +479,7 @@ struct Channel {
 // keeps the channel sums over them; kStats leaves the channel sums of a chunk.
 // sum dz xh is gathered as sum dz (x - k), k the mean of the slab's first
 // group, and completed once a channel: r (sum dz (x - k) - (m - k) sum dz).
-template <int DT, bool WIDE, int NT, int R, int MODE, int ACT>
+template <int DT, bool WIDE, int NT, int R, int MODE, int ACT, bool ONE>
 __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
     using P = Pack<DT, WIDE>;
     constexpr int VEC = P::kN;
@@ -496,22 +496,22 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
         for (int ch = threadIdx.x; ch < W; ch += NT) s.total[ch] = 0.0f, s.total[W + ch] = 0.0f;
     constexpr int H = MODE == kApply && R > 2 ? 2 : R;
 
-    for (p.i = begin; p.i < a.n; p.i += MODE == kHeld ? a.series : a.n) {
+    P hx[H], hg[H];
+    int64_t first, T = rocket::steps_of(a.lengths, begin, a.L);
+    int own = chunk_rows(a, T, p.chunk, per, first);
+    p.i = begin;
+    const char *x = column_at<DT>(a.x, p, first), *dy = column_at<DT>(a.dy, p, first);
+    auto load = [&](int j, int j0) {
+        load_row<P>(hx[j], x, (j0 + j) * a.rows, a.rows, p.row, own, a.x.ts);
+        load_row<P>(hg[j], dy, (j0 + j) * a.rows, a.rows, p.row, own, a.dy.ts);
+    };
+    if (MODE != kApply) {
+#pragma unroll
+        for (int j = 0; j < H; j++) load(j, 0);
+    }
+    for (;;) {
         // as if new: what follows from them is not kept across series
         asm("" : "+v"(p.row), "+v"(p.c), "+s"(a.x.ts), "+s"(a.dy.ts), "+s"(a.out.ts));
-        const int64_t T = rocket::steps_of(a.lengths, p.i, a.L);
-        int64_t first;
-        const int own = chunk_rows(a, T, p.chunk, per, first);
-        P hx[H], hg[H];
-        const char *x = column_at<DT>(a.x, p, first), *dy = column_at<DT>(a.dy, p, first);
-        auto load = [&](int j0) {
-#pragma unroll
-            for (int j = 0; j < H; j++) {
-                load_row<P>(hx[j], x, (j0 + j) * a.rows, a.rows, p.row, own, a.x.ts);
-                load_row<P>(hg[j], dy, (j0 + j) * a.rows, a.rows, p.row, own, a.dy.ts);
-            }
-        };
-        if (MODE != kApply) load(0);
         const float *mean = a.mean + p.i * a.G + p.g0, *rstd = a.rstd + p.i * a.G + p.g0;
         for_channels<NT>(a, p, [&](int ch, int g) {
             const float m = mean[g], r = rstd[g], w = a.w ? a.w[p.c0 + ch] : 1.0f, bias = a.b ? a.b[p.c0 + ch] : 0.0f;
@@ -590,34 +590,45 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
             s.first[ch] = __builtin_fmaf(-m, D, r * (s.group[g] * inv));
         });
         __syncthreads();
-        if (p.active) {
-            Channel<VEC, ACT> of;
-            float D[VEC], E[VEC];
-            of.take(s, p);
-            of_column<VEC>(s.chan, p, D);
-            of_column<VEC>(s.first, p, E);
-            char *out = column_at<DT>(a.out, p, first);
-            const int64_t rest = a.L - first;
-            for (int j0 = 0; j0 < R && j0 * a.rows < rest; j0 += H) {
-                if (MODE == kApply) load(j0);
+        const int64_t rest = a.L - first, next = p.i + (MODE == kHeld ? a.series : a.n);
+        char *out = column_at<DT>(a.out, p, first);
+        const int had = own;
+        if (MODE == kHeld) {   // the next series' columns are loaded as these are done with
+            T = next < a.n ? rocket::steps_of(a.lengths, next, a.L) : 0;
+            own = chunk_rows(a, T, 0, per, first);
+            p.i = next < a.n ? next : p.i;
+            x = column_at<DT>(a.x, p, first), dy = column_at<DT>(a.dy, p, first);
+        }
+        Channel<VEC, ACT> of;
+        of.take(s, p);
+        constexpr int kOwn = ONE ? 1 : VEC;
+        float D[kOwn], E[kOwn];
+        of_column<kOwn>(s.chan, p, D);
+        of_column<kOwn>(s.first, p, E);
+        for (int j0 = 0; j0 < R && j0 * a.rows < rest; j0 += H) {
+            if (MODE == kApply) {
 #pragma unroll
-                for (int j = 0; j < H; j++) {
-                    const int pass = (j0 + j) * a.rows, r = p.row + pass;
-                    float dx[VEC];
+                for (int j = 0; j < H; j++) load(j, j0);
+            }
 #pragma unroll
-                    for (int e = 0; e < VEC; e++) dx[e] = 0.0f;
-                    if (r < own) {
-                        hx[j].renew(), hg[j].renew();
+            for (int j = 0; j < H; j++) {
+                const int pass = (j0 + j) * a.rows, r = p.row + pass;
+                float dx[VEC];
 #pragma unroll
-                        for (int e = 0; e < VEC; e++) {
-                            const float v = hx[j].get(e), dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
-                            dx[e] = __builtin_fmaf(dz, of.scale(e), -__builtin_fmaf(v, D[e], E[e]));
-                        }
+                for (int e = 0; e < VEC; e++) dx[e] = 0.0f;
+                if (r < had) {
+                    hx[j].renew(), hg[j].renew();
+#pragma unroll
+                    for (int e = 0; e < VEC; e++) {
+                        const float v = hx[j].get(e), dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
+                        dx[e] = __builtin_fmaf(dz, of.scale(e), -__builtin_fmaf(v, D[ONE ? 0 : e], E[ONE ? 0 : e]));
                     }
-                    if (r < rest) P::store(out + pass * a.out.ts, dx);
                 }
+                if (r < rest && p.active) P::store(out + pass * a.out.ts, dx);
+                if (MODE == kHeld) load(j, 0);
             }
         }
+        if (next >= a.n) break;
         if (MODE == kHeld) __syncthreads();   // the shared arrays are free again
     }
     if (MODE == kHeld)
@@ -651,6 +662,7 @@ __global__ __launch_bounds__(1024) void fold_kernel(const float *in, int64_t row
 // How a call is cut.
 struct Cut {
     bool wide, held;
+    bool one;           // every 16-byte column lies in one group
     int32_t width, slabs, parts, cols, rows, threads, run, chunks;
     int32_t series;     // backward, held
     int32_t groups;     // of a slab, at most
@@ -689,6 +701,7 @@ bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut)
     cut->wide = C >= vec_wide;
     cut->width = (int32_t)width;
     const int vec = cut->wide ? vec_wide : 1;
+    cut->one = width % vec == 0;
     const int64_t most = 256 * (int64_t)vec;   // channels of a slab
     cut->parts = 1;
     cut->held = false;
@@ -747,11 +760,23 @@ void go(const NormArgs &a, const Cut &c, hipStream_t s) {
     if constexpr (!BACK) {
         norm_kernel<DT, WIDE, NT, R, MODE><<<grid, NT, lds, s>>>(a);
     } else {
+        // columns that lie in one group each, where registers are short
+        const bool one = WIDE && MODE == kHeld && R > 4 && c.one;
+        auto act = [&](auto k) {
+            constexpr int ACT = decltype(k)::value;
+            if constexpr (WIDE && MODE == kHeld && R > 4) {
+                if (one) {
+                    norm_back_kernel<DT, WIDE, NT, R, MODE, ACT, true><<<grid, NT, lds, s>>>(a);
+                    return;
+                }
+            }
+            norm_back_kernel<DT, WIDE, NT, R, MODE, ACT, false><<<grid, NT, lds, s>>>(a);
+        };
         switch (a.act) {
-        case ROCKET_ACT_RELU: norm_back_kernel<DT, WIDE, NT, R, MODE, ROCKET_ACT_RELU><<<grid, NT, lds, s>>>(a); break;
-        case ROCKET_ACT_SILU: norm_back_kernel<DT, WIDE, NT, R, MODE, ROCKET_ACT_SILU><<<grid, NT, lds, s>>>(a); break;
-        case ROCKET_ACT_GELU: norm_back_kernel<DT, WIDE, NT, R, MODE, ROCKET_ACT_GELU><<<grid, NT, lds, s>>>(a); break;
-        default: norm_back_kernel<DT, WIDE, NT, R, MODE, ROCKET_ACT_NONE><<<grid, NT, lds, s>>>(a);
+        case ROCKET_ACT_RELU: act(std::integral_constant<int, ROCKET_ACT_RELU>()); break;
+        case ROCKET_ACT_SILU: act(std::integral_constant<int, ROCKET_ACT_SILU>()); break;
+        case ROCKET_ACT_GELU: act(std::integral_constant<int, ROCKET_ACT_GELU>()); break;
+        default: act(std::integral_constant<int, ROCKET_ACT_NONE>());
         }
     }
 }
