@@ -18,12 +18,20 @@
 // Layout: a lane takes one 32-bit word of channels (one fp32, two 16-bit) of
 // 16 elements' worth of steps; 32 lanes side by side take 128 contiguous bytes
 // of a step, and the lanes left over take further runs.  A workgroup covers a
-// tile of 128 steps (more where few channels leave lanes over) and goes through
-// the tiles of a segment of one series, the state carried from tile to tile.
-// Where series and channels alone do not fill the chip, a series is cut into
-// segments: a first launch leaves each segment's map, and the second starts
-// each segment from the maps before it.  The backward pass starts each tile
-// from the state that the forward pass kept there.
+// tile of 128 steps (more where few channels leave lanes over) of one row, a
+// row being a block of channels of one series.  Where the rows fill the chip, a
+// workgroup goes through all tiles of its row, the state carried on, the next
+// tile's loads in flight.  Where they do not, every tile has a workgroup of its
+// own, and the tiles of a row meet through memory: a workgroup takes the row's
+// next tile by a counter, publishes its tile's map, and waits for the maps of
+// the tiles before it.  Tiles before it were taken before it and publish their
+// maps without waiting for anything, so every wait ends.  To bound what a tile
+// reads, every 32nd tile publishes the state behind it, and tiles start from
+// that; it waits for earlier tiles only, so these waits end as well.  A map or
+// state is one word written and read whole, and never equals the pattern that
+// the workspace is filled with, so that it needs no flag and no fence.
+// Everything is read once.  The backward pass goes through the tiles from the
+// last to the first, each from the state that the forward pass kept there.
 #include <climits>
 #include <type_traits>
 
@@ -38,7 +46,9 @@ constexpr int kElems = 16;                       // elements of a thread in a ti
 constexpr int kMostLanes = 32;                   // lanes over channels
 constexpr int kMostWaves = 8;
 constexpr int kMostChannels = 64;                // of a workgroup: 32 lanes x 2
-constexpr int64_t kFill = 1024;                  // workgroups that fill the chip
+constexpr int64_t kFill = 512;                   // rows that fill the chip
+constexpr int kGroup = 32;                       // tiles from one published state to the next
+constexpr uint32_t kNone = 0xffffffffu;          // not published yet
 
 struct View {
     char *p;
@@ -55,11 +65,13 @@ struct RecArgs {
     float *states;          // kept states [n, ceil(L / kEvery), C]: written (or null) forward, read backward
     const float *dh_last;   // backward, or null
     float *dh0;             // backward
-    float2 *maps;           // [n, segments, C], segments > 1
+    uint64_t *maps;         // [rows, tiles, 64], split
+    uint32_t *reached;      // [rows, ceil(tiles / kGroup), 64]: states, split
+    uint32_t *taken;        // [rows]: tiles taken, less one, split
     int32_t blocks;         // channel blocks
     int32_t lanes;          // lanes over channels, a power of two
     int32_t waves;          // wavefronts of a workgroup
-    int32_t segments, tiles;  // segments of a series, tiles of a segment
+    int32_t tiles;          // tiles of a row
 };
 
 template <int DT>
@@ -74,7 +86,8 @@ struct Place {
     int64_t i, len;   // series, its steps
     int64_t c, c_ld;  // first channel, and the channel it loads from
     int64_t tile;     // steps of a tile
-    int segment, wave, lane, cl, run;
+    int64_t row;
+    int wave, lane, cl, run;
     int count;        // channels it owns: 0, 1 or 2
     bool high;        // its one channel is the high half of the word at c_ld
     bool single;      // C == 1 and 16-bit elements: no whole word to load
@@ -85,10 +98,10 @@ __device__ inline Place place_of(const RecArgs &a) {
     constexpr int P = Elem<DT>::kPerWord;
     Place p;
     const int64_t b = rocket::item_of_block();
-    const int64_t cb = b % a.blocks, rest = b / a.blocks;
-    p.i = rest % a.n;
-    p.segment = (int)(rest / a.n);
-    p.wave = threadIdx.x >> 6;
+    p.row = b % (a.n * a.blocks);
+    const int64_t cb = p.row % a.blocks;
+    p.i = p.row / a.blocks;
+    p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     p.lane = threadIdx.x & 63;
     const int runs = 64 / a.lanes;
     p.cl = p.lane & (a.lanes - 1);
@@ -200,82 +213,157 @@ __device__ inline void scan_waves(int waves, int ch, float &carry, Scan &s) {
     }
 }
 
-// The state at a segment's start: the maps of the segments before it (REVERSE:
-// after it), applied in order.
-template <bool REVERSE>
-__device__ inline float scan_segments(const RecArgs &a, const Place &p, int64_t c, float h) {
-    const int before = REVERSE ? a.segments - 1 - p.segment : p.segment;
-    const float2 *m = a.maps + (p.i * a.segments + (REVERSE ? a.segments - 1 : 0)) * a.C + c;
-    const int64_t step = REVERSE ? -a.C : a.C;
-#pragma unroll 8
-    for (int k = 0; k < before; k++) {
-        const float2 x = m[k * step];
-        h = __builtin_fmaf(x.x, h, x.y);
+// What a split row's tiles publish.
+struct Meet {
+    float2 map[kMostWaves][kMostChannels];
+    int tile;
+};
+
+__device__ inline uint32_t published(float x) {
+    const uint32_t w = __builtin_bit_cast(uint32_t, x);
+    return w == kNone ? 0x7fc00000u : w;   // a NaN that is not the pattern
+}
+
+// The row's next tile.
+__device__ inline int take_tile(const RecArgs &a, const Place &p, Meet &m) {
+    if (threadIdx.x == 0)
+        m.tile = (int)(__hip_atomic_fetch_add(a.taken + p.row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(m.tile);
+}
+
+// After the wavefronts' maps are in s.map: publishes the map of the row's
+// order-th tile, waits for those before it back to the last published state,
+// and returns, in the threads that scan, the state at the tile's start.  The
+// whole workgroup calls it.
+template <int P, bool REVERSE>
+__device__ inline float meet(const RecArgs &a, const Place &p, int order, bool scans, float h, const Scan &s, Meet &m) {
+    uint64_t *row = a.maps + p.row * a.tiles * kMostChannels;
+    const int ch = threadIdx.x, channels = a.lanes * P;   // channels that are published
+    if (scans) {
+        float A = 1.0f, B = 0.0f;
+        for (int k = 0; k < a.waves; k++) {
+            const float2 x = s.map[REVERSE ? a.waves - 1 - k : k][ch];
+            B = __builtin_fmaf(x.x, B, x.y);
+            A *= x.x;
+        }
+        __hip_atomic_store(row + (int64_t)order * kMostChannels + ch,
+                           (uint64_t)published(A) | (uint64_t)__builtin_bit_cast(uint32_t, B) << 32,
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    asm volatile("" ::: "memory");   // published before anything is waited for
+    const int from = order / kGroup * kGroup, before = order - from;
+    {
+        // each wavefront composes a range of the maps, four on their way at once
+        float A = 1.0f, B = 0.0f;
+        const int lo = from + before * p.wave / a.waves, hi = from + before * (p.wave + 1) / a.waves;
+        if (p.lane < channels) {
+            for (int k = lo; k < hi; k += 4) {
+                uint64_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (k + j < hi)
+                        w[j] = __hip_atomic_load(row + (int64_t)(k + j) * kMostChannels + p.lane, __ATOMIC_RELAXED,
+                                                 __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (k + j < hi) {
+                        while ((uint32_t)w[j] == kNone) {
+                            __builtin_amdgcn_s_sleep(1);
+                            w[j] = __hip_atomic_load(row + (int64_t)(k + j) * kMostChannels + p.lane,
+                                                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        }
+                        const float x = __builtin_bit_cast(float, (uint32_t)w[j]);
+                        B = __builtin_fmaf(x, B, __builtin_bit_cast(float, (uint32_t)(w[j] >> 32)));
+                        A *= x;
+                    }
+            }
+            m.map[p.wave][p.lane] = make_float2(A, B);
+        }
+    }
+    __syncthreads();
+    if (scans) {
+        if (from > 0) {
+            const uint32_t *at = a.reached + (p.row * ((a.tiles + kGroup - 1) / kGroup) + from / kGroup) *
+                                                 kMostChannels + ch;
+            uint32_t w;
+            while ((w = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == kNone)
+                __builtin_amdgcn_s_sleep(1);
+            h = __builtin_bit_cast(float, w);
+        }
+        for (int w = 0; w < a.waves; w++) {
+            const float2 x = m.map[w][ch];
+            h = __builtin_fmaf(x.x, h, x.y);
+        }
     }
     return h;
 }
 
-// The forward pass over a segment.  MAPS: only its map.
-template <int DT, bool MAPS, bool GATE>
+// Publishes the state behind the order-th tile where a later tile starts from it.
+__device__ inline void reach(const RecArgs &a, const Place &p, int order, float h) {
+    if ((order + 1) % kGroup == 0 && order + 1 < a.tiles)
+        __hip_atomic_store(a.reached + (p.row * ((a.tiles + kGroup - 1) / kGroup) + (order + 1) / kGroup) *
+                                           kMostChannels + threadIdx.x,
+                           published(h), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The forward pass: over a row, or over one tile of it (SPLIT).
+template <int DT, bool SPLIT, bool GATE>
 __global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) {
     constexpr int P = Elem<DT>::kPerWord, S = kRun<DT>;
     __shared__ Scan scan;
-    const Place p = place_of<DT>(a);
+    __shared__ typename std::conditional<SPLIT, Meet, int>::type met;
+    Place p = place_of<DT>(a);
     const bool scans = threadIdx.x < a.lanes * P;   // the threads that go through the wavefronts, one a channel
-    const int64_t ch = (p.c - p.cl * P) + threadIdx.x;
-    float carry = 0.0f, carry_a = 1.0f;
-    if (scans && ch < a.C && !MAPS) {
-        if (a.h0) carry = a.h0[p.i * a.C + ch];
-        if (a.segments > 1) carry = scan_segments<false>(a, p, ch, carry);
-    }
-    const int64_t first = (int64_t)p.segment * a.tiles * p.tile, per = (a.L + kEvery - 1) / kEvery;
+    const int64_t ch = (p.c - p.cl * P) + threadIdx.x, per = (a.L + kEvery - 1) / kEvery;
+    float carry = scans && ch < a.C && a.h0 ? a.h0[p.i * a.C + ch] : 0.0f;
+    int k = 0;
+    if constexpr (SPLIT) k = take_tile(a, p, met);
     uint32_t wv[S], wf[S], wo[S];
-    load_run<DT>(a.v, p, first + p.run * S, 0, wv);
-    load_run<DT>(a.f, p, first + p.run * S, kKeep<DT>, wf);
-    if (GATE && !MAPS) load_run<DT>(a.o, p, first + p.run * S, 0, wo);
+    auto load = [&](int64_t t0) {
+        load_run<DT>(a.v, p, t0, 0, wv);
+        load_run<DT>(a.f, p, t0, kKeep<DT>, wf);
+        if (GATE) load_run<DT>(a.o, p, t0, 0, wo);
+    };
+    load(k * p.tile + p.run * S);
 
-    for (int k = 0; k < a.tiles; k++) {
-        const int64_t tile0 = first + k * p.tile, t0 = tile0 + p.run * S;
-        if (k > 0 && tile0 >= a.L) break;
+    for (;; k++) {
+        // as if new: what follows from them is not kept across tiles
+        if (!SPLIT) asm("" : "+v"(p.c), "+v"(p.c_ld), "+s"(a.v.ts), "+s"(a.f.ts), "+s"(a.o.ts), "+s"(a.y.ts));
+        const int64_t t0 = k * p.tile + p.run * S;
+        const bool live = k * p.tile + p.wave * (64 / a.lanes) * S < p.len;   // of the wavefront
         float fa[S][P], fb[S][P], A[P], B[P];
 #pragma unroll
         for (int j = 0; j < P; j++) A[j] = 1.0f, B[j] = 0.0f;
+        if (live) {
 #pragma unroll
-        for (int s = 0; s < S; s++)
+            for (int s = 0; s < S; s++)
 #pragma unroll
-            for (int j = 0; j < P; j++) {
-                float in;
-                rocket::logistic<DT>(Elem<DT>::get(wf[s], j), fa[s][j], in);
-                fb[s][j] = in * Elem<DT>::get(wv[s], j);
-                B[j] = __builtin_fmaf(fa[s][j], B[j], fb[s][j]);
-                A[j] *= fa[s][j];
-            }
+                for (int j = 0; j < P; j++) {
+                    float in;
+                    rocket::logistic<DT>(Elem<DT>::get(wf[s], j), fa[s][j], in);
+                    fb[s][j] = in * Elem<DT>::get(wv[s], j);
+                    B[j] = __builtin_fmaf(fa[s][j], B[j], fb[s][j]);
+                    A[j] *= fa[s][j];
+                }
+        } else {
+#pragma unroll
+            for (int s = 0; s < S; s++)
+#pragma unroll
+                for (int j = 0; j < P; j++) fa[s][j] = 1.0f, fb[s][j] = 0.0f;
+        }
         uint32_t go[S];   // the next tile's words go over these
-        if (GATE && !MAPS) {
+        if (GATE) {
 #pragma unroll
             for (int s = 0; s < S; s++) go[s] = wo[s];
         }
-        const int64_t next = t0 + p.tile;
-        if (k + 1 < a.tiles && tile0 + p.tile < a.L) {   // on their way during the scan
-            load_run<DT>(a.v, p, next, 0, wv);
-            load_run<DT>(a.f, p, next, kKeep<DT>, wf);
-            if (GATE && !MAPS) load_run<DT>(a.o, p, next, 0, wo);
-        }
+        if (!SPLIT && k + 1 < a.tiles) load(t0 + p.tile);   // on their way during the scan
         scan_lanes<P, false>(a, p, A, B, scan);
         __syncthreads();
-        if (scans) {
-            if (MAPS) {
-                for (int w = 0; w < a.waves; w++) {
-                    const float2 m = scan.map[w][threadIdx.x];
-                    carry = __builtin_fmaf(m.x, carry, m.y);
-                    carry_a *= m.x;
-                }
-            } else {
-                scan_waves<false>(a.waves, threadIdx.x, carry, scan);
-            }
-        }
+        if constexpr (SPLIT) carry = meet<P, false>(a, p, k, scans, carry, scan, met);
+        if (scans) scan_waves<false>(a.waves, threadIdx.x, carry, scan);
+        if (SPLIT && scans) reach(a, p, k, carry);
         __syncthreads();
-        if (MAPS) continue;
         float h[P];
 #pragma unroll
         for (int j = 0; j < P; j++) h[j] = __builtin_fmaf(A[j], scan.start[p.wave][p.cl * P + j], B[j]);
@@ -301,100 +389,108 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) 
                 store_step<DT, whole.value>(at, a.y.ts, p, s, a.L - t0, t0 + s < p.len ? Elem<DT>::put(out) : 0);
             }
         };
-        if (whole_run<DT>(p, t0, a.L))
+        if (!live) {
+#pragma unroll
+            for (int s = 0; s < S; s++) store_step<DT, false>(at, a.y.ts, p, s, a.L - t0, 0);
+        } else if (whole_run<DT>(p, t0, a.L)) {
             steps(std::true_type());
-        else
+        } else {
             steps(std::false_type());
+        }
+        if (SPLIT || k + 1 == a.tiles) break;
     }
-    if (scans && ch < a.C) {
-        if (MAPS)
-            a.maps[(p.i * a.segments + p.segment) * a.C + ch] = make_float2(carry_a, carry);
-        else if (p.segment == a.segments - 1)
-            a.h_last[p.i * a.C + ch] = carry;
-    }
+    if (k == a.tiles - 1 && scans && ch < a.C) a.h_last[p.i * a.C + ch] = carry;
 }
 
-// The backward pass over a segment, from its last tile to its first.  MAPS:
-// only the map of the gradient that runs towards its start.
-template <int DT, bool MAPS, bool GATE>
+// The backward pass: over a row from its last tile to its first, or over one
+// tile of it (SPLIT).
+template <int DT, bool SPLIT, bool GATE>
 __global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a) {
     constexpr int P = Elem<DT>::kPerWord, S = kRun<DT>;
     __shared__ Scan scan, fscan;
-    const Place p = place_of<DT>(a);
+    __shared__ typename std::conditional<SPLIT, Meet, int>::type met;
+    Place p = place_of<DT>(a);
     const int channels = a.lanes * P;
     const bool scans = threadIdx.x < channels;                    // the threads that go through the gradients' maps
     const int other = a.waves > 1 ? 64 : 0;                       // and those that go through the states'
     const bool fscans = (int)threadIdx.x >= other && (int)threadIdx.x < other + channels;
     const int64_t c0 = p.c - p.cl * P, ch = c0 + threadIdx.x, fch = c0 + threadIdx.x - other;
-    float carry = 0.0f, carry_a = 1.0f;
-    if (scans && ch < a.C && !MAPS) {
-        if (a.dh_last) carry = a.dh_last[p.i * a.C + ch];
-        if (a.segments > 1) carry = scan_segments<true>(a, p, ch, carry);
-    }
-    const int64_t first = (int64_t)p.segment * a.tiles * p.tile, per = (a.L + kEvery - 1) / kEvery;
-    for (int k = a.tiles - 1; k >= 0; k--) {
-        const int64_t tile0 = first + k * p.tile, t0 = tile0 + p.run * S;
-        if (k > 0 && tile0 >= a.L) continue;
+    const int64_t per = (a.L + kEvery - 1) / kEvery;
+    float carry = scans && ch < a.C && a.dh_last ? a.dh_last[p.i * a.C + ch] : 0.0f;
+    int order = 0;
+    if constexpr (SPLIT) order = take_tile(a, p, met);
+    for (;; order++) {
+        // as if new: what follows from them is not kept across tiles
+        if (!SPLIT) {
+            asm("" : "+v"(p.c), "+v"(p.c_ld), "+s"(a.v.ts), "+s"(a.f.ts), "+s"(a.o.ts), "+s"(a.dy.ts));
+            asm("" : "+s"(a.dv.ts), "+s"(a.df.ts), "+s"(a.dO.ts));
+        }
+        const int64_t tile0 = (a.tiles - 1 - order) * p.tile, t0 = tile0 + p.run * S;
+        const bool live = tile0 + p.wave * (64 / a.lanes) * S < p.len;   // of the wavefront
         uint32_t wv[S], wf[S], wo[S], wg[S];
         load_run<DT>(a.f, p, t0, kKeep<DT>, wf);
         load_run<DT>(a.dy, p, t0, 0, wg);
         if (GATE) load_run<DT>(a.o, p, t0, 0, wo);
-        if (!MAPS) load_run<DT>(a.v, p, t0, 0, wv);
+        load_run<DT>(a.v, p, t0, 0, wv);
         float state = 0.0f;
-        if (!MAPS && fscans && tile0 < a.L && fch < a.C) state = a.states[(p.i * per + tile0 / kEvery) * a.C + fch];
+        if (fscans && tile0 < a.L && fch < a.C) state = a.states[(p.i * per + tile0 / kEvery) * a.C + fch];
 
         float fa[S][P], in[S][P], A[P], R[P], FA[P], B[P];
 #pragma unroll
         for (int j = 0; j < P; j++) A[j] = 1.0f, R[j] = 0.0f, B[j] = 0.0f;
+        if (live) {
 #pragma unroll
-        for (int s = S - 1; s >= 0; s--)
+            for (int s = S - 1; s >= 0; s--)
 #pragma unroll
-            for (int j = 0; j < P; j++) {
-                float so = 1.0f, rest;
-                rocket::logistic<DT>(Elem<DT>::get(wf[s], j), fa[s][j], in[s][j]);
-                if (GATE) rocket::logistic<DT>(Elem<DT>::get(wo[s], j), so, rest);
-                const float g = GATE ? Elem<DT>::get(wg[s], j) * so : Elem<DT>::get(wg[s], j);
-                R[j] = fa[s][j] * (R[j] + g);
-                if (!MAPS) B[j] = __builtin_fmaf(A[j], in[s][j] * Elem<DT>::get(wv[s], j), B[j]);
-                A[j] *= fa[s][j];
-            }
+                for (int j = 0; j < P; j++) {
+                    float so = 1.0f, rest;
+                    rocket::logistic<DT>(Elem<DT>::get(wf[s], j), fa[s][j], in[s][j]);
+                    if (GATE) rocket::logistic<DT>(Elem<DT>::get(wo[s], j), so, rest);
+                    const float g = GATE ? Elem<DT>::get(wg[s], j) * so : Elem<DT>::get(wg[s], j);
+                    R[j] = fa[s][j] * (R[j] + g);
+                    B[j] = __builtin_fmaf(A[j], in[s][j] * Elem<DT>::get(wv[s], j), B[j]);
+                    A[j] *= fa[s][j];
+                }
+        } else {
+#pragma unroll
+            for (int s = 0; s < S; s++)
+#pragma unroll
+                for (int j = 0; j < P; j++) fa[s][j] = 1.0f, in[s][j] = 0.0f;
+        }
 #pragma unroll
         for (int j = 0; j < P; j++) FA[j] = A[j];
         scan_lanes<P, true>(a, p, A, R, scan);
-        if (!MAPS) scan_lanes<P, false>(a, p, FA, B, fscan);
+        scan_lanes<P, false>(a, p, FA, B, fscan);
         __syncthreads();
-        if (MAPS) {
-            if (scans)
-                for (int w = a.waves - 1; w >= 0; w--) {
-                    const float2 m = scan.map[w][threadIdx.x];
-                    carry = __builtin_fmaf(m.x, carry, m.y);
-                    carry_a *= m.x;
-                }
-            __syncthreads();
-            continue;
-        }
-        if (scans) scan_waves<true>(a.waves, threadIdx.x, carry, scan);
         if (fscans) scan_waves<false>(a.waves, (int)threadIdx.x - other, state, fscan);
+        if constexpr (SPLIT) carry = meet<P, true>(a, p, order, scans, carry, scan, met);
+        if (scans) scan_waves<true>(a.waves, threadIdx.x, carry, scan);
+        if (SPLIT && scans) reach(a, p, order, carry);
         __syncthreads();
 
         rocket::renew(wv);
         rocket::renew(wg);
         if (GATE) rocket::renew(wo);
-        float h[S][P], e[P];   // the state before each step
-#pragma unroll
-        for (int j = 0; j < P; j++) {
-            const int at = p.cl * P + j;
-            e[j] = __builtin_fmaf(A[j], scan.start[p.wave][at], R[j]);
-            h[0][j] = __builtin_fmaf(FA[j], fscan.start[p.wave][at], B[j]);
-        }
-#pragma unroll
-        for (int s = 0; s + 1 < S; s++)
-#pragma unroll
-            for (int j = 0; j < P; j++)
-                h[s + 1][j] = __builtin_fmaf(fa[s][j], h[s][j], in[s][j] * Elem<DT>::get(wv[s], j));
         char *at_v = run_at<DT>(a.dv, p, t0), *at_f = run_at<DT>(a.df, p, t0);
         char *at_o = GATE ? run_at<DT>(a.dO, p, t0) : nullptr;
+        auto store = [&](auto whole, int s, uint32_t gv, uint32_t gf, uint32_t go) {
+            store_step<DT, whole.value>(at_v, a.dv.ts, p, s, a.L - t0, gv);
+            store_step<DT, whole.value>(at_f, a.df.ts, p, s, a.L - t0, gf);
+            if (GATE) store_step<DT, whole.value>(at_o, a.dO.ts, p, s, a.L - t0, go);
+        };
         auto steps = [&](auto whole) {
+            float h[S][P], e[P];   // the state before each step
+#pragma unroll
+            for (int j = 0; j < P; j++) {
+                const int at = p.cl * P + j;
+                e[j] = __builtin_fmaf(A[j], scan.start[p.wave][at], R[j]);
+                h[0][j] = __builtin_fmaf(FA[j], fscan.start[p.wave][at], B[j]);
+            }
+#pragma unroll
+            for (int s = 0; s + 1 < S; s++)
+#pragma unroll
+                for (int j = 0; j < P; j++)
+                    h[s + 1][j] = __builtin_fmaf(fa[s][j], h[s][j], in[s][j] * Elem<DT>::get(wv[s], j));
 #pragma unroll
             for (int s = S - 1; s >= 0; s--) {
                 float xv[P], xf[P], xo[P];
@@ -409,23 +505,28 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a)
                     if (GATE) xo[j] = dy * __builtin_fmaf(fa[s][j], h[s][j], in[s][j] * v) * so * rest;
                     e[j] = fa[s][j] * dh;
                 }
-                const bool live = t0 + s < p.len;
-                store_step<DT, whole.value>(at_v, a.dv.ts, p, s, a.L - t0, live ? Elem<DT>::put(xv) : 0);
-                store_step<DT, whole.value>(at_f, a.df.ts, p, s, a.L - t0, live ? Elem<DT>::put(xf) : 0);
-                if (GATE) store_step<DT, whole.value>(at_o, a.dO.ts, p, s, a.L - t0, live ? Elem<DT>::put(xo) : 0);
+                const bool own = t0 + s < p.len;
+                store(whole, s, own ? Elem<DT>::put(xv) : 0, own ? Elem<DT>::put(xf) : 0,
+                      GATE && own ? Elem<DT>::put(xo) : 0);
             }
         };
-        if (whole_run<DT>(p, t0, a.L))
+        if (!live) {
+#pragma unroll
+            for (int s = 0; s < S; s++) store(std::false_type(), s, 0, 0, 0);
+        } else if (whole_run<DT>(p, t0, a.L)) {
             steps(std::true_type());
-        else
+        } else {
             steps(std::false_type());
+        }
+        if (SPLIT || order + 1 == a.tiles) break;
     }
-    if (scans && ch < a.C) {
-        if (MAPS)
-            a.maps[(p.i * a.segments + p.segment) * a.C + ch] = make_float2(carry_a, carry);
-        else if (p.segment == 0)
-            a.dh0[p.i * a.C + ch] = carry;
-    }
+    if (order == a.tiles - 1 && scans && ch < a.C) a.dh0[p.i * a.C + ch] = carry;
+}
+
+// Nothing is published yet, and no tile taken.
+__global__ __launch_bounds__(256) void clear_kernel(uint64_t *p, int64_t words) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < words) p[i] = ~0ull;
 }
 
 // One step of every series: a word of channels per thread.
@@ -483,33 +584,51 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
 
 // How a call is cut.
 struct Cut {
-    int32_t lanes, waves, blocks, segments, tiles;
-    int64_t grid;
+    int32_t lanes, waves, blocks, tiles;
+    bool split;
+    int64_t rows, grid;
 };
 
 // Lanes over channels: the power of two that covers the words of channels, 32
 // at most; the wavefront's other lanes take further runs of steps, so that
-// few channels do not leave lanes idle.  Segments: as many as fill the chip
-// beside series and channel blocks, one where those do so alone.
+// few channels do not leave lanes idle.  Split: where rows alone do not fill
+// the chip.
 bool cut_of(const rocket_sequence_shape *s, Cut *cut) {
     const int64_t per_word = rocket::elem_size(s->dtype) == 4 ? 1 : 2;
     const int64_t words = (s->channels + per_word - 1) / per_word;
     cut->lanes = 1;
     while (cut->lanes < kMostLanes && cut->lanes < words) cut->lanes *= 2;
     const int64_t in_wave = (64 / cut->lanes) * (kElems / per_word);   // steps of a wavefront
+    const int64_t L = s->steps > 0 ? s->steps : 1;
     cut->waves = (int32_t)(in_wave < kEvery ? kEvery / in_wave : 1);
-    const int64_t tile = cut->waves * in_wave, tiles = s->steps > tile ? (s->steps + tile - 1) / tile : 1;
+    if (L <= cut->waves * in_wave) cut->waves = (int32_t)((L + in_wave - 1) / in_wave);   // one tile holds the series
+    const int64_t tile = cut->waves * in_wave;
+    cut->tiles = (int32_t)((L + tile - 1) / tile);
     cut->blocks = (int32_t)((words + cut->lanes - 1) / cut->lanes);
-    const int64_t rows = s->n * cut->blocks;
-    int64_t segments = rows > 0 ? (kFill + rows - 1) / rows : 1;
-    if (segments > tiles) segments = tiles;
-    cut->tiles = (int32_t)((tiles + segments - 1) / segments);
-    cut->segments = (int32_t)((tiles + cut->tiles - 1) / cut->tiles);
-    return !__builtin_mul_overflow(rows, (int64_t)cut->segments, &cut->grid) && cut->grid <= INT_MAX;
+    cut->rows = s->n * cut->blocks;
+    cut->split = cut->tiles > 1 && cut->rows < kFill;
+    return !__builtin_mul_overflow(cut->rows, (int64_t)(cut->split ? cut->tiles : 1), &cut->grid) &&
+           cut->grid <= INT_MAX;
 }
 
-int64_t workspace_of(const rocket_sequence_shape *s, const Cut &cut) {
-    return cut.segments > 1 ? s->n * cut.segments * s->channels * (int64_t)sizeof(float2) : 0;
+// 8-byte words of a split call's maps, published states and counters.
+int64_t map_words(const Cut &c) { return c.rows * c.tiles * kMostChannels; }
+int64_t reached_words(const Cut &c) { return c.rows * ((c.tiles + kGroup - 1) / kGroup) * (kMostChannels / 2); }
+int64_t workspace_words(const Cut &c) { return c.split ? map_words(c) + reached_words(c) + (c.rows + 1) / 2 : 0; }
+int64_t workspace_of(const Cut &c) { return workspace_words(c) * 8; }
+
+void set_cut(RecArgs &a, const Cut &c, void *workspace) {
+    a.blocks = c.blocks, a.lanes = c.lanes, a.waves = c.waves, a.tiles = c.tiles;
+    a.maps = (uint64_t *)workspace;
+    if (c.split) {
+        a.reached = (uint32_t *)(a.maps + map_words(c));
+        a.taken = (uint32_t *)(a.maps + map_words(c) + reached_words(c));
+    }
+}
+
+void clear(const RecArgs &a, const Cut &c, hipStream_t s) {
+    const int64_t words = workspace_words(c);
+    clear_kernel<<<(uint32_t)((words + 255) / 256), 256, 0, s>>>(a.maps, words);
 }
 
 View view(const rocket_sequence *q, int size) {
@@ -520,14 +639,22 @@ bool aligned(const void *p, uintptr_t to) { return (uintptr_t)p % to == 0; }
 
 template <int DT, bool GATE>
 void run_forward(const RecArgs &a, const Cut &cut, hipStream_t s) {
-    if (cut.segments > 1) forward_kernel<DT, true, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
-    forward_kernel<DT, false, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+    if (cut.split) {
+        clear(a, cut, s);
+        forward_kernel<DT, true, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+    } else {
+        forward_kernel<DT, false, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+    }
 }
 
 template <int DT, bool GATE>
 void run_backward(const RecArgs &a, const Cut &cut, hipStream_t s) {
-    if (cut.segments > 1) backward_kernel<DT, true, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
-    backward_kernel<DT, false, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+    if (cut.split) {
+        clear(a, cut, s);
+        backward_kernel<DT, true, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+    } else {
+        backward_kernel<DT, false, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+    }
 }
 
 template <int DT, bool GATE>
@@ -551,7 +678,7 @@ void run_step(const StepArgs &a, hipStream_t s) {
 extern "C" rocket_status rocket_recurrence_workspace(const rocket_sequence_shape *shape, int64_t *bytes) {
     Cut cut;
     if (!bytes || !rocket::shape_ok(shape) || !cut_of(shape, &cut)) return ROCKET_ERR_INVALID_ARG;
-    *bytes = workspace_of(shape, cut);
+    *bytes = workspace_of(cut);
     return ROCKET_OK;
 }
 
@@ -563,7 +690,7 @@ extern "C" rocket_status rocket_recurrence_forward(const rocket_sequence_shape *
     if (!rocket::shape_ok(shape) || !cut_of(shape, &cut) || !rocket::view_ok(v, shape) || !rocket::view_ok(f, shape) ||
         (o && !rocket::view_ok(o, shape)) || !rocket::out_ok(y, shape) || (shape->n > 0 && !h_last))
         return ROCKET_ERR_INVALID_ARG;
-    const int64_t need = workspace_of(shape, cut);
+    const int64_t need = workspace_of(cut);
     if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 8)))) return ROCKET_ERR_INVALID_ARG;
     if (!aligned(h0, 4) || !aligned(h_last, 4) || !aligned(states, 4) || !aligned(shape->lengths, 4))
         return ROCKET_ERR_INVALID_ARG;
@@ -572,9 +699,8 @@ extern "C" rocket_status rocket_recurrence_forward(const rocket_sequence_shape *
     RecArgs a = {};
     a.v = view(v, size), a.f = view(f, size), a.o = view(o, size), a.y = view(y, size);
     a.n = shape->n, a.L = shape->steps, a.C = shape->channels, a.lengths = shape->lengths;
-    a.h0 = h0, a.h_last = h_last, a.states = states, a.maps = (float2 *)workspace;
-    a.blocks = cut.blocks, a.lanes = cut.lanes, a.waves = cut.waves;
-    a.segments = cut.segments, a.tiles = cut.tiles;
+    a.h0 = h0, a.h_last = h_last, a.states = states;
+    set_cut(a, cut, workspace);
     BY_TYPE(run_forward, shape->dtype, o != nullptr, a, cut, (hipStream_t)hip_stream);
     return rocket::launched();
 }
@@ -591,7 +717,7 @@ extern "C" rocket_status rocket_recurrence_backward(const rocket_sequence_shape 
         !rocket::out_ok(dv, shape) || !rocket::out_ok(df, shape) || (o != nullptr) != (dO != nullptr) ||
         (dO && !rocket::out_ok(dO, shape)) || (shape->n > 0 && !dh0) || (!rocket::empty(shape) && !states))
         return ROCKET_ERR_INVALID_ARG;
-    const int64_t need = workspace_of(shape, cut);
+    const int64_t need = workspace_of(cut);
     if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 8)))) return ROCKET_ERR_INVALID_ARG;
     if (!aligned(states, 4) || !aligned(dh_last, 4) || !aligned(dh0, 4) || !aligned(shape->lengths, 4))
         return ROCKET_ERR_INVALID_ARG;
@@ -601,9 +727,8 @@ extern "C" rocket_status rocket_recurrence_backward(const rocket_sequence_shape 
     a.v = view(v, size), a.f = view(f, size), a.o = view(o, size);
     a.dy = view(dy, size), a.dv = view(dv, size), a.df = view(df, size), a.dO = view(dO, size);
     a.n = shape->n, a.L = shape->steps, a.C = shape->channels, a.lengths = shape->lengths;
-    a.states = const_cast<float *>(states), a.dh_last = dh_last, a.dh0 = dh0, a.maps = (float2 *)workspace;
-    a.blocks = cut.blocks, a.lanes = cut.lanes, a.waves = cut.waves;
-    a.segments = cut.segments, a.tiles = cut.tiles;
+    a.states = const_cast<float *>(states), a.dh_last = dh_last, a.dh0 = dh0;
+    set_cut(a, cut, workspace);
     BY_TYPE(run_backward, shape->dtype, o != nullptr, a, cut, (hipStream_t)hip_stream);
     return rocket::launched();
 }
