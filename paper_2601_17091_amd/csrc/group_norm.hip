@@ -37,7 +37,7 @@ struct View {
 
 struct NormArgs {
     View x, dy, out;   // out: y, or dx
-    int64_t n, L;
+    int32_t n, L;
     int32_t C, G, width;       // width: channels of a group
     int32_t slabs, parts;      // slabs per series; parts > 1: slabs per group
     int32_t cols, rows;        // columns of a slab; steps a workgroup passes at once
@@ -142,7 +142,7 @@ __device__ inline float slope(float z) {
 
 // Where a workgroup and a thread work.
 struct Place {
-    int64_t i;            // series
+    uint32_t i;           // series
     int slab, chunk;
     int c0, c1, g0, ng;   // the slab's channels and groups
     int row, col;         // the thread's first step in a pass, its column
@@ -309,10 +309,10 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a)
     constexpr int VEC = P::kN;
     const Scratch s = scratch_of<NT, VEC>(a);
     Place p;
-    const int64_t b = rocket::item_of_block();
-    p.slab = (int)(b % a.slabs);
-    p.chunk = (int)(b / a.slabs % a.chunks);
-    p.i = b / a.slabs / a.chunks;
+    const uint32_t b = rocket::item_of_block(), rest_of = rocket::uniform(b / a.slabs);
+    p.slab = rocket::uniform(b - rest_of * a.slabs);
+    p.i = rocket::uniform(rest_of / a.chunks);
+    p.chunk = rocket::uniform(rest_of - p.i * a.chunks);
     place_thread<NT, VEC>(a, p);
     const int64_t T = rocket::steps_of(a.lengths, p.i, a.L), per = (int64_t)R * a.rows;
     int64_t first;
@@ -364,14 +364,14 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a)
         if (MODE == kStats) {
             const int K = a.chunks * a.parts, k = p.chunk * a.parts + (a.parts > 1 ? p.slab % a.parts : 0);
             for (int g = threadIdx.x; g < p.ng; g += NT)
-                a.stats[(p.i * a.G + p.g0 + g) * K + k] = make_float2(s.group[g] * inv, s.group2[g]);
+                a.stats[((int64_t)p.i * a.G + p.g0 + g) * K + k] = make_float2(s.group[g] * inv, s.group2[g]);
             return;
         }
         for (int g = threadIdx.x; g < p.ng; g += NT) {
             const float mean = s.group[g] * inv, rstd = own ? 1.0f / sqrtf(s.group2[g] * inv + a.eps) : 0.0f;
             s.group[g] = mean, s.group2[g] = rstd;
-            a.mean[p.i * a.G + p.g0 + g] = mean;
-            a.rstd[p.i * a.G + p.g0 + g] = rstd;
+            a.mean[(int64_t)p.i * a.G + p.g0 + g] = mean;
+            a.rstd[(int64_t)p.i * a.G + p.g0 + g] = rstd;
         }
     } else {
         // merge the chunks' statistics: N = sum n_k, m = sum n_k m_k / N,
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a)
         const int K = a.chunks * a.parts;
         const float inv = T ? 1.0f / ((float)T * (float)a.width) : 0.0f;
         for (int g = threadIdx.x >> 6; g < p.ng; g += NT >> 6) {
-            const float2 *st = a.stats + (p.i * a.G + p.g0 + g) * K;
+            const float2 *st = a.stats + ((int64_t)p.i * a.G + p.g0 + g) * K;
             float mean = 0.0f, sq = 0.0f;
             for (int pass = 0; pass < 2; pass++) {
                 float t = 0.0f;
@@ -403,8 +403,8 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a)
                 const float rstd = T ? 1.0f / sqrtf(sq * inv + a.eps) : 0.0f;
                 s.group[g] = mean, s.group2[g] = rstd;
                 if (p.chunk == 0 && (a.parts == 1 || p.slab % a.parts == 0)) {
-                    a.mean[p.i * a.G + p.g0 + g] = mean;
-                    a.rstd[p.i * a.G + p.g0 + g] = rstd;
+                    a.mean[(int64_t)p.i * a.G + p.g0 + g] = mean;
+                    a.rstd[(int64_t)p.i * a.G + p.g0 + g] = rstd;
                 }
             }
         }
@@ -485,10 +485,10 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
     constexpr int VEC = P::kN;
     const Scratch s = scratch_of<NT, VEC>(a);
     Place p;
-    const int64_t b = rocket::item_of_block();
-    p.slab = (int)(b % a.slabs);
-    p.chunk = MODE == kHeld ? 0 : (int)(b / a.slabs % a.chunks);
-    const int64_t begin = MODE == kHeld ? b / a.slabs : b / a.slabs / a.chunks;
+    const uint32_t b = rocket::item_of_block(), rest_of = rocket::uniform(b / a.slabs);
+    p.slab = rocket::uniform(b - rest_of * a.slabs);
+    const uint32_t begin = MODE == kHeld ? rest_of : (uint32_t)rocket::uniform(rest_of / a.chunks);
+    p.chunk = MODE == kHeld ? 0 : rocket::uniform(rest_of - begin * a.chunks);
     place_thread<NT, VEC>(a, p);
     const int W = p.c1 - p.c0;
     const int64_t per = (int64_t)R * a.rows;
@@ -512,7 +512,7 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
     for (;;) {
         // as if new: what follows from them is not kept across series
         asm("" : "+v"(p.row), "+v"(p.c), "+s"(a.x.ts), "+s"(a.dy.ts), "+s"(a.out.ts));
-        const float *mean = a.mean + p.i * a.G + p.g0, *rstd = a.rstd + p.i * a.G + p.g0;
+        const float *mean = a.mean + (int64_t)p.i * a.G + p.g0, *rstd = a.rstd + (int64_t)p.i * a.G + p.g0;
         for_channels<NT>(a, p, [&](int ch, int g) {
             const float m = mean[g], r = rstd[g], w = a.w ? a.w[p.c0 + ch] : 1.0f, bias = a.b ? a.b[p.c0 + ch] : 0.0f;
             if (ACT == ROCKET_ACT_RELU) {
@@ -556,7 +556,7 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
                 if (MODE == kHeld) {
                     s.total[ch] += d, s.total[W + ch] += t;
                 } else {
-                    float *sum = a.sums + (p.i * a.chunks + p.chunk) * 2 * a.C + p.c0 + ch;
+                    float *sum = a.sums + ((int64_t)p.i * a.chunks + p.chunk) * 2 * a.C + p.c0 + ch;
                     sum[0] = d, sum[a.C] = t;
                 }
                 s.first[ch] = t;
@@ -571,7 +571,7 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
                 float t = 0.0f;
                 for (int ch = threadIdx.x & 63; ch < a.width; ch += 64) {
                     const int c = (p.g0 + g) * a.width + ch;
-                    const float *sum = a.sums + (p.i * a.chunks * 2 + q) * a.C + c;
+                    const float *sum = a.sums + ((int64_t)p.i * a.chunks * 2 + q) * a.C + c;
                     float u = 0.0f;
                     for (int chunk = 0; chunk < a.chunks; chunk++) u += sum[(int64_t)chunk * 2 * a.C];
                     t += a.w ? a.w[c] * u : u;
@@ -590,13 +590,13 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
             s.first[ch] = __builtin_fmaf(-m, D, r * (s.group[g] * inv));
         });
         __syncthreads();
-        const int64_t rest = a.L - first, next = p.i + (MODE == kHeld ? a.series : a.n);
+        const int64_t rest = a.L - first, next = (int64_t)p.i + (MODE == kHeld ? a.series : a.n);
         char *out = column_at<DT>(a.out, p, first);
         const int had = own;
         if (MODE == kHeld) {   // the next series' columns are loaded as these are done with
             T = next < a.n ? rocket::steps_of(a.lengths, next, a.L) : 0;
             own = chunk_rows(a, T, 0, per, first);
-            p.i = next < a.n ? next : p.i;
+            p.i = next < a.n ? (uint32_t)next : p.i;
             x = column_at<DT>(a.x, p, first), dy = column_at<DT>(a.dy, p, first);
         }
         Channel<VEC, ACT> of;
@@ -634,7 +634,7 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
     if (MODE == kHeld)
         for (int q = 0; q < 2; q++)
             for (int ch = threadIdx.x; ch < W; ch += NT)
-                a.sums[(begin * 2 + q) * a.C + p.c0 + ch] = s.total[q * W + ch];
+                a.sums[((int64_t)begin * 2 + q) * a.C + p.c0 + ch] = s.total[q * W + ch];
 }
 
 // Rows of channel sums to fewer rows: out[o, q, c] = the sum of in[r, q, c]
@@ -830,7 +830,7 @@ bool args_ok(const rocket_sequence_shape *shape, int32_t groups, int32_t act, co
 NormArgs args_of(const rocket_sequence_shape *shape, int32_t groups, int32_t act, const float *w, const float *b,
                  const Cut &cut) {
     NormArgs a = {};
-    a.n = shape->n, a.L = shape->steps, a.C = (int32_t)shape->channels, a.G = groups, a.width = cut.width;
+    a.n = (int32_t)shape->n, a.L = (int32_t)shape->steps, a.C = (int32_t)shape->channels, a.G = groups, a.width = cut.width;
     a.slabs = cut.slabs, a.parts = cut.parts, a.cols = cut.cols, a.rows = cut.rows, a.chunks = cut.chunks;
     a.most_groups = cut.groups, a.act = act, a.w = w, a.b = b, a.lengths = shape->lengths, a.series = cut.series;
     return a;

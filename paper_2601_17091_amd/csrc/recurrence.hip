@@ -58,7 +58,8 @@ struct View {
 struct RecArgs {
     View v, f, o, y;        // y: forward
     View dy, dv, df, dO;    // backward
-    int64_t n, L, C;
+    int32_t n, L;
+    int64_t C;
     const int32_t *lengths;
     const float *h0;        // forward, or null
     float *h_last;          // forward
@@ -83,10 +84,9 @@ constexpr uint32_t kKeep = DT == ROCKET_FLOAT32 ? 0x7f800000u : DT == ROCKET_BFL
 
 // Where a thread works.
 struct Place {
-    int64_t i, len;   // series, its steps
-    int64_t c, c_ld;  // first channel, and the channel it loads from
-    int64_t tile;     // steps of a tile
-    int64_t row;
+    uint32_t i, len;  // series, its steps
+    uint32_t row, tile;   // row; steps of a tile
+    int c, c_ld;      // first channel, and the channel it loads from
     int wave, lane, cl, run;
     int count;        // channels it owns: 0, 1 or 2
     bool high;        // its one channel is the high half of the word at c_ld
@@ -97,31 +97,31 @@ template <int DT>
 __device__ inline Place place_of(const RecArgs &a) {
     constexpr int P = Elem<DT>::kPerWord;
     Place p;
-    const int64_t b = rocket::item_of_block();
-    p.row = b % (a.n * a.blocks);
-    const int64_t cb = p.row % a.blocks;
-    p.i = p.row / a.blocks;
-    p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t b = rocket::item_of_block();
+    p.row = rocket::uniform(b % ((uint32_t)a.n * a.blocks));
+    p.i = rocket::uniform(p.row / a.blocks);
+    const int cb = (int)(p.row - p.i * a.blocks);
+    p.wave = rocket::uniform(threadIdx.x >> 6);
     p.lane = threadIdx.x & 63;
     const int runs = 64 / a.lanes;
     p.cl = p.lane & (a.lanes - 1);
     p.run = p.wave * runs + p.lane / a.lanes;
-    p.tile = (int64_t)a.waves * runs * kRun<DT>;
+    p.tile = (uint32_t)a.waves * runs * kRun<DT>;
     p.c = (cb * a.lanes + p.cl) * P;
-    int64_t left = a.C - p.c;
+    const int C = (int)a.C, left = C - p.c;
     p.count = left <= 0 ? 0 : left < P ? 1 : P;
-    p.high = P == 2 && p.count == 1 && a.C > 1;
-    p.single = P == 2 && a.C == 1;
-    p.c_ld = p.c + P <= a.C ? p.c : a.C > P ? a.C - P : 0;
+    p.high = P == 2 && p.count == 1 && C > 1;
+    p.single = P == 2 && C == 1;
+    p.c_ld = p.c + P <= C ? p.c : C > P ? C - P : 0;
     p.len = rocket::steps_of(a.lengths, p.i, a.L);
     return p;
 }
 
 // The words of a run from step t0; steps past the series' length get `fill`.
 template <int DT>
-__device__ inline void load_run(const View &x, const Place &p, int64_t t0, uint32_t fill, uint32_t (&w)[kRun<DT>]) {
+__device__ inline void load_run(const View &x, const Place &p, uint32_t t0, uint32_t fill, uint32_t (&w)[kRun<DT>]) {
     using raw = typename Elem<DT>::raw;
-    const char *at = x.p + p.i * x.ss + t0 * x.ts + p.c_ld * Elem<DT>::kSize;
+    const char *at = x.p + p.i * x.ss + t0 * x.ts + (int64_t)p.c_ld * Elem<DT>::kSize;
     if (p.single) {
 #pragma unroll
         for (int s = 0; s < kRun<DT>; s++) w[s] = t0 + s < p.len ? (uint32_t)*(const raw *)(at + s * x.ts) : fill;
@@ -140,26 +140,26 @@ __device__ inline void load_run(const View &x, const Place &p, int64_t t0, uint3
 
 // Whether a run's stores need no checks: whole words, all steps inside.
 template <int DT>
-__device__ inline bool whole_run(const Place &p, int64_t t0, int64_t L) {
+__device__ inline bool whole_run(const Place &p, uint32_t t0, uint32_t L) {
     return p.count == Elem<DT>::kPerWord && t0 + kRun<DT> <= L;
 }
 
 // Writes the packed word of step t of a run that starts at `at`, checked
 // unless the run is whole.
 template <int DT, bool WHOLE>
-__device__ inline void store_step(char *at, int64_t stride, const Place &p, int s, int64_t left, uint32_t w) {
+__device__ inline void store_step(char *at, int64_t stride, const Place &p, int s, uint32_t left, uint32_t w) {
     using raw = typename Elem<DT>::raw;
     if (WHOLE)
         rocket::store_at(at + s * stride, w);
-    else if (s < left && p.count == Elem<DT>::kPerWord)
+    else if ((uint32_t)s < left && p.count == Elem<DT>::kPerWord)
         rocket::store_at(at + s * stride, w);
-    else if (s < left && p.count == 1)
+    else if ((uint32_t)s < left && p.count == 1)
         *(raw *)(at + s * stride) = (raw)w;
 }
 
 template <int DT>
-__device__ inline char *run_at(const View &x, const Place &p, int64_t t0) {
-    return x.p + p.i * x.ss + t0 * x.ts + p.c * Elem<DT>::kSize;
+__device__ inline char *run_at(const View &x, const Place &p, uint32_t t0) {
+    return x.p + p.i * x.ss + t0 * x.ts + (int64_t)p.c * Elem<DT>::kSize;
 }
 
 // Shared memory of one scan over the wavefronts of a workgroup.
@@ -238,7 +238,7 @@ __device__ inline int take_tile(const RecArgs &a, const Place &p, Meet &m) {
 // whole workgroup calls it.
 template <int P, bool REVERSE>
 __device__ inline float meet(const RecArgs &a, const Place &p, int order, bool scans, float h, const Scan &s, Meet &m) {
-    uint64_t *row = a.maps + p.row * a.tiles * kMostChannels;
+    uint64_t *row = a.maps + (int64_t)p.row * a.tiles * kMostChannels;
     const int ch = threadIdx.x, channels = a.lanes * P;   // channels that are published
     if (scans) {
         float A = 1.0f, B = 0.0f;
@@ -284,7 +284,7 @@ __device__ inline float meet(const RecArgs &a, const Place &p, int order, bool s
     __syncthreads();
     if (scans) {
         if (from > 0) {
-            const uint32_t *at = a.reached + (p.row * ((a.tiles + kGroup - 1) / kGroup) + from / kGroup) *
+            const uint32_t *at = a.reached + ((int64_t)p.row * ((a.tiles + kGroup - 1) / kGroup) + from / kGroup) *
                                                  kMostChannels + ch;
             uint32_t w;
             while ((w = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == kNone)
@@ -302,7 +302,7 @@ __device__ inline float meet(const RecArgs &a, const Place &p, int order, bool s
 // Publishes the state behind the order-th tile where a later tile starts from it.
 __device__ inline void reach(const RecArgs &a, const Place &p, int order, float h) {
     if ((order + 1) % kGroup == 0 && order + 1 < a.tiles)
-        __hip_atomic_store(a.reached + (p.row * ((a.tiles + kGroup - 1) / kGroup) + (order + 1) / kGroup) *
+        __hip_atomic_store(a.reached + ((int64_t)p.row * ((a.tiles + kGroup - 1) / kGroup) + (order + 1) / kGroup) *
                                            kMostChannels + threadIdx.x,
                            published(h), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -315,12 +315,13 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) 
     __shared__ typename std::conditional<SPLIT, Meet, int>::type met;
     Place p = place_of<DT>(a);
     const bool scans = threadIdx.x < a.lanes * P;   // the threads that go through the wavefronts, one a channel
-    const int64_t ch = (p.c - p.cl * P) + threadIdx.x, per = (a.L + kEvery - 1) / kEvery;
+    const int64_t ch = (p.c - p.cl * P) + (int)threadIdx.x, per = ((int64_t)a.L + kEvery - 1) / kEvery;
+    const uint32_t L = a.L;
     float carry = scans && ch < a.C && a.h0 ? a.h0[p.i * a.C + ch] : 0.0f;
     int k = 0;
     if constexpr (SPLIT) k = take_tile(a, p, met);
     uint32_t wv[S], wf[S], wo[S];
-    auto load = [&](int64_t t0) {
+    auto load = [&](uint32_t t0) {
         load_run<DT>(a.v, p, t0, 0, wv);
         load_run<DT>(a.f, p, t0, kKeep<DT>, wf);
         if (GATE) load_run<DT>(a.o, p, t0, 0, wo);
@@ -329,8 +330,11 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) 
 
     for (;; k++) {
         // as if new: what follows from them is not kept across tiles
-        if (!SPLIT) asm("" : "+v"(p.c), "+v"(p.c_ld), "+s"(a.v.ts), "+s"(a.f.ts), "+s"(a.o.ts), "+s"(a.y.ts));
-        const int64_t t0 = k * p.tile + p.run * S;
+        if (!SPLIT) {
+            asm("" : "+v"(p.c), "+v"(p.c_ld), "+v"(p.run), "+v"(p.cl), "+v"(p.lane), "+s"(p.i));
+            asm("" : "+s"(a.v.ts), "+s"(a.f.ts), "+s"(a.o.ts), "+s"(a.y.ts));
+        }
+        const uint32_t t0 = k * p.tile + p.run * S;
         const bool live = k * p.tile + p.wave * (64 / a.lanes) * S < p.len;   // of the wavefront
         float fa[S][P], fb[S][P], A[P], B[P];
 #pragma unroll
@@ -367,11 +371,12 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) 
         float h[P];
 #pragma unroll
         for (int j = 0; j < P; j++) h[j] = __builtin_fmaf(A[j], scan.start[p.wave][p.cl * P + j], B[j]);
-        if (a.states && t0 % kEvery == 0 && t0 < a.L)
+        if (a.states && t0 % kEvery == 0 && t0 < L)
 #pragma unroll
             for (int j = 0; j < P; j++)
                 if (j < p.count) a.states[(p.i * per + t0 / kEvery) * a.C + p.c + j] = h[j];
         char *at = run_at<DT>(a.y, p, t0);
+        const uint32_t left = t0 < L ? L - t0 : 0;
         auto steps = [&](auto whole) {
 #pragma unroll
             for (int s = 0; s < S; s++) {
@@ -386,13 +391,13 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) 
                         out[j] *= so;
                     }
                 }
-                store_step<DT, whole.value>(at, a.y.ts, p, s, a.L - t0, t0 + s < p.len ? Elem<DT>::put(out) : 0);
+                store_step<DT, whole.value>(at, a.y.ts, p, s, left, t0 + s < p.len ? Elem<DT>::put(out) : 0);
             }
         };
         if (!live) {
 #pragma unroll
-            for (int s = 0; s < S; s++) store_step<DT, false>(at, a.y.ts, p, s, a.L - t0, 0);
-        } else if (whole_run<DT>(p, t0, a.L)) {
+            for (int s = 0; s < S; s++) store_step<DT, false>(at, a.y.ts, p, s, left, 0);
+        } else if (whole_run<DT>(p, t0, L)) {
             steps(std::true_type());
         } else {
             steps(std::false_type());
@@ -415,17 +420,19 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a)
     const int other = a.waves > 1 ? 64 : 0;                       // and those that go through the states'
     const bool fscans = (int)threadIdx.x >= other && (int)threadIdx.x < other + channels;
     const int64_t c0 = p.c - p.cl * P, ch = c0 + threadIdx.x, fch = c0 + threadIdx.x - other;
-    const int64_t per = (a.L + kEvery - 1) / kEvery;
+    const int64_t per = ((int64_t)a.L + kEvery - 1) / kEvery;
+    const uint32_t L = a.L;
     float carry = scans && ch < a.C && a.dh_last ? a.dh_last[p.i * a.C + ch] : 0.0f;
     int order = 0;
     if constexpr (SPLIT) order = take_tile(a, p, met);
     for (;; order++) {
         // as if new: what follows from them is not kept across tiles
         if (!SPLIT) {
-            asm("" : "+v"(p.c), "+v"(p.c_ld), "+s"(a.v.ts), "+s"(a.f.ts), "+s"(a.o.ts), "+s"(a.dy.ts));
+            asm("" : "+v"(p.c), "+v"(p.c_ld), "+v"(p.run), "+v"(p.cl), "+v"(p.lane), "+s"(p.i));
+            asm("" : "+s"(a.v.ts), "+s"(a.f.ts), "+s"(a.o.ts), "+s"(a.dy.ts));
             asm("" : "+s"(a.dv.ts), "+s"(a.df.ts), "+s"(a.dO.ts));
         }
-        const int64_t tile0 = (a.tiles - 1 - order) * p.tile, t0 = tile0 + p.run * S;
+        const uint32_t tile0 = (uint32_t)(a.tiles - 1 - order) * p.tile, t0 = tile0 + p.run * S;
         const bool live = tile0 + p.wave * (64 / a.lanes) * S < p.len;   // of the wavefront
         uint32_t wv[S], wf[S], wo[S], wg[S];
         load_run<DT>(a.f, p, t0, kKeep<DT>, wf);
@@ -433,7 +440,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a)
         if (GATE) load_run<DT>(a.o, p, t0, 0, wo);
         load_run<DT>(a.v, p, t0, 0, wv);
         float state = 0.0f;
-        if (fscans && tile0 < a.L && fch < a.C) state = a.states[(p.i * per + tile0 / kEvery) * a.C + fch];
+        if (fscans && tile0 < L && fch < a.C) state = a.states[(p.i * per + tile0 / kEvery) * a.C + fch];
 
         float fa[S][P], in[S][P], A[P], R[P], FA[P], B[P];
 #pragma unroll
@@ -472,11 +479,12 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a)
         rocket::renew(wg);
         if (GATE) rocket::renew(wo);
         char *at_v = run_at<DT>(a.dv, p, t0), *at_f = run_at<DT>(a.df, p, t0);
+        const uint32_t left = t0 < L ? L - t0 : 0;
         char *at_o = GATE ? run_at<DT>(a.dO, p, t0) : nullptr;
         auto store = [&](auto whole, int s, uint32_t gv, uint32_t gf, uint32_t go) {
-            store_step<DT, whole.value>(at_v, a.dv.ts, p, s, a.L - t0, gv);
-            store_step<DT, whole.value>(at_f, a.df.ts, p, s, a.L - t0, gf);
-            if (GATE) store_step<DT, whole.value>(at_o, a.dO.ts, p, s, a.L - t0, go);
+            store_step<DT, whole.value>(at_v, a.dv.ts, p, s, left, gv);
+            store_step<DT, whole.value>(at_f, a.df.ts, p, s, left, gf);
+            if (GATE) store_step<DT, whole.value>(at_o, a.dO.ts, p, s, left, go);
         };
         auto steps = [&](auto whole) {
             float h[S][P], e[P];   // the state before each step
@@ -513,7 +521,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a)
         if (!live) {
 #pragma unroll
             for (int s = 0; s < S; s++) store(std::false_type(), s, 0, 0, 0);
-        } else if (whole_run<DT>(p, t0, a.L)) {
+        } else if (whole_run<DT>(p, t0, L)) {
             steps(std::true_type());
         } else {
             steps(std::false_type());
@@ -698,7 +706,7 @@ extern "C" rocket_status rocket_recurrence_forward(const rocket_sequence_shape *
     const int size = rocket::elem_size(shape->dtype);
     RecArgs a = {};
     a.v = view(v, size), a.f = view(f, size), a.o = view(o, size), a.y = view(y, size);
-    a.n = shape->n, a.L = shape->steps, a.C = shape->channels, a.lengths = shape->lengths;
+    a.n = (int32_t)shape->n, a.L = (int32_t)shape->steps, a.C = shape->channels, a.lengths = shape->lengths;
     a.h0 = h0, a.h_last = h_last, a.states = states;
     set_cut(a, cut, workspace);
     BY_TYPE(run_forward, shape->dtype, o != nullptr, a, cut, (hipStream_t)hip_stream);
@@ -726,7 +734,7 @@ extern "C" rocket_status rocket_recurrence_backward(const rocket_sequence_shape 
     RecArgs a = {};
     a.v = view(v, size), a.f = view(f, size), a.o = view(o, size);
     a.dy = view(dy, size), a.dv = view(dv, size), a.df = view(df, size), a.dO = view(dO, size);
-    a.n = shape->n, a.L = shape->steps, a.C = shape->channels, a.lengths = shape->lengths;
+    a.n = (int32_t)shape->n, a.L = (int32_t)shape->steps, a.C = shape->channels, a.lengths = shape->lengths;
     a.states = const_cast<float *>(states), a.dh_last = dh_last, a.dh0 = dh0;
     set_cut(a, cut, workspace);
     BY_TYPE(run_backward, shape->dtype, o != nullptr, a, cut, (hipStream_t)hip_stream);

@@ -115,15 +115,18 @@ __device__ inline void renew(uint32_t (&w)[N]) {
 // The work item of a workgroup: workgroups go to the 8 XCDs in turn, and each
 // XCD has an L2 of its own, so that items in a row (which share cache lines at
 // their borders) are given to workgroups of one XCD.
-__device__ inline int64_t item_of_block() {
+__device__ inline uint32_t item_of_block() {
     const uint32_t b = blockIdx.x, x = b & 7, each = gridDim.x >> 3, more = gridDim.x & 7;
-    return (int64_t)x * each + (x < more ? x : more) + (b >> 3);
+    return x * each + (x < more ? x : more) + (b >> 3);
 }
 
+// A value that is the same for the whole wavefront, into a scalar register.
+__device__ inline int uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane((int)x); }
+
 // Steps of series i: its length, clamped into [0, L].
-__device__ inline int64_t steps_of(const int32_t *lengths, int64_t i, int64_t L) {
+__device__ inline int32_t steps_of(const int32_t *lengths, int64_t i, int32_t L) {
     if (!lengths) return L;
-    int64_t t = lengths[i];
+    int32_t t = lengths[i];
     return t < 0 ? 0 : t > L ? L : t;
 }
 

@@ -20,7 +20,6 @@ stream is the caller's to order and to keep alive (Tensor.record_stream).
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 
 import torch
@@ -31,15 +30,16 @@ from .rocket import CSequence, CSequenceShape
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 EVERY = 128   # steps between the states a recurrence keeps (ROCKET_RECURRENCE_EVERY)
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-_SAME_STREAM = contextlib.nullcontext()
+_byref, _empty, _f32 = ctypes.byref, torch.empty, torch.float32
 
-
-def _on(stream):
-    """The context in which a call allocates, and its stream's handle."""
-    current = torch.cuda.current_stream()
-    if stream is None or stream == current:
-        return _SAME_STREAM, current.cuda_stream
-    return torch.cuda.stream(stream), stream.cuda_stream
+# The current GPU and the handle of its current stream; torch.cuda's own
+# functions make objects of them, which takes as long as a small kernel.
+_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):
+    _stream = torch._C._cuda_getCurrentRawStream
+else:
+    def _stream(device):
+        return torch.cuda.current_stream(device).cuda_stream
 
 
 def _dtype(x, name: str) -> int:
@@ -48,7 +48,7 @@ def _dtype(x, name: str) -> int:
     code = _DTYPES.get(x.dtype)
     if code is None:
         raise ValueError("%s must be float32, bfloat16 or float16" % name)
-    if x.device.index != torch.cuda.current_device():
+    if x.get_device() != _device():
         raise ValueError("%s must be on the current GPU" % name)
     return code
 
@@ -56,7 +56,7 @@ def _dtype(x, name: str) -> int:
 def _like(t, x, name: str):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a torch tensor on the GPU" % name)
-    if t.dtype != x.dtype or t.shape != x.shape or t.device != x.device:
+    if t.dtype != x.dtype or t.shape != x.shape or t.get_device() != x.get_device():
         raise ValueError("%s must have the shape, type and device of the call's first sequence" % name)
 
 
@@ -75,7 +75,7 @@ def _shape(x, lengths, name: str) -> CSequenceShape:
     if lengths is not None:
         if not isinstance(lengths, torch.Tensor) or not lengths.is_cuda:
             raise TypeError("lengths must be a torch tensor on the GPU")
-        if (lengths.dtype != torch.int32 or lengths.shape != (n,) or lengths.device != x.device
+        if (lengths.dtype != torch.int32 or lengths.shape != (n,) or lengths.get_device() != x.get_device()
                 or not lengths.is_contiguous()):
             raise ValueError("lengths must be contiguous int32 [%d] on the sequences' GPU" % n)
         lengths = lengths.data_ptr()
@@ -88,7 +88,7 @@ def _floats(t, shape, x, name: str):
         return None
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a torch tensor on the GPU" % name)
-    if t.dtype != torch.float32 or tuple(t.shape) != shape or t.device != x.device or not t.is_contiguous():
+    if t.dtype != torch.float32 or t.shape != shape or t.get_device() != x.get_device() or not t.is_contiguous():
         raise ValueError("%s must be contiguous float32 %s on the sequences' GPU" % (name, list(shape)))
     return t.data_ptr()
 
@@ -104,13 +104,13 @@ def _workspace(size: int, device):
     """A workspace tensor (or None) and its address, on the current stream."""
     if size == 0:
         return None, None
-    t = torch.empty(size, dtype=torch.uint8, device=device)
+    t = _empty(size, dtype=torch.uint8, device=device)
     return t, t.data_ptr()
 
 
 def _norm_workspace(lib, shape, groups: int, backward: int) -> int:
     size = ctypes.c_int64()
-    rocket._check(lib.rocket_group_norm_workspace(ctypes.byref(shape), groups, backward, ctypes.byref(size)),
+    rocket._check(lib.rocket_group_norm_workspace(_byref(shape), groups, backward, _byref(size)),
                   "rocket_group_norm_workspace")
     return size.value
 
@@ -119,24 +119,24 @@ def group_norm(x, groups: int, weight=None, bias=None, *, eps: float = 1e-5, act
                out=None, stream=None):
     """rocket_group_norm_forward: (y, mean [n, groups], rstd [n, groups]).
     `out` (may be x) takes y."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return group_norm(x, groups, weight, bias, eps=eps, activation=activation, lengths=lengths, out=out)
     lib = rocket.library()
     shape, act = _shape(x, lengths, "x"), _activation(activation)
     n, _, channels = x.shape
     w, b = _floats(weight, (channels,), x, "weight"), _floats(bias, (channels,), x, "bias")
-    ctx, handle = _on(stream)
-    with ctx:
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        else:
-            _like(out, x, "out")
-        size = _norm_workspace(lib, shape, groups, 0)
-        stats = torch.empty((2, n, groups), dtype=torch.float32, device=x.device)
-        mean, rstd = stats[0], stats[1]
-        work, at = _workspace(size, x.device)
-        rocket._check(lib.rocket_group_norm_forward(
-            ctypes.byref(shape), groups, ctypes.byref(_sequence(x, "x")), w, b, eps, act,
-            ctypes.byref(_sequence(out, "out")), mean.data_ptr(), rstd.data_ptr(), at, size, handle),
-            "rocket_group_norm_forward")
+    if out is None:
+        out = _empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _like(out, x, "out")
+    size = _norm_workspace(lib, shape, groups, 0)
+    mean, rstd = (_empty((n, groups), dtype=_f32, device=x.device) for _ in range(2))
+    work, at = _workspace(size, x.device)
+    status = lib.rocket_group_norm_forward(
+        _byref(shape), groups, _byref(_sequence(x, "x")), w, b, eps, act, _byref(_sequence(out, "out")),
+        mean.data_ptr(), rstd.data_ptr(), at, size, _stream(x.get_device()))
+    rocket._check(status, "rocket_group_norm_forward")
     return out, mean, rstd
 
 
@@ -144,6 +144,10 @@ def group_norm_backward(dy, x, groups: int, mean, rstd, weight=None, bias=None, 
                         lengths=None, out=None, stream=None):
     """rocket_group_norm_backward: (dx, dweight, dbias), from the forward pass's
     mean and rstd.  `out` (may be dy or x) takes dx."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return group_norm_backward(dy, x, groups, mean, rstd, weight, bias, activation=activation,
+                                       lengths=lengths, out=out)
     lib = rocket.library()
     shape, act = _shape(x, lengths, "x"), _activation(activation)
     _like(dy, x, "dy")
@@ -151,39 +155,38 @@ def group_norm_backward(dy, x, groups: int, mean, rstd, weight=None, bias=None, 
     w, b = _floats(weight, (channels,), x, "weight"), _floats(bias, (channels,), x, "bias")
     if mean is None or rstd is None:
         raise TypeError("mean and rstd must be torch tensors on the GPU")
-    ctx, handle = _on(stream)
-    with ctx:
-        size = _norm_workspace(lib, shape, groups, 1)
-        m, r = _floats(mean, (n, groups), x, "mean"), _floats(rstd, (n, groups), x, "rstd")
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        else:
-            _like(out, x, "out")
-        grads = torch.empty((2, channels), dtype=torch.float32, device=x.device)
-        dweight, dbias = grads[0], grads[1]
-        work, at = _workspace(size, x.device)
-        rocket._check(lib.rocket_group_norm_backward(
-            ctypes.byref(shape), groups, ctypes.byref(_sequence(dy, "dy")), ctypes.byref(_sequence(x, "x")), w, b, act,
-            m, r, ctypes.byref(_sequence(out, "out")), dweight.data_ptr(), dbias.data_ptr(), at, size, handle),
-            "rocket_group_norm_backward")
+    size = _norm_workspace(lib, shape, groups, 1)
+    m, r = _floats(mean, (n, groups), x, "mean"), _floats(rstd, (n, groups), x, "rstd")
+    if out is None:
+        out = _empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _like(out, x, "out")
+    dweight, dbias = (_empty((channels,), dtype=_f32, device=x.device) for _ in range(2))
+    work, at = _workspace(size, x.device)
+    status = lib.rocket_group_norm_backward(
+        _byref(shape), groups, _byref(_sequence(dy, "dy")), _byref(_sequence(x, "x")), w, b, act, m, r,
+        _byref(_sequence(out, "out")), dweight.data_ptr(), dbias.data_ptr(), at, size, _stream(x.get_device()))
+    rocket._check(status, "rocket_group_norm_backward")
     return out, dweight, dbias
 
 
 def _recurrence_workspace(lib, shape) -> int:
     size = ctypes.c_int64()
-    rocket._check(lib.rocket_recurrence_workspace(ctypes.byref(shape), ctypes.byref(size)),
-                  "rocket_recurrence_workspace")
+    rocket._check(lib.rocket_recurrence_workspace(_byref(shape), _byref(size)), "rocket_recurrence_workspace")
     return size.value
 
 
 def _optional(t, name: str):
-    return None if t is None else ctypes.byref(_sequence(t, name))
+    return None if t is None else _byref(_sequence(t, name))
 
 
 def recurrence(v, f, o=None, *, h0=None, lengths=None, keep_states: bool = False, out=None, stream=None):
     """rocket_recurrence_forward: (y, h_last [n, channels], states), states
     [n, ceil(steps / EVERY), channels] with keep_states (for
     recurrence_backward), else None.  `out` (may be v, f or o) takes y."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return recurrence(v, f, o, h0=h0, lengths=lengths, keep_states=keep_states, out=out)
     lib = rocket.library()
     shape = _shape(v, lengths, "v")
     _like(f, v, "f")
@@ -191,21 +194,19 @@ def recurrence(v, f, o=None, *, h0=None, lengths=None, keep_states: bool = False
         _like(o, v, "o")
     n, steps, channels = v.shape
     first = _floats(h0, (n, channels), v, "h0")
-    ctx, handle = _on(stream)
-    with ctx:
-        if out is None:
-            out = torch.empty(v.shape, dtype=v.dtype, device=v.device)
-        else:
-            _like(out, v, "out")
-        size = _recurrence_workspace(lib, shape)
-        h_last = torch.empty((n, channels), dtype=torch.float32, device=v.device)
-        states = torch.empty((n, -(-steps // EVERY), channels), dtype=torch.float32,
-                             device=v.device) if keep_states else None
-        work, at = _workspace(size, v.device)
-        rocket._check(lib.rocket_recurrence_forward(
-            ctypes.byref(shape), ctypes.byref(_sequence(v, "v")), ctypes.byref(_sequence(f, "f")), _optional(o, "o"),
-            first, ctypes.byref(_sequence(out, "out")), h_last.data_ptr(),
-            None if states is None else states.data_ptr(), at, size, handle), "rocket_recurrence_forward")
+    if out is None:
+        out = _empty(v.shape, dtype=v.dtype, device=v.device)
+    else:
+        _like(out, v, "out")
+    size = _recurrence_workspace(lib, shape)
+    h_last = _empty((n, channels), dtype=_f32, device=v.device)
+    states = _empty((n, -(-steps // EVERY), channels), dtype=_f32, device=v.device) if keep_states else None
+    work, at = _workspace(size, v.device)
+    status = lib.rocket_recurrence_forward(
+        _byref(shape), _byref(_sequence(v, "v")), _byref(_sequence(f, "f")), _optional(o, "o"), first,
+        _byref(_sequence(out, "out")), h_last.data_ptr(), None if states is None else states.data_ptr(), at, size,
+        _stream(v.get_device()))
+    rocket._check(status, "rocket_recurrence_forward")
     return out, h_last, states
 
 
@@ -213,34 +214,37 @@ def recurrence_backward(dy, v, f, states, o=None, *, dh_last=None, lengths=None,
     """rocket_recurrence_backward: (dv, df, do, dh0 [n, channels]); do is None
     without an output gate.  `out`: the tensors that take dv, df (and do), for
     example blocks of a projection's gradient."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return recurrence_backward(dy, v, f, states, o, dh_last=dh_last, lengths=lengths, out=out)
     lib = rocket.library()
     shape = _shape(v, lengths, "v")
-    for t, name in ((dy, "dy"), (f, "f")) + (((o, "o"),) if o is not None else ()):
-        _like(t, v, name)
+    _like(dy, v, "dy")
+    _like(f, v, "f")
+    if o is not None:
+        _like(o, v, "o")
     n, steps, channels = v.shape
     if states is None:
         raise TypeError("states must be the forward pass's (keep_states)")
     kept = _floats(states, (n, -(-steps // EVERY), channels), v, "states")
     last = _floats(dh_last, (n, channels), v, "dh_last")
     wanted = 2 if o is None else 3
-    ctx, handle = _on(stream)
-    with ctx:
-        if out is None:
-            out = [torch.empty(v.shape, dtype=v.dtype, device=v.device) for _ in range(wanted)]
-        elif len(out) != wanted:
-            raise ValueError("out must hold %d tensors" % wanted)
-        else:
-            for t in out:
-                _like(t, v, "out")
-        size = _recurrence_workspace(lib, shape)
-        dh0 = torch.empty((n, channels), dtype=torch.float32, device=v.device)
-        work, at = _workspace(size, v.device)
-        do = out[2] if o is not None else None
-        rocket._check(lib.rocket_recurrence_backward(
-            ctypes.byref(shape), ctypes.byref(_sequence(dy, "dy")), ctypes.byref(_sequence(v, "v")),
-            ctypes.byref(_sequence(f, "f")), _optional(o, "o"), kept, last, ctypes.byref(_sequence(out[0], "out")),
-            ctypes.byref(_sequence(out[1], "out")), _optional(do, "out"), dh0.data_ptr(), at, size, handle),
-            "rocket_recurrence_backward")
+    if out is None:
+        out = [_empty(v.shape, dtype=v.dtype, device=v.device) for _ in range(wanted)]
+    elif len(out) != wanted:
+        raise ValueError("out must hold %d tensors" % wanted)
+    else:
+        for t in out:
+            _like(t, v, "out")
+    size = _recurrence_workspace(lib, shape)
+    dh0 = _empty((n, channels), dtype=_f32, device=v.device)
+    work, at = _workspace(size, v.device)
+    do = out[2] if o is not None else None
+    status = lib.rocket_recurrence_backward(
+        _byref(shape), _byref(_sequence(dy, "dy")), _byref(_sequence(v, "v")), _byref(_sequence(f, "f")),
+        _optional(o, "o"), kept, last, _byref(_sequence(out[0], "out")), _byref(_sequence(out[1], "out")),
+        _optional(do, "out"), dh0.data_ptr(), at, size, _stream(v.get_device()))
+    rocket._check(status, "rocket_recurrence_backward")
     return out[0], out[1], do, dh0
 
 
@@ -248,14 +252,18 @@ def _matrix(t, name: str):
     """Address and row stride of [n, channels] with contiguous channels."""
     if t is None:
         return None, 0
-    if t.stride(1) != 1 and t.shape[1] > 1:
+    rows, channels = t.stride()
+    if channels != 1 and t.shape[1] > 1:
         raise ValueError("%s must have contiguous channels" % name)
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), rows
 
 
 def recurrence_step(v, f, h, o=None, *, h_out=None, out=None, stream=None):
     """rocket_recurrence_step on [n, channels]: (y, the new state).  `h_out`
     (may be h) takes the new state, `out` takes y."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return recurrence_step(v, f, h, o, h_out=h_out, out=out)
     lib = rocket.library()
     code = _dtype(v, "v")
     if v.dim() != 2:
@@ -265,22 +273,18 @@ def recurrence_step(v, f, h, o=None, *, h_out=None, out=None, stream=None):
         _like(o, v, "o")
     if h is None:
         raise TypeError("h must be a torch tensor on the GPU")
-    at_h = _floats(h, tuple(v.shape), v, "h")
-    ctx, handle = _on(stream)
-    with ctx:
-        if out is None:
-            out = torch.empty(v.shape, dtype=v.dtype, device=v.device)
-        else:
-            _like(out, v, "out")
-        if h_out is None:
-            h_out = torch.empty_like(h)
-        at_out = _floats(h_out, tuple(v.shape), v, "h_out")
-        pv, vs = _matrix(v, "v")
-        pf, fs = _matrix(f, "f")
-        po, os = _matrix(o, "o")
-        py, ys = _matrix(out, "out")
-        rocket._check(lib.rocket_recurrence_step(v.shape[0], v.shape[1], code, pv, vs, pf, fs, po, os, at_h, at_out,
-                                                 py, ys, handle), "rocket_recurrence_step")
+    at_h = _floats(h, v.shape, v, "h")
+    if out is None:
+        out = _empty(v.shape, dtype=v.dtype, device=v.device)
+    else:
+        _like(out, v, "out")
+    if h_out is None:
+        h_out = _empty(v.shape, dtype=_f32, device=v.device)
+    at_out = _floats(h_out, v.shape, v, "h_out")
+    n, channels = v.shape
+    status = lib.rocket_recurrence_step(n, channels, code, *_matrix(v, "v"), *_matrix(f, "f"), *_matrix(o, "o"), at_h,
+                                        at_out, *_matrix(out, "out"), _stream(v.get_device()))
+    rocket._check(status, "rocket_recurrence_step")
     return out, h_out
 
 
@@ -308,25 +312,26 @@ def dropout(x, p: float, seed: int, call: int = 0, *, residual=None, out=None, s
     """rocket_dropout over all elements of x in their order: dropout(x), plus
     `residual` where given.  `seed` and `call` are taken modulo 2^64.  `out`
     (may be x or residual) takes the result."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return dropout(x, p, seed, call, residual=residual, out=out)
     lib = rocket.library()
     code = _dtype(x, "x")
     if residual is not None:
         _like(residual, x, "residual")
-    ctx, handle = _on(stream)
-    with ctx:
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        else:
-            _like(out, x, "out")
-        given = [(x, "x"), (residual, "residual"), (out, "out")]
-        views = [(None, None, None, 0) if t is None else _rows(t, name) for t, name in given]
-        rows, cols = max(v[1] for v in views if v[1] is not None), x.numel()
-        if rows > 1:   # a contiguous operand beside one in rows
-            cols = x.shape[-1]
-            views = [(v[0], rows, cols, cols) if v[1] == 1 else v for v in views]
-        rocket._check(lib.rocket_dropout(views[0][0], views[1][0], views[2][0], rows, cols, views[0][3], views[1][3],
-                                         views[2][3], code, p, seed & (2 ** 64 - 1), call & (2 ** 64 - 1), handle),
-                      "rocket_dropout")
+    if out is None:
+        out = _empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _like(out, x, "out")
+    vx, vy = _rows(x, "x"), _rows(out, "out")
+    vr = (None, 1, 0, 0) if residual is None else _rows(residual, "residual")
+    rows, cols = max(vx[1], vr[1], vy[1]), x.numel()
+    if rows > 1:   # a contiguous operand beside one in rows
+        cols = x.shape[-1]
+        vx, vr, vy = ((v[0], rows, cols, cols) if v[1] == 1 else v for v in (vx, vr, vy))
+    status = lib.rocket_dropout(vx[0], vr[0], vy[0], rows, cols, vx[3], vr[3], vy[3], code, p, seed & (2 ** 64 - 1),
+                                call & (2 ** 64 - 1), _stream(x.get_device()))
+    rocket._check(status, "rocket_dropout")
     return out
 
 
