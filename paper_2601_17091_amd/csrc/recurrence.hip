@@ -599,9 +599,17 @@ struct Cut {
 
 // Lanes over channels: the power of two that covers the words of channels, 32
 // at most; the wavefront's other lanes take further runs of steps, so that
-// few channels do not leave lanes idle.  Split: where rows alone do not fill
-// the chip.
-bool cut_of(const rocket_sequence_shape *s, Cut *cut) {
+// few channels do not leave lanes idle.
+//
+// Split where rows alone do not fill the chip (8 x 10000 x 256, fp32, backward:
+// 93 us, against 140 us with a first launch for the maps), and for two kinds of
+// calls whose loop over tiles leaves more to be waited for than tiles that
+// meet cost: fp32 rows of 8 tiles and more (1000 x 1000 x 256, backward: 945 us
+// against 1027 us; 256 x 300 x 512, 3 tiles: 188 against 167 us), and the gated
+// backward pass of 16-bit elements, short of registers in its loop, where the
+// tiles are mostly full (1000 x 1000 x 256: 786 us against 904 us; 1000 x 129 x
+// 256, a last tile of one step: 198 against 172 us).
+bool cut_of(const rocket_sequence_shape *s, bool back, bool gate, Cut *cut) {
     const int64_t per_word = rocket::elem_size(s->dtype) == 4 ? 1 : 2;
     const int64_t words = (s->channels + per_word - 1) / per_word;
     cut->lanes = 1;
@@ -614,7 +622,8 @@ bool cut_of(const rocket_sequence_shape *s, Cut *cut) {
     cut->tiles = (int32_t)((L + tile - 1) / tile);
     cut->blocks = (int32_t)((words + cut->lanes - 1) / cut->lanes);
     cut->rows = s->n * cut->blocks;
-    cut->split = cut->tiles > 1 && cut->rows < kFill;
+    cut->split = cut->tiles > 1 && (cut->rows < kFill || (per_word == 1 && cut->tiles >= 8) ||
+                                    (per_word == 2 && back && gate && 4 * L >= 3 * tile * cut->tiles));
     return !__builtin_mul_overflow(cut->rows, (int64_t)(cut->split ? cut->tiles : 1), &cut->grid) &&
            cut->grid <= INT_MAX;
 }
@@ -684,9 +693,14 @@ void run_step(const StepArgs &a, hipStream_t s) {
 }  // namespace
 
 extern "C" rocket_status rocket_recurrence_workspace(const rocket_sequence_shape *shape, int64_t *bytes) {
-    Cut cut;
-    if (!bytes || !rocket::shape_ok(shape) || !cut_of(shape, &cut)) return ROCKET_ERR_INVALID_ARG;
-    *bytes = workspace_of(cut);
+    if (!bytes || !rocket::shape_ok(shape)) return ROCKET_ERR_INVALID_ARG;
+    int64_t most = 0;
+    for (int k = 0; k < 4; k++) {   // either pass, gated or not
+        Cut cut;
+        if (!cut_of(shape, k & 1, k & 2, &cut)) return ROCKET_ERR_INVALID_ARG;
+        if (workspace_of(cut) > most) most = workspace_of(cut);
+    }
+    *bytes = most;
     return ROCKET_OK;
 }
 
@@ -695,7 +709,7 @@ extern "C" rocket_status rocket_recurrence_forward(const rocket_sequence_shape *
                                                    const rocket_sequence *y, float *h_last, float *states,
                                                    void *workspace, int64_t workspace_bytes, void *hip_stream) {
     Cut cut;
-    if (!rocket::shape_ok(shape) || !cut_of(shape, &cut) || !rocket::view_ok(v, shape) || !rocket::view_ok(f, shape) ||
+    if (!rocket::shape_ok(shape) || !cut_of(shape, false, o != nullptr, &cut) || !rocket::view_ok(v, shape) || !rocket::view_ok(f, shape) ||
         (o && !rocket::view_ok(o, shape)) || !rocket::out_ok(y, shape) || (shape->n > 0 && !h_last))
         return ROCKET_ERR_INVALID_ARG;
     const int64_t need = workspace_of(cut);
@@ -720,7 +734,7 @@ extern "C" rocket_status rocket_recurrence_backward(const rocket_sequence_shape 
                                                     const rocket_sequence *df, const rocket_sequence *dO, float *dh0,
                                                     void *workspace, int64_t workspace_bytes, void *hip_stream) {
     Cut cut;
-    if (!rocket::shape_ok(shape) || !cut_of(shape, &cut) || !rocket::view_ok(dy, shape) ||
+    if (!rocket::shape_ok(shape) || !cut_of(shape, true, o != nullptr, &cut) || !rocket::view_ok(dy, shape) ||
         !rocket::view_ok(v, shape) || !rocket::view_ok(f, shape) || (o && !rocket::view_ok(o, shape)) ||
         !rocket::out_ok(dv, shape) || !rocket::out_ok(df, shape) || (o != nullptr) != (dO != nullptr) ||
         (dO && !rocket::out_ok(dO, shape)) || (shape->n > 0 && !dh0) || (!rocket::empty(shape) && !states))
