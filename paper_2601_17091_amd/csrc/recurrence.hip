@@ -48,6 +48,8 @@ constexpr int kMostWaves = 8;
 constexpr int kMostChannels = 64;                // of a workgroup: 32 lanes x 2
 constexpr int64_t kFill = 512;                   // rows that fill the chip
 constexpr int kGroup = 32;                       // tiles from one published state to the next
+// A workgroup's way through a row: all its tiles, one of many, the only one.
+enum Way { kLoop, kSplit, kOne };
 constexpr uint32_t kNone = 0xffffffffu;          // not published yet
 
 struct View {
@@ -307,10 +309,11 @@ __device__ inline void reach(const RecArgs &a, const Place &p, int order, float 
                            published(h), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// The forward pass: over a row, or over one tile of it (SPLIT).
-template <int DT, bool SPLIT, bool GATE>
+// The forward pass over a row, or over one tile of it.
+template <int DT, int WAY, bool GATE>
 __global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) {
     constexpr int P = Elem<DT>::kPerWord, S = kRun<DT>;
+    constexpr bool SPLIT = WAY == kSplit;
     __shared__ Scan scan;
     __shared__ typename std::conditional<SPLIT, Meet, int>::type met;
     Place p = place_of<DT>(a);
@@ -330,7 +333,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) 
 
     for (;; k++) {
         // as if new: what follows from them is not kept across tiles
-        if (!SPLIT) {
+        if (WAY == kLoop) {
             asm("" : "+v"(p.c), "+v"(p.c_ld), "+v"(p.run), "+v"(p.cl), "+v"(p.lane), "+s"(p.i));
             asm("" : "+s"(a.v.ts), "+s"(a.f.ts), "+s"(a.o.ts), "+s"(a.y.ts));
         }
@@ -361,7 +364,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) 
 #pragma unroll
             for (int s = 0; s < S; s++) go[s] = wo[s];
         }
-        if (!SPLIT && k + 1 < a.tiles) load(t0 + p.tile);   // on their way during the scan
+        if (WAY == kLoop && k + 1 < a.tiles) load(t0 + p.tile);   // on their way during the scan
         scan_lanes<P, false>(a, p, A, B, scan);
         __syncthreads();
         if constexpr (SPLIT) carry = meet<P, false>(a, p, k, scans, carry, scan, met);
@@ -402,16 +405,17 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) 
         } else {
             steps(std::false_type());
         }
-        if (SPLIT || k + 1 == a.tiles) break;
+        if (WAY != kLoop || k + 1 == a.tiles) break;
     }
     if (k == a.tiles - 1 && scans && ch < a.C) a.h_last[p.i * a.C + ch] = carry;
 }
 
-// The backward pass: over a row from its last tile to its first, or over one
-// tile of it (SPLIT).
-template <int DT, bool SPLIT, bool GATE>
+// The backward pass over a row from its last tile to its first, or over one
+// tile of it.
+template <int DT, int WAY, bool GATE>
 __global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a) {
     constexpr int P = Elem<DT>::kPerWord, S = kRun<DT>;
+    constexpr bool SPLIT = WAY == kSplit;
     __shared__ Scan scan, fscan;
     __shared__ typename std::conditional<SPLIT, Meet, int>::type met;
     Place p = place_of<DT>(a);
@@ -427,7 +431,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a)
     if constexpr (SPLIT) order = take_tile(a, p, met);
     for (;; order++) {
         // as if new: what follows from them is not kept across tiles
-        if (!SPLIT) {
+        if (WAY == kLoop) {
             asm("" : "+v"(p.c), "+v"(p.c_ld), "+v"(p.run), "+v"(p.cl), "+v"(p.lane), "+s"(p.i));
             asm("" : "+s"(a.v.ts), "+s"(a.f.ts), "+s"(a.o.ts), "+s"(a.dy.ts));
             asm("" : "+s"(a.dv.ts), "+s"(a.df.ts), "+s"(a.dO.ts));
@@ -526,7 +530,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a)
         } else {
             steps(std::false_type());
         }
-        if (SPLIT || order + 1 == a.tiles) break;
+        if (WAY != kLoop || order + 1 == a.tiles) break;
     }
     if (order == a.tiles - 1 && scans && ch < a.C) a.dh0[p.i * a.C + ch] = carry;
 }
@@ -656,21 +660,27 @@ bool aligned(const void *p, uintptr_t to) { return (uintptr_t)p % to == 0; }
 
 template <int DT, bool GATE>
 void run_forward(const RecArgs &a, const Cut &cut, hipStream_t s) {
+    const uint32_t grid = (uint32_t)cut.grid, threads = 64 * cut.waves;
     if (cut.split) {
         clear(a, cut, s);
-        forward_kernel<DT, true, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+        forward_kernel<DT, kSplit, GATE><<<grid, threads, 0, s>>>(a);
+    } else if (cut.tiles > 1) {
+        forward_kernel<DT, kLoop, GATE><<<grid, threads, 0, s>>>(a);
     } else {
-        forward_kernel<DT, false, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+        forward_kernel<DT, kOne, GATE><<<grid, threads, 0, s>>>(a);
     }
 }
 
 template <int DT, bool GATE>
 void run_backward(const RecArgs &a, const Cut &cut, hipStream_t s) {
+    const uint32_t grid = (uint32_t)cut.grid, threads = 64 * cut.waves;
     if (cut.split) {
         clear(a, cut, s);
-        backward_kernel<DT, true, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+        backward_kernel<DT, kSplit, GATE><<<grid, threads, 0, s>>>(a);
+    } else if (cut.tiles > 1) {
+        backward_kernel<DT, kLoop, GATE><<<grid, threads, 0, s>>>(a);
     } else {
-        backward_kernel<DT, false, GATE><<<(uint32_t)cut.grid, 64 * cut.waves, 0, s>>>(a);
+        backward_kernel<DT, kOne, GATE><<<grid, threads, 0, s>>>(a);
     }
 }
 
