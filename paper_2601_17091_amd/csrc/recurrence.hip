@@ -47,6 +47,7 @@ constexpr int kMostLanes = 32;                   // lanes over channels
 constexpr int kMostWaves = 8;
 constexpr int kMostChannels = 64;                // of a workgroup: 32 lanes x 2
 constexpr int64_t kFill = 512;                   // rows that fill the chip
+constexpr int kApart = 64;                       // words from counter to counter: each has its own cache line
 constexpr int kGroup = 32;                       // tiles from one published state to the next
 // A workgroup's way through a row: all its tiles, one of many, the only one.
 enum Way { kLoop, kSplit, kOne };
@@ -70,7 +71,7 @@ struct RecArgs {
     float *dh0;             // backward
     uint64_t *maps;         // [rows, tiles, 64], split
     uint32_t *reached;      // [rows, ceil(tiles / kGroup), 64]: states, split
-    uint32_t *taken;        // [rows]: tiles taken, less one, split
+    uint32_t *taken;        // [rows][kApart]: tiles taken, less one, split
     int32_t blocks;         // channel blocks
     int32_t lanes;          // lanes over channels, a power of two
     int32_t waves;          // wavefronts of a workgroup
@@ -229,7 +230,7 @@ __device__ inline uint32_t published(float x) {
 // The row's next tile.
 __device__ inline int take_tile(const RecArgs &a, const Place &p, Meet &m) {
     if (threadIdx.x == 0)
-        m.tile = (int)(__hip_atomic_fetch_add(a.taken + p.row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u);
+        m.tile = (int)(__hip_atomic_fetch_add(a.taken + (int64_t)p.row * kApart, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u);
     __syncthreads();
     return __builtin_amdgcn_readfirstlane(m.tile);
 }
@@ -311,7 +312,7 @@ __device__ inline void reach(const RecArgs &a, const Place &p, int order, float 
 
 // The forward pass over a row, or over one tile of it.
 template <int DT, int WAY, bool GATE>
-__global__ __launch_bounds__(64 * kMostWaves, 4) void forward_kernel(RecArgs a) {
+__global__ __launch_bounds__(64 * kMostWaves, WAY == kSplit && !GATE ? 8 : 4) void forward_kernel(RecArgs a) {
     constexpr int P = Elem<DT>::kPerWord, S = kRun<DT>;
     constexpr bool SPLIT = WAY == kSplit;
     __shared__ Scan scan;
@@ -606,13 +607,15 @@ struct Cut {
 // few channels do not leave lanes idle.
 //
 // Split where rows alone do not fill the chip (8 x 10000 x 256, fp32, backward:
-// 93 us, against 140 us with a first launch for the maps), and for two kinds of
-// calls whose loop over tiles leaves more to be waited for than tiles that
-// meet cost: fp32 rows of 8 tiles and more (1000 x 1000 x 256, backward: 945 us
-// against 1027 us; 256 x 300 x 512, 3 tiles: 188 against 167 us), and the gated
-// backward pass of 16-bit elements, short of registers in its loop, where the
-// tiles are mostly full (1000 x 1000 x 256: 786 us against 904 us; 1000 x 129 x
-// 256, a last tile of one step: 198 against 172 us).
+// 90 us, against 140 us with a first launch for the maps), and for three kinds
+// of calls whose loop over tiles leaves more to be waited for than tiles that
+// meet cost: long rows that fill it badly at last (600 rows of 4,000 steps,
+// bf16: 187 us against 231 us; 1,000 rows: 83 against 86 us forward, 87 against
+// 75 us backward); fp32 rows of 8 tiles and more (1000 x 1000 x 256, backward:
+// 945 us against 1027 us; 256 x 300 x 512, 3 tiles: 188 against 167 us); and the
+// gated backward pass of 16-bit elements, short of registers in its loop, where
+// the tiles are mostly full (1000 x 1000 x 256: 788 us against 904 us; 1000 x
+// 129 x 256, a last tile of one step: 197 against 173 us).
 bool cut_of(const rocket_sequence_shape *s, bool back, bool gate, Cut *cut) {
     const int64_t per_word = rocket::elem_size(s->dtype) == 4 ? 1 : 2;
     const int64_t words = (s->channels + per_word - 1) / per_word;
@@ -626,8 +629,11 @@ bool cut_of(const rocket_sequence_shape *s, bool back, bool gate, Cut *cut) {
     cut->tiles = (int32_t)((L + tile - 1) / tile);
     cut->blocks = (int32_t)((words + cut->lanes - 1) / cut->lanes);
     cut->rows = s->n * cut->blocks;
-    cut->split = cut->tiles > 1 && (cut->rows < kFill || (per_word == 1 && cut->tiles >= 8) ||
-                                    (per_word == 2 && back && gate && 4 * L >= 3 * tile * cut->tiles));
+    const int64_t slots = (cut->rows + kFill - 1) / kFill * kFill;   // of all rounds of a loop
+    cut->split = cut->tiles > 1 &&
+                 (cut->rows < kFill || (cut->tiles >= 8 && cut->rows < 4 * kFill && 4 * cut->rows < 3 * slots) ||
+                  (per_word == 1 && cut->tiles >= 8) ||
+                  (per_word == 2 && back && gate && 4 * L >= 3 * tile * cut->tiles));
     return !__builtin_mul_overflow(cut->rows, (int64_t)(cut->split ? cut->tiles : 1), &cut->grid) &&
            cut->grid <= INT_MAX;
 }
@@ -635,7 +641,7 @@ bool cut_of(const rocket_sequence_shape *s, bool back, bool gate, Cut *cut) {
 // 8-byte words of a split call's maps, published states and counters.
 int64_t map_words(const Cut &c) { return c.rows * c.tiles * kMostChannels; }
 int64_t reached_words(const Cut &c) { return c.rows * ((c.tiles + kGroup - 1) / kGroup) * (kMostChannels / 2); }
-int64_t workspace_words(const Cut &c) { return c.split ? map_words(c) + reached_words(c) + (c.rows + 1) / 2 : 0; }
+int64_t workspace_words(const Cut &c) { return c.split ? map_words(c) + reached_words(c) + c.rows * (kApart / 2) : 0; }
 int64_t workspace_of(const Cut &c) { return workspace_words(c) * 8; }
 
 void set_cut(RecArgs &a, const Cut &c, void *workspace) {
