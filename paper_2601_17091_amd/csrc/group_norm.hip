@@ -19,7 +19,9 @@
 // A thread owns one column of 16 bytes of channels in every `rows`-th step.
 // The last column of a slab is moved back so that it ends with the slab; the
 // channels it shares with its neighbour are computed twice and counted once.
+#include <algorithm>
 #include <climits>
+#include <iterator>
 #include <type_traits>
 
 #include "sequence.h"
@@ -673,9 +675,13 @@ struct Cut {
 
 constexpr int kFold = 128;
 // Workgroups that hold a slab: threads, and 16-byte columns of a thread (of
-// each operand); the last is also the size of a chunk's workgroup.
-constexpr int kSizes[4][2] = {{64, 4}, {256, 4}, {256, 16}, {512, 16}};
-constexpr int kBackSizes[4][2] = {{64, 4}, {256, 4}, {256, 8}, {512, 8}};
+// each operand).
+struct Size {
+    int threads, run;
+};
+constexpr Size kSizes[] = {{64, 4}, {256, 4}, {256, 8}, {512, 8}, {512, 16}};
+constexpr Size kBackSizes[] = {{64, 4}, {256, 4}, {256, 8}, {512, 8}};
+constexpr Size kChunk = {256, 16}, kBackChunk = {256, 8};   // of a chunk, and of rows of less than 16 bytes
 
 // The slabs for `per` groups each, and the smallest workgroup that holds one.
 bool hold(const rocket_sequence_shape *s, int32_t groups, int64_t per, int vec, bool back, Cut *cut) {
@@ -684,15 +690,13 @@ bool hold(const rocket_sequence_shape *s, int32_t groups, int64_t per, int vec, 
     const int64_t most = (groups + cut->slabs - 1) / cut->slabs;   // the most groups a slab gets
     cut->cols = (int32_t)((most * cut->width + vec - 1) / vec);
     cut->groups = (int32_t)most;
-    const int(*sizes)[2] = back ? kBackSizes : kSizes;
-    for (int k = cut->wide ? 0 : 2; k < (cut->wide ? 4 : 3); k++) {
-        const int rows = sizes[k][0] / cut->cols;
-        if (rows >= 1 && (int64_t)rows * sizes[k][1] >= L) {
-            cut->threads = sizes[k][0], cut->run = sizes[k][1], cut->rows = rows;
-            return true;
-        }
-    }
-    return false;
+    auto holds = [&](const Size &z) {
+        cut->threads = z.threads, cut->run = z.run, cut->rows = z.threads / cut->cols;
+        return cut->rows >= 1 && (int64_t)cut->rows * z.run >= L;
+    };
+    if (!cut->wide) return holds(back ? kBackChunk : kChunk);
+    if (back) return std::any_of(std::begin(kBackSizes), std::end(kBackSizes), holds);
+    return std::any_of(std::begin(kSizes), std::end(kSizes), holds);
 }
 
 bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut) {
@@ -728,7 +732,8 @@ bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut)
     cut->chunks = 1;
     cut->folded = 0;
     if (!cut->held) {
-        cut->threads = 256, cut->run = back ? kBackSizes[2][1] : kSizes[2][1], cut->rows = 256 / cut->cols;
+        cut->threads = kChunk.threads, cut->run = (back ? kBackChunk : kChunk).run;
+        cut->rows = cut->threads / cut->cols;
         const int64_t step = (int64_t)cut->rows * cut->run, chunks = (L + step - 1) / step;
         if (chunks > INT_MAX) return false;
         cut->chunks = (int32_t)chunks;
@@ -781,27 +786,32 @@ void go(const NormArgs &a, const Cut &c, hipStream_t s) {
     }
 }
 
+// The held kernel of the size that the call was cut for.
+template <int DT, bool BACK, int K = 0>
+void run_held(const NormArgs &a, const Cut &c, hipStream_t s) {
+    constexpr int kCount = BACK ? (int)std::size(kBackSizes) : (int)std::size(kSizes);
+    if constexpr (K < kCount) {
+        constexpr Size z = BACK ? kBackSizes[BACK ? K : 0] : kSizes[K];
+        if (c.threads == z.threads && c.run == z.run)
+            go<DT, BACK, true, z.threads, z.run, kHeld>(a, c, s);
+        else
+            run_held<DT, BACK, K + 1>(a, c, s);
+    }
+}
+
 template <int DT, bool BACK>
 void run(const NormArgs &a, const Cut &c, hipStream_t s) {
-    constexpr int kLong = BACK ? kBackSizes[2][1] : kSizes[2][1];   // columns of a thread in the larger sizes
-    if (!c.held) {
-        if (c.wide) {
-            go<DT, BACK, true, 256, kLong, kStats>(a, c, s);
-            go<DT, BACK, true, 256, kLong, kApply>(a, c, s);
-        } else {
-            go<DT, BACK, false, 256, kLong, kStats>(a, c, s);
-            go<DT, BACK, false, 256, kLong, kApply>(a, c, s);
-        }
-    } else if (!c.wide) {
-        go<DT, BACK, false, 256, kLong, kHeld>(a, c, s);
-    } else if (c.threads == 64) {
-        go<DT, BACK, true, 64, 4, kHeld>(a, c, s);
-    } else if (c.threads == 256 && c.run == 4) {
-        go<DT, BACK, true, 256, 4, kHeld>(a, c, s);
-    } else if (c.threads == 256) {
-        go<DT, BACK, true, 256, kLong, kHeld>(a, c, s);
+    constexpr Size z = BACK ? kBackChunk : kChunk;
+    if (c.held && c.wide) {
+        run_held<DT, BACK>(a, c, s);
+    } else if (c.held) {
+        go<DT, BACK, false, z.threads, z.run, kHeld>(a, c, s);
+    } else if (c.wide) {
+        go<DT, BACK, true, z.threads, z.run, kStats>(a, c, s);
+        go<DT, BACK, true, z.threads, z.run, kApply>(a, c, s);
     } else {
-        go<DT, BACK, true, 512, kLong, kHeld>(a, c, s);
+        go<DT, BACK, false, z.threads, z.run, kStats>(a, c, s);
+        go<DT, BACK, false, z.threads, z.run, kApply>(a, c, s);
     }
 }
 
