@@ -175,34 +175,41 @@ __device__ inline void place_thread(const NormArgs &a, Place &p) {
     if (!p.active) p.c = p.c0, p.skip = 0;
 }
 
-// Shared memory of a slab, sized by the launch.  Arrays of W start on 16 bytes.
+// Shared memory of a slab, sized by the launch.  Arrays start on 16 bytes.
 struct Scratch {
-    float *rows;             // [rows][W]: the threads' sums
-    float *chan;             // parts of the channels' sums
     float *group, *group2;   // [groups of a slab]
+    float *rows;             // [rows][W]: the threads' sums, or [2][threads]
+    float *chan;             // parts of the channels' sums
     float *of[4];            // [4][W]: what the elements of a channel are scaled by
     float *first;            // [W], backward
     float *total;            // [2][W], backward, held
 };
 
-__host__ __device__ inline int64_t scratch_floats(int threads, int vec, int cols, int rows, int groups, bool back) {
-    const int W = cols * vec;
-    return (int64_t)rows * W + ((threads > W ? threads : W) + 3) / 4 * 4 + 2 * ((groups + 3) / 4 * 4) +
-           (back ? 7 : 4) * W;
+// What a call's kernels keep there.  Where every column lies in one group, a
+// thread's sums are one number a quantity, and the scales are read as needed.
+enum Keep { kSums, kSumsBack, kOne, kOneBack };
+
+__host__ __device__ inline int pad4(int n) { return (n + 3) / 4 * 4; }
+
+__host__ __device__ inline int64_t scratch_floats(int threads, int vec, int cols, int rows, int groups, int keep) {
+    const int W = cols * vec, head = 2 * pad4(groups);
+    if (keep == kOne) return head + 2 * threads + 2 * W;
+    if (keep == kOneBack) return head + 2 * threads + 2 * W + 2 * (int64_t)threads * vec;
+    return head + (int64_t)rows * W + pad4(threads > W ? threads : W) + (keep == kSumsBack ? 7 : 4) * W;
 }
 
 template <int NT, int VEC>
 __device__ inline Scratch scratch_of(const NormArgs &a) {
     extern __shared__ __attribute__((aligned(16))) float shared[];
-    const int W = a.cols * VEC, groups = (a.most_groups + 3) / 4 * 4;
+    const int W = a.cols * VEC;
     Scratch s;
-    s.of[0] = shared;
-    for (int k = 1; k < 4; k++) s.of[k] = s.of[k - 1] + W;
-    s.rows = s.of[3] + W;
+    s.group = shared;
+    s.group2 = s.group + pad4(a.most_groups);
+    s.rows = s.group2 + pad4(a.most_groups);
     s.chan = s.rows + a.rows * W;
-    s.group = s.chan + ((NT > W ? NT : W) + 3) / 4 * 4;
-    s.group2 = s.group + groups;
-    s.first = s.group2 + groups;
+    s.of[0] = s.chan + pad4(NT > W ? NT : W);
+    for (int k = 1; k < 4; k++) s.of[k] = s.of[k - 1] + W;
+    s.first = s.of[3] + W;
     s.total = s.first + W;
     return s;
 }
@@ -280,6 +287,53 @@ __device__ inline void sum_groups(const Place &p, const float *of, int parts, co
     __syncthreads();
 }
 
+// Where every column lies in one group: t1 and t2 become their sums over the
+// threads of the thread's own group, in all of them.  `g`: its group of the slab.
+template <int NT, int VEC>
+__device__ inline void sum_two(const NormArgs &a, const Place &p, int g, float &t1, float &t2, float *rows,
+                               float *group, float *group2) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (!p.active) t1 = 0.0f, t2 = 0.0f;
+    if (p.ng == 1) {
+#pragma unroll
+        for (int off = 32; off; off /= 2) t1 += __shfl_xor(t1, off), t2 += __shfl_xor(t2, off);
+        if (NT == 64) return;
+        __syncthreads();   // rows is free
+        if (lane == 0) rows[wave] = t1, rows[NT + wave] = t2;
+        __syncthreads();
+        t1 = 0.0f, t2 = 0.0f;
+        for (int k = 0; k < NT / 64; k++) t1 += rows[k], t2 += rows[NT + k];
+        return;
+    }
+    __syncthreads();   // rows and the groups are free
+    rows[threadIdx.x] = t1, rows[NT + threadIdx.x] = t2;
+    __syncthreads();
+    const int each = a.width / VEC;   // columns of a group
+    if (each * a.rows <= 16) {
+        for (int k = threadIdx.x; k < 2 * p.ng; k += NT) {
+            const float *at = rows + (k & 1) * NT + (k >> 1) * each;
+            float u = 0.0f;
+            for (int r = 0; r < a.rows; r++)
+                for (int c = 0; c < each; c++) u += at[r * a.cols + c];
+            (k & 1 ? group2 : group)[k >> 1] = u;
+        }
+    } else {
+        const int side = each < 64 ? each : 64, down = 64 / side, r0 = lane / side, c0 = lane - r0 * side;
+        for (int k = wave; k < 2 * p.ng; k += NT / 64) {
+            const float *at = rows + (k & 1) * NT + (k >> 1) * each;
+            float u = 0.0f;
+            if (r0 < down)
+                for (int r = r0; r < a.rows; r += down)
+                    for (int c = c0; c < each; c += side) u += at[r * a.cols + c];
+#pragma unroll
+            for (int off = 32; off; off /= 2) u += __shfl_xor(u, off);
+            if (lane == 0) (k & 1 ? group2 : group)[k >> 1] = u;
+        }
+    }
+    __syncthreads();
+    t1 = group[g], t2 = group2[g];
+}
+
 // The steps of chunk k, and how many of them are the series' own.
 __device__ inline int chunk_rows(const NormArgs &a, int64_t T, int chunk, int64_t per, int64_t &first) {
     first = chunk * per;
@@ -305,7 +359,7 @@ __device__ inline char *column_at(const View &x, const Place &p, int64_t first) 
 }
 
 // Forward.  R: passes over the rows that a thread holds.
-template <int DT, bool WIDE, int NT, int R, int MODE>
+template <int DT, bool WIDE, int NT, int R, int MODE, bool ONE>
 __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a) {
     using P = Pack<DT, WIDE>;
     constexpr int VEC = P::kN;
@@ -330,6 +384,9 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a)
     };
 
     const int W = p.c1 - p.c0, each = W / p.ng;
+    constexpr bool one = ONE;
+    const int g = one && p.ng > 1 ? (p.c - p.c0) / a.width : 0;   // one: the column's group of the slab
+    float m[VEC], sc[VEC], sh[VEC];
     if (MODE != kApply) {
         load(0);
         float acc[VEC];
@@ -341,13 +398,28 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a)
 #pragma unroll
                 for (int e = 0; e < VEC; e++) acc[e] += held[j].get(e);
             }
-        int parts = sum_rows<NT, VEC>(a, p, acc, s);
-        sum_groups<NT>(p, s.chan, parts, nullptr, s.group);
         const float inv = own ? 1.0f / ((float)own * (float)each) : 0.0f;
-        for_channels<NT>(a, p, [&](int ch, int g) { s.of[0][ch] = s.group[g] * inv; });
-        __syncthreads();
-        float m[VEC];
-        of_column<VEC>(s.of[0], p, m);
+        auto own_sum = [&]() {   // of the channels that this column counts
+            float t = 0.0f;
+#pragma unroll
+            for (int e = 0; e < VEC; e++) t += e >= p.skip ? acc[e] : 0.0f;
+            return t;
+        };
+        float mean = 0.0f, squares = 0.0f;   // one: of the column's group
+        if (one) {
+            float none = 0.0f;
+            mean = own_sum();
+            sum_two<NT, VEC>(a, p, g, mean, none, s.rows, s.group, s.group2);
+            mean *= inv;
+#pragma unroll
+            for (int e = 0; e < VEC; e++) m[e] = mean;
+        } else {
+            const int parts = sum_rows<NT, VEC>(a, p, acc, s);
+            sum_groups<NT>(p, s.chan, parts, nullptr, s.group);
+            for_channels<NT>(a, p, [&](int ch, int k) { s.of[0][ch] = s.group[k] * inv; });
+            __syncthreads();
+            of_column<VEC>(s.of[0], p, m);
+        }
 #pragma unroll
         for (int e = 0; e < VEC; e++) acc[e] = 0.0f;
 #pragma unroll
@@ -361,19 +433,37 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a)
                     acc[e] = __builtin_fmaf(d, d, acc[e]);
                 }
             }
-        parts = sum_rows<NT, VEC>(a, p, acc, s);
-        sum_groups<NT>(p, s.chan, parts, nullptr, s.group2);
+        if (one) {
+            float none = 0.0f;
+            squares = own_sum();
+            sum_two<NT, VEC>(a, p, g, squares, none, s.rows, s.group, s.group2);
+        } else {
+            const int parts = sum_rows<NT, VEC>(a, p, acc, s);
+            sum_groups<NT>(p, s.chan, parts, nullptr, s.group2);
+        }
+        // one: the first thread of a group writes for it
+        const bool leads = one && p.active && p.row == 0 && p.c == p.c0 + g * a.width;
         if (MODE == kStats) {
             const int K = a.chunks * a.parts, k = p.chunk * a.parts + (a.parts > 1 ? p.slab % a.parts : 0);
-            for (int g = threadIdx.x; g < p.ng; g += NT)
-                a.stats[((int64_t)p.i * a.G + p.g0 + g) * K + k] = make_float2(s.group[g] * inv, s.group2[g]);
+            float2 *at = a.stats + ((int64_t)p.i * a.G + p.g0) * K + k;
+            if (leads) at[(int64_t)g * K] = make_float2(mean, squares);
+            if (!one)
+                for (int q = threadIdx.x; q < p.ng; q += NT)
+                    at[(int64_t)q * K] = make_float2(s.group[q] * inv, s.group2[q]);
             return;
         }
-        for (int g = threadIdx.x; g < p.ng; g += NT) {
-            const float mean = s.group[g] * inv, rstd = own ? 1.0f / sqrtf(s.group2[g] * inv + a.eps) : 0.0f;
-            s.group[g] = mean, s.group2[g] = rstd;
-            a.mean[(int64_t)p.i * a.G + p.g0 + g] = mean;
-            a.rstd[(int64_t)p.i * a.G + p.g0 + g] = rstd;
+        float *means = a.mean + (int64_t)p.i * a.G + p.g0, *rstds = a.rstd + (int64_t)p.i * a.G + p.g0;
+        if (one) {
+            const float rstd = own ? 1.0f / sqrtf(squares * inv + a.eps) : 0.0f;
+            if (leads) means[g] = mean, rstds[g] = rstd;
+#pragma unroll
+            for (int e = 0; e < VEC; e++) sc[e] = rstd;
+        } else {
+            for (int q = threadIdx.x; q < p.ng; q += NT) {
+                const float rstd = own ? 1.0f / sqrtf(s.group2[q] * inv + a.eps) : 0.0f;
+                s.group[q] *= inv, s.group2[q] = rstd;
+                means[q] = s.group[q], rstds[q] = rstd;
+            }
         }
     } else {
         // merge the chunks' statistics: N = sum n_k, m = sum n_k m_k / N,
@@ -411,19 +501,31 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a)
             }
         }
     }
-    __syncthreads();
-    for_channels<NT>(a, p, [&](int ch, int g) {
-        s.of[0][ch] = s.group[g];
-        s.of[1][ch] = s.group2[g] * (a.w ? a.w[p.c0 + ch] : 1.0f);
-        s.of[2][ch] = a.b ? a.b[p.c0 + ch] : 0.0f;
-    });
-    __syncthreads();
-
-    if (!p.active) return;
-    float m[VEC], sc[VEC], sh[VEC];
-    of_column<VEC>(s.of[0], p, m);
-    of_column<VEC>(s.of[1], p, sc);
-    of_column<VEC>(s.of[2], p, sh);
+    if (one) {
+        if (MODE == kApply) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < VEC; e++) m[e] = s.group[g], sc[e] = s.group2[g];
+        }
+        if (!p.active) return;
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+            if (a.w) sc[e] *= a.w[p.c + e];
+            sh[e] = a.b ? a.b[p.c + e] : 0.0f;
+        }
+    } else {
+        __syncthreads();
+        for_channels<NT>(a, p, [&](int ch, int k) {
+            s.of[0][ch] = s.group[k];
+            s.of[1][ch] = s.group2[k] * (a.w ? a.w[p.c0 + ch] : 1.0f);
+            s.of[2][ch] = a.b ? a.b[p.c0 + ch] : 0.0f;
+        });
+        __syncthreads();
+        if (!p.active) return;
+        of_column<VEC>(s.of[0], p, m);
+        of_column<VEC>(s.of[1], p, sc);
+        of_column<VEC>(s.of[2], p, sh);
+    }
     char *out = column_at<DT>(a.out, p, first);
     const int64_t rest = a.L - first;
     auto write = [&](int j0, auto act) {
@@ -454,6 +556,119 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a)
     }
 }
 
+// Forward, held, every column in one group: a workgroup goes through the
+// series b, b + a.series, ..., and the next series' columns load as this one's
+// are written.
+template <int DT, int NT, int R>
+__global__ __launch_bounds__(NT, 5) void norm_one_kernel(NormArgs a) {
+    using P = Pack<DT, true>;
+    constexpr int VEC = P::kN;
+    extern __shared__ __attribute__((aligned(16))) float shared[];
+    const int W = a.cols * VEC;
+    float *group = shared, *group2 = group + pad4(a.most_groups), *rows = group2 + pad4(a.most_groups);
+    float *weight = rows + 2 * NT, *bias = weight + W;   // of the slab's channels
+    Place p;
+    const uint32_t b = rocket::item_of_block(), begin = rocket::uniform(b / a.slabs);
+    p.slab = rocket::uniform(b - begin * a.slabs);
+    p.chunk = 0;
+    place_thread<NT, VEC>(a, p);
+    for (int ch = threadIdx.x; ch < p.c1 - p.c0; ch += NT) {
+        weight[ch] = a.w ? a.w[p.c0 + ch] : 1.0f;
+        bias[ch] = a.b ? a.b[p.c0 + ch] : 0.0f;
+    }
+    const int g = p.ng > 1 ? (p.c - p.c0) / a.width : 0;
+    const bool leads = p.active && p.row == 0 && p.c == p.c0 + g * a.width;   // writes for its group
+    __syncthreads();
+
+    P held[R];
+    int own = rocket::steps_of(a.lengths, begin, a.L);   // all of them are held
+    p.i = begin;
+    const char *x = column_at<DT>(a.x, p, 0);
+#pragma unroll
+    for (int j = 0; j < R; j++) load_row<P>(held[j], x, j * a.rows, a.rows, p.row, own, a.x.ts);
+    for (;;) {
+        // as if new: what follows from them is not kept across series
+        asm("" : "+v"(p.row), "+v"(p.c), "+s"(a.x.ts), "+s"(a.out.ts));
+        float acc[VEC];
+        auto own_sum = [&]() {   // of the channels that this column counts
+            float t = 0.0f;
+#pragma unroll
+            for (int e = 0; e < VEC; e++) t += e >= p.skip ? acc[e] : 0.0f;
+            return t;
+        };
+#pragma unroll
+        for (int e = 0; e < VEC; e++) acc[e] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < R; j++)
+            if (j * a.rows < own) {   // columns past the own steps hold 0
+#pragma unroll
+                for (int e = 0; e < VEC; e++) acc[e] += held[j].get(e);
+            }
+        const float inv = own ? 1.0f / ((float)own * (float)a.width) : 0.0f;
+        float mean = own_sum(), squares, none = 0.0f;
+        sum_two<NT, VEC>(a, p, g, mean, none, rows, group, group2);
+        mean *= inv;
+#pragma unroll
+        for (int e = 0; e < VEC; e++) acc[e] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < R; j++) held[j].renew();
+#pragma unroll
+        for (int j = 0; j < R; j++)
+            if (p.row + j * a.rows < own) {
+#pragma unroll
+                for (int e = 0; e < VEC; e++) {
+                    const float d = held[j].get(e) - mean;
+                    acc[e] = __builtin_fmaf(d, d, acc[e]);
+                }
+            }
+        squares = own_sum(), none = 0.0f;
+        sum_two<NT, VEC>(a, p, g, squares, none, rows, group, group2);
+        const float rstd = own ? 1.0f / sqrtf(squares * inv + a.eps) : 0.0f;
+        if (leads) {
+            a.mean[(int64_t)p.i * a.G + p.g0 + g] = mean;
+            a.rstd[(int64_t)p.i * a.G + p.g0 + g] = rstd;
+        }
+        float sc[VEC], sh[VEC];
+        of_column<VEC>(weight, p, sc);
+        of_column<VEC>(bias, p, sh);
+#pragma unroll
+        for (int e = 0; e < VEC; e++) sc[e] *= rstd;
+
+        const uint32_t next = p.i + a.series;   // below 2^32
+        char *out = column_at<DT>(a.out, p, 0);
+        const int had = own;
+        const bool more = next < (uint32_t)a.n;
+        own = more ? rocket::steps_of(a.lengths, next, a.L) : 0;
+        p.i = more ? next : p.i;
+        x = column_at<DT>(a.x, p, 0);
+        auto write = [&](auto act) {
+#pragma unroll
+            for (int j = 0; j < R; j++) {
+                const int pass = j * a.rows, r = p.row + pass;
+                if (pass >= a.L) break;
+                float y[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; e++) y[e] = 0.0f;
+                if (r < had) {
+                    held[j].renew();
+#pragma unroll
+                    for (int e = 0; e < VEC; e++)
+                        y[e] = activate<DT, act.value>(__builtin_fmaf(held[j].get(e) - mean, sc[e], sh[e]));
+                }
+                if (r < a.L && p.active) P::store(out + pass * a.out.ts, y);
+                load_row<P>(held[j], x, pass, a.rows, p.row, own, a.x.ts);
+            }
+        };
+        switch (a.act) {
+        case ROCKET_ACT_RELU: write(std::integral_constant<int, ROCKET_ACT_RELU>()); break;
+        case ROCKET_ACT_SILU: write(std::integral_constant<int, ROCKET_ACT_SILU>()); break;
+        case ROCKET_ACT_GELU: write(std::integral_constant<int, ROCKET_ACT_GELU>()); break;
+        default: write(std::integral_constant<int, ROCKET_ACT_NONE>());
+        }
+        if (!more) break;
+    }
+}
+
 // What the backward pass keeps of an element's channel.  z is the fused
 // x A + B with A = r w and B = b - m A, but for ReLU: there z is rounded step by
 // step as the formula is written, since the slope jumps with z's sign.
@@ -481,7 +696,7 @@ struct Channel {
 // keeps the channel sums over them; kStats leaves the channel sums of a chunk.
 // sum dz xh is gathered as sum dz (x - k), k the mean of the slab's first
 // group, and completed once a channel: r (sum dz (x - k) - (m - k) sum dz).
-template <int DT, bool WIDE, int NT, int R, int MODE, int ACT, bool ONE>
+template <int DT, bool WIDE, int NT, int R, int MODE, int ACT>
 __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
     using P = Pack<DT, WIDE>;
     constexpr int VEC = P::kN;
@@ -603,10 +818,9 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
         }
         Channel<VEC, ACT> of;
         of.take(s, p);
-        constexpr int kOwn = ONE ? 1 : VEC;
-        float D[kOwn], E[kOwn];
-        of_column<kOwn>(s.chan, p, D);
-        of_column<kOwn>(s.first, p, E);
+        float D[VEC], E[VEC];
+        of_column<VEC>(s.chan, p, D);
+        of_column<VEC>(s.first, p, E);
         for (int j0 = 0; j0 < R && j0 * a.rows < rest; j0 += H) {
             if (MODE == kApply) {
 #pragma unroll
@@ -623,7 +837,7 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
 #pragma unroll
                     for (int e = 0; e < VEC; e++) {
                         const float v = hx[j].get(e), dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
-                        dx[e] = __builtin_fmaf(dz, of.scale(e), -__builtin_fmaf(v, D[ONE ? 0 : e], E[ONE ? 0 : e]));
+                        dx[e] = __builtin_fmaf(dz, of.scale(e), -__builtin_fmaf(v, D[e], E[e]));
                     }
                 }
                 if (r < rest && p.active) P::store(out + pass * a.out.ts, dx);
@@ -637,6 +851,143 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
         for (int q = 0; q < 2; q++)
             for (int ch = threadIdx.x; ch < W; ch += NT)
                 a.sums[((int64_t)begin * 2 + q) * a.C + p.c0 + ch] = s.total[q * W + ch];
+}
+
+// Backward, held, every column in one group: a thread's sums for its group are
+// one number each, and the channel sums stay in its own slots of shared memory
+// until the workgroup's last series, so that a series takes three barriers.
+// The next series' columns load as this one's are written.
+template <int DT, int NT, int R, int ACT>
+__global__ __launch_bounds__(NT, 4) void norm_back_one_kernel(NormArgs a) {
+    using P = Pack<DT, true>;
+    constexpr int VEC = P::kN, Q = VEC / 4;
+    extern __shared__ __attribute__((aligned(16))) float shared[];
+    const int W = a.cols * VEC;
+    float *group = shared, *group2 = group + pad4(a.most_groups), *rows = group2 + pad4(a.most_groups);
+    float *weight = rows + 2 * NT, *bias = weight + W;                       // of the slab's channels
+    typedef float vec4 __attribute__((ext_vector_type(4)));
+    vec4 *total = (vec4 *)(bias + W);                                        // [2 Q][NT]
+    Place p;
+    const uint32_t b = rocket::item_of_block(), begin = rocket::uniform(b / a.slabs);
+    p.slab = rocket::uniform(b - begin * a.slabs);
+    p.chunk = 0;
+    place_thread<NT, VEC>(a, p);
+    for (int ch = threadIdx.x; ch < p.c1 - p.c0; ch += NT) {
+        weight[ch] = a.w ? a.w[p.c0 + ch] : 1.0f;
+        bias[ch] = a.b ? a.b[p.c0 + ch] : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * Q; k++) total[k * NT + threadIdx.x] = vec4{0, 0, 0, 0};
+    const int g = p.ng > 1 ? (p.c - p.c0) / a.width : 0;
+    __syncthreads();
+
+    P hx[R], hg[R];
+    int own = rocket::steps_of(a.lengths, begin, a.L);   // all of them are held
+    p.i = begin;
+    const char *x = column_at<DT>(a.x, p, 0), *dy = column_at<DT>(a.dy, p, 0);
+    auto load = [&](int j) {
+        load_row<P>(hx[j], x, j * a.rows, a.rows, p.row, own, a.x.ts);
+        load_row<P>(hg[j], dy, j * a.rows, a.rows, p.row, own, a.dy.ts);
+    };
+#pragma unroll
+    for (int j = 0; j < R; j++) load(j);
+    for (;;) {
+        // as if new: what follows from them is not kept across series
+        asm("" : "+v"(p.row), "+v"(p.c), "+s"(a.x.ts), "+s"(a.dy.ts), "+s"(a.out.ts));
+        const float mean = a.mean[(int64_t)p.i * a.G + p.g0 + g], rstd = a.rstd[(int64_t)p.i * a.G + p.g0 + g];
+        Channel<VEC, ACT> of;
+        auto scales = [&]() {
+            float w[VEC], c[VEC];
+            of_column<VEC>(weight, p, w);
+            of_column<VEC>(bias, p, c);
+#pragma unroll
+            for (int e = 0; e < VEC; e++) {
+                if constexpr (ACT == ROCKET_ACT_RELU) {
+                    of.A[e] = w[e], of.B[e] = c[e], of.m[e] = mean, of.r[e] = rstd;
+                } else {
+                    of.A[e] = rstd * w[e];
+                    of.B[e] = __builtin_fmaf(-mean, of.A[e], c[e]);
+                }
+            }
+        };
+        scales();
+        float sd[VEC], sx[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; e++) sd[e] = 0.0f, sx[e] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < R; j++)
+            if (p.row + j * a.rows < own) {
+#pragma unroll
+                for (int e = 0; e < VEC; e++) {
+                    const float v = hx[j].get(e);
+                    const float dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
+                    sd[e] += dz;
+                    sx[e] = __builtin_fmaf(dz, v - mean, sx[e]);
+                    if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // four at a time: registers are short
+                }
+            }
+        // r mean(g) N and mean(g xh) N of the thread's elements, and the channel sums
+        float t1 = 0.0f, t2 = 0.0f;
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+            t1 = __builtin_fmaf(e >= p.skip ? of.scale(e) : 0.0f, sd[e], t1);
+            t2 = __builtin_fmaf(e >= p.skip ? of.scale(e) : 0.0f, sx[e], t2);
+        }
+#pragma unroll
+        for (int k = 0; k < Q; k++) {
+            vec4 d = total[k * NT + threadIdx.x], q = total[(Q + k) * NT + threadIdx.x];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                d[e] += sd[4 * k + e];
+                q[e] = __builtin_fmaf(rstd, sx[4 * k + e], q[e]);
+            }
+            total[k * NT + threadIdx.x] = d, total[(Q + k) * NT + threadIdx.x] = q;
+        }
+        sum_two<NT, VEC>(a, p, g, t1, t2, rows, group, group2);
+        // dx = r (dz w - mean(g) - xh mean(g xh)) = dz r w - (x D + E)
+        const float inv = own ? 1.0f / ((float)own * (float)a.width) : 0.0f;
+        const float D = rstd * rstd * (t2 * inv), E = __builtin_fmaf(-mean, D, t1 * inv);
+        scales();
+
+        const uint32_t next = p.i + a.series;   // below 2^32
+        char *out = column_at<DT>(a.out, p, 0);
+        const int had = own;
+        const bool more = next < (uint32_t)a.n;
+        own = more ? rocket::steps_of(a.lengths, next, a.L) : 0;
+        p.i = more ? next : p.i;
+        x = column_at<DT>(a.x, p, 0), dy = column_at<DT>(a.dy, p, 0);
+#pragma unroll
+        for (int j = 0; j < R; j++) {
+            const int pass = j * a.rows, r = p.row + pass;
+            float dx[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; e++) dx[e] = 0.0f;
+            if (r < had) {
+                hx[j].renew(), hg[j].renew();
+#pragma unroll
+                for (int e = 0; e < VEC; e++) {
+                    const float v = hx[j].get(e), dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
+                    dx[e] = __builtin_fmaf(dz, of.scale(e), -__builtin_fmaf(v, D, E));
+                    if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if (r < a.L && p.active) P::store(out + pass * a.out.ts, dx);
+            load(j);
+        }
+        if (!more) break;
+    }
+    __syncthreads();
+    // over the rows: channel ch is element ch % VEC of column ch / VEC; the last
+    // column starts early
+    const int wide = p.c1 - p.c0;
+    for (int q = 0; q < 2; q++)
+        for (int ch = threadIdx.x; ch < wide; ch += NT) {
+            const int col = ch / VEC, at = col * VEC;
+            const int e = ch - at + (at + VEC > wide ? at + VEC - wide : 0);
+            float t = 0.0f;
+            for (int r = 0; r < a.rows; r++) t += ((const float *)&total[(q * Q + e / 4) * NT + r * a.cols + col])[e % 4];
+            a.sums[((int64_t)begin * 2 + q) * a.C + p.c0 + ch] = t;
+        }
 }
 
 // Rows of channel sums to fewer rows: out[o, q, c] = the sum of in[r, q, c]
@@ -674,6 +1025,7 @@ struct Cut {
 };
 
 constexpr int kFold = 128;
+constexpr int kLoopRun = 4;   // forward: columns a thread holds where a workgroup goes through many series
 // Workgroups that hold a slab: threads, and 16-byte columns of a thread (of
 // each operand).
 struct Size {
@@ -705,7 +1057,6 @@ bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut)
     cut->wide = C >= vec_wide;
     cut->width = (int32_t)width;
     const int vec = cut->wide ? vec_wide : 1;
-    cut->one = width % vec == 0;
     const int64_t most = 256 * (int64_t)vec;   // channels of a slab
     cut->parts = 1;
     cut->held = false;
@@ -722,13 +1073,15 @@ bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut)
         int64_t per = 1, half = 1;
         while (half < groups && half * width * size < 64) half++;
         while (per < groups && per * width * size < 128) per++;
-        while (per * 2 <= groups && per * 2 * width <= most && per * width * size * L < (16 << 10) &&
+        while (per * 2 <= groups && per * 2 * width <= (width <= 64 * vec ? 64 * vec : most) && per * width * size * L < (16 << 10) &&
                s->n * ((groups + 2 * per - 1) / (2 * per)) >= 1024)
             per *= 2;
         cut->held = hold(s, groups, per, vec, back, cut) ||
                     (half < per && hold(s, groups, half, vec, back, cut));
         if (!cut->held) hold(s, groups, per, vec, back, cut);
     }
+    // every column lies in one group: groups of whole columns, or one a slab
+    cut->one = cut->wide && (width % vec == 0 || cut->groups == 1);
     cut->chunks = 1;
     cut->folded = 0;
     if (!cut->held) {
@@ -739,10 +1092,14 @@ bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut)
         cut->chunks = (int32_t)chunks;
         if (__builtin_mul_overflow(s->n * chunks, (int64_t)cut->slabs, &cut->grid)) return false;
         cut->sum_rows = s->n * chunks;
-    } else if (back) {
-        int64_t series = (1024 + cut->slabs - 1) / cut->slabs;
+    } else if (back || (cut->one && cut->run <= kLoopRun)) {
+        // as many workgroups as the registers take (20 wavefronts a CU), backward
+        // more of them, whose loads and sums then overlap; all with as many series
+        int64_t series = (256 * (back ? 32 : 20) * 64 / cut->threads + cut->slabs - 1) / cut->slabs;
         if (series > s->n) series = s->n;
-        cut->series = (int32_t)(series > 0 ? series : 1);
+        if (series < 1) series = 1;
+        const int64_t each = (s->n + series - 1) / series;
+        cut->series = (int32_t)(each > 0 ? (s->n + each - 1) / each : 1);
         cut->grid = (int64_t)cut->series * cut->slabs;
         cut->sum_rows = cut->series;
     } else {
@@ -761,21 +1118,35 @@ int64_t workspace_of(const rocket_sequence_shape *s, int32_t groups, bool back, 
 template <int DT, bool BACK, bool WIDE, int NT, int R, int MODE>
 void go(const NormArgs &a, const Cut &c, hipStream_t s) {
     const uint32_t grid = (uint32_t)c.grid;
-    const int lds = (int)scratch_floats(NT, Pack<DT, WIDE>::kN, c.cols, c.rows, c.groups, BACK) * 4;
-    if constexpr (!BACK) {
-        norm_kernel<DT, WIDE, NT, R, MODE><<<grid, NT, lds, s>>>(a);
+    const bool one = WIDE && c.one && (!BACK || MODE == kHeld);
+    const int keep = one ? (BACK ? kOneBack : kOne) : (BACK ? kSumsBack : kSums);
+    const int lds = (int)scratch_floats(NT, Pack<DT, WIDE>::kN, c.cols, c.rows, c.groups, keep) * 4;
+    if constexpr (!BACK && WIDE && MODE == kHeld) {
+        if constexpr (R <= kLoopRun) {
+            if (one) {
+                norm_one_kernel<DT, NT, R><<<grid, NT, lds, s>>>(a);
+                return;
+            }
+        }
+        if (one)
+            norm_kernel<DT, true, NT, R, MODE, true><<<grid, NT, lds, s>>>(a);
+        else
+            norm_kernel<DT, true, NT, R, MODE, false><<<grid, NT, lds, s>>>(a);
+    } else if constexpr (!BACK) {
+        if (WIDE && one)
+            norm_kernel<DT, WIDE, NT, R, MODE, WIDE><<<grid, NT, lds, s>>>(a);
+        else
+            norm_kernel<DT, WIDE, NT, R, MODE, false><<<grid, NT, lds, s>>>(a);
     } else {
-        // columns that lie in one group each, where registers are short
-        const bool one = WIDE && MODE == kHeld && R > 4 && c.one;
         auto act = [&](auto k) {
             constexpr int ACT = decltype(k)::value;
-            if constexpr (WIDE && MODE == kHeld && R > 4) {
+            if constexpr (WIDE && MODE == kHeld) {
                 if (one) {
-                    norm_back_kernel<DT, WIDE, NT, R, MODE, ACT, true><<<grid, NT, lds, s>>>(a);
+                    norm_back_one_kernel<DT, NT, R, ACT><<<grid, NT, lds, s>>>(a);
                     return;
                 }
             }
-            norm_back_kernel<DT, WIDE, NT, R, MODE, ACT, false><<<grid, NT, lds, s>>>(a);
+            norm_back_kernel<DT, WIDE, NT, R, MODE, ACT><<<grid, NT, lds, s>>>(a);
         };
         switch (a.act) {
         case ROCKET_ACT_RELU: act(std::integral_constant<int, ROCKET_ACT_RELU>()); break;
