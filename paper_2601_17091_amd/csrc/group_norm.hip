@@ -50,7 +50,7 @@ struct NormArgs {
     const float *w, *b;        // or null
     const int32_t *lengths;
     float *mean, *rstd;        // [n, G]: written forward, read backward
-    float2 *stats;             // forward: [n, G, chunks * parts] (mean, squares)
+    float2 *stats;             // [n, G, chunks * parts]: (mean, squares), backward sums of dz w and of dz w xh
     float *sums;               // backward: [rows of sums, 2, C] sums of dz and dz xh
     int32_t series;            // backward, held: workgroups along the series
 };
@@ -763,7 +763,7 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
                 for (int q = 0; q < parts; q++) t += s.chan[q * W + ch];
                 s.first[ch] = t;
             }
-            if (MODE == kHeld) sum_groups<NT>(p, s.chan, parts, a.w, s.group);
+            sum_groups<NT>(p, s.chan, parts, a.w, s.group);
             parts = sum_rows<NT, VEC>(a, p, sx, s);
             for_channels<NT>(a, p, [&](int ch, int g) {
                 const float d = s.first[ch];
@@ -778,24 +778,24 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
                 }
                 s.first[ch] = t;
             });
-            if (MODE == kStats) return;
             __syncthreads();
             sum_groups<NT>(p, s.first, 1, a.w, s.group2);
+            if (MODE == kStats) {
+                const int K = a.chunks * a.parts, k = p.chunk * a.parts + (a.parts > 1 ? p.slab % a.parts : 0);
+                for (int g = threadIdx.x; g < p.ng; g += NT)
+                    a.stats[((int64_t)p.i * a.G + p.g0 + g) * K + k] = make_float2(s.group[g], s.group2[g]);
+                return;
+            }
         } else {
-            // the groups' sums from the chunks' channel sums
-            for (int k = threadIdx.x >> 6; k < 2 * p.ng; k += NT >> 6) {
-                const int q = k & 1, g = k >> 1;
-                float t = 0.0f;
-                for (int ch = threadIdx.x & 63; ch < a.width; ch += 64) {
-                    const int c = (p.g0 + g) * a.width + ch;
-                    const float *sum = a.sums + ((int64_t)p.i * a.chunks * 2 + q) * a.C + c;
-                    float u = 0.0f;
-                    for (int chunk = 0; chunk < a.chunks; chunk++) u += sum[(int64_t)chunk * 2 * a.C];
-                    t += a.w ? a.w[c] * u : u;
-                }
+            // the groups' sums over the chunks
+            const int K = a.chunks * a.parts;
+            for (int g = threadIdx.x >> 6; g < p.ng; g += NT >> 6) {
+                const float2 *st = a.stats + ((int64_t)p.i * a.G + p.g0 + g) * K;
+                float t1 = 0.0f, t2 = 0.0f;
+                for (int k = threadIdx.x & 63; k < K; k += 64) t1 += st[k].x, t2 += st[k].y;
 #pragma unroll
-                for (int off = 32; off; off /= 2) t += __shfl_xor(t, off);
-                if ((threadIdx.x & 63) == 0) (q ? s.group2 : s.group)[g] = t;
+                for (int off = 32; off; off /= 2) t1 += __shfl_xor(t1, off), t2 += __shfl_xor(t2, off);
+                if ((threadIdx.x & 63) == 0) s.group[g] = t1, s.group2[g] = t2;
             }
             __syncthreads();
         }
@@ -1110,9 +1110,13 @@ bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut)
     return cut->grid <= INT_MAX && (!back || fold_grid <= INT_MAX);
 }
 
+int64_t stats_of(const rocket_sequence_shape *s, int32_t groups, const Cut &c) {
+    return c.held ? 0 : s->n * groups * (int64_t)c.chunks * c.parts;
+}
+
 int64_t workspace_of(const rocket_sequence_shape *s, int32_t groups, bool back, const Cut &c) {
-    if (back) return (c.sum_rows + c.folded) * 2 * s->channels * (int64_t)sizeof(float);
-    return c.held ? 0 : s->n * groups * (int64_t)c.chunks * c.parts * (int64_t)sizeof(float2);
+    const int64_t sums = back ? (c.sum_rows + c.folded) * 2 * s->channels * (int64_t)sizeof(float) : 0;
+    return stats_of(s, groups, c) * (int64_t)sizeof(float2) + sums;
 }
 
 template <int DT, bool BACK, bool WIDE, int NT, int R, int MODE>
@@ -1263,15 +1267,16 @@ extern "C" rocket_status rocket_group_norm_backward(const rocket_sequence_shape 
         !aligned(dbias, 4))
         return ROCKET_ERR_INVALID_ARG;
     const int64_t need = workspace_of(shape, groups, true, cut);
-    if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 4)))) return ROCKET_ERR_INVALID_ARG;
+    if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 8)))) return ROCKET_ERR_INVALID_ARG;
     hipStream_t s = (hipStream_t)hip_stream;
     const int size = rocket::elem_size(shape->dtype), C = (int)shape->channels;
-    float *sums = (float *)workspace;
+    float *sums = (float *)((float2 *)workspace + stats_of(shape, groups, cut));
     int64_t rows = 0;
     if (!rocket::empty(shape)) {
         NormArgs a = args_of(shape, groups, activation, weight, bias, cut);
         a.x = view(x, size), a.dy = view(dy, size), a.out = view(dx, size);
         a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd), a.sums = sums;
+        a.stats = (float2 *)workspace;
         run_type<true>(shape->dtype, a, cut, s);
         rows = cut.sum_rows;
     }
