@@ -1067,13 +1067,19 @@ bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut)
         int64_t part = (width + cut->parts - 1) / cut->parts;
         cut->cols = (int32_t)((part + vec - 1) / vec);
     } else {
-        // A slab is at least 128 bytes wide (a cache line), and wider while
-        // that leaves workgroups for the whole chip and the slab is small.
-        // 64 bytes where only that is held.
+        // A slab is at least 128 bytes wide (a cache line), and wider while that
+        // leaves workgroups for the whole chip and the slab is small: up to the
+        // columns of a wavefront, or of 4 where a group is wider (8000 x 1 x 2000
+        // in groups of 100, fp32, forward: 86 us with 2 groups a slab, 120 us with
+        // 20), and not where columns would then lie in two groups (1000 x 16 x
+        // 2000 in groups of 100, bf16: 25 us with a group a slab, 47 us with
+        // more).  64 bytes where only that is held.
         int64_t per = 1, half = 1;
         while (half < groups && half * width * size < 64) half++;
         while (per < groups && per * width * size < 128) per++;
-        while (per * 2 <= groups && per * 2 * width <= (width <= 64 * vec ? 64 * vec : most) && per * width * size * L < (16 << 10) &&
+        const int64_t limit = width <= 64 * vec ? 64 * vec : most;
+        const bool whole = width % vec == 0 || per > 1;
+        while (whole && per * 2 <= groups && per * 2 * width <= limit && per * width * size * L < (16 << 10) &&
                s->n * ((groups + 2 * per - 1) / (2 * per)) >= 1024)
             per *= 2;
         cut->held = hold(s, groups, per, vec, back, cut) ||
