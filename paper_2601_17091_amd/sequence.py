@@ -32,6 +32,13 @@ EVERY = 128   # steps between the states a recurrence keeps (ROCKET_RECURRENCE_E
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _byref, _empty, _f32 = ctypes.byref, torch.empty, torch.float32
 
+
+def _dense(x):
+    """A contiguous tensor of x's shape and type (the quickest way to one)."""
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
+
 # The current GPU and the handle of its current stream; torch.cuda's own
 # functions make objects of them, which takes as long as a small kernel.
 _device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
@@ -127,11 +134,12 @@ def group_norm(x, groups: int, weight=None, bias=None, *, eps: float = 1e-5, act
     n, _, channels = x.shape
     w, b = _floats(weight, (channels,), x, "weight"), _floats(bias, (channels,), x, "bias")
     if out is None:
-        out = _empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _dense(x)
     else:
         _like(out, x, "out")
     size = _norm_workspace(lib, shape, groups, 0)
-    mean, rstd = (_empty((n, groups), dtype=_f32, device=x.device) for _ in range(2))
+    mean = _empty(n, groups, dtype=_f32, device=x.device)
+    rstd = _dense(mean)
     work, at = _workspace(size, x.device)
     status = lib.rocket_group_norm_forward(
         _byref(shape), groups, _byref(_sequence(x, "x")), w, b, eps, act, _byref(_sequence(out, "out")),
@@ -158,10 +166,11 @@ def group_norm_backward(dy, x, groups: int, mean, rstd, weight=None, bias=None, 
     size = _norm_workspace(lib, shape, groups, 1)
     m, r = _floats(mean, (n, groups), x, "mean"), _floats(rstd, (n, groups), x, "rstd")
     if out is None:
-        out = _empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _dense(x)
     else:
         _like(out, x, "out")
-    dweight, dbias = (_empty((channels,), dtype=_f32, device=x.device) for _ in range(2))
+    dweight = _empty(channels, dtype=_f32, device=x.device)
+    dbias = _dense(dweight)
     work, at = _workspace(size, x.device)
     status = lib.rocket_group_norm_backward(
         _byref(shape), groups, _byref(_sequence(dy, "dy")), _byref(_sequence(x, "x")), w, b, act, m, r,
@@ -195,12 +204,12 @@ def recurrence(v, f, o=None, *, h0=None, lengths=None, keep_states: bool = False
     n, steps, channels = v.shape
     first = _floats(h0, (n, channels), v, "h0")
     if out is None:
-        out = _empty(v.shape, dtype=v.dtype, device=v.device)
+        out = _dense(v)
     else:
         _like(out, v, "out")
     size = _recurrence_workspace(lib, shape)
-    h_last = _empty((n, channels), dtype=_f32, device=v.device)
-    states = _empty((n, -(-steps // EVERY), channels), dtype=_f32, device=v.device) if keep_states else None
+    h_last = _empty(n, channels, dtype=_f32, device=v.device)
+    states = _empty(n, -(-steps // EVERY), channels, dtype=_f32, device=v.device) if keep_states else None
     work, at = _workspace(size, v.device)
     status = lib.rocket_recurrence_forward(
         _byref(shape), _byref(_sequence(v, "v")), _byref(_sequence(f, "f")), _optional(o, "o"), first,
@@ -230,14 +239,14 @@ def recurrence_backward(dy, v, f, states, o=None, *, dh_last=None, lengths=None,
     last = _floats(dh_last, (n, channels), v, "dh_last")
     wanted = 2 if o is None else 3
     if out is None:
-        out = [_empty(v.shape, dtype=v.dtype, device=v.device) for _ in range(wanted)]
+        out = [_dense(v) for _ in range(wanted)]
     elif len(out) != wanted:
         raise ValueError("out must hold %d tensors" % wanted)
     else:
         for t in out:
             _like(t, v, "out")
     size = _recurrence_workspace(lib, shape)
-    dh0 = _empty((n, channels), dtype=_f32, device=v.device)
+    dh0 = _empty(n, channels, dtype=_f32, device=v.device)
     work, at = _workspace(size, v.device)
     do = out[2] if o is not None else None
     status = lib.rocket_recurrence_backward(
@@ -275,11 +284,11 @@ def recurrence_step(v, f, h, o=None, *, h_out=None, out=None, stream=None):
         raise TypeError("h must be a torch tensor on the GPU")
     at_h = _floats(h, v.shape, v, "h")
     if out is None:
-        out = _empty(v.shape, dtype=v.dtype, device=v.device)
+        out = _dense(v)
     else:
         _like(out, v, "out")
     if h_out is None:
-        h_out = _empty(v.shape, dtype=_f32, device=v.device)
+        h_out = _dense(h)
     at_out = _floats(h_out, v.shape, v, "h_out")
     n, channels = v.shape
     status = lib.rocket_recurrence_step(n, channels, code, *_matrix(v, "v"), *_matrix(f, "f"), *_matrix(o, "o"), at_h,
@@ -320,7 +329,7 @@ def dropout(x, p: float, seed: int, call: int = 0, *, residual=None, out=None, s
     if residual is not None:
         _like(residual, x, "residual")
     if out is None:
-        out = _empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _dense(x)
     else:
         _like(out, x, "out")
     vx, vy = _rows(x, "x"), _rows(out, "out")
