@@ -44,7 +44,8 @@ using rocket::Elem;
 constexpr int kEvery = ROCKET_RECURRENCE_EVERY;  // steps between kept states
 constexpr int kElems = 16;                       // elements of a thread in a tile
 constexpr int kMostLanes = 32;                   // lanes over channels
-constexpr int kMostWaves = 8;
+constexpr int kMostWaves = 16;                   // of a workgroup that takes a whole series at once
+constexpr int kTileWaves = 8;                    // of one that takes a tile of 128 steps
 constexpr int kMostChannels = 64;                // of a workgroup: 32 lanes x 2
 constexpr int64_t kFill = 512;                   // rows that fill the chip
 constexpr int kApart = 64;                       // words from counter to counter: each has its own cache line
@@ -166,16 +167,18 @@ __device__ inline char *run_at(const View &x, const Place &p, uint32_t t0) {
 }
 
 // Shared memory of one scan over the wavefronts of a workgroup.
+template <int WAY>
 struct Scan {
-    float2 map[kMostWaves][kMostChannels];
-    float start[kMostWaves][kMostChannels];
+    static constexpr int kWaves = WAY == kOne ? kMostWaves : kTileWaves;
+    float2 map[kWaves][kMostChannels];
+    float start[kWaves][kMostChannels];
 };
 
 // Inclusive scan of the runs' maps over the lanes of a wavefront, then
 // (A, B) becomes the map of the runs before the thread's own (REVERSE: after
 // it), and the wavefront's whole map goes to shared memory.
-template <int P, bool REVERSE>
-__device__ inline void scan_lanes(const RecArgs &a, const Place &p, float *A, float *B, Scan &s) {
+template <int P, bool REVERSE, int WAY>
+__device__ inline void scan_lanes(const RecArgs &a, const Place &p, float *A, float *B, Scan<WAY> &s) {
     for (int off = a.lanes; off < 64; off *= 2) {
         const bool on = REVERSE ? p.lane + off < 64 : p.lane >= off;
 #pragma unroll
@@ -206,8 +209,8 @@ __device__ inline void scan_lanes(const RecArgs &a, const Place &p, float *A, fl
 
 // One thread per channel goes through the wavefronts' maps: the state at each
 // wavefront's start, and in `carry` the state past the tile.
-template <bool REVERSE>
-__device__ inline void scan_waves(int waves, int ch, float &carry, Scan &s) {
+template <bool REVERSE, int WAY>
+__device__ inline void scan_waves(int waves, int ch, float &carry, Scan<WAY> &s) {
     for (int k = 0; k < waves; k++) {
         const int w = REVERSE ? waves - 1 - k : k;
         const float2 m = s.map[w][ch];
@@ -218,7 +221,7 @@ __device__ inline void scan_waves(int waves, int ch, float &carry, Scan &s) {
 
 // What a split row's tiles publish.
 struct Meet {
-    float2 map[kMostWaves][kMostChannels];
+    float2 map[kTileWaves][kMostChannels];
     int tile;
 };
 
@@ -240,7 +243,7 @@ __device__ inline int take_tile(const RecArgs &a, const Place &p, Meet &m) {
 // and returns, in the threads that scan, the state at the tile's start.  The
 // whole workgroup calls it.
 template <int P, bool REVERSE>
-__device__ inline float meet(const RecArgs &a, const Place &p, int order, bool scans, float h, const Scan &s, Meet &m) {
+__device__ inline float meet(const RecArgs &a, const Place &p, int order, bool scans, float h, const Scan<kSplit> &s, Meet &m) {
     uint64_t *row = a.maps + (int64_t)p.row * a.tiles * kMostChannels;
     const int ch = threadIdx.x, channels = a.lanes * P;   // channels that are published
     if (scans) {
@@ -312,10 +315,10 @@ __device__ inline void reach(const RecArgs &a, const Place &p, int order, float 
 
 // The forward pass over a row, or over one tile of it.
 template <int DT, int WAY, bool GATE>
-__global__ __launch_bounds__(64 * kMostWaves, WAY == kSplit && !GATE ? 8 : 4) void forward_kernel(RecArgs a) {
+__global__ __launch_bounds__(64 * (WAY == kOne ? kMostWaves : kTileWaves), WAY == kSplit && !GATE ? 8 : 4) void forward_kernel(RecArgs a) {
     constexpr int P = Elem<DT>::kPerWord, S = kRun<DT>;
     constexpr bool SPLIT = WAY == kSplit;
-    __shared__ Scan scan;
+    __shared__ Scan<WAY> scan;
     __shared__ typename std::conditional<SPLIT, Meet, int>::type met;
     Place p = place_of<DT>(a);
     const bool scans = threadIdx.x < a.lanes * P;   // the threads that go through the wavefronts, one a channel
@@ -414,10 +417,10 @@ __global__ __launch_bounds__(64 * kMostWaves, WAY == kSplit && !GATE ? 8 : 4) vo
 // The backward pass over a row from its last tile to its first, or over one
 // tile of it.
 template <int DT, int WAY, bool GATE>
-__global__ __launch_bounds__(64 * kMostWaves, 4) void backward_kernel(RecArgs a) {
+__global__ __launch_bounds__(64 * (WAY == kOne ? kMostWaves : kTileWaves), 4) void backward_kernel(RecArgs a) {
     constexpr int P = Elem<DT>::kPerWord, S = kRun<DT>;
     constexpr bool SPLIT = WAY == kSplit;
-    __shared__ Scan scan, fscan;
+    __shared__ Scan<WAY> scan, fscan;
     __shared__ typename std::conditional<SPLIT, Meet, int>::type met;
     Place p = place_of<DT>(a);
     const int channels = a.lanes * P;
@@ -606,6 +609,14 @@ struct Cut {
 // at most; the wavefront's other lanes take further runs of steps, so that
 // few channels do not leave lanes idle.
 //
+// A series that is not much longer than a tile is one larger tile (777 x 129 x
+// 331, fp16, gated, ragged: 67 us, against 92 us in two tiles): of up to 16
+// wavefronts where rows are few (50 x 200 x 256: 10 us, split 16 us) and in the
+// forward pass of 16-bit elements (1000 x 190 x 256: 72 against 89 us), 10 in
+// its gated backward pass (1000 x 160 x 256: 154 against 182 us; of 12, 248
+// against 243 us) and 8 else (fp32, 13 wavefronts, 1000 x 400 x 128, backward:
+// 232 against 214 us).
+//
 // Split where rows alone do not fill the chip (8 x 10000 x 256, fp32, backward:
 // 90 us, against 140 us with a first launch for the maps), and for three kinds
 // of calls whose loop over tiles leaves more to be waited for than tiles that
@@ -624,11 +635,14 @@ bool cut_of(const rocket_sequence_shape *s, bool back, bool gate, Cut *cut) {
     const int64_t in_wave = (64 / cut->lanes) * (kElems / per_word);   // steps of a wavefront
     const int64_t L = s->steps > 0 ? s->steps : 1;
     cut->waves = (int32_t)(in_wave < kEvery ? kEvery / in_wave : 1);
-    if (L <= cut->waves * in_wave) cut->waves = (int32_t)((L + in_wave - 1) / in_wave);   // one tile holds the series
-    const int64_t tile = cut->waves * in_wave;
-    cut->tiles = (int32_t)((L + tile - 1) / tile);
     cut->blocks = (int32_t)((words + cut->lanes - 1) / cut->lanes);
     cut->rows = s->n * cut->blocks;
+    // One tile holds the series.
+    const int64_t one = (L + in_wave - 1) / in_wave;
+    const int most = cut->rows < kFill || (per_word == 2 && !back) ? kMostWaves : per_word == 2 && gate ? 10 : kTileWaves;
+    if (one <= most) cut->waves = (int32_t)one;
+    const int64_t tile = cut->waves * in_wave;
+    cut->tiles = (int32_t)((L + tile - 1) / tile);
     const int64_t slots = (cut->rows + kFill - 1) / kFill * kFill;   // of all rounds of a loop
     cut->split = cut->tiles > 1 &&
                  (cut->rows < kFill || (cut->tiles >= 8 && cut->rows < 4 * kFill && 4 * cut->rows < 3 * slots) ||
