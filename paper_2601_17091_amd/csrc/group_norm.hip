@@ -187,7 +187,8 @@ struct Scratch {
 
 // What a call's kernels keep there.  Where every column lies in one group, a
 // thread's sums are one number a quantity, and the scales are read as needed.
-enum Keep { kSums, kSumsBack, kOne, kOneBack };
+// At most 57 KB: 256 columns of 16 bytes, the widest slab, are chunks or kOne.
+enum Keep { kSums, kSumsBack, kChunkBack, kOne, kOneBack };
 
 __host__ __device__ inline int pad4(int n) { return (n + 3) / 4 * 4; }
 
@@ -195,7 +196,7 @@ __host__ __device__ inline int64_t scratch_floats(int threads, int vec, int cols
     const int W = cols * vec, head = 2 * pad4(groups);
     if (keep == kOne) return head + 2 * threads + 2 * W;
     if (keep == kOneBack) return head + 2 * threads + 2 * W + 2 * (int64_t)threads * vec;
-    return head + (int64_t)rows * W + pad4(threads > W ? threads : W) + (keep == kSumsBack ? 7 : 4) * W;
+    return head + (int64_t)rows * W + pad4(threads > W ? threads : W) + (keep == kSumsBack ? 7 : keep == kChunkBack ? 5 : 4) * W;
 }
 
 template <int NT, int VEC>
@@ -1129,7 +1130,7 @@ template <int DT, bool BACK, bool WIDE, int NT, int R, int MODE>
 void go(const NormArgs &a, const Cut &c, hipStream_t s) {
     const uint32_t grid = (uint32_t)c.grid;
     const bool one = WIDE && c.one && (!BACK || MODE == kHeld);
-    const int keep = one ? (BACK ? kOneBack : kOne) : (BACK ? kSumsBack : kSums);
+    const int keep = one ? (BACK ? kOneBack : kOne) : !BACK ? kSums : MODE == kHeld ? kSumsBack : kChunkBack;
     const int lds = (int)scratch_floats(NT, Pack<DT, WIDE>::kN, c.cols, c.rows, c.groups, keep) * 4;
     if constexpr (!BACK && WIDE && MODE == kHeld) {
         if constexpr (R <= kLoopRun) {

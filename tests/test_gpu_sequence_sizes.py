@@ -1,0 +1,50 @@
+"""Sequence operators on the GPU at the sizes where a call is cut in another
+way: workgroups that go through many series or tiles, rows whose tiles meet
+through memory (more than one published state among them), one large tile,
+chunks of wide and of odd groups.  Against the 64-bit oracle, within its bounds."""
+import pytest
+
+from test_gpu_sequence import check_norm, check_rec, env  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# n, L, C: rows are n times blocks of 64 channels (16 bits) or 32 (fp32)
+@pytest.mark.parametrize("gate", [False, True])
+@pytest.mark.parametrize("n,L,C,dtype", [
+    (1, 9000, 66, "bfloat16"), (2, 8500, 33, "float32"),    # tiles that meet, three published states
+    (2, 4224, 70, "float16"),                               # 33 tiles: the last one starts from a state
+    (1, 20001, 3, "bfloat16"), (1, 33000, 1, "float16"),    # few channels: tiles of many runs
+    (130, 300, 260, "bfloat16"), (130, 600, 140, "float32"),   # loops over three tiles, and five
+    (70, 1100, 256, "float32"),                             # long fp32 rows, split though they are many
+    (100, 1030, 384, "float16"),                            # 600 rows: a badly filled last round
+    (130, 250, 260, "float16"),                             # gated backward: split in two; else one tile or two
+    (3, 250, 64, "bfloat16"), (3, 500, 30, "float32"),      # one tile of 16 wavefronts
+    (600, 150, 64, "bfloat16"), (600, 140, 31, "float32"),  # one tile of 10 and of 5
+    (2000, 3, 40, "bfloat16")])
+def test_recurrence_cuts(env, n, L, C, dtype, gate):  # noqa: F811
+    check_rec(*env, n, L, C, dtype, gate)
+
+
+@pytest.mark.parametrize("n,L,C,dtype", [(6, 8500, 66, "bfloat16"), (140, 600, 130, "float32"),
+                                         (40, 1030, 70, "float16")])
+def test_recurrence_cuts_ragged(env, n, L, C, dtype):  # noqa: F811
+    check_rec(*env, n, L, C, dtype, True, with_lengths=True, packed=True)
+
+
+@pytest.mark.parametrize("n,L,C,G", [
+    (2, 3000, 2000, 1), (2, 700, 2042, 1), (2, 300, 4100, 2),   # chunks of the widest slabs, and of parts
+    (20, 34, 5512, 106),                                         # held, columns in two groups
+    (2, 1982, 1159, 19),                                         # chunks of odd groups
+    (3, 5000, 24, 3), (2, 9000, 5, 5),                           # many chunks, of narrow rows too
+    (3000, 1, 200, 2), (5000, 3, 64, 4), (900, 2, 1000, 1),      # many series in turn
+    (1300, 40, 256, 16), (600, 100, 66, 2), (1100, 5, 7, 7)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_group_norm_cuts(env, n, L, C, G, dtype):  # noqa: F811
+    check_norm(*env, n, L, C, G, dtype, "gelu", False)
+
+
+@pytest.mark.parametrize("act", ["relu", "silu"])
+@pytest.mark.parametrize("n,L,C,G", [(900, 20, 48, 6), (5, 2500, 99, 3), (40, 900, 64, 2)])
+def test_group_norm_cuts_ragged(env, n, L, C, G, act):  # noqa: F811
+    check_norm(*env, n, L, C, G, "float16", act, True)
