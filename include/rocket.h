@@ -545,8 +545,8 @@ rocket_status rocket_minirocket_plan_create(const rocket_minirocket_params *m, u
  *     length are not read (they may hold anything), and results there are 0.
  *   - Values may be infinite or NaN; they give what the formulas give.
  *   - n, steps and the series' lengths may be 0.
- *   - An output may be one of the inputs of its own shape, type and strides;
- *     operands must not overlap otherwise.
+ *   - A sequence that is written may be one of the sequences that are read, as
+ *     it stands (same address and strides); operands must not overlap otherwise.
  *   - Results do not change from call to call, nor with the alignment.
  *   - No device memory is allocated.  A workspace is caller-owned DEVICE memory
  *     of the size the query gives for the same shape, 8-byte aligned, and free
@@ -638,8 +638,7 @@ rocket_status rocket_group_norm_workspace(const rocket_sequence_shape *shape, in
  * Socher 2017).  Steps past a series' length leave h as it is.
  *   o       output gate, or NULL: y_t = h_t
  *   h0      DEVICE fp32 [n, channels], the state before step 0, or NULL: 0
- *   h_last  DEVICE fp32 [n, channels]: the state after the last step; may be
- *           h0
+ *   h_last  DEVICE fp32 [n, channels]: the state after the last step
  *   states  DEVICE fp32 [n, ceil(steps / ROCKET_RECURRENCE_EVERY), channels],
  *           or NULL: the states before the steps 0, 128, 256, ..., which the
  *           backward pass starts from
@@ -660,7 +659,7 @@ rocket_status rocket_recurrence_forward(const rocket_sequence_shape *shape, cons
  *     dv = dh (1 - a),  df = dh (h_{t-1} - v) a (1 - a),  dO = dy h S(o) (1 - S(o))
  *   dO    given where o is, NULL where o is NULL
  *   dh0   DEVICE fp32 [n, channels]: the gradient of the first state
- *         (dh_last for a series of no steps); may be dh_last
+ *         (dh_last for a series of no steps)
  * dv, df and dO may be blocks of one matrix, the gradient of a projection.
  * Errors as rocket_recurrence_forward.
  */
@@ -697,7 +696,7 @@ rocket_status rocket_recurrence_step(int64_t n, int64_t channels, int32_t dtype,
  * A dropped element does not pass on what x holds there, NaN and infinities
  * included.  Calls with another seed or call number draw other masks.
  * The gradient is the same call on dy with residual NULL (residual's own
- * gradient is dy).  y may be x or residual.  rows * cols at most 2^41.
+ * gradient is dy).  y may be x or residual as they stand.  rows * cols at most 2^41.
  * Errors: ROCKET_ERR_INVALID_ARG; ROCKET_ERR_HIP.
  */
 rocket_status rocket_dropout(const void *x, const void *residual, void *y, int64_t rows, int64_t cols,

@@ -45,6 +45,7 @@ struct NormArgs {
     int32_t cols, rows;        // columns of a slab; steps a workgroup passes at once
     int32_t chunks;            // of steps
     int32_t most_groups;       // groups of a slab, at most
+    int32_t in_place;          // the output is one of the inputs
     int32_t act;
     float eps;
     const float *w, *b;        // or null
@@ -354,6 +355,21 @@ __device__ inline void load_row(P &v, const char *at, int pass, int rows, int ro
     }
 }
 
+// Writes a column.  Where the output goes over an input that other threads
+// have not read yet (a second launch over chunks, in place), a column that was
+// moved back leaves the channels that its neighbour counts to the neighbour.
+template <int DT, class P>
+__device__ inline void store_column(char *at, const float (&f)[P::kN], const Place &p, bool in_place) {
+    if (!in_place || p.skip == 0) {
+        P::store(at, f);
+        return;
+    }
+    using raw = typename Elem<DT>::raw;
+#pragma unroll
+    for (int e = 0; e < P::kN; e++)
+        if (e >= p.skip) ((raw *)at)[e] = Elem<DT>::round(f[e]);
+}
+
 template <int DT>
 __device__ inline char *column_at(const View &x, const Place &p, int64_t first) {
     return x.p + p.i * x.ss + (first + p.row) * x.ts + (int64_t)p.c * Elem<DT>::kSize;
@@ -541,7 +557,7 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a)
                 for (int e = 0; e < VEC; e++)
                     y[e] = activate<DT, act.value>(__builtin_fmaf(held[j].get(e) - m[e], sc[e], sh[e]));
             }
-            if (r < rest) P::store(out + pass * a.out.ts, y);
+            if (r < rest) store_column<DT, P>(out + pass * a.out.ts, y, p, MODE == kApply && a.in_place);
         }
     };
     for (int j0 = 0; j0 < R && j0 * a.rows < rest; j0 += H) {
@@ -841,7 +857,8 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
                         dx[e] = __builtin_fmaf(dz, of.scale(e), -__builtin_fmaf(v, D[e], E[e]));
                     }
                 }
-                if (r < rest && p.active) P::store(out + pass * a.out.ts, dx);
+                if (r < rest && p.active)
+                    store_column<DT, P>(out + pass * a.out.ts, dx, p, MODE == kApply && a.in_place);
                 if (MODE == kHeld) load(j, 0);
             }
         }
@@ -1256,6 +1273,7 @@ extern "C" rocket_status rocket_group_norm_forward(const rocket_sequence_shape *
     const int size = rocket::elem_size(shape->dtype);
     NormArgs a = args_of(shape, groups, activation, weight, bias, cut);
     a.x = view(x, size), a.out = view(y, size);
+    a.in_place = x->data == y->data;
     a.eps = eps, a.mean = mean, a.rstd = rstd, a.stats = (float2 *)workspace;
     run_type<false>(shape->dtype, a, cut, (hipStream_t)hip_stream);
     return rocket::launched();
@@ -1282,6 +1300,7 @@ extern "C" rocket_status rocket_group_norm_backward(const rocket_sequence_shape 
     if (!rocket::empty(shape)) {
         NormArgs a = args_of(shape, groups, activation, weight, bias, cut);
         a.x = view(x, size), a.dy = view(dy, size), a.out = view(dx, size);
+        a.in_place = dx->data == dy->data || dx->data == x->data;
         a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd), a.sums = sums;
         a.stats = (float2 *)workspace;
         run_type<true>(shape->dtype, a, cut, s);

@@ -48,3 +48,17 @@ def test_group_norm_cuts(env, n, L, C, G, dtype):  # noqa: F811
 @pytest.mark.parametrize("n,L,C,G", [(900, 20, 48, 6), (5, 2500, 99, 3), (40, 900, 64, 2)])
 def test_group_norm_cuts_ragged(env, n, L, C, G, act):  # noqa: F811
     check_norm(*env, n, L, C, G, "float16", act, True)
+
+
+@pytest.mark.parametrize("n,L,C,G", [(2, 20000, 33, 3), (3, 6000, 99, 3), (1, 9000, 331, 1)])
+def test_chunks_in_place(env, n, L, C, G):  # noqa: F811
+    """Columns that share channels with their neighbours, over the inputs."""
+    torch, seq = env
+    x, dy = (torch.randn(n, L, C, device="cuda").to(torch.bfloat16) for _ in range(2))
+    y, mean, rstd = seq.group_norm(x, G, activation="silu")
+    dx = seq.group_norm_backward(dy, x, G, mean, rstd, activation="silu")[0]
+    a = x.clone()
+    assert torch.equal(seq.group_norm(a, G, activation="silu", out=a)[0], y)
+    for k in range(2):
+        a = [x.clone(), dy.clone()]
+        assert torch.equal(seq.group_norm_backward(a[1], a[0], G, mean, rstd, activation="silu", out=a[k])[0], dx)
