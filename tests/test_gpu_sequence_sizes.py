@@ -62,3 +62,10 @@ def test_chunks_in_place(env, n, L, C, G):  # noqa: F811
     for k in range(2):
         a = [x.clone(), dy.clone()]
         assert torch.equal(seq.group_norm_backward(a[1], a[0], G, mean, rstd, activation="silu", out=a[k])[0], dx)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16"])
+def test_group_norm_many_long_series(env, dtype):  # noqa: F811
+    """More than 1,024 slabs of more steps than 512 threads hold: the largest
+    workgroup of the backward pass, several series in turn."""
+    check_norm(*env, 1100, 530, 32 if dtype == "float32" else 64, 2, dtype, "silu", False)
