@@ -16,4 +16,11 @@ With ROCKET_DEBUG=1 in the environment the checked build is loaded
 from .rocket import (EXPORTED, MiniRocketPlan, Plan, RocketError, check_flags, checked_build,  # noqa: F401
                      generate_kernels, generate_kernels_multi, library, library_at, minirocket_fit,
                      plan_tables, status_string, transform, transform_batched)
-from . import sequence  # noqa: F401
+
+
+def __getattr__(name):
+    """`sequence` on first use: it imports torch, which the rest does not need."""
+    if name == "sequence":
+        import importlib
+        return importlib.import_module(".sequence", __name__)
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))

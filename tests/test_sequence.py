@@ -249,3 +249,13 @@ def test_binding_refuses_host_tensors(lib):
         with pytest.raises(TypeError):
             call()
     assert sequence.EVERY == so.EVERY == 128
+
+
+def test_package_imports_without_torch():
+    """The generator, planner and fit do not wait for torch; `sequence` brings it."""
+    import subprocess
+    import sys
+    code = ("import sys, paper_2601_17091_amd as rk; rk.library(); assert 'torch' not in sys.modules; "
+            "rk.sequence.EVERY; assert 'torch' in sys.modules")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", code], cwd=root, check=True)
