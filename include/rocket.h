@@ -710,7 +710,8 @@ const char *rocket_status_string(rocket_status s);
  * Checked builds, for debugging (a second library, librocket_checked.so,
  * compiled with ROCKET_CHECKED=1; the Python binding loads it when the
  * environment sets ROCKET_DEBUG=1).  Every entry point works as documented
- * above; in addition the device code checks every LDS tile read against the
+ * above (the sequence operators run the same code in both); in addition the
+ * transform's device code checks every LDS tile read against the
  * bytes its workgroup staged, every feature store of the workgroup kernels
  * against the rows and columns of its launch, and every slot column the
  * series-lane permutation reads against the plan's slots.  A failed check

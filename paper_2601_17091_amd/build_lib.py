@@ -60,15 +60,15 @@ def compile_flags(src: str = "transform.hip") -> list[str]:
 
 def build(verbose: bool = False) -> str:
     """Compile every source and link librocket.so, and the checked build
-    librocket_checked.so (the .hip sources with ROCKET_CHECKED=1: device-side
-    bounds checks for debugging); always rebuilds.  The compilations run in
+    librocket_checked.so (the transform's .hip sources with ROCKET_CHECKED=1:
+    device-side bounds checks for debugging); always rebuilds.  The compilations run in
     parallel."""
     os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
     jobs = []   # (command, object)
     objs = {False: [], True: []}
     for checked in (False, True):
         for src in SOURCES:
-            if checked and not src.endswith(".hip"):
+            if checked and (not src.endswith(".hip") or src in NAN_SOURCES):
                 objs[True].append(os.path.join(HERE, "_build", src + ".o"))
                 continue
             obj = os.path.join(HERE, "_build", src + (".checked.o" if checked else ".o"))

@@ -32,6 +32,14 @@
 // the workspace is filled with, so that it needs no flag and no fence.
 // Everything is read once.  The backward pass goes through the tiles from the
 // last to the first, each from the state that the forward pass kept there.
+//
+// Bound: HBM.  Measured: 64 x 1000 x 512, bf16, gated, backward 115 us, 4.0 TB/s
+// of the 459 MB that have to move (a large copy reaches 5.0 to 5.3 TB/s); 8 x
+// 10000 x 256, fp32, backward 89 us, 4.6 TB/s; 1000 x 1000 x 256, fp32, forward
+// 550 us, 5.6 TB/s; 4 x 16384 x 256, bf16, forward 26 us, 3.9 TB/s: 16 rows,
+// whose tiles wait for each other; 777 x 129 x 331, fp16, gated, ragged 65 us.
+// One counter a cache line: with the 16 rows' counters side by side the last
+// but one took 40 us.
 #include <climits>
 #include <type_traits>
 
