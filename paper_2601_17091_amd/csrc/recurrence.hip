@@ -651,7 +651,7 @@ bool cut_of(const rocket_sequence_shape *s, bool back, bool gate, Cut *cut) {
     if (one <= most) cut->waves = (int32_t)one;
     const int64_t tile = cut->waves * in_wave;
     cut->tiles = (int32_t)((L + tile - 1) / tile);
-    const int64_t slots = (cut->rows + kFill - 1) / kFill * kFill;   // of all rounds of a loop
+    const int64_t slots = (cut->rows + kFill - 1) / kFill * kFill;   // of a loop, whole waves of workgroups
     cut->split = cut->tiles > 1 &&
                  (cut->rows < kFill || (cut->tiles >= 8 && cut->rows < 4 * kFill && 4 * cut->rows < 3 * slots) ||
                   (per_word == 1 && cut->tiles >= 8) ||

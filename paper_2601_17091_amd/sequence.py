@@ -14,6 +14,9 @@ Statistics, weights, states and their gradients are float32 and contiguous.
     dropout(x, p, seed, call)               -> y
     dropout_backward(dy, p, seed, call)     -> dx
 
+The backward passes are calls of their own: nothing here records itself for
+torch's autograd (examples/window_head.py wraps them for it).
+
 Every call is asynchronous on `stream` (default: torch's current stream); what
 it returns is allocated for that stream.  An operand that belongs to another
 stream is the caller's to order and to keep alive (Tensor.record_stream).
