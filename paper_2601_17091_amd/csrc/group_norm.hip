@@ -1057,10 +1057,16 @@ struct Cut {
     int64_t folded;     // rows after the first fold, 0: one fold is enough
 };
 
+// Rows of channel sums that one workgroup adds up before a second launch adds
+// the rest; up to 4 times as many take one launch.
 constexpr int kFold = 128;
-constexpr int kLoopRun = 4;   // forward: columns a thread holds where a workgroup goes through many series
-// Workgroups that hold a slab: threads, and 16-byte columns of a thread (of
-// each operand).
+// Forward, a workgroup goes through many series where a thread holds this many
+// columns at most (10000 x 16 x 256, bf16: 63 us, against 86 us with a workgroup
+// a series).  With 8 columns the next series' do not fit beside them (777 x 129 x
+// 924 in groups of 33, fp32: 253 us against 187 us).
+constexpr int kLoopRun = 4;
+// Workgroups that hold a slab, the smallest that does is taken: threads, and
+// 16-byte columns of a thread (of each operand).
 struct Size {
     int threads, run;
 };

@@ -69,3 +69,21 @@ def test_group_norm_many_long_series(env, dtype):  # noqa: F811
     """More than 1,024 slabs of more steps than 512 threads hold: the largest
     workgroup of the backward pass, several series in turn."""
     check_norm(*env, 1100, 530, 32 if dtype == "float32" else 64, 2, dtype, "silu", False)
+
+
+def test_largest_workgroup_in_a_graph(env):  # noqa: F811
+    """Its shared memory is asked for at the launch, also while capturing."""
+    torch, seq = env
+    x, dy = (torch.randn(1100, 530, 64, device="cuda").half() for _ in range(2))
+    _, mean, rstd = seq.group_norm(x, 2)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = seq.group_norm_backward(dy, x, 2, mean, rstd, activation="silu")
+    for _ in range(3):
+        dy.normal_()
+        want = seq.group_norm_backward(dy, x, 2, mean, rstd, activation="silu")
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
