@@ -188,7 +188,8 @@ __device__ inline void place_thread(const NormArgs &a, Place &p) {
     p.active = p.row < a.rows && nominal < p.c1;
     p.c = nominal + VEC <= p.c1 ? nominal : p.c1 - VEC;
     p.skip = nominal - p.c;
-    if (!p.active) p.c = p.c0, p.skip = 0;
+    // the threads left over load the slab's first column, which is in bounds
+    if (!p.active) p.c = p.c0, p.skip = 0, p.row = 0;
 }
 
 // Shared memory of a slab, sized by the launch.  Arrays start on 16 bytes.

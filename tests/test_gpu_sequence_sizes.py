@@ -50,6 +50,18 @@ def test_group_norm_cuts_ragged(env, n, L, C, G, act):  # noqa: F811
     check_norm(*env, n, L, C, G, "float16", act, True)
 
 
+# The slab's columns do not divide the workgroup (3 in 64 threads: 21 rows and a
+# thread left over), and the series end with a whole pass over the rows: the
+# threads left over have no step of their own to load.
+@pytest.mark.parametrize("n,L,C,G", [
+    (3, 21, 24, 3), (3, 84, 24, 3), (40, 85, 24, 3), (2, 340, 24, 3),   # held, by 64 and by 256 threads
+    (3, 28, 66, 2), (3, 112, 66, 2),                                    # columns in two groups
+    (2, 1360, 24, 3), (2, 5440, 24, 3), (2, 4480, 66, 2)])              # held by more threads, chunks
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_group_norm_whole_passes_with_threads_left_over(env, n, L, C, G, dtype):  # noqa: F811
+    check_norm(*env, n, L, C, G, dtype, "silu", False)
+
+
 @pytest.mark.parametrize("n,L,C,G", [(2, 20000, 33, 3), (3, 6000, 99, 3), (1, 9000, 331, 1)])
 def test_chunks_in_place(env, n, L, C, G):  # noqa: F811
     """Columns that share channels with their neighbours, over the inputs."""
