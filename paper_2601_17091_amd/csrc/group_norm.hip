@@ -708,27 +708,25 @@ __global__ __launch_bounds__(NT, 5) void norm_one_kernel(NormArgs a) {
 template <int VEC, int ACT>
 struct Channel {
     static constexpr bool kSteps = ACT == ROCKET_ACT_RELU;
-    float A[VEC], B[VEC];                                // x A + B; in steps: w and b
-    float m[kSteps ? VEC : 1], r[kSteps ? VEC : 1];
+    float A[VEC], B[VEC], m[VEC];   // x A + B; in steps: w and b
+    float r[kSteps ? VEC : 1];
     __device__ float z(float x, int e) const {
-        if (kSteps) return (x - m[kSteps ? e : 0]) * r[kSteps ? e : 0] * A[e] + B[e];
+        if (kSteps) return (x - m[e]) * r[kSteps ? e : 0] * A[e] + B[e];
         return __builtin_fmaf(x, A[e], B[e]);
     }
     __device__ float scale(int e) const { return kSteps ? A[e] * r[kSteps ? e : 0] : A[e]; }
     __device__ void take(const Scratch &s, const Place &p) {
         of_column<VEC>(s.of[0], p, A);
         of_column<VEC>(s.of[1], p, B);
-        if constexpr (kSteps) {
-            of_column<VEC>(s.of[2], p, m);
-            of_column<VEC>(s.of[3], p, r);
-        }
+        of_column<VEC>(s.of[2], p, m);
+        if constexpr (kSteps) of_column<VEC>(s.of[3], p, r);
     }
 };
 
 // Backward.  Held: a workgroup goes through the series b, b + a.series, ... and
 // keeps the channel sums over them; kStats leaves the channel sums of a chunk.
-// sum dz xh is gathered as sum dz (x - k), k the mean of the slab's first
-// group, and completed once a channel: r (sum dz (x - k) - (m - k) sum dz).
+// sum dz xh is gathered as sum dz (x - m), m the mean of the channel's own
+// group, and multiplied by r once a channel: no group's values reach another's.
 template <int DT, bool WIDE, int NT, int R, int MODE, int ACT>
 __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
     using P = Pack<DT, WIDE>;
@@ -765,8 +763,9 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
         const float *mean = a.mean + (int64_t)p.i * a.G + p.g0, *rstd = a.rstd + (int64_t)p.i * a.G + p.g0;
         for_channels<NT>(a, p, [&](int ch, int g) {
             const float m = mean[g], r = rstd[g], w = a.w ? a.w[p.c0 + ch] : 1.0f, bias = a.b ? a.b[p.c0 + ch] : 0.0f;
+            s.of[2][ch] = m;
             if (ACT == ROCKET_ACT_RELU) {
-                s.of[0][ch] = w, s.of[1][ch] = bias, s.of[2][ch] = m, s.of[3][ch] = r;
+                s.of[0][ch] = w, s.of[1][ch] = bias, s.of[3][ch] = r;
             } else {
                 s.of[0][ch] = r * w, s.of[1][ch] = __builtin_fmaf(-m, r * w, bias);
             }
@@ -775,7 +774,6 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
         if (MODE != kApply) {
             Channel<VEC, ACT> of;
             of.take(s, p);
-            const float k = mean[0];
             float sd[VEC], sx[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; e++) sd[e] = 0.0f, sx[e] = 0.0f;
@@ -787,7 +785,7 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
                         const float v = hx[j].get(e);
                         const float dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
                         sd[e] += dz;
-                        sx[e] = __builtin_fmaf(dz, v - k, sx[e]);
+                        sx[e] = __builtin_fmaf(dz, v - of.m[e], sx[e]);
                     }
                 }
             int parts = sum_rows<NT, VEC>(a, p, sd, s);
@@ -802,7 +800,7 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
                 const float d = s.first[ch];
                 float t = 0.0f;
                 for (int q = 0; q < parts; q++) t += s.chan[q * W + ch];
-                t = rstd[g] * __builtin_fmaf(k - mean[g], d, t);
+                t *= rstd[g];
                 if (MODE == kHeld) {
                     s.total[ch] += d, s.total[W + ch] += t;
                 } else {
