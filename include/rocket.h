@@ -615,6 +615,8 @@ rocket_status rocket_group_norm_forward(const rocket_sequence_shape *shape, int3
  *     dx = r (g - mean(g) - xh mean(g xh)),  means over the group's N elements
  *     dweight_c = sum dz xh,  dbias_c = sum dz, over all series and steps
  *   dweight, dbias  DEVICE fp32 [channels], or NULL: not wanted
+ * x enters as x - m everywhere, so a level far above the spread costs no digits
+ * here either.  r * r has to be finite in fp32: s + eps of 2^-126 or more.
  * dx may be dy or x.  Errors as rocket_group_norm_forward.
  */
 rocket_status rocket_group_norm_backward(const rocket_sequence_shape *shape, int32_t groups,

@@ -79,12 +79,28 @@ struct Pack {
     vec v;
     __device__ void load(const char *p) { v = rocket::load_at<vec>(p); }
     __device__ float get(int e) const { return Elem<DT>::get(v[e / Elem<DT>::kPerWord], e % Elem<DT>::kPerWord); }
-    __device__ static void store(char *p, const float *f) {
-        vec o;
-#pragma unroll
-        for (int k = 0; k < 4; k++) o[k] = Elem<DT>::put(f + k * Elem<DT>::kPerWord);
-        rocket::store_at(p, o);
+    __device__ typename Elem<DT>::raw element(int e) const {
+        using bits = typename Elem<DT>::bits;
+        return __builtin_bit_cast(typename Elem<DT>::raw, (bits)(v[e / Elem<DT>::kPerWord] >> 16 * (e % Elem<DT>::kPerWord)));
     }
+    __device__ void set(int e, float f) { v[e] = __builtin_bit_cast(uint32_t, f); }   // fp32 elements
+    // Elements e to e + N, rounded.  Two neighbours write the channels that they
+    // share, each at another e, so that all conversions are the same instruction.
+    // Left to itself the compiler fuses some of those to fp16 with the operation
+    // before them, which rounds that operation's exact result and may differ.
+    template <int N>
+    __device__ void put(int e, const float (&f)[N]) {
+#pragma unroll
+        for (int k = 0; k < N / Elem<DT>::kPerWord; k++) {
+            uint32_t w;
+            if (DT == ROCKET_FLOAT16)
+                asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(w) : "v"(f[2 * k]), "v"(f[2 * k + 1]));
+            else
+                w = Elem<DT>::put(f + k * Elem<DT>::kPerWord);
+            v[e / Elem<DT>::kPerWord + k] = w;
+        }
+    }
+    __device__ void store(char *p) const { rocket::store_at(p, v); }
     __device__ void clear() { v = vec{0, 0, 0, 0}; }
     __device__ void renew() {
         uint32_t w[4] = {v[0], v[1], v[2], v[3]};
@@ -100,7 +116,10 @@ struct Pack<DT, false> {
     raw v;
     __device__ void load(const char *p) { v = *(const raw *)p; }
     __device__ float get(int) const { return Elem<DT>::one(v); }
-    __device__ static void store(char *p, const float *f) { *(raw *)p = Elem<DT>::round(f[0]); }
+    __device__ raw element(int) const { return v; }
+    __device__ void set(int, float f) { v = f; }
+    __device__ void put(int, const float (&f)[1]) { v = Elem<DT>::round(f[0]); }
+    __device__ void store(char *p) const { *(raw *)p = v; }
     __device__ void clear() { v = 0; }
     __device__ void renew() {}
 };
@@ -232,12 +251,13 @@ __device__ inline Scratch scratch_of(const NormArgs &a) {
     return s;
 }
 
-// The values of an array of channels for a thread's column.
-template <int VEC>
-__device__ inline void of_column(const float *of, const Place &p, float (&v)[VEC]) {
-    const float *at = of + (p.c - p.c0);
+// The values of an array of channels for a thread's column, from its element
+// `from` on.
+template <int N>
+__device__ inline void of_column(const float *of, const Place &p, float (&v)[N], int from = 0) {
+    const float *at = of + (p.c - p.c0) + from;
 #pragma unroll
-    for (int e = 0; e < VEC; e++) v[e] = at[e];
+    for (int e = 0; e < N; e++) v[e] = at[e];
 }
 
 // fn(channel of the slab, its group of the slab), a thread a channel.
@@ -375,15 +395,15 @@ __device__ inline void load_row(P &v, const char *at, int pass, int rows, int ro
 // have not read yet (a second launch over chunks, in place), a column that was
 // moved back leaves the channels that its neighbour counts to the neighbour.
 template <int DT, class P>
-__device__ inline void store_column(char *at, const float (&f)[P::kN], const Place &p, bool in_place) {
+__device__ inline void store_column(char *at, const P &v, const Place &p, bool in_place) {
     if (!in_place || p.skip == 0) {
-        P::store(at, f);
+        v.store(at);
         return;
     }
     using raw = typename Elem<DT>::raw;
 #pragma unroll
     for (int e = 0; e < P::kN; e++)
-        if (e >= p.skip) ((raw *)at)[e] = Elem<DT>::round(f[e]);
+        if (e >= p.skip) ((raw *)at)[e] = v.element(e);
 }
 
 template <int DT>
@@ -573,7 +593,11 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 3) void norm_kernel(NormArgs a)
                 for (int e = 0; e < VEC; e++)
                     y[e] = activate<DT, act.value>(__builtin_fmaf(held[j].get(e) - m[e], sc[e], sh[e]));
             }
-            if (r < rest) store_column<DT, P>(out + pass * a.out.ts, y, p, MODE == kApply && a.in_place);
+            if (r < rest) {
+                P to;
+                to.put(0, y);
+                store_column<DT>(out + pass * a.out.ts, to, p, MODE == kApply && a.in_place);
+            }
         }
     };
     for (int j0 = 0; j0 < R && j0 * a.rows < rest; j0 += H) {
@@ -688,7 +712,11 @@ __global__ __launch_bounds__(NT, 5) void norm_one_kernel(NormArgs a) {
                     for (int e = 0; e < VEC; e++)
                         y[e] = activate<DT, act.value>(__builtin_fmaf(held[j].get(e) - mean, sc[e], sh[e]));
                 }
-                if (r < a.L && p.active) P::store(out + pass * a.out.ts, y);
+                if (r < a.L && p.active) {
+                    P to;
+                    to.put(0, y);
+                    to.store(out + pass * a.out.ts);
+                }
                 load_row<P>(held[j], x, pass, a.rows, p.row, own, a.x.ts);
             }
         };
@@ -702,26 +730,35 @@ __global__ __launch_bounds__(NT, 5) void norm_one_kernel(NormArgs a) {
     }
 }
 
-// What the backward pass keeps of an element's channel.  z is the fused
-// x A + B with A = r w and B = b - m A, but for ReLU: there z is rounded step by
-// step as the formula is written, since the slope jumps with z's sign.
-template <int VEC, int ACT>
+// What the backward pass keeps of an element's channel.  Everything is taken
+// of d = x - m, whose rounding goes with the spread and not with the level.  z is
+// the fused d A + B with A = r w and B = b, as in the forward pass, but for ReLU:
+// there z is rounded step by step as the formula is written, since the slope
+// jumps with z's sign.
+template <int N, int ACT>
 struct Channel {
     static constexpr bool kSteps = ACT == ROCKET_ACT_RELU;
-    float A[VEC], B[VEC], m[VEC];   // x A + B; in steps: w and b
-    float r[kSteps ? VEC : 1];
-    __device__ float z(float x, int e) const {
-        if (kSteps) return (x - m[e]) * r[kSteps ? e : 0] * A[e] + B[e];
-        return __builtin_fmaf(x, A[e], B[e]);
+    float A[N], B[N], m[N];   // d A + B; in steps: w and b
+    float r[kSteps ? N : 1];
+    __device__ float z(float d, int e) const {
+        if (kSteps) return d * r[kSteps ? e : 0] * A[e] + B[e];
+        return __builtin_fmaf(d, A[e], B[e]);
     }
     __device__ float scale(int e) const { return kSteps ? A[e] * r[kSteps ? e : 0] : A[e]; }
-    __device__ void take(const Scratch &s, const Place &p) {
-        of_column<VEC>(s.of[0], p, A);
-        of_column<VEC>(s.of[1], p, B);
-        of_column<VEC>(s.of[2], p, m);
-        if constexpr (kSteps) of_column<VEC>(s.of[3], p, r);
+    __device__ void take(const Scratch &s, const Place &p, int from) {
+        of_column(s.of[0], p, A, from);
+        of_column(s.of[1], p, B, from);
+        of_column(s.of[2], p, m, from);
+        if constexpr (kSteps) of_column(s.of[3], p, r, from);
     }
 };
+
+// Elements of a column that norm_back_kernel takes at a time, through all the
+// columns that the thread holds: what it keeps of eight channels at once does
+// not fit beside 8 columns of x and of dy (777 x 129 x 924 in groups of 33, bf16,
+// SiLU: 221 us, against 285 us with all eight).
+template <int VEC>
+constexpr int kAtOnce = VEC < 4 ? VEC : 4;
 
 // Backward.  Held: a workgroup goes through the series b, b + a.series, ... and
 // keeps the channel sums over them; kStats leaves the channel sums of a chunk.
@@ -730,7 +767,8 @@ struct Channel {
 template <int DT, bool WIDE, int NT, int R, int MODE, int ACT>
 __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
     using P = Pack<DT, WIDE>;
-    constexpr int VEC = P::kN;
+    constexpr int VEC = P::kN, N = kAtOnce<VEC>;
+    constexpr bool CENTRED = DT == ROCKET_FLOAT32 && MODE == kHeld;   // x - m goes over x's words
     const Scratch s = scratch_of<NT, VEC>(a);
     Place p;
     const uint32_t b = rocket::item_of_block(), rest_of = rocket::uniform(b / a.slabs);
@@ -763,31 +801,33 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
         const float *mean = a.mean + (int64_t)p.i * a.G + p.g0, *rstd = a.rstd + (int64_t)p.i * a.G + p.g0;
         for_channels<NT>(a, p, [&](int ch, int g) {
             const float m = mean[g], r = rstd[g], w = a.w ? a.w[p.c0 + ch] : 1.0f, bias = a.b ? a.b[p.c0 + ch] : 0.0f;
-            s.of[2][ch] = m;
-            if (ACT == ROCKET_ACT_RELU) {
-                s.of[0][ch] = w, s.of[1][ch] = bias, s.of[3][ch] = r;
-            } else {
-                s.of[0][ch] = r * w, s.of[1][ch] = __builtin_fmaf(-m, r * w, bias);
-            }
+            s.of[0][ch] = ACT == ROCKET_ACT_RELU ? w : r * w;
+            s.of[1][ch] = bias, s.of[2][ch] = m;
+            if (ACT == ROCKET_ACT_RELU) s.of[3][ch] = r;
         });
         __syncthreads();
         if (MODE != kApply) {
-            Channel<VEC, ACT> of;
-            of.take(s, p);
             float sd[VEC], sx[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; e++) sd[e] = 0.0f, sx[e] = 0.0f;
 #pragma unroll
-            for (int j = 0; j < R; j++)
-                if (p.row + j * a.rows < own) {
+            for (int q = 0; q < VEC; q += N) {
+                Channel<N, ACT> of;
+                of.take(s, p, q);
 #pragma unroll
-                    for (int e = 0; e < VEC; e++) {
-                        const float v = hx[j].get(e);
-                        const float dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
-                        sd[e] += dz;
-                        sx[e] = __builtin_fmaf(dz, v - of.m[e], sx[e]);
+                for (int j = 0; j < R; j++)
+                    if (p.row + j * a.rows < own) {
+#pragma unroll
+                        for (int e = 0; e < N; e++) {
+                            const float d = hx[j].get(q + e) - of.m[e];
+                            const float dz = hg[j].get(q + e) * slope<DT, ACT>(of.z(d, e));
+                            sd[q + e] += dz;
+                            sx[q + e] = __builtin_fmaf(dz, d, sx[q + e]);
+                            if (CENTRED) hx[j].set(q + e, d);
+                        }
                     }
-                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
             int parts = sum_rows<NT, VEC>(a, p, sd, s);
             for (int ch = threadIdx.x; ch < W; ch += NT) {
                 float t = 0.0f;
@@ -830,12 +870,12 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
             }
             __syncthreads();
         }
-        // dx = r (dz w - mean(g) - xh mean(g xh)) = dz r w - (x D + E)
+        // dx = r (dz w - mean(g) - xh mean(g xh)) = dz r w - (d D + E)
         const float inv = T ? 1.0f / ((float)T * (float)a.width) : 0.0f;
         for_channels<NT>(a, p, [&](int ch, int g) {
-            const float m = mean[g], r = rstd[g], D = r * r * (s.group2[g] * inv);
-            s.chan[ch] = D;
-            s.first[ch] = __builtin_fmaf(-m, D, r * (s.group[g] * inv));
+            const float r = rstd[g];
+            s.chan[ch] = r * r * (s.group2[g] * inv);
+            s.first[ch] = r * (s.group[g] * inv);
         });
         __syncthreads();
         const int64_t rest = a.L - first, next = (int64_t)p.i + (MODE == kHeld ? a.series : a.n);
@@ -847,33 +887,40 @@ __global__ __launch_bounds__(NT, 4) void norm_back_kernel(NormArgs a) {
             p.i = next < a.n ? (uint32_t)next : p.i;
             x = column_at<DT>(a.x, p, first), dy = column_at<DT>(a.dy, p, first);
         }
-        Channel<VEC, ACT> of;
-        of.take(s, p);
-        float D[VEC], E[VEC];
-        of_column<VEC>(s.chan, p, D);
-        of_column<VEC>(s.first, p, E);
         for (int j0 = 0; j0 < R && j0 * a.rows < rest; j0 += H) {
             if (MODE == kApply) {
 #pragma unroll
                 for (int j = 0; j < H; j++) load(j, j0);
             }
 #pragma unroll
-            for (int j = 0; j < H; j++) {
-                const int pass = (j0 + j) * a.rows, r = p.row + pass;
-                float dx[VEC];
+            for (int q = 0; q < VEC; q += N) {   // dx goes over dy's words
+                Channel<N, ACT> of;
+                of.take(s, p, q);
+                float D[N], E[N];
+                of_column(s.chan, p, D, q);
+                of_column(s.first, p, E, q);
 #pragma unroll
-                for (int e = 0; e < VEC; e++) dx[e] = 0.0f;
-                if (r < had) {
-                    hx[j].renew(), hg[j].renew();
+                for (int j = 0; j < H; j++) {
+                    const int pass = (j0 + j) * a.rows, r = p.row + pass;
+                    float dx[N];
 #pragma unroll
-                    for (int e = 0; e < VEC; e++) {
-                        const float v = hx[j].get(e), dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
-                        dx[e] = __builtin_fmaf(dz, of.scale(e), -__builtin_fmaf(v, D[e], E[e]));
+                    for (int e = 0; e < N; e++) dx[e] = 0.0f;
+                    if (r < had) {
+                        if (q == 0) hx[j].renew(), hg[j].renew();
+#pragma unroll
+                        for (int e = 0; e < N; e++) {
+                            const float d = CENTRED ? hx[j].get(q + e) : hx[j].get(q + e) - of.m[e];
+                            const float dz = hg[j].get(q + e) * slope<DT, ACT>(of.z(d, e));
+                            dx[e] = __builtin_fmaf(dz, of.scale(e), -__builtin_fmaf(d, D[e], E[e]));
+                        }
                     }
+                    hg[j].put(q, dx);
+                    if (q + N < VEC) continue;
+                    if (r < rest && p.active)
+                        store_column<DT>(out + pass * a.out.ts, hg[j], p, MODE == kApply && a.in_place);
+                    if (MODE == kHeld) load(j, 0);
                 }
-                if (r < rest && p.active)
-                    store_column<DT, P>(out + pass * a.out.ts, dx, p, MODE == kApply && a.in_place);
-                if (MODE == kHeld) load(j, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (next >= a.n) break;
@@ -893,6 +940,8 @@ template <int DT, int NT, int R, int ACT>
 __global__ __launch_bounds__(NT, 4) void norm_back_one_kernel(NormArgs a) {
     using P = Pack<DT, true>;
     constexpr int VEC = P::kN, Q = VEC / 4;
+    constexpr bool CENTRED = DT == ROCKET_FLOAT32;   // x - m goes over x's words, which saves
+    // the second pass a subtraction (500 x 1000 x 256, fp32, SiLU: 370 us against 381 us)
     extern __shared__ __attribute__((aligned(16))) float shared[];
     const int W = a.cols * VEC;
     float *group = shared, *group2 = group + pad4(a.most_groups), *rows = group2 + pad4(a.most_groups);
@@ -929,17 +978,14 @@ __global__ __launch_bounds__(NT, 4) void norm_back_one_kernel(NormArgs a) {
         const float mean = a.mean[(int64_t)p.i * a.G + p.g0 + g], rstd = a.rstd[(int64_t)p.i * a.G + p.g0 + g];
         Channel<VEC, ACT> of;
         auto scales = [&]() {
-            float w[VEC], c[VEC];
-            of_column<VEC>(weight, p, w);
-            of_column<VEC>(bias, p, c);
+            of_column(weight, p, of.A);
+            of_column(bias, p, of.B);
 #pragma unroll
             for (int e = 0; e < VEC; e++) {
-                if constexpr (ACT == ROCKET_ACT_RELU) {
-                    of.A[e] = w[e], of.B[e] = c[e], of.m[e] = mean, of.r[e] = rstd;
-                } else {
-                    of.A[e] = rstd * w[e];
-                    of.B[e] = __builtin_fmaf(-mean, of.A[e], c[e]);
-                }
+                if constexpr (ACT == ROCKET_ACT_RELU)
+                    of.r[e] = rstd;
+                else
+                    of.A[e] *= rstd;
             }
         };
         scales();
@@ -951,10 +997,11 @@ __global__ __launch_bounds__(NT, 4) void norm_back_one_kernel(NormArgs a) {
             if (p.row + j * a.rows < own) {
 #pragma unroll
                 for (int e = 0; e < VEC; e++) {
-                    const float v = hx[j].get(e);
-                    const float dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
+                    const float d = hx[j].get(e) - mean;
+                    const float dz = hg[j].get(e) * slope<DT, ACT>(of.z(d, e));
                     sd[e] += dz;
-                    sx[e] = __builtin_fmaf(dz, v - mean, sx[e]);
+                    sx[e] = __builtin_fmaf(dz, d, sx[e]);
+                    if (CENTRED) hx[j].set(e, d);
                     if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // four at a time: registers are short
                 }
             }
@@ -976,9 +1023,9 @@ __global__ __launch_bounds__(NT, 4) void norm_back_one_kernel(NormArgs a) {
             total[k * NT + threadIdx.x] = d, total[(Q + k) * NT + threadIdx.x] = q;
         }
         sum_two<NT, VEC>(a, p, g, t1, t2, rows, group, group2);
-        // dx = r (dz w - mean(g) - xh mean(g xh)) = dz r w - (x D + E)
+        // dx = r (dz w - mean(g) - xh mean(g xh)) = dz r w - (d D + E)
         const float inv = own ? 1.0f / ((float)own * (float)a.width) : 0.0f;
-        const float D = rstd * rstd * (t2 * inv), E = __builtin_fmaf(-mean, D, t1 * inv);
+        const float D = rstd * rstd * (t2 * inv), E = t1 * inv;
         scales();
 
         const uint32_t next = p.i + a.series;   // below 2^32
@@ -998,12 +1045,17 @@ __global__ __launch_bounds__(NT, 4) void norm_back_one_kernel(NormArgs a) {
                 hx[j].renew(), hg[j].renew();
 #pragma unroll
                 for (int e = 0; e < VEC; e++) {
-                    const float v = hx[j].get(e), dz = hg[j].get(e) * slope<DT, ACT>(of.z(v, e));
-                    dx[e] = __builtin_fmaf(dz, of.scale(e), -__builtin_fmaf(v, D, E));
+                    const float d = CENTRED ? hx[j].get(e) : hx[j].get(e) - mean;
+                    const float dz = hg[j].get(e) * slope<DT, ACT>(of.z(d, e));
+                    dx[e] = __builtin_fmaf(dz, of.scale(e), -__builtin_fmaf(d, D, E));
                     if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            if (r < a.L && p.active) P::store(out + pass * a.out.ts, dx);
+            if (r < a.L && p.active) {
+                P to;
+                to.put(0, dx);
+                to.store(out + pass * a.out.ts);
+            }
             load(j);
         }
         if (!more) break;

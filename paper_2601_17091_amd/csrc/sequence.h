@@ -19,6 +19,7 @@ struct Elem;
 template <>
 struct Elem<ROCKET_FLOAT32> {
     using raw = float;
+    using bits = uint32_t;
     static constexpr int kSize = 4, kPerWord = 1;
     static __device__ float get(uint32_t w, int) { return __builtin_bit_cast(float, w); }
     static __device__ uint32_t put(const float *x) { return __builtin_bit_cast(uint32_t, x[0]); }
@@ -29,6 +30,7 @@ struct Elem<ROCKET_FLOAT32> {
 template <>
 struct Elem<ROCKET_BFLOAT16> {
     using raw = uint16_t;
+    using bits = uint16_t;
     typedef __bf16 pair __attribute__((ext_vector_type(2)));
     static constexpr int kSize = 2, kPerWord = 2;
     static __device__ float get(uint32_t w, int j) {
@@ -47,6 +49,7 @@ struct Elem<ROCKET_BFLOAT16> {
 template <>
 struct Elem<ROCKET_FLOAT16> {
     using raw = uint16_t;
+    using bits = uint16_t;
     typedef _Float16 pair __attribute__((ext_vector_type(2)));
     static constexpr int kSize = 2, kPerWord = 2;
     static __device__ float get(uint32_t w, int j) { return (float)__builtin_bit_cast(pair, w)[j]; }

@@ -65,3 +65,43 @@ def test_groups_of_unequal_levels(env, n, L, C, G, dtype, act, level):  # noqa: 
     close(dx[:, :, near], want["dx"][:, :, near], want["dx_tol"][:, :, near], "dx")
     close(dw[near], want["dweight"][near], want["dweight_tol"][near], "dweight")
     close(db[near], want["dbias"][near], want["dbias_tol"][near], "dbias")
+
+
+@pytest.mark.parametrize("dtype,level", [("float32", 1e3), ("float32", 1e4), ("float32", 1e5), ("float16", 1e3)])
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
+@pytest.mark.parametrize("n,L,C,G", CUTS)
+def test_level_far_above_the_spread(env, n, L, C, G, act, dtype, level):  # noqa: F811
+    """All values far above their spread of 1: x - m loses nothing, and neither
+    do the gradients."""
+    torch, seq = env
+    rng = np.random.default_rng(n + L + C + 1)
+    x, xv = typed(torch, level + rng.standard_normal((n, L, C)), dtype)
+    dy, dyv = typed(torch, rng.standard_normal((n, L, C)), dtype)
+    w = (1 + 0.2 * rng.standard_normal(C)).astype(np.float32)
+    b = (0.2 * rng.standard_normal(C)).astype(np.float32)
+    mean, rstd, dx, dw, db = backward(torch, seq, x, dy, G, f32(torch, w), f32(torch, b), act)
+    want = so.group_norm_backward(dyv, xv, G, host(mean), host(rstd), w, b, activation=act, dtype=dtype)
+    close(dx, want["dx"], want["dx_tol"], "dx")
+    close(dw, want["dweight"], want["dweight_tol"], "dweight")
+    close(db, want["dbias"], want["dbias_tol"], "dbias")
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
+@pytest.mark.parametrize("n,L,C,G", [(3, 6000, 99, 3), (2, 300, 4100, 2), (2, 5000, 33, 1), (50, 30, 99, 3)])
+def test_channels_of_two_columns_have_one_value(env, n, L, C, G, act, dtype):  # noqa: F811
+    """Channels that two threads compute, and either may write last: the same
+    bits from both, over the input or beside it, call after call."""
+    torch, seq = env
+    torch.manual_seed(1)
+    x, dy = (torch.randn(n, L, C, device="cuda").to(getattr(torch, dtype)) for _ in range(2))
+    w, b = torch.linspace(0.5, 1.5, C, device="cuda"), torch.linspace(-0.2, 0.2, C, device="cuda")
+    y, mean, rstd = seq.group_norm(x, G, w, b, activation=act)
+    dx = seq.group_norm_backward(dy, x, G, mean, rstd, w, b, activation=act)[0]
+    for _ in range(5):
+        assert torch.equal(seq.group_norm(x, G, w, b, activation=act)[0], y)
+        assert torch.equal(seq.group_norm_backward(dy, x, G, mean, rstd, w, b, activation=act)[0], dx)
+    t = x.clone()
+    assert torch.equal(seq.group_norm(t, G, w, b, activation=act, out=t)[0], y)
+    t = dy.clone()
+    assert torch.equal(seq.group_norm_backward(t, x, G, mean, rstd, w, b, activation=act, out=t)[0], dx)
