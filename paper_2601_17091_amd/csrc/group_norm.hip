@@ -124,21 +124,50 @@ struct Pack<DT, false> {
     __device__ void renew() {}
 };
 
-// The normal distribution function and e = exp(-z^2 / 2).  fp32 elements: the
-// library's erf.  16-bit elements: formula 7.1.26 of Abramowitz and Stegun
-// (1964), erf to 1.5e-7, far below the elements' own rounding; its tail is a
-// product, so that small values of z < 0 keep their digits.
+// The normal distribution function and e = exp(-z^2 / 2).  Its lower tail is
+// e t P(t) with t = 1 / (1 + p |z|): exp(z^2 / 2) times the tail is smooth in t, and
+// P is a polynomial fitted to it in the relative error (Lawson's weighted least
+// squares), so that values far below 0 keep their digits.
+//   fp32 elements: P of degree 8, 2e-8 relative; z^2 in two parts, so that the tail
+//   is good to 12 units of 2^-24 down to z = -12.5; where |z| < 1, 1/2 + z Q(z^2)
+//   with Q of degree 5, whose rounding is the result's own.
+//   16-bit elements: P of degree 5, the lesser of 7.3e-8 and 1e-4 of the tail, a
+//   fifth of an fp16 rounding.
 template <int DT>
 __device__ inline float normal_cdf(float z, float &e) {
-    e = rocket::exp_neg_abs<DT>(0.5f * z * z);
-    if (DT == ROCKET_FLOAT32) return 0.5f + 0.5f * erff(z * 0.70710678118654752f);
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(z), 0.3275911f * 0.70710678f, 1.0f));
-    float q = __builtin_fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
-    q = __builtin_fmaf(t, q, 0.5f * 1.421413741f);
-    q = __builtin_fmaf(t, q, 0.5f * -0.284496736f);
-    q = __builtin_fmaf(t, q, 0.5f * 0.254829592f);
+    if (DT != ROCKET_FLOAT32) {
+        e = rocket::exp_neg_abs<DT>(0.5f * z * z);
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(z), 0.29f, 1.0f));
+        float q = __builtin_fmaf(t, -0.08850604f, 0.28376429f);
+        q = __builtin_fmaf(t, q, -0.09162589f);
+        q = __builtin_fmaf(t, q, 0.17847331f);
+        q = __builtin_fmaf(t, q, 0.10106501f);
+        q = __builtin_fmaf(t, q, 0.11682939f);
+        const float tail = q * t * e;
+        return z < 0.0f ? tail : 1.0f - tail;
+    }
+    // at 15 e is 0; a NaN goes on through the callers' products with z
+    const float u = __builtin_amdgcn_fmed3f(__builtin_fabsf(z), 0.0f, 15.0f);
+    const float s = u * u, low = __builtin_fmaf(u, u, -s);
+    e = rocket::exp_neg_abs<DT>(0.5f * s);
+    e = __builtin_fmaf(e, -0.5f * low, e);
+    float c = __builtin_fmaf(s, -7.654199180251453e-06f, 0.0001134863487095572f);
+    c = __builtin_fmaf(s, c, -0.001186329871416092f);
+    c = __builtin_fmaf(s, c, 0.009973322972655296f);
+    c = __builtin_fmaf(s, c, -0.06649035960435867f);
+    c = __builtin_fmaf(s, c, 0.3989422917366028f);
+    c = __builtin_fmaf(z, c, 0.5f);
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(u, 0.21f, 1.0f));
+    float q = __builtin_fmaf(t, -0.07122398912906647f, 0.28145527839660645f);
+    q = __builtin_fmaf(t, q, -0.3257579207420349f);
+    q = __builtin_fmaf(t, q, 0.34412485361099243f);
+    q = __builtin_fmaf(t, q, -0.09015858173370361f);
+    q = __builtin_fmaf(t, q, 0.12320016324520111f);
+    q = __builtin_fmaf(t, q, 0.06964277476072311f);
+    q = __builtin_fmaf(t, q, 0.08500158041715622f);
+    q = __builtin_fmaf(t, q, 0.08371583372354507f);
     const float tail = q * t * e;
-    return z < 0.0f ? tail : 1.0f - tail;
+    return u < 1.0f ? c : z < 0.0f ? tail : 1.0f - tail;
 }
 
 template <int DT, int ACT>
