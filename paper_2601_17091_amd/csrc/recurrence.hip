@@ -364,7 +364,7 @@ __global__ __launch_bounds__(64 * (WAY == kOne ? kMostWaves : kTileWaves), WAY =
 #pragma unroll
                 for (int j = 0; j < P; j++) {
                     float in;
-                    rocket::logistic<DT>(Elem<DT>::get(wf[s], j), fa[s][j], in);
+                    rocket::logistic<DT, true>(Elem<DT>::get(wf[s], j), fa[s][j], in);
                     fb[s][j] = in * Elem<DT>::get(wv[s], j);
                     B[j] = __builtin_fmaf(fa[s][j], B[j], fb[s][j]);
                     A[j] *= fa[s][j];
@@ -471,7 +471,7 @@ __global__ __launch_bounds__(64 * (WAY == kOne ? kMostWaves : kTileWaves), 4) vo
 #pragma unroll
                 for (int j = 0; j < P; j++) {
                     float so = 1.0f, rest;
-                    rocket::logistic<DT>(Elem<DT>::get(wf[s], j), fa[s][j], in[s][j]);
+                    rocket::logistic<DT, true>(Elem<DT>::get(wf[s], j), fa[s][j], in[s][j]);
                     if (GATE) rocket::logistic<DT>(Elem<DT>::get(wo[s], j), so, rest);
                     const float g = GATE ? Elem<DT>::get(wg[s], j) * so : Elem<DT>::get(wg[s], j);
                     R[j] = fa[s][j] * (R[j] + g);
@@ -592,7 +592,7 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
 #pragma unroll
     for (int j = 0; j < P; j++) {
         float keep, in;
-        rocket::logistic<DT>(Elem<DT>::get(wf, j), keep, in);
+        rocket::logistic<DT, true>(Elem<DT>::get(wf, j), keep, in);
         h[j] = __builtin_fmaf(keep, h[j], in * Elem<DT>::get(wv, j));
         y[j] = h[j];
         if (GATE) {
