@@ -179,6 +179,10 @@ inline bool out_ok(const rocket_sequence *q, const rocket_sequence_shape *s) {
            q->step_stride >= (s->n - 1) * q->series_stride + C;
 }
 
+// Workgroups that one launch takes: HIP refuses 2^32 threads and more.  Larger
+// calls are cut into several launches.
+inline int64_t most_groups(int64_t threads) { return (int64_t)UINT32_MAX / threads; }
+
 inline rocket_status launched() { return hipGetLastError() == hipSuccess ? ROCKET_OK : ROCKET_ERR_HIP; }
 
 }  // namespace rocket
