@@ -40,7 +40,7 @@
 // whose tiles wait for each other; 777 x 129 x 331, fp16, gated, ragged 65 us.
 // One counter a cache line: with the 16 rows' counters side by side the last
 // but one took 40 us.
-#include <climits>
+#include <algorithm>
 #include <type_traits>
 
 #include "sequence.h"
@@ -614,8 +614,14 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
 struct Cut {
     int32_t lanes, waves, blocks, tiles;
     bool split;
-    int64_t rows, grid;
+    int64_t series, rows;   // of a launch
 };
+
+// 8-byte words of a split launch's maps, published states and counters.
+int64_t map_words(const Cut &c) { return c.rows * c.tiles * kMostChannels; }
+int64_t reached_words(const Cut &c) { return c.rows * ((c.tiles + kGroup - 1) / kGroup) * (kMostChannels / 2); }
+int64_t workspace_words(const Cut &c) { return c.split ? map_words(c) + reached_words(c) + c.rows * (kApart / 2) : 0; }
+int64_t workspace_of(const Cut &c) { return workspace_words(c) * 8; }
 
 // Lanes over channels: the power of two that covers the words of channels, 32
 // at most; the wavefront's other lanes take further runs of steps, so that
@@ -639,7 +645,7 @@ struct Cut {
 // gated backward pass of 16-bit elements, short of registers in its loop, where
 // the tiles are mostly full (1000 x 1000 x 256: 788 us against 904 us; 1000 x
 // 129 x 256, a last tile of one step: 197 against 173 us).
-bool cut_of(const rocket_sequence_shape *s, bool back, bool gate, Cut *cut) {
+void cut_of(const rocket_sequence_shape *s, bool back, bool gate, Cut *cut) {
     const int64_t per_word = rocket::elem_size(s->dtype) == 4 ? 1 : 2;
     const int64_t words = (s->channels + per_word - 1) / per_word;
     cut->lanes = 1;
@@ -648,27 +654,29 @@ bool cut_of(const rocket_sequence_shape *s, bool back, bool gate, Cut *cut) {
     const int64_t L = s->steps > 0 ? s->steps : 1;
     cut->waves = (int32_t)(in_wave < kEvery ? kEvery / in_wave : 1);
     cut->blocks = (int32_t)((words + cut->lanes - 1) / cut->lanes);
-    cut->rows = s->n * cut->blocks;
+    const int64_t rows = s->n * cut->blocks;
     // One tile holds the series.
     const int64_t one = (L + in_wave - 1) / in_wave;
-    const int most = cut->rows < kFill || (per_word == 2 && !back) ? kMostWaves : per_word == 2 && gate ? 10 : kTileWaves;
+    const int most = rows < kFill || (per_word == 2 && !back) ? kMostWaves : per_word == 2 && gate ? 10 : kTileWaves;
     if (one <= most) cut->waves = (int32_t)one;
     const int64_t tile = cut->waves * in_wave;
     cut->tiles = (int32_t)((L + tile - 1) / tile);
-    const int64_t slots = (cut->rows + kFill - 1) / kFill * kFill;   // of a loop, whole waves of workgroups
+    const int64_t slots = (rows + kFill - 1) / kFill * kFill;   // of a loop, whole waves of workgroups
     cut->split = cut->tiles > 1 &&
-                 (cut->rows < kFill || (cut->tiles >= 8 && cut->rows < 4 * kFill && 4 * cut->rows < 3 * slots) ||
+                 (rows < kFill || (cut->tiles >= 8 && rows < 4 * kFill && 4 * rows < 3 * slots) ||
                   (per_word == 1 && cut->tiles >= 8) ||
                   (per_word == 2 && back && gate && 4 * L >= 3 * tile * cut->tiles));
-    return !__builtin_mul_overflow(cut->rows, (int64_t)(cut->split ? cut->tiles : 1), &cut->grid) &&
-           cut->grid <= INT_MAX;
+    // Series of a launch: as many as its threads allow, and those of the launch
+    // that clears the workspace (a word each).  A series whose tiles are too many
+    // for one launch is not split.
+    const int64_t limit = rocket::most_groups(256) * 256;
+    cut->rows = cut->blocks;
+    int64_t each = std::max<int64_t>((int64_t)cut->blocks * cut->tiles * 64 * cut->waves, workspace_words(*cut));
+    cut->split = cut->split && each <= limit;
+    if (!cut->split) each = (int64_t)cut->blocks * 64 * cut->waves;
+    cut->series = std::min(std::max<int64_t>(s->n, 1), limit / each);
+    cut->rows = cut->series * cut->blocks;
 }
-
-// 8-byte words of a split call's maps, published states and counters.
-int64_t map_words(const Cut &c) { return c.rows * c.tiles * kMostChannels; }
-int64_t reached_words(const Cut &c) { return c.rows * ((c.tiles + kGroup - 1) / kGroup) * (kMostChannels / 2); }
-int64_t workspace_words(const Cut &c) { return c.split ? map_words(c) + reached_words(c) + c.rows * (kApart / 2) : 0; }
-int64_t workspace_of(const Cut &c) { return workspace_words(c) * 8; }
 
 void set_cut(RecArgs &a, const Cut &c, void *workspace) {
     a.blocks = c.blocks, a.lanes = c.lanes, a.waves = c.waves, a.tiles = c.tiles;
@@ -690,36 +698,62 @@ View view(const rocket_sequence *q, int size) {
 
 bool aligned(const void *p, uintptr_t to) { return (uintptr_t)p % to == 0; }
 
+// The call's series from i on, as many as a launch takes.
+RecArgs part_of(RecArgs a, const Cut &cut, int64_t i) {
+    a.n = (int32_t)std::min<int64_t>(cut.series, a.n - i);
+    for (View *x : {&a.v, &a.f, &a.o, &a.y, &a.dy, &a.dv, &a.df, &a.dO})
+        if (x->p) x->p += i * x->ss;
+    if (a.lengths) a.lengths += i;
+    for (const float **x : {&a.h0, &a.dh_last})
+        if (*x) *x += i * a.C;
+    for (float **x : {&a.h_last, &a.dh0})
+        if (*x) *x += i * a.C;
+    if (a.states) a.states += i * (((int64_t)a.L + kEvery - 1) / kEvery) * a.C;
+    return a;
+}
+
 template <int DT, bool GATE>
-void run_forward(const RecArgs &a, const Cut &cut, hipStream_t s) {
-    const uint32_t grid = (uint32_t)cut.grid, threads = 64 * cut.waves;
-    if (cut.split) {
-        clear(a, cut, s);
-        forward_kernel<DT, kSplit, GATE><<<grid, threads, 0, s>>>(a);
-    } else if (cut.tiles > 1) {
-        forward_kernel<DT, kLoop, GATE><<<grid, threads, 0, s>>>(a);
-    } else {
-        forward_kernel<DT, kOne, GATE><<<grid, threads, 0, s>>>(a);
+void run_forward(const RecArgs &call, const Cut &cut, hipStream_t s) {
+    for (int64_t i = 0; i < call.n; i += cut.series) {
+        const RecArgs a = part_of(call, cut, i);
+        const uint32_t rows = (uint32_t)a.n * a.blocks, threads = 64 * cut.waves;
+        if (cut.split) {
+            clear(a, cut, s);
+            forward_kernel<DT, kSplit, GATE><<<rows * cut.tiles, threads, 0, s>>>(a);
+        } else if (cut.tiles > 1) {
+            forward_kernel<DT, kLoop, GATE><<<rows, threads, 0, s>>>(a);
+        } else {
+            forward_kernel<DT, kOne, GATE><<<rows, threads, 0, s>>>(a);
+        }
     }
 }
 
 template <int DT, bool GATE>
-void run_backward(const RecArgs &a, const Cut &cut, hipStream_t s) {
-    const uint32_t grid = (uint32_t)cut.grid, threads = 64 * cut.waves;
-    if (cut.split) {
-        clear(a, cut, s);
-        backward_kernel<DT, kSplit, GATE><<<grid, threads, 0, s>>>(a);
-    } else if (cut.tiles > 1) {
-        backward_kernel<DT, kLoop, GATE><<<grid, threads, 0, s>>>(a);
-    } else {
-        backward_kernel<DT, kOne, GATE><<<grid, threads, 0, s>>>(a);
+void run_backward(const RecArgs &call, const Cut &cut, hipStream_t s) {
+    for (int64_t i = 0; i < call.n; i += cut.series) {
+        const RecArgs a = part_of(call, cut, i);
+        const uint32_t rows = (uint32_t)a.n * a.blocks, threads = 64 * cut.waves;
+        if (cut.split) {
+            clear(a, cut, s);
+            backward_kernel<DT, kSplit, GATE><<<rows * cut.tiles, threads, 0, s>>>(a);
+        } else if (cut.tiles > 1) {
+            backward_kernel<DT, kLoop, GATE><<<rows, threads, 0, s>>>(a);
+        } else {
+            backward_kernel<DT, kOne, GATE><<<rows, threads, 0, s>>>(a);
+        }
     }
 }
 
 template <int DT, bool GATE>
-void run_step(const StepArgs &a, hipStream_t s) {
-    const int64_t threads = a.n * a.words;
-    step_kernel<DT, GATE><<<(uint32_t)((threads + 255) / 256), 256, 0, s>>>(a);
+void run_step(StepArgs a, hipStream_t s) {
+    const int64_t n = a.n, most = rocket::most_groups(256) * 256 / a.words;   // series of a launch
+    for (int64_t i = 0; i < n; i += most) {
+        a.n = std::min(most, n - i);
+        step_kernel<DT, GATE><<<(uint32_t)((a.n * a.words + 255) / 256), 256, 0, s>>>(a);
+        a.v += most * a.vs, a.f += most * a.fs, a.y += most * a.ys;
+        if (GATE) a.o += most * a.os;
+        a.h_in += most * a.C, a.h_out += most * a.C;
+    }
 }
 
 #define BY_TYPE(fn, dtype, gate, ...)                                                                       \
@@ -739,7 +773,7 @@ extern "C" rocket_status rocket_recurrence_workspace(const rocket_sequence_shape
     int64_t most = 0;
     for (int k = 0; k < 4; k++) {   // either pass, gated or not
         Cut cut;
-        if (!cut_of(shape, k & 1, k & 2, &cut)) return ROCKET_ERR_INVALID_ARG;
+        cut_of(shape, k & 1, k & 2, &cut);
         if (workspace_of(cut) > most) most = workspace_of(cut);
     }
     *bytes = most;
@@ -750,10 +784,11 @@ extern "C" rocket_status rocket_recurrence_forward(const rocket_sequence_shape *
                                                    const rocket_sequence *f, const rocket_sequence *o, const float *h0,
                                                    const rocket_sequence *y, float *h_last, float *states,
                                                    void *workspace, int64_t workspace_bytes, void *hip_stream) {
-    Cut cut;
-    if (!rocket::shape_ok(shape) || !cut_of(shape, false, o != nullptr, &cut) || !rocket::view_ok(v, shape) || !rocket::view_ok(f, shape) ||
+    if (!rocket::shape_ok(shape) || !rocket::view_ok(v, shape) || !rocket::view_ok(f, shape) ||
         (o && !rocket::view_ok(o, shape)) || !rocket::out_ok(y, shape) || (shape->n > 0 && !h_last))
         return ROCKET_ERR_INVALID_ARG;
+    Cut cut;
+    cut_of(shape, false, o != nullptr, &cut);
     const int64_t need = workspace_of(cut);
     if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 8)))) return ROCKET_ERR_INVALID_ARG;
     if (!aligned(h0, 4) || !aligned(h_last, 4) || !aligned(states, 4) || !aligned(shape->lengths, 4))
@@ -775,12 +810,13 @@ extern "C" rocket_status rocket_recurrence_backward(const rocket_sequence_shape 
                                                     const float *dh_last, const rocket_sequence *dv,
                                                     const rocket_sequence *df, const rocket_sequence *dO, float *dh0,
                                                     void *workspace, int64_t workspace_bytes, void *hip_stream) {
-    Cut cut;
-    if (!rocket::shape_ok(shape) || !cut_of(shape, true, o != nullptr, &cut) || !rocket::view_ok(dy, shape) ||
+    if (!rocket::shape_ok(shape) || !rocket::view_ok(dy, shape) ||
         !rocket::view_ok(v, shape) || !rocket::view_ok(f, shape) || (o && !rocket::view_ok(o, shape)) ||
         !rocket::out_ok(dv, shape) || !rocket::out_ok(df, shape) || (o != nullptr) != (dO != nullptr) ||
         (dO && !rocket::out_ok(dO, shape)) || (shape->n > 0 && !dh0) || (!rocket::empty(shape) && !states))
         return ROCKET_ERR_INVALID_ARG;
+    Cut cut;
+    cut_of(shape, true, o != nullptr, &cut);
     const int64_t need = workspace_of(cut);
     if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 8)))) return ROCKET_ERR_INVALID_ARG;
     if (!aligned(states, 4) || !aligned(dh_last, 4) || !aligned(dh0, 4) || !aligned(shape->lengths, 4))
@@ -816,7 +852,6 @@ extern "C" rocket_status rocket_recurrence_step(int64_t n, int64_t channels, int
     a.h_in = h_in, a.h_out = h_out, a.n = n, a.C = channels;
     const int64_t per_word = size == 4 ? 1 : 2;
     a.words = (channels + per_word - 1) / per_word;
-    if ((n * a.words + 255) / 256 > INT_MAX) return ROCKET_ERR_INVALID_ARG;
     BY_TYPE(run_step, dtype, o != nullptr, a, (hipStream_t)hip_stream);
     return rocket::launched();
 }

@@ -24,3 +24,40 @@ def test_dropout_of_more_elements_than_a_launch(env):  # noqa: F811
                          np.arange((1 << 35) - 20, (1 << 35) + 20), np.arange(n - 30, n)])
     want = expected_dropout(torch, torch.ones(1, dtype=torch.bfloat16).expand(n), None, 0.25, 11, 3, ix)
     assert torch.equal(y[torch.from_numpy(ix).cuda()].cpu(), want)
+
+
+def test_recurrence_of_more_series_than_a_launch(env):  # noqa: F811
+    """2^26 series of one step and channel and a few more, a wavefront each: all
+    of them against the formula, in fp32 on the way."""
+    torch, seq = env
+    n = (1 << 26) + 5
+    v, f, dy = (torch.randn(n, 1, 1, device="cuda").to(torch.bfloat16) for _ in range(3))
+    h0 = torch.randn(n, 1, device="cuda")
+    y, h, states = seq.recurrence(v, f, h0=h0, keep_states=True)
+    assert torch.equal(states[:, 0], h0)
+    a, keep = torch.sigmoid(f.float())[:, 0], torch.sigmoid(-f.float())[:, 0]
+    want = a * h0 + keep * v.float()[:, 0]
+    # a few roundings of fp32 operands of up to 6
+    assert float((h - want).abs().max()) < 1e-5
+    assert float((y[:, 0].float() - want).abs().sub_(want.abs() * 2.0 ** -8).max()) < 2e-5
+    dv, df, _, dh0 = seq.recurrence_backward(dy, v, f, states, dh_last=h0)
+    dh = dy.float()[:, 0] + h0
+    assert float((dh0 - a * dh).abs().max()) < 1e-5
+    for got, want in ((dv, dh * keep), (df, dh * (h0 - v.float()[:, 0]) * a * keep)):
+        assert float((got[:, 0].float() - want).abs().sub_(want.abs() * 2.0 ** -8).max()) < 5e-5
+
+
+def test_recurrence_step_of_more_words_than_a_launch(env):  # noqa: F811
+    """2^32 words of channels and more: 1,025 channels of 2^23 series, the inputs
+    a few rows repeated."""
+    torch, seq = env
+    n, C = (1 << 23) + 7, 1025
+    v, f = (torch.randn(1, C, device="cuda").to(torch.bfloat16) for _ in range(2))
+    h = torch.ones(n, C, device="cuda")
+    y, h = seq.recurrence_step(v.expand(n, C), f.expand(n, C), h, h_out=h)
+    small_y, small_h = seq.recurrence_step(v, f, torch.ones(1, C, device="cuda"))
+    per = ((1 << 32) - 256) // 513   # series of a launch
+    for at in (0, per - 3, n - 1000):
+        assert torch.equal(h[at:at + 1000], small_h.expand(len(h[at:at + 1000]), C))
+        assert torch.equal(y[at:at + 1000], small_y.expand(len(y[at:at + 1000]), C))
+    assert float(h.sum(0, dtype=torch.float64).sub_(small_h[0].double() * n).abs().max()) < 1e-6 * n
