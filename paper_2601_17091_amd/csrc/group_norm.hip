@@ -35,7 +35,6 @@
 // slabs being read twice (15 us and 32 us).  777 x 129 x 924 in groups of 33,
 // fp16, ReLU, ragged: 88 to 94 us.
 #include <algorithm>
-#include <climits>
 #include <iterator>
 #include <type_traits>
 
@@ -1132,7 +1131,8 @@ struct Cut {
     int32_t width, slabs, parts, cols, rows, threads, run, chunks;
     int32_t series;     // backward, held
     int32_t groups;     // of a slab, at most
-    int64_t grid;
+    int64_t each;       // workgroups of a series; 0: `series` times slabs go through all of them
+    int64_t launch;     // series of a launch
     int64_t sum_rows;   // backward: rows of channel sums
     int64_t folded;     // rows after the first fold, 0: one fold is enough
 };
@@ -1217,9 +1217,8 @@ bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut)
         cut->threads = kChunk.threads, cut->run = (back ? kBackChunk : kChunk).run;
         cut->rows = cut->threads / cut->cols;
         const int64_t step = (int64_t)cut->rows * cut->run, chunks = (L + step - 1) / step;
-        if (chunks > INT_MAX) return false;
         cut->chunks = (int32_t)chunks;
-        if (__builtin_mul_overflow(s->n * chunks, (int64_t)cut->slabs, &cut->grid)) return false;
+        cut->each = chunks * cut->slabs;
         cut->sum_rows = s->n * chunks;
     } else if (back || (cut->one && cut->run <= kLoopRun)) {
         // as many workgroups as the registers take (20 wavefronts a CU), backward
@@ -1229,18 +1228,20 @@ bool cut_of(const rocket_sequence_shape *s, int32_t groups, bool back, Cut *cut)
         if (series < 1) series = 1;
         const int64_t each = (s->n + series - 1) / series;
         cut->series = (int32_t)(each > 0 ? (s->n + each - 1) / each : 1);
-        cut->grid = (int64_t)cut->series * cut->slabs;
+        cut->each = 0;
         cut->sum_rows = cut->series;
     } else {
-        cut->grid = s->n * cut->slabs;
+        cut->each = cut->slabs;
     }
+    cut->launch = s->n > 0 ? s->n : 1;
+    if (cut->each) cut->launch = std::min(cut->launch, rocket::most_groups(cut->threads) / cut->each);
     if (back && cut->sum_rows > 4 * kFold) cut->folded = (cut->sum_rows + kFold - 1) / kFold;
     const int64_t fold_grid = (cut->folded ? cut->folded : 1) * 2 * ((C + 63) / 64);
-    return cut->grid <= INT_MAX && (!back || fold_grid <= INT_MAX);
+    return cut->launch >= 1 && (!back || fold_grid <= rocket::most_groups(1024));
 }
 
 int64_t stats_of(const rocket_sequence_shape *s, int32_t groups, const Cut &c) {
-    return c.held ? 0 : s->n * groups * (int64_t)c.chunks * c.parts;
+    return c.held ? 0 : c.launch * groups * (int64_t)c.chunks * c.parts;
 }
 
 int64_t workspace_of(const rocket_sequence_shape *s, int32_t groups, bool back, const Cut &c) {
@@ -1250,7 +1251,7 @@ int64_t workspace_of(const rocket_sequence_shape *s, int32_t groups, bool back, 
 
 template <int DT, bool BACK, bool WIDE, int NT, int R, int MODE>
 void go(const NormArgs &a, const Cut &c, hipStream_t s) {
-    const uint32_t grid = (uint32_t)c.grid;
+    const uint32_t grid = (uint32_t)(c.each ? a.n * c.each : (int64_t)c.series * c.slabs);
     const bool one = WIDE && c.one && (!BACK || MODE == kHeld);
     const int keep = one ? (BACK ? kOneBack : kOne) : !BACK ? kSums : MODE == kHeld ? kSumsBack : kChunkBack;
     const int lds = (int)scratch_floats(NT, Pack<DT, WIDE>::kN, c.cols, c.rows, c.groups, keep) * 4;
@@ -1307,6 +1308,18 @@ void run_held(const NormArgs &a, const Cut &c, hipStream_t s) {
     }
 }
 
+// The call's series from i on, as many as a launch takes.
+template <bool BACK>
+NormArgs part_of(NormArgs a, const Cut &c, int64_t i) {
+    a.n = (int32_t)std::min<int64_t>(c.launch, a.n - i);
+    for (View *x : {&a.x, &a.dy, &a.out})
+        if (x->p) x->p += i * x->ss;
+    if (a.lengths) a.lengths += i;
+    a.mean += i * a.G, a.rstd += i * a.G;
+    if (BACK) a.sums += i * c.chunks * 2 * a.C;   // several launches: a row of sums a chunk
+    return a;
+}
+
 template <int DT, bool BACK>
 void run(const NormArgs &a, const Cut &c, hipStream_t s) {
     constexpr Size z = BACK ? kBackChunk : kChunk;
@@ -1324,13 +1337,16 @@ void run(const NormArgs &a, const Cut &c, hipStream_t s) {
 }
 
 template <bool BACK>
-void run_type(int32_t dtype, const NormArgs &a, const Cut &c, hipStream_t s) {
-    if (dtype == ROCKET_FLOAT32)
-        run<ROCKET_FLOAT32, BACK>(a, c, s);
-    else if (dtype == ROCKET_BFLOAT16)
-        run<ROCKET_BFLOAT16, BACK>(a, c, s);
-    else
-        run<ROCKET_FLOAT16, BACK>(a, c, s);
+void run_type(int32_t dtype, const NormArgs &call, const Cut &c, hipStream_t s) {
+    for (int64_t i = 0; i < call.n; i += c.launch) {
+        const NormArgs a = part_of<BACK>(call, c, i);
+        if (dtype == ROCKET_FLOAT32)
+            run<ROCKET_FLOAT32, BACK>(a, c, s);
+        else if (dtype == ROCKET_BFLOAT16)
+            run<ROCKET_BFLOAT16, BACK>(a, c, s);
+        else
+            run<ROCKET_FLOAT16, BACK>(a, c, s);
+    }
 }
 
 View view(const rocket_sequence *q, int size) {
