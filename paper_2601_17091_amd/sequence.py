@@ -15,7 +15,9 @@ Statistics, weights, states and their gradients are float32 and contiguous.
     dropout_backward(dy, p, seed, call)     -> dx
 
 The backward passes are calls of their own: nothing here records itself for
-torch's autograd (examples/window_head.py wraps them for it).
+torch's autograd (examples/window_head.py wraps them for it).  Where autograd
+records, operands that require gradients are refused, since their gradients
+would be lost: call under torch.no_grad(), or in a torch.autograd.Function.
 
 Every call is asynchronous on `stream` (default: torch's current stream); what
 it returns is allocated for that stream.  An operand that belongs to another
@@ -33,13 +35,12 @@ from .rocket import CSequence, CSequenceShape
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 EVERY = 128   # steps between the states a recurrence keeps (ROCKET_RECURRENCE_EVERY)
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-_byref, _empty, _f32 = ctypes.byref, torch.empty, torch.float32
+_byref, _empty, _f32, _recording = ctypes.byref, torch.empty, torch.float32, torch.is_grad_enabled
 
 
 def _dense(x):
     """A contiguous tensor of x's shape and type (the quickest way to one)."""
     return torch.empty_like(x, memory_format=torch.contiguous_format)
-
 
 
 # The current GPU and the handle of its current stream; torch.cuda's own
@@ -68,6 +69,15 @@ def _like(t, x, name: str):
         raise TypeError("%s must be a torch tensor on the GPU" % name)
     if t.dtype != x.dtype or t.shape != x.shape or t.get_device() != x.get_device():
         raise ValueError("%s must have the shape, type and device of the call's first sequence" % name)
+
+
+def _unrecorded(*operands):
+    """Refuses operands whose gradients autograd would miss."""
+    if _recording():
+        for t in operands:
+            if t is not None and t.requires_grad:
+                raise ValueError("an operand requires gradients, which this call does not record: call it under "
+                                 "torch.no_grad() or in a torch.autograd.Function")
 
 
 def _sequence(t, name: str) -> CSequence:
@@ -136,10 +146,11 @@ def group_norm(x, groups: int, weight=None, bias=None, *, eps: float = 1e-5, act
     shape, act = _shape(x, lengths, "x"), _activation(activation)
     n, _, channels = x.shape
     w, b = _floats(weight, (channels,), x, "weight"), _floats(bias, (channels,), x, "bias")
+    if out is not None:
+        _like(out, x, "out")
+    _unrecorded(x, weight, bias, out)
     if out is None:
         out = _dense(x)
-    else:
-        _like(out, x, "out")
     size = _norm_workspace(lib, shape, groups, 0)
     mean = _empty(n, groups, dtype=_f32, device=x.device)
     rstd = _dense(mean)
@@ -168,10 +179,11 @@ def group_norm_backward(dy, x, groups: int, mean, rstd, weight=None, bias=None, 
         raise TypeError("mean and rstd must be torch tensors on the GPU")
     size = _norm_workspace(lib, shape, groups, 1)
     m, r = _floats(mean, (n, groups), x, "mean"), _floats(rstd, (n, groups), x, "rstd")
+    if out is not None:
+        _like(out, x, "out")
+    _unrecorded(dy, x, mean, rstd, weight, bias, out)
     if out is None:
         out = _dense(x)
-    else:
-        _like(out, x, "out")
     dweight = _empty(channels, dtype=_f32, device=x.device)
     dbias = _dense(dweight)
     work, at = _workspace(size, x.device)
@@ -206,10 +218,11 @@ def recurrence(v, f, o=None, *, h0=None, lengths=None, keep_states: bool = False
         _like(o, v, "o")
     n, steps, channels = v.shape
     first = _floats(h0, (n, channels), v, "h0")
+    if out is not None:
+        _like(out, v, "out")
+    _unrecorded(v, f, o, h0, out)
     if out is None:
         out = _dense(v)
-    else:
-        _like(out, v, "out")
     size = _recurrence_workspace(lib, shape)
     h_last = _empty(n, channels, dtype=_f32, device=v.device)
     states = _empty(n, -(-steps // EVERY), channels, dtype=_f32, device=v.device) if keep_states else None
@@ -248,6 +261,7 @@ def recurrence_backward(dy, v, f, states, o=None, *, dh_last=None, lengths=None,
     else:
         for t in out:
             _like(t, v, "out")
+    _unrecorded(dy, v, f, states, o, dh_last, *out)
     size = _recurrence_workspace(lib, shape)
     dh0 = _empty(n, channels, dtype=_f32, device=v.device)
     work, at = _workspace(size, v.device)
@@ -286,13 +300,15 @@ def recurrence_step(v, f, h, o=None, *, h_out=None, out=None, stream=None):
     if h is None:
         raise TypeError("h must be a torch tensor on the GPU")
     at_h = _floats(h, v.shape, v, "h")
+    if out is not None:
+        _like(out, v, "out")
+    at_out = _floats(h_out, v.shape, v, "h_out")
+    _unrecorded(v, f, h, o, h_out, out)
     if out is None:
         out = _dense(v)
-    else:
-        _like(out, v, "out")
     if h_out is None:
         h_out = _dense(h)
-    at_out = _floats(h_out, v.shape, v, "h_out")
+        at_out = h_out.data_ptr()
     n, channels = v.shape
     status = lib.rocket_recurrence_step(n, channels, code, *_matrix(v, "v"), *_matrix(f, "f"), *_matrix(o, "o"), at_h,
                                         at_out, *_matrix(out, "out"), _stream(v.get_device()))
@@ -331,10 +347,11 @@ def dropout(x, p: float, seed: int, call: int = 0, *, residual=None, out=None, s
     code = _dtype(x, "x")
     if residual is not None:
         _like(residual, x, "residual")
+    if out is not None:
+        _like(out, x, "out")
+    _unrecorded(x, residual, out)
     if out is None:
         out = _dense(x)
-    else:
-        _like(out, x, "out")
     vx, vy = _rows(x, "x"), _rows(out, "out")
     vr = (None, 1, 0, 0) if residual is None else _rows(residual, "residual")
     rows, cols = max(vx[1], vr[1], vy[1]), x.numel()
