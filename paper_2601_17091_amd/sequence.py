@@ -71,6 +71,12 @@ def _like(t, x, name: str):
         raise ValueError("%s must have the shape, type and device of the call's first sequence" % name)
 
 
+def _written(*tensors):
+    """Tells autograd that these tensors of the caller's were written: what it
+    saved of them before is no longer what it was."""
+    torch.autograd.graph.increment_version(tensors)
+
+
 def _unrecorded(*operands):
     """Refuses operands whose gradients autograd would miss."""
     if _recording():
@@ -149,6 +155,7 @@ def group_norm(x, groups: int, weight=None, bias=None, *, eps: float = 1e-5, act
     if out is not None:
         _like(out, x, "out")
     _unrecorded(x, weight, bias, out)
+    given = out
     if out is None:
         out = _dense(x)
     size = _norm_workspace(lib, shape, groups, 0)
@@ -159,6 +166,8 @@ def group_norm(x, groups: int, weight=None, bias=None, *, eps: float = 1e-5, act
         _byref(shape), groups, _byref(_sequence(x, "x")), w, b, eps, act, _byref(_sequence(out, "out")),
         mean.data_ptr(), rstd.data_ptr(), at, size, _stream(x.get_device()))
     rocket._check(status, "rocket_group_norm_forward")
+    if given is not None:
+        _written(given)
     return out, mean, rstd
 
 
@@ -182,6 +191,7 @@ def group_norm_backward(dy, x, groups: int, mean, rstd, weight=None, bias=None, 
     if out is not None:
         _like(out, x, "out")
     _unrecorded(dy, x, mean, rstd, weight, bias, out)
+    given = out
     if out is None:
         out = _dense(x)
     dweight = _empty(channels, dtype=_f32, device=x.device)
@@ -191,6 +201,8 @@ def group_norm_backward(dy, x, groups: int, mean, rstd, weight=None, bias=None, 
         _byref(shape), groups, _byref(_sequence(dy, "dy")), _byref(_sequence(x, "x")), w, b, act, m, r,
         _byref(_sequence(out, "out")), dweight.data_ptr(), dbias.data_ptr(), at, size, _stream(x.get_device()))
     rocket._check(status, "rocket_group_norm_backward")
+    if given is not None:
+        _written(given)
     return out, dweight, dbias
 
 
@@ -221,6 +233,7 @@ def recurrence(v, f, o=None, *, h0=None, lengths=None, keep_states: bool = False
     if out is not None:
         _like(out, v, "out")
     _unrecorded(v, f, o, h0, out)
+    given = out
     if out is None:
         out = _dense(v)
     size = _recurrence_workspace(lib, shape)
@@ -232,6 +245,8 @@ def recurrence(v, f, o=None, *, h0=None, lengths=None, keep_states: bool = False
         _byref(_sequence(out, "out")), h_last.data_ptr(), None if states is None else states.data_ptr(), at, size,
         _stream(v.get_device()))
     rocket._check(status, "rocket_recurrence_forward")
+    if given is not None:
+        _written(given)
     return out, h_last, states
 
 
@@ -254,6 +269,7 @@ def recurrence_backward(dy, v, f, states, o=None, *, dh_last=None, lengths=None,
     kept = _floats(states, (n, -(-steps // EVERY), channels), v, "states")
     last = _floats(dh_last, (n, channels), v, "dh_last")
     wanted = 2 if o is None else 3
+    given = out
     if out is None:
         out = [_dense(v) for _ in range(wanted)]
     elif len(out) != wanted:
@@ -271,6 +287,8 @@ def recurrence_backward(dy, v, f, states, o=None, *, dh_last=None, lengths=None,
         _optional(o, "o"), kept, last, _byref(_sequence(out[0], "out")), _byref(_sequence(out[1], "out")),
         _optional(do, "out"), dh0.data_ptr(), at, size, _stream(v.get_device()))
     rocket._check(status, "rocket_recurrence_backward")
+    if given is not None:
+        _written(*given)
     return out[0], out[1], do, dh0
 
 
@@ -304,6 +322,7 @@ def recurrence_step(v, f, h, o=None, *, h_out=None, out=None, stream=None):
         _like(out, v, "out")
     at_out = _floats(h_out, v.shape, v, "h_out")
     _unrecorded(v, f, h, o, h_out, out)
+    given = [t for t in (out, h_out) if t is not None]
     if out is None:
         out = _dense(v)
     if h_out is None:
@@ -313,6 +332,8 @@ def recurrence_step(v, f, h, o=None, *, h_out=None, out=None, stream=None):
     status = lib.rocket_recurrence_step(n, channels, code, *_matrix(v, "v"), *_matrix(f, "f"), *_matrix(o, "o"), at_h,
                                         at_out, *_matrix(out, "out"), _stream(v.get_device()))
     rocket._check(status, "rocket_recurrence_step")
+    if given:
+        _written(*given)
     return out, h_out
 
 
@@ -350,6 +371,7 @@ def dropout(x, p: float, seed: int, call: int = 0, *, residual=None, out=None, s
     if out is not None:
         _like(out, x, "out")
     _unrecorded(x, residual, out)
+    given = out
     if out is None:
         out = _dense(x)
     vx, vy = _rows(x, "x"), _rows(out, "out")
@@ -361,6 +383,8 @@ def dropout(x, p: float, seed: int, call: int = 0, *, residual=None, out=None, s
     status = lib.rocket_dropout(vx[0], vr[0], vy[0], rows, cols, vx[3], vr[3], vy[3], code, p, seed & (2 ** 64 - 1),
                                 call & (2 ** 64 - 1), _stream(x.get_device()))
     rocket._check(status, "rocket_dropout")
+    if given is not None:
+        _written(given)
     return out
 
 

@@ -44,3 +44,27 @@ def test_outputs_that_require_gradients_are_refused(env):  # noqa: F811
                  lambda: seq.recurrence_step(h, h, h, out=leaf_h), lambda: seq.recurrence_step(h, h, h, h_out=leaf_h)):
         with pytest.raises(ValueError, match="requires gradients"):
             call()
+
+
+def test_outputs_over_saved_tensors_are_noticed(env):  # noqa: F811
+    """What autograd saved and a call wrote over is an error in the backward
+    pass, as after torch's own operations in place."""
+    torch, seq = env
+    x, h = torch.randn(2, 6, 8, device="cuda"), torch.randn(2, 8, device="cuda")
+    m, states = torch.randn(2, 4, device="cuda"), torch.randn(2, 1, 8, device="cuda")
+    for like, call in ((x, lambda t: seq.group_norm(t, 4, out=t)), (x, lambda t: seq.recurrence(t, x, out=t)),
+                       (x, lambda t: seq.group_norm_backward(t, x, 4, m, m, out=t)),
+                       (x, lambda t: seq.recurrence_backward(x, x, x, states, out=[x.clone(), t])),
+                       (h, lambda t: seq.recurrence_step(h, h, t, h_out=t)),
+                       (h, lambda t: seq.recurrence_step(t, h, h, out=t)),
+                       (x, lambda t: seq.dropout(t, 0.5, 1, out=t)),
+                       (x, lambda t: seq.dropout_backward(t, 0.5, 1, out=t))):
+        saved = like.clone()
+        w = torch.ones_like(like, requires_grad=True)
+        loss = (saved * w).sum()
+        call(saved)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    with torch.inference_mode():   # such tensors keep no versions
+        t = x.clone()
+        seq.group_norm(t, 4, out=t)
