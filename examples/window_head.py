@@ -35,7 +35,7 @@ class GroupNorm(torch.autograd.Function):
     def backward(ctx, dy):
         x, mean, rstd, weight, bias = ctx.saved_tensors
         groups, activation = ctx.kind
-        dx, dweight, dbias = sequence.group_norm_backward(dy, x, groups, mean, rstd, weight, bias,
+        dx, dweight, dbias = sequence.group_norm_backward(dy.contiguous(), x, groups, mean, rstd, weight, bias,
                                                           activation=activation)
         return dx, dweight, dbias, None, None
 

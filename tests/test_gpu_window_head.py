@@ -70,3 +70,24 @@ def test_window_head_gradients_against_plain_torch():
         scale = float(t.grad.abs().max())
         # fp32 products of 60 and sums over 45 rows: about 1e-6 of the largest
         assert float((got[k] - t.grad).abs().max()) < 2e-5 * scale + 1e-7, k
+
+
+def test_wrappers_take_gradients_of_any_strides():
+    """A sum's gradient is one number for every element (strides of 0)."""
+    import torch
+
+    sys.path.insert(0, os.path.join(ROOT, "examples"))
+    try:
+        import window_head
+    finally:
+        sys.path.pop(0)
+    n, T, C = 3, 7, 12
+    x, p, r = (torch.randn(n, T, c, device="cuda", requires_grad=True) for c in (C, 3 * C, C))
+    w, b = (torch.randn(C, device="cuda", requires_grad=True) for _ in range(2))
+    lengths = torch.tensor([7, 0, 3], dtype=torch.int32, device="cuda")
+    for call, inputs in ((lambda: window_head.GroupNorm.apply(x, w, b, 4, "silu"), (x, w, b)),
+                         (lambda: window_head.Recurrence.apply(p, lengths), (p,)),
+                         (lambda: window_head.Dropout.apply(x, r, 0.5, 1, 2), (x, r))):
+        got = torch.autograd.grad(call().sum(), inputs)
+        want = torch.autograd.grad(call(), inputs, torch.ones(n, T, C, device="cuda"))
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
