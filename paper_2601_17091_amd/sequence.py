@@ -135,6 +135,8 @@ def _workspace(size: int, device):
 
 
 def _norm_workspace(lib, shape, groups: int, backward: int) -> int:
+    if not -(1 << 31) <= groups < 1 << 31:   # ctypes would take it modulo 2^32
+        raise ValueError("groups must divide the channels")
     size = ctypes.c_int64()
     rocket._check(lib.rocket_group_norm_workspace(_byref(shape), groups, backward, _byref(size)),
                   "rocket_group_norm_workspace")
