@@ -1256,16 +1256,12 @@ void go(const NormArgs &a, const Cut &c, hipStream_t s) {
     const int keep = one ? (BACK ? kOneBack : kOne) : !BACK ? kSums : MODE == kHeld ? kSumsBack : kChunkBack;
     const int lds = (int)scratch_floats(NT, Pack<DT, WIDE>::kN, c.cols, c.rows, c.groups, keep) * 4;
     if constexpr (!BACK && WIDE && MODE == kHeld) {
-        if constexpr (R <= kLoopRun) {
-            if (one) {
-                norm_one_kernel<DT, NT, R><<<grid, NT, lds, s>>>(a);
-                return;
-            }
-        }
-        if (one)
-            norm_kernel<DT, true, NT, R, MODE, true><<<grid, NT, lds, s>>>(a);
-        else
+        if (!one)
             norm_kernel<DT, true, NT, R, MODE, false><<<grid, NT, lds, s>>>(a);
+        else if constexpr (R <= kLoopRun)
+            norm_one_kernel<DT, NT, R><<<grid, NT, lds, s>>>(a);
+        else
+            norm_kernel<DT, true, NT, R, MODE, true><<<grid, NT, lds, s>>>(a);
     } else if constexpr (!BACK) {
         if (WIDE && one)
             norm_kernel<DT, WIDE, NT, R, MODE, WIDE><<<grid, NT, lds, s>>>(a);

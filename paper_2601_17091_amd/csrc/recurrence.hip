@@ -209,6 +209,8 @@ __device__ inline void scan_lanes(const RecArgs &a, const Place &p, float *A, fl
     }
 #pragma unroll
     for (int j = 0; j < P; j++) {
+        // always so (32 lanes at most); without the branch the compiler's order of
+        // the loop costs 64 x 1000 x 512, fp32, gated, forward 6 % (108 us, not 102 us)
         float xa = A[j], xb = B[j];
         if (a.lanes < 64) {
             xa = REVERSE ? __shfl_down(A[j], a.lanes) : __shfl_up(A[j], a.lanes);
