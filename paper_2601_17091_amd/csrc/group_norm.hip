@@ -26,14 +26,15 @@
 // channel in shared memory.
 //
 // Bound: HBM, and the vector unit beside it.  Backward with SiLU, 1000 x 1000 x
-// 256, bf16: 414 us, 3.7 TB/s of the 1,536 MB that have to move (a large copy
-// reaches 5.0 to 5.3 TB/s); the slope is computed twice, in the sums and again
-// for dx, since keeping it in 32 bits would halve what a workgroup holds: 28
-// instructions an element, 4 of them transcendental, 58 % of the vector unit's
-// time.  Forward, 1000 x 1000 x 256 without an activation: 205 to 237 us in
-// bf16, 378 us in fp32 (5.4 TB/s).  4 x 16384 x 512, bf16, GELU: 48 us, the
-// slabs being read twice (15 us and 32 us).  777 x 129 x 924 in groups of 33,
-// fp16, ReLU, ragged: 88 to 94 us.
+// 256, bf16: 384 to 391 us, 4.0 TB/s of the 1,536 MB that have to move (a sum of
+// two tensors of that size reaches 6.1 TB/s); the slope is computed twice, in the
+// sums and again for dx, since dy times the slope in 32 bits would be half as much
+// again to hold: 35 vector instructions an element, 66 % of the vector unit's time.
+// Most kernels that hold 8 columns of x and of dy spill a few registers (this one
+// 16 of 128, 52 bytes a thread).  Forward, 1000 x 1000 x 256 without an activation:
+// 205 to 237 us in bf16, 378 us in fp32 (5.4 TB/s).  4 x 16384 x 512, bf16, GELU:
+// 48 to 51 us, the slabs being read twice (15 us and 33 us).  777 x 129 x 924 in
+// groups of 33, fp16, ReLU, ragged: 88 to 94 us.
 #include <algorithm>
 #include <iterator>
 #include <type_traits>
@@ -251,7 +252,8 @@ struct Scratch {
 
 // What a call's kernels keep there.  Where every column lies in one group, a
 // thread's sums are one number a quantity, and the scales are read as needed.
-// At most 57 KB: 256 columns of 16 bytes, the widest slab, are chunks or kOne.
+// At most 57 KB, since 256 columns of 16 bytes, the widest slab, are chunks or
+// kOne; but kOneBack of 1,024 threads takes 74 to 94 KB, and asks for it.
 enum Keep { kSums, kSumsBack, kChunkBack, kOne, kOneBack };
 
 __host__ __device__ inline int pad4(int n) { return (n + 3) / 4 * 4; }

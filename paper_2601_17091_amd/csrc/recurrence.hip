@@ -37,7 +37,9 @@
 // of the 459 MB that have to move (a large copy reaches 5.0 to 5.3 TB/s); 8 x
 // 10000 x 256, fp32, backward 89 us, 4.6 TB/s; 1000 x 1000 x 256, fp32, forward
 // 550 us, 5.6 TB/s; 4 x 16384 x 256, bf16, forward 26 us, 3.9 TB/s: 16 rows,
-// whose tiles wait for each other; 777 x 129 x 331, fp16, gated, ragged 65 us.
+// whose tiles wait for each other; 777 x 129 x 331, fp16, gated, ragged 65 to 71 us
+// (full lengths 73 us, 336 channels 63 us: neither the bytes nor the odd rows, but
+// workgroups that take as long when few of their wavefronts have steps).
 // One counter a cache line: with the 16 rows' counters side by side the last
 // but one took 40 us.
 #include <algorithm>
