@@ -93,7 +93,7 @@ struct Pack {
 #pragma unroll
         for (int k = 0; k < N / Elem<DT>::kPerWord; k++) {
             uint32_t w;
-            if (DT == ROCKET_FLOAT16)
+            if constexpr (DT == ROCKET_FLOAT16)
                 asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(w) : "v"(f[2 * k]), "v"(f[2 * k + 1]));
             else
                 w = Elem<DT>::put(f + k * Elem<DT>::kPerWord);
