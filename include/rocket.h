@@ -705,6 +705,141 @@ rocket_status rocket_dropout(const void *x, const void *residual, void *y, int64
                              int64_t x_stride, int64_t residual_stride, int64_t y_stride, int32_t dtype,
                              double p, uint64_t seed, uint64_t call, void *hip_stream);
 
+/*
+ * RMS norm of rows, with a residual's addition: row (i, t) of C channels,
+ *     s = x + residual, rounded to the type,  k = 1 / sqrt(sum s^2 / C + eps)
+ *     y = s k weight_c
+ *   residual, total  both given or both NULL; total takes s (without them s is
+ *                    x as it stands).  What is normalised is s as it is stored,
+ *                    so that the backward pass sees what this one saw.
+ *   weight  DEVICE fp32 [channels], or NULL: 1
+ *   eps     finite, >= 0
+ *   rstd    DEVICE fp32 [n, steps]: k, 0 for steps past a series' length
+ * The sum of squares has to be finite in fp32 (values below 2^63 / sqrt C are).
+ * y may be x or residual, total may be the other one of them.
+ * Errors: ROCKET_ERR_INVALID_ARG (a NULL pointer, a shape, view, stride, type or
+ *         eps outside the above, one of residual and total alone); ROCKET_ERR_HIP.
+ */
+rocket_status rocket_rms_norm_forward(const rocket_sequence_shape *shape, const rocket_sequence *x,
+                                      const rocket_sequence *residual, const float *weight, float eps,
+                                      const rocket_sequence *y, const rocket_sequence *total, float *rstd,
+                                      void *hip_stream);
+
+/*
+ * 8-bit rows, what rocket_linear_bytes reads: row (i, t) of a sequence as
+ *     a = max |v_c|,  q_c = v_c 127 / a to the nearest whole number (ties to even),
+ *     scale = a / 127,  v_c stands for q_c scale
+ *   q      DEVICE int8 [n, steps, P], P = channels rounded up to a multiple of
+ *          ROCKET_ROWS8_PAD, the columns past the channels 0; 16-byte aligned
+ *   scale  DEVICE fp32 [n, steps]
+ * A row that holds a NaN or an infinity has the scale NaN and zeros; a row whose a is
+ * below 2^-100, and a step past a series' length, the scale 0 and zeros.
+ */
+#define ROCKET_ROWS8_PAD 64
+
+/*
+ * rocket_rms_norm_forward with the output as 8-bit rows: v = s weight, and scale
+ * is k a / 127.  Errors as there (q, scale NULL or not aligned too).
+ */
+rocket_status rocket_rms_norm_bytes_forward(const rocket_sequence_shape *shape, const rocket_sequence *x,
+                                       const rocket_sequence *residual, const float *weight, float eps,
+                                       int8_t *q, float *scale, const rocket_sequence *total, float *rstd,
+                                       void *hip_stream);
+
+/* 8-bit rows of x as it stands (weights: one series whose steps are the rows).
+ * Errors as rocket_rms_norm_bytes_forward. */
+rocket_status rocket_quantize_rows(const rocket_sequence_shape *shape, const rocket_sequence *x, int8_t *q,
+                                   float *scale, void *hip_stream);
+
+/*
+ * The gradient of either norm (through 8 bits as if they had not rounded): from
+ * dy, s (the forward pass's total, or x), k and the gradient of total that comes
+ * in beside (dtotal, or NULL),
+ *     g = dy weight_c,  dx = k (g - s k mean(g s k)) + dtotal,  dweight_c = sum dy s k
+ *   dx       the gradient of x, and of the residual
+ *   dweight  DEVICE fp32 [channels], or NULL: not wanted
+ * dx may be dy, total or dtotal.  The workspace is needed for dweight only.
+ * Errors as rocket_rms_norm_forward (a workspace too small too).
+ */
+rocket_status rocket_rms_norm_backward(const rocket_sequence_shape *shape, const rocket_sequence *dy,
+                                       const rocket_sequence *total, const float *weight, const float *rstd,
+                                       const rocket_sequence *dtotal, const rocket_sequence *dx, float *dweight,
+                                       void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/* Workspace of the backward pass for this shape.  Host only.
+ * Errors: ROCKET_ERR_INVALID_ARG (bytes NULL, a shape outside the above). */
+rocket_status rocket_rms_norm_workspace(const rocket_sequence_shape *shape, int64_t *bytes);
+
+/*
+ * Product of 8-bit rows with 8-bit weights:
+ *     y[i, t, m] = scale[i, t] weight_scale[m] (sum over k of q[i, t, k] weight[m, k]) + bias[m]
+ *   shape         that of y; channels: the weights' rows
+ *   columns       of q and weight: a positive multiple of ROCKET_ROWS8_PAD, at most
+ *                 131,072 (the sum is of whole numbers and exact in 32 bits)
+ *   q, scale      DEVICE int8 [n, steps, columns], fp32 [n, steps]: 8-bit rows
+ *   weight, weight_scale  DEVICE int8 [channels, columns], fp32 [channels]:
+ *                 8-bit rows of the weights
+ *   bias          DEVICE fp32 [channels], or NULL: 0
+ * q and weight are 16-byte aligned.  scale of steps past a series' length is not
+ * looked at; y there is 0.
+ * Errors: ROCKET_ERR_INVALID_ARG (as above, or a workspace too small); ROCKET_ERR_HIP.
+ */
+rocket_status rocket_linear_bytes(const rocket_sequence_shape *shape, int64_t columns, const int8_t *q,
+                             const float *scale, const int8_t *weight, const float *weight_scale,
+                             const float *bias, const rocket_sequence *y, void *workspace,
+                             int64_t workspace_bytes, void *hip_stream);
+
+/* Its workspace for this shape of y and these columns.  Host only.
+ * Errors: ROCKET_ERR_INVALID_ARG (bytes NULL, a shape or columns outside the above). */
+rocket_status rocket_linear_bytes_workspace(const rocket_sequence_shape *shape, int64_t columns, int64_t *bytes);
+
+/*
+ * Checkpoint in 8 bits: a sequence kept for the backward pass.  All series'
+ * steps in a row are rows; block b holds the rows R b .. R b + R - 1
+ * (R = ROCKET_CHECKPOINT_ROWS), and a channel of a block has a scale of its own,
+ * since channels (features) differ in level:
+ *     a = max |x_c| over the block's rows,  scale[b, c] = a / 127
+ *     q[b, c, r - R b] = x[r, c] 127 / a to the nearest whole number (ties to even)
+ *   q      DEVICE int8 [ceil(n steps / R), channels, R], 16-byte aligned
+ *   scale  DEVICE fp32 [ceil(n steps / R), channels]
+ * Rows past the last, and steps past a series' length, are zeros.  A channel of
+ * a block that holds a NaN or an infinity has the scale NaN and zeros, one
+ * whose a is below 2^-100 the scale 0.
+ * Errors: ROCKET_ERR_INVALID_ARG (as above); ROCKET_ERR_HIP.
+ */
+#define ROCKET_CHECKPOINT_ROWS 128
+rocket_status rocket_checkpoint(const rocket_sequence_shape *shape, const rocket_sequence *x, int8_t *q,
+                                float *scale, void *hip_stream);
+
+/* Its inverse: x = q scale, rounded to shape's type (which need not be the type
+ * that was kept); 0 at steps past a series' length.  Errors as rocket_checkpoint. */
+rocket_status rocket_restore(const rocket_sequence_shape *shape, const int8_t *q, const float *scale,
+                             const rocket_sequence *x, void *hip_stream);
+
+/*
+ * Gradient of the weights and bias of y = x W^T + b from a checkpoint of x,
+ * which is read as it is kept:
+ *     dweight[m, c] = sum over rows r of dy[r, m] q[b, c, r - R b] scale[b, c],  b = r / R
+ *     dbias[m] = sum over rows of dy[r, m]
+ *   shape     that of dy (channels: the weights' rows)
+ *   channels  of the checkpoint; shape's channels times these at most 2^34
+ *   dweight   DEVICE fp32 [shape's channels, channels]
+ *   dbias     DEVICE fp32 [shape's channels], or NULL: not wanted
+ * No product is rounded before the sums, which are fp32 (dy of the type fp32
+ * enters as the exact sum of three parts, whose smallest counts from 2^-126 on).
+ * A sum of no rows is 0.
+ * Errors: ROCKET_ERR_INVALID_ARG (as above, or a workspace too small); ROCKET_ERR_HIP.
+ */
+rocket_status rocket_linear_weight_gradient(const rocket_sequence_shape *shape, int64_t channels,
+                                            const rocket_sequence *dy, const int8_t *q, const float *scale,
+                                            float *dweight, float *dbias, void *workspace,
+                                            int64_t workspace_bytes, void *hip_stream);
+
+/* Its workspace for this shape of dy and these channels.  Host only.
+ * Errors: ROCKET_ERR_INVALID_ARG (bytes NULL, a shape or channels outside the above). */
+rocket_status rocket_linear_weight_gradient_workspace(const rocket_sequence_shape *shape, int64_t channels,
+                                                      int64_t *bytes);
+
 /* Static, human-readable name of a status code ("unknown status" otherwise). */
 const char *rocket_status_string(rocket_status s);
 

@@ -19,10 +19,12 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "librocket.so")
 CHECKED_LIB = os.path.join(HERE, "librocket_checked.so")
 SOURCES = ["transform.hip", "split.hip", "plan.cpp", "plan_split.cpp", "generate.cpp", "minirocket.cpp",
-           "group_norm.hip", "recurrence.hip", "dropout.hip"]
+           "group_norm.hip", "recurrence.hip", "dropout.hip", "rms_norm.hip", "linear8.hip", "checkpoint.hip",
+           "weight_gradient.hip"]
 # sources whose device code keeps IEEE NaN semantics: their operands may hold
 # NaN (the transform's series are finite)
-NAN_SOURCES = ("group_norm.hip", "recurrence.hip", "dropout.hip")
+NAN_SOURCES = ("group_norm.hip", "recurrence.hip", "dropout.hip", "rms_norm.hip", "linear8.hip", "checkpoint.hip",
+               "weight_gradient.hip")
 ARCH = "gfx950"
 
 

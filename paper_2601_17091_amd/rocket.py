@@ -65,6 +65,17 @@ EXPORTED = (
     "rocket_recurrence_workspace",
     "rocket_recurrence_step",
     "rocket_dropout",
+    "rocket_rms_norm_forward",
+    "rocket_rms_norm_bytes_forward",
+    "rocket_rms_norm_backward",
+    "rocket_rms_norm_workspace",
+    "rocket_quantize_rows",
+    "rocket_linear_bytes",
+    "rocket_linear_bytes_workspace",
+    "rocket_checkpoint",
+    "rocket_restore",
+    "rocket_linear_weight_gradient",
+    "rocket_linear_weight_gradient_workspace",
 )
 
 
@@ -179,6 +190,17 @@ def _signatures() -> dict:
         "rocket_recurrence_workspace": ([shp, out64], st),
         "rocket_recurrence_step": ([i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp], st),
         "rocket_dropout": ([vp, vp, vp, i64, i64, i64, i64, i64, i32, f64, u64, u64, vp], st),
+        "rocket_rms_norm_forward": ([shp, seq, seq, vp, f32, seq, seq, vp, vp], st),
+        "rocket_rms_norm_bytes_forward": ([shp, seq, seq, vp, f32, vp, vp, seq, vp, vp], st),
+        "rocket_rms_norm_backward": ([shp, seq, seq, vp, vp, seq, seq, vp, vp, i64, vp], st),
+        "rocket_rms_norm_workspace": ([shp, out64], st),
+        "rocket_quantize_rows": ([shp, seq, vp, vp, vp], st),
+        "rocket_linear_bytes": ([shp, i64, vp, vp, vp, vp, vp, seq, vp, i64, vp], st),
+        "rocket_linear_bytes_workspace": ([shp, i64, out64], st),
+        "rocket_checkpoint": ([shp, seq, vp, vp, vp], st),
+        "rocket_restore": ([shp, vp, vp, seq, vp], st),
+        "rocket_linear_weight_gradient": ([shp, i64, seq, vp, vp, vp, vp, vp, i64, vp], st),
+        "rocket_linear_weight_gradient_workspace": ([shp, i64, out64], st),
     }
 
 

@@ -14,6 +14,23 @@ Statistics, weights, states and their gradients are float32 and contiguous.
     dropout(x, p, seed, call)               -> y
     dropout_backward(dy, p, seed, call)     -> dx
 
+and the operators of its linear layers, whose sequences may also be rows
+[rows, channels]:
+
+    rms_norm(x, weight, residual=r)         -> y, total, rstd
+    rms_norm8(x, weight, residual=r)        -> q, scale, total, rstd
+    rms_norm_backward(dy, total, rstd, weight, dtotal=d) -> dx, dweight
+    quantize_rows(x)                        -> q, scale
+    linear8(q, scale, wq, wscale, bias)     -> y
+    checkpoint(x)                           -> q, scale
+    restore(q, scale, leading shape)        -> x
+    linear_weight_gradient(dy, q, scale)    -> dweight, dbias
+
+rms_norm8 and quantize_rows give 8-bit rows (int8 [..., channels padded to a
+multiple of ROWS8_PAD], a scale a row) for linear8, whose weights are 8-bit rows
+too; a checkpoint is int8 [blocks, channels, CHECKPOINT_ROWS] with a scale for
+each channel of a block of rows.
+
 The backward passes are calls of their own: nothing here records itself for
 torch's autograd (examples/window_head.py wraps them for it).  Where autograd
 records, operands that require gradients are refused, since their gradients
@@ -34,6 +51,8 @@ from .rocket import CSequence, CSequenceShape
 
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 EVERY = 128   # steps between the states a recurrence keeps (ROCKET_RECURRENCE_EVERY)
+ROWS8_PAD = 64   # columns of 8-bit rows come in multiples of this
+CHECKPOINT_ROWS = 128   # rows that share a channel's scale in a checkpoint
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _byref, _empty, _f32, _recording = ctypes.byref, torch.empty, torch.float32, torch.is_grad_enabled
 
@@ -394,3 +413,309 @@ def dropout_backward(dy, p: float, seed: int, call: int = 0, *, out=None, stream
     """The gradient of dropout with respect to x: the same map on dy (that of
     the residual is dy itself)."""
     return dropout(dy, p, seed, call, out=out, stream=stream)
+
+
+def _rows_shape(x, lengths, name: str) -> CSequenceShape:
+    """The shape of sequences [n, steps, channels] or of rows [rows, channels]."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        return _shape(x, lengths, name)
+    code = _dtype(x, name)
+    if lengths is not None:
+        raise ValueError("lengths come with sequences [n, steps, channels]")
+    return CSequenceShape(1, x.shape[0], x.shape[1], code, None)
+
+
+def _rows_view(t, name: str) -> CSequence:
+    s = t.stride()
+    if s[-1] != 1 and t.shape[-1] > 1:
+        raise ValueError("%s must have contiguous channels" % name)
+    return CSequence(t.data_ptr(), s[0], s[1]) if len(s) == 3 else CSequence(t.data_ptr(), 0, s[0])
+
+
+def _optional_rows(t, name: str):
+    return None if t is None else _byref(_rows_view(t, name))
+
+
+def _bytes8(t, like, name: str, shape=None):
+    """The address of a contiguous int8 tensor, of that shape where one is given."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a torch tensor on the GPU" % name)
+    if t.dtype != torch.int8 or not t.is_contiguous() or t.get_device() != _device():
+        raise ValueError("%s must be contiguous int8 on the current GPU" % name)
+    if like is not None and t.get_device() != like.get_device() or shape is not None and t.shape != shape:
+        raise ValueError("%s must be int8 %s on the call's GPU" % (name, shape and list(shape)))
+    return t.data_ptr()
+
+
+def _pad8(channels: int) -> int:
+    return -(-channels // ROWS8_PAD) * ROWS8_PAD
+
+
+def _norm_operands(x, weight, residual, lengths, total_out):
+    """What the two forward passes share: the shape, the weight's address, the
+    residual and where its sum goes."""
+    shape = _rows_shape(x, lengths, "x")
+    w = _floats(weight, x.shape[-1:], x, "weight")
+    if residual is not None:
+        _like(residual, x, "residual")
+    if total_out is not None:
+        if residual is None:
+            raise ValueError("total_out takes the sum with a residual")
+        _like(total_out, x, "total_out")
+    return shape, w
+
+
+def rms_norm(x, weight=None, *, residual=None, eps: float = 1e-5, lengths=None, out=None, total_out=None, stream=None):
+    """rocket_rms_norm_forward: (y, total, rstd [n, steps] or [rows]); total is
+    x + residual as it was normalised (x itself without a residual).  `out` takes
+    y and `total_out` the sum (they may be x and residual, either way round)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rms_norm(x, weight, residual=residual, eps=eps, lengths=lengths, out=out, total_out=total_out)
+    lib = rocket.library()
+    shape, w = _norm_operands(x, weight, residual, lengths, total_out)
+    if out is not None:
+        _like(out, x, "out")
+    _unrecorded(x, weight, residual, out, total_out)
+    given = [t for t in (out, total_out) if t is not None]
+    if out is None:
+        out = _dense(x)
+    total = x if residual is None else _dense(x) if total_out is None else total_out
+    rstd = _empty(x.shape[:-1], dtype=_f32, device=x.device)
+    status = lib.rocket_rms_norm_forward(
+        _byref(shape), _byref(_rows_view(x, "x")), _optional_rows(residual, "residual"), w, eps,
+        _byref(_rows_view(out, "out")), None if residual is None else _byref(_rows_view(total, "total_out")),
+        rstd.data_ptr(), _stream(x.get_device()))
+    rocket._check(status, "rocket_rms_norm_forward")
+    if given:
+        _written(*given)
+    return out, total, rstd
+
+
+def rms_norm8(x, weight=None, *, residual=None, eps: float = 1e-5, lengths=None, total_out=None, stream=None):
+    """rocket_rms_norm_bytes_forward: (q, scale, total, rstd), the normalised rows as
+    8-bit rows for linear8; total and rstd as rms_norm gives them."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rms_norm8(x, weight, residual=residual, eps=eps, lengths=lengths, total_out=total_out)
+    lib = rocket.library()
+    shape, w = _norm_operands(x, weight, residual, lengths, total_out)
+    _unrecorded(x, weight, residual, total_out)
+    total = x if residual is None else _dense(x) if total_out is None else total_out
+    rows = x.shape[:-1]
+    q = _empty(*rows, _pad8(x.shape[-1]), dtype=torch.int8, device=x.device)
+    scale = _empty(rows, dtype=_f32, device=x.device)
+    rstd = _dense(scale)
+    status = lib.rocket_rms_norm_bytes_forward(
+        _byref(shape), _byref(_rows_view(x, "x")), _optional_rows(residual, "residual"), w, eps, q.data_ptr(),
+        scale.data_ptr(), None if residual is None else _byref(_rows_view(total, "total_out")), rstd.data_ptr(),
+        _stream(x.get_device()))
+    rocket._check(status, "rocket_rms_norm_bytes_forward")
+    if total_out is not None:
+        _written(total_out)
+    return q, scale, total, rstd
+
+
+def rms_norm_backward(dy, total, rstd, weight=None, *, dtotal=None, lengths=None, out=None, stream=None):
+    """rocket_rms_norm_backward: (dx, dweight), from the forward pass's total (or
+    x) and rstd; dtotal is the gradient that reaches the sum besides.  dx is the
+    gradient of x and of the residual.  `out` (may be dy, total or dtotal) takes it."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rms_norm_backward(dy, total, rstd, weight, dtotal=dtotal, lengths=lengths, out=out)
+    lib = rocket.library()
+    shape = _rows_shape(total, lengths, "total")
+    _like(dy, total, "dy")
+    if dtotal is not None:
+        _like(dtotal, total, "dtotal")
+    if rstd is None:
+        raise TypeError("rstd must be a torch tensor on the GPU")
+    w, r = _floats(weight, total.shape[-1:], total, "weight"), _floats(rstd, total.shape[:-1], total, "rstd")
+    if out is not None:
+        _like(out, total, "out")
+    _unrecorded(dy, total, rstd, weight, dtotal, out)
+    given = out
+    if out is None:
+        out = _dense(total)
+    size = ctypes.c_int64()
+    rocket._check(lib.rocket_rms_norm_workspace(_byref(shape), _byref(size)), "rocket_rms_norm_workspace")
+    dweight = _empty(total.shape[-1], dtype=_f32, device=total.device)
+    work, at = _workspace(size.value, total.device)
+    status = lib.rocket_rms_norm_backward(
+        _byref(shape), _byref(_rows_view(dy, "dy")), _byref(_rows_view(total, "total")), w, r,
+        _optional_rows(dtotal, "dtotal"), _byref(_rows_view(out, "out")), dweight.data_ptr(), at, size.value,
+        _stream(total.get_device()))
+    rocket._check(status, "rocket_rms_norm_backward")
+    if given is not None:
+        _written(given)
+    return out, dweight
+
+
+def quantize_rows(x, *, lengths=None, stream=None):
+    """rocket_quantize_rows: (q, scale), 8-bit rows of x as it stands, for
+    example of a weight matrix [channels out, channels in]."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return quantize_rows(x, lengths=lengths)
+    lib = rocket.library()
+    shape = _rows_shape(x, lengths, "x")
+    _unrecorded(x)
+    q = _empty(*x.shape[:-1], _pad8(x.shape[-1]), dtype=torch.int8, device=x.device)
+    scale = _empty(x.shape[:-1], dtype=_f32, device=x.device)
+    status = lib.rocket_quantize_rows(_byref(shape), _byref(_rows_view(x, "x")), q.data_ptr(), scale.data_ptr(),
+                                      _stream(x.get_device()))
+    rocket._check(status, "rocket_quantize_rows")
+    return q, scale
+
+
+def _type_code(dtype) -> int:
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise ValueError("dtype must be float32, bfloat16 or float16")
+    return code
+
+
+def _steps_pointer(lengths, leading, like):
+    """The address of lengths for sequences of that leading shape, or None."""
+    if lengths is None:
+        return None
+    if len(leading) != 2:
+        raise ValueError("lengths come with sequences [n, steps, channels]")
+    if not isinstance(lengths, torch.Tensor) or not lengths.is_cuda:
+        raise TypeError("lengths must be a torch tensor on the GPU")
+    if (lengths.dtype != torch.int32 or lengths.shape != leading[:1] or lengths.get_device() != like.get_device()
+            or not lengths.is_contiguous()):
+        raise ValueError("lengths must be contiguous int32 [%d] on the sequences' GPU" % leading[0])
+    return lengths.data_ptr()
+
+
+def _result(out, shape, dtype, like):
+    """`out` checked, or a new tensor."""
+    if out is None:
+        return _empty(shape, dtype=dtype, device=like.device)
+    if not isinstance(out, torch.Tensor) or not out.is_cuda:
+        raise TypeError("out must be a torch tensor on the GPU")
+    if out.shape != shape or out.dtype != dtype or out.get_device() != like.get_device():
+        raise ValueError("out must be %s %s on the call's GPU" % (dtype, list(shape)))
+    return out
+
+
+def linear8(q, scale, wq, wscale, bias=None, *, dtype=None, lengths=None, out=None, stream=None):
+    """rocket_linear_bytes: y [..., channels out] of 8-bit rows q [..., columns] with
+    the weights' 8-bit rows wq [channels out, columns].  dtype: that of y (that of
+    `out`, else bfloat16)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return linear8(q, scale, wq, wscale, bias, dtype=dtype, lengths=lengths, out=out)
+    lib = rocket.library()
+    at_q = _bytes8(q, None, "q")
+    if q.dim() not in (2, 3):
+        raise ValueError("q must be [n, steps, columns] or [rows, columns]")
+    leading, columns = q.shape[:-1], q.shape[-1]
+    if not isinstance(wq, torch.Tensor) or wq.dim() != 2:
+        raise TypeError("wq must be a torch tensor [channels, columns] on the GPU")
+    channels = wq.shape[0]
+    at_w = _bytes8(wq, q, "wq", (channels, columns))
+    if scale is None or wscale is None:
+        raise TypeError("scale and wscale must be torch tensors on the GPU")
+    at_scale, at_wscale = _floats(scale, leading, q, "scale"), _floats(wscale, (channels,), q, "wscale")
+    at_bias = _floats(bias, (channels,), q, "bias")
+    if dtype is None:
+        dtype = torch.bfloat16 if out is None else getattr(out, "dtype", None)
+    code, steps = _type_code(dtype), _steps_pointer(lengths, leading, q)
+    _unrecorded(scale, wscale, bias, out)
+    given = out
+    out = _result(out, (*leading, channels), dtype, q)
+    n, rows = leading if len(leading) == 2 else (1, leading[0])
+    shape = CSequenceShape(n, rows, channels, code, steps)
+    size = ctypes.c_int64()
+    rocket._check(lib.rocket_linear_bytes_workspace(_byref(shape), columns, _byref(size)),
+                  "rocket_linear_bytes_workspace")
+    work, at = _workspace(size.value, q.device)
+    status = lib.rocket_linear_bytes(_byref(shape), columns, at_q, at_scale, at_w, at_wscale, at_bias,
+                                _byref(_rows_view(out, "out")), at, size.value, _stream(q.get_device()))
+    rocket._check(status, "rocket_linear_bytes")
+    if given is not None:
+        _written(given)
+    return out
+
+
+def checkpoint(x, *, lengths=None, stream=None):
+    """rocket_checkpoint: (q [blocks, channels, CHECKPOINT_ROWS], scale [blocks,
+    channels]), x kept in 8 bits for restore or linear_weight_gradient."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return checkpoint(x, lengths=lengths)
+    lib = rocket.library()
+    shape = _rows_shape(x, lengths, "x")
+    _unrecorded(x)
+    blocks, channels = -(-shape.n * shape.steps // CHECKPOINT_ROWS), x.shape[-1]
+    q = _empty(blocks, channels, CHECKPOINT_ROWS, dtype=torch.int8, device=x.device)
+    scale = _empty(blocks, channels, dtype=_f32, device=x.device)
+    status = lib.rocket_checkpoint(_byref(shape), _byref(_rows_view(x, "x")), q.data_ptr(), scale.data_ptr(),
+                                   _stream(x.get_device()))
+    rocket._check(status, "rocket_checkpoint")
+    return q, scale
+
+
+def _kept(q, scale, rows: int):
+    """Addresses of a checkpoint of that many rows, and its channels."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise TypeError("q must be a checkpoint's torch tensor [blocks, channels, %d] on the GPU" % CHECKPOINT_ROWS)
+    blocks, channels = -(-rows // CHECKPOINT_ROWS), q.shape[1]
+    at_q = _bytes8(q, None, "q", (blocks, channels, CHECKPOINT_ROWS))
+    if scale is None:
+        raise TypeError("scale must be a torch tensor on the GPU")
+    return at_q, _floats(scale, (blocks, channels), q, "scale"), channels
+
+
+def restore(q, scale, leading, *, dtype=None, lengths=None, out=None, stream=None):
+    """rocket_restore: what checkpoint kept, [*leading, channels] with leading (n,
+    steps) or (rows,).  dtype: that of the result (that of `out`, else bfloat16)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return restore(q, scale, leading, dtype=dtype, lengths=lengths, out=out)
+    lib = rocket.library()
+    leading = torch.Size(leading)
+    if len(leading) not in (1, 2):
+        raise ValueError("leading must be (n, steps) or (rows,)")
+    n, rows = leading if len(leading) == 2 else (1, leading[0])
+    at_q, at_scale, channels = _kept(q, scale, n * rows)
+    if dtype is None:
+        dtype = torch.bfloat16 if out is None else getattr(out, "dtype", None)
+    code, steps = _type_code(dtype), _steps_pointer(lengths, leading, q)
+    _unrecorded(scale, out)
+    given = out
+    out = _result(out, (*leading, channels), dtype, q)
+    shape = CSequenceShape(n, rows, channels, code, steps)
+    status = lib.rocket_restore(_byref(shape), at_q, at_scale, _byref(_rows_view(out, "out")),
+                                _stream(q.get_device()))
+    rocket._check(status, "rocket_restore")
+    if given is not None:
+        _written(given)
+    return out
+
+
+def linear_weight_gradient(dy, q, scale, *, lengths=None, stream=None):
+    """rocket_linear_weight_gradient: (dweight [channels out, channels in], dbias
+    [channels out]) of y = x W^T + b, from dy and a checkpoint of x."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return linear_weight_gradient(dy, q, scale, lengths=lengths)
+    lib = rocket.library()
+    shape = _rows_shape(dy, lengths, "dy")
+    at_q, at_scale, channels = _kept(q, scale, shape.n * shape.steps)
+    if q.get_device() != dy.get_device():
+        raise ValueError("q must be on dy's GPU")
+    _unrecorded(dy, scale)
+    size = ctypes.c_int64()
+    rocket._check(lib.rocket_linear_weight_gradient_workspace(_byref(shape), channels, _byref(size)),
+                  "rocket_linear_weight_gradient_workspace")
+    dweight = _empty(dy.shape[-1], channels, dtype=_f32, device=dy.device)
+    dbias = _empty(dy.shape[-1], dtype=_f32, device=dy.device)
+    work, at = _workspace(size.value, dy.device)
+    status = lib.rocket_linear_weight_gradient(_byref(shape), channels, _byref(_rows_view(dy, "dy")), at_q, at_scale,
+                                               dweight.data_ptr(), dbias.data_ptr(), at, size.value,
+                                               _stream(dy.get_device()))
+    rocket._check(status, "rocket_linear_weight_gradient")
+    return dweight, dbias
