@@ -835,10 +835,12 @@ rocket_status rocket_linear_weight_gradient(const rocket_sequence_shape *shape, 
                                             float *dweight, float *dbias, void *workspace,
                                             int64_t workspace_bytes, void *hip_stream);
 
-/* Its workspace for this shape of dy and these channels.  Host only.
- * Errors: ROCKET_ERR_INVALID_ARG (bytes NULL, a shape or channels outside the above). */
+/* Its workspace for this shape, these channels and dy's strides and alignment (its
+ * values are not looked at): rows of fp32, of an odd number of channels or of unequal
+ * distances are laid out anew in it.  Host only.
+ * Errors: ROCKET_ERR_INVALID_ARG (bytes NULL, a shape, channels or view outside the above). */
 rocket_status rocket_linear_weight_gradient_workspace(const rocket_sequence_shape *shape, int64_t channels,
-                                                      int64_t *bytes);
+                                                      const rocket_sequence *dy, int64_t *bytes);
 
 /* Static, human-readable name of a status code ("unknown status" otherwise). */
 const char *rocket_status_string(rocket_status s);

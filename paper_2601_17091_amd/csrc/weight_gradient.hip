@@ -9,8 +9,11 @@
 #include <algorithm>
 
 #include "rows.h"
+#include "stage.h"
 
 namespace {
+
+using rocket::Int4;
 
 using rocket::Elem;
 using rocket::kKeepRows;
@@ -141,6 +144,305 @@ __global__ __launch_bounds__(256) void gradient_kernel(GradArgs a) {
         a.dbias[(int64_t)part_of * a.m + m0 + threadIdx.x] = bias;
 }
 
+// ------------------------------------------------------- many rows: staged tiles
+struct StagedArgs {
+    const char *dy;       // rows of 16-bit values at one distance, 4-byte aligned
+    int64_t dy_stride;    // bytes
+    int64_t dy_plane;     // bytes between the parts of fp32 values
+    const uint64_t *live; // a bit for each row, or null: all of them
+    const int8_t *q;
+    const float *scale;
+    float *dweight, *dbias;  // the parts' sums, [parts, m, c] and [parts, tiles along c, m]
+    int64_t rows, blocks, each;
+    int32_t m, c, tiles_m, tiles_c;
+    int32_t width;  // values of a row of dy: m, or m rounded up where it was laid out anew
+};
+
+typedef short Short4 __attribute__((ext_vector_type(4)));
+typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
+typedef const __attribute__((address_space(3))) Words4 *SharedWords;
+typedef _Float16 Half2 __attribute__((ext_vector_type(2)));
+
+// 8 signed bytes as 8 values of the operands' type, exactly.
+template <bool HALF>
+__device__ inline Words4 widen(uint32_t lo, uint32_t hi) {
+    Words4 w;
+    if (HALF) {
+        // 1024 + (q + 128) has q + 128 as its lowest bits
+        const uint32_t u[2] = {lo ^ 0x80808080u, hi ^ 0x80808080u};
+        const Half2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const uint32_t pair = __builtin_amdgcn_perm(0x64646464u, u[k / 2], k % 2 ? 0x04030402u : 0x04010400u);
+            w[k] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(Half2, pair) + off);
+        }
+    } else {
+        // whole numbers below 2^8 leave the lower half of an fp32 value empty
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const uint32_t b = k / 2 ? hi : lo;
+            const float x = (float)(int8_t)(b >> (16 * (k % 2))), y = (float)(int8_t)(b >> (16 * (k % 2) + 8));
+            w[k] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);
+        }
+    }
+    return w;
+}
+
+template <bool HALF>
+__device__ inline float value16(uint32_t w, int j) {
+    return HALF ? Elem<ROCKET_FLOAT16>::get(w, j) : Elem<ROCKET_BFLOAT16>::get(w, j);
+}
+
+// 8 values of one column of shared memory, four rows apart by `LINE` bytes and the
+// next four: what a lane holds of the first operand.
+template <int LINE>
+__device__ inline Words4 turned(rocket::Shared p) {
+    typedef __attribute__((address_space(3))) Short4 *Lds;
+    const Short4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p));
+    const Short4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 4 * LINE));
+    const uint64_t w0 = __builtin_bit_cast(uint64_t, v0), w1 = __builtin_bit_cast(uint64_t, v1);
+    return Words4{(uint32_t)w0, (uint32_t)(w0 >> 32), (uint32_t)w1, (uint32_t)(w1 >> 32)};
+}
+
+// A tile of dW: WM x WC wavefronts, each MT x NT matrices of 32 x 32.  A stage is
+// 64 rows: dy as it lies ([row][m], a row's 16-byte pieces moved by its number so
+// that the transposing reads meet every bank alike) and q ([c][64 rows], moved
+// alike), three stages in shared memory: while one is read, the next is there or
+// on its way and the one after is asked for.
+//
+// The sum is kept in units of the current block's scale: at a block's first stage
+// it is multiplied by (last scale / this scale), so that one set of registers
+// holds it.  Where that quotient leaves 2^-40 .. 2^40 the sum is added to `dweight`
+// and begins anew.
+//
+// PLANES: parts of dy's values, the smallest first.
+template <bool HALF, int PLANES, int MT, int NT, int WM, int WC>
+__global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
+    constexpr int kWaves = WM * WC, kM = 32 * MT * WM, kC = 32 * NT * WC;
+    constexpr int kPieces = kM / 8, kRowsA = 64 / kPieces;           // of a row; rows of a load
+    constexpr int kTurn = kPieces >= 16 ? 3 : kPieces / 4 - 1;       // rows whose pieces are moved differently
+    constexpr int kLoadsA = kM / 8 / kWaves, kLoadsC = kC / 16 / kWaves;
+    constexpr int kBytesA = 64 * kM * 2, kBytesC = kC * 64, kBytesS = kWaves * 256;
+    constexpr int kStage = kBytesA + kBytesC + kBytesS;
+    constexpr int kLoads = kLoadsA + kLoadsC + 1;
+    static_assert(kLoadsA * kWaves * 8 == kM && kLoadsC * kWaves * 16 == kC && NT <= 2, "whole loads");
+    __shared__ __attribute__((aligned(1024))) char shared[3 * kStage];
+    const uint32_t base = rocket::shared_address(shared);
+    const int lane = threadIdx.x % 64, wave = rocket::uniform(threadIdx.x / 64);
+    const int wm = wave % WM, wc = wave / WM;
+    const uint32_t item = rocket::item_of_block(), tiles = a.tiles_m * a.tiles_c;
+    const uint32_t part = item / tiles, tile = item % tiles;
+    const int tile_c = tile % a.tiles_c;
+    const int m0 = tile / a.tiles_c * kM, c0 = tile_c * kC;
+    const int64_t first = part * a.each, last = first + a.each < a.blocks ? first + a.each : a.blocks;
+    const int stages = (int)(last - first) * 2 * PLANES;
+
+    // where this lane's pieces of a stage come from
+    uint32_t from_a[kLoadsA], from_c[kLoadsC];
+    int row_a[kLoadsA];
+#pragma unroll
+    for (int k = 0; k < kLoadsA; k++) {
+        const int row = (wave * kLoadsA + k) * kRowsA + lane / kPieces;
+        const int piece = lane % kPieces ^ (row & kTurn) << 2;
+        row_a[k] = row;
+        from_a[k] = (uint32_t)(row * a.dy_stride) + piece * 16;
+    }
+#pragma unroll
+    for (int k = 0; k < kLoadsC; k++) {
+        const int ch = (wave * kLoadsC + k) * 16 + lane / 4;
+        from_c[k] = ch * kKeepRows + (lane % 4 ^ (ch >> 1 & 3)) * 16;
+    }
+    auto ask = [&](int stage) {
+        const int step = stage / PLANES, plane = PLANES - 1 - stage % PLANES, half = step & 1;
+        const int64_t block = first + step / 2, row0 = block * kKeepRows + half * 64;
+        const bool some = stage < stages;
+        const int64_t left_a = some ? (a.rows - 1 - row0) * a.dy_stride + (a.width - m0) * 2 : 0;
+        const Int4 dy = rocket::buffer_of(a.dy + plane * a.dy_plane + row0 * a.dy_stride + m0 * 2,
+                                          row0 < a.rows ? left_a : 0);
+        const Int4 q = rocket::buffer_of(a.q + (block * a.c + c0) * kKeepRows + half * 64,
+                                         some ? (int64_t)(a.c - c0) * kKeepRows - half * 64 : 0);
+        const Int4 scale = rocket::buffer_of(a.scale + block * a.c + c0, some ? (int64_t)(a.c - c0) * 4 : 0);
+        const uint32_t to = base + stage % 3 * kStage;
+        uint64_t live = ~(uint64_t)0;
+        if (a.live && some) live = a.live[row0 / 64];
+#pragma unroll
+        for (int k = 0; k < kLoadsA; k++) {
+            const uint32_t at = live >> row_a[k] & 1 ? from_a[k] : rocket::kNowhere;
+            rocket::load_stage16(dy, to + (wave * kLoadsA + k) * 1024, at);
+        }
+#pragma unroll
+        for (int k = 0; k < kLoadsC; k++)
+            rocket::load_stage16(q, to + kBytesA + (wave * kLoadsC + k) * 1024, from_c[k]);
+        rocket::load_stage4(scale, to + kBytesA + kBytesC + wave * 256,
+                            lane < 32 * NT ? (wc * 32 * NT + lane) * 4 : rocket::kNowhere);
+    };
+
+    // where it reads a stage: groups of 16 lanes turn 4 rows of 16 values about
+    const int group = lane / 16, in = lane % 16, half = lane / 32;
+    uint32_t read_a[MT], read_c[NT];
+    const auto place_a = [&](int matrix) {
+        const int piece = matrix * 4 + (group & 1) * 2 + in % 4 / 2;
+        return (16 * half + in / 4) * (kM * 2) + (piece ^ (in / 4 & kTurn) << 2) * 16 + in % 2 * 8;
+    };
+#pragma unroll
+    for (int k = 0; k < MT; k++) read_a[k] = place_a(wm * MT + k);
+    const uint32_t read_b = place_a(wm * MT + (wc < MT ? wc : 0));
+#pragma unroll
+    for (int k = 0; k < NT; k++) read_c[k] = kBytesA + ((wc * NT + k) * 32 + lane % 32) * 64;
+    const int turn_c = lane % 32 >> 1 & 3;
+    const uint32_t read_s = kBytesA + kBytesC + wave * 256 + lane % 32 * 4;
+
+    Float16 sum[MT][NT] = {};
+    float unit[NT], bias = 0.0f;
+    uint32_t held[NT];
+#pragma unroll
+    for (int k = 0; k < NT; k++) unit[k] = 0.0f, held[k] = 0u;
+    const int64_t to0 = ((int64_t)part * a.m + m0 + wm * 32 * MT + 4 * half) * a.c + c0 + wc * 32 * NT + lane % 32;
+    bool begun = false;   // whether dweight holds a sum already
+    auto put = [&](bool add) {
+#pragma unroll
+        for (int y = 0; y < NT; y++) {
+            float *to = a.dweight + to0 + y * 32;
+            int left = c0 + (wc * NT + y) * 32 + lane % 32 < a.c ? a.m - m0 - wm * 32 * MT - 4 * half : 0;
+#pragma unroll
+            for (int x = 0; x < MT; x++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    if (left > 0) *to = (add ? *to : 0.0f) + sum[x][y][i] * unit[y];
+                    to += i % 4 == 3 ? (int64_t)5 * a.c : (int64_t)a.c;
+                    left -= i % 4 == 3 ? 5 : 1;
+                    asm volatile("" : "+v"(to), "+v"(left)::"memory");   // one after the other: few registers
+                }
+        }
+    };
+
+    ask(0);
+    ask(1);
+    for (int stage = 0; stage < stages; stage++) {
+        rocket::wait_loads<kLoads>();
+        ask(stage + 2);
+        const uint32_t at = base + stage % 3 * kStage;
+        rocket::Shared from[MT];
+#pragma unroll
+        for (int k = 0; k < MT; k++) from[k] = rocket::shared_at(at + read_a[k]);
+        if (stage % (2 * PLANES) == 0) {
+            float factor[NT];
+            bool far = false;
+            float next[NT];
+#pragma unroll
+            for (int k = 0; k < NT; k++) {
+                next[k] = *(const __attribute__((address_space(3))) float *)(rocket::shared_at(at + read_s) + k * 128);
+                held[k] = next[k] == 0.0f ? 0u : ~0u;   // a scale of 0: whatever q holds counts nothing
+                if (next[k] == 0.0f) next[k] = unit[k];
+                factor[k] = unit[k] == 0.0f ? 1.0f : unit[k] / next[k];
+                const float size = __builtin_fabsf(factor[k]);
+                far |= size > 0x1p40f || size < 0x1p-40f;
+            }
+            if (__any(far)) {
+                put(begun);
+                begun = true;
+#pragma unroll
+                for (int k = 0; k < NT; k++) factor[k] = 0.0f;
+            }
+#pragma unroll
+            for (int x = 0; x < MT; x++)
+#pragma unroll
+                for (int y = 0; y < NT; y++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) sum[x][y][i] *= factor[y];
+#pragma unroll
+            for (int k = 0; k < NT; k++) unit[k] = next[k];
+        }
+#pragma unroll
+        for (int pair = 0; pair < 2; pair++) {
+            Words4 bytes[NT], wide[2][NT];
+#pragma unroll
+            for (int k = 0; k < NT; k++)
+                bytes[k] =
+                    *(SharedWords)rocket::shared_at(at + read_c[k] + ((2 * pair + half) ^ turn_c) * 16) & held[k];
+#pragma unroll
+            for (int k = 0; k < NT; k++) {
+                wide[0][k] = widen<HALF>(bytes[k][0], bytes[k][1]);
+                wide[1][k] = widen<HALF>(bytes[k][2], bytes[k][3]);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int x = 0; x < MT; x++) {
+                    const int t = 32 * pair + 8 * u;
+                    const Words4 fa = turned<kM * 2>(from[x] + t * (kM * 2));
+#pragma unroll
+                    for (int y = 0; y < NT; y++) {
+                        const Words4 fb = wide[u][y];
+                        if constexpr (HALF)
+                            sum[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                                __builtin_bit_cast(Half8, fa), __builtin_bit_cast(Half8, fb), sum[x][y], 0, 0, 0);
+                        else
+                            sum[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                                __builtin_bit_cast(Bf8, fa), __builtin_bit_cast(Bf8, fb), sum[x][y], 0, 0, 0);
+                    }
+                }
+        }
+        // dy's own sums: the tiles along c take the stages in turn, a wavefront one
+        // matrix' rows
+        if (a.dbias && stage / PLANES % a.tiles_c == tile_c && wc < MT)
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const Words4 fa =
+                    turned<kM * 2>(rocket::shared_at(at + read_b) + (32 * (k / 2) + 8 * (k % 2)) * (kM * 2));
+#pragma unroll
+                for (int e = 0; e < 8; e++) bias += value16<HALF>(fa[e / 2], e % 2);
+            }
+    }
+    rocket::wait_loads<0>();
+    put(begun);
+    if (a.dbias) {
+        static_assert(MT <= WC, "a wavefront counts at most one matrix' rows");
+        bias += __shfl_xor(bias, 32);
+        const int m = m0 + (wm * MT + wc) * 32 + lane;
+        if (wc < MT && lane < 32 && m < a.m)
+            a.dbias[((int64_t)part * a.tiles_c + tile_c) * a.m + m] = bias;
+    }
+}
+
+// A bit for each row: whether it holds data.
+__global__ __launch_bounds__(256) void live_kernel(Rows rows, uint64_t *live) {
+    const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint64_t bits = __ballot(r < rows.count && rocket::place_of(rows, r).live);
+    if (threadIdx.x % 64 == 0 && r < rows.count) live[r / 64] = bits;
+}
+
+// dy's rows laid out for the staged kernel: 16-bit parts, 16-byte aligned rows,
+// zeros where a row holds no data.  A thread takes 8 columns.
+template <int DT>
+__global__ __launch_bounds__(256) void lay_kernel(Rows rows, View dy, int32_t m, int64_t pieces, uint16_t *to,
+                                                  int64_t plane, int64_t begin) {
+    const int64_t i = begin + (int64_t)blockIdx.x * 256 + threadIdx.x, r = i / pieces;
+    if (r >= rows.count) return;
+    const int c = (int)(i - r * pieces) * 8;
+    using raw = typename Elem<DT>::raw;
+    const Place p = rocket::place_of(rows, r);
+    raw x[8] = {};
+    if (p.live) {
+        const raw *from = (const raw *)rocket::row_at(dy, p) + c;
+        if (c + 8 <= m)
+            __builtin_memcpy(x, from, sizeof(x));
+        else
+            for (int e = 0; e < 8; e++)
+                if (c + e < m) x[e] = from[e];
+    }
+    uint16_t v[kPlanes<DT>][8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        uint16_t s[kPlanes<DT>];
+        split<DT>(x[e], s);
+#pragma unroll
+        for (int k = 0; k < kPlanes<DT>; k++) v[k][e] = s[k];
+    }
+#pragma unroll
+    for (int k = 0; k < kPlanes<DT>; k++) rocket::store_at(to + k * plane + i * 8, __builtin_bit_cast(Words4, v[k]));
+}
+
 // Sums of the parts, in their order.
 __global__ __launch_bounds__(256) void join_kernel(const float *parts, float *sum, int64_t count, int32_t n) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -151,18 +453,68 @@ __global__ __launch_bounds__(256) void join_kernel(const float *parts, float *su
 }
 
 struct Cut {
+    bool staged;
+    bool lay;                // dy is laid out anew first
     int64_t blocks, each, parts;
+    int64_t tiles_m, tiles_c;
+    int64_t stride;          // bytes of a laid row
+    int64_t at_live, at_bias, at_dy, bytes;   // places in the workspace: after the parts of dW
 };
 
-// Parts of the rows, so that the workgroups fill the chip.
-Cut cut_of(const rocket_sequence_shape *s, int64_t channels) {
-    Cut c;
-    c.blocks = (s->n * s->steps + kKeepRows - 1) / kKeepRows;
-    const int64_t tiles = ((s->channels + kTile - 1) / kTile) * ((channels + kTile - 1) / kTile);
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({c.blocks, 1024 / std::max<int64_t>(tiles, 1), 64}));
-    c.each = std::max<int64_t>(1, (c.blocks + parts - 1) / parts);
-    c.parts = std::max<int64_t>(1, (c.blocks + c.each - 1) / c.each);
+constexpr int64_t kCus = 256;
+
+// Parts of the rows, so that the workgroups fill the chip (`at_once` run at a
+// time) in rounds of which the last is not nearly empty; each part costs its
+// sums' way through memory.
+void cut_parts(Cut &c, int64_t tiles, int64_t at_once, double block_us, double part_us) {
+    double best = 1e300;
+    for (int64_t p = 1; p <= std::min<int64_t>(c.blocks, 64); p++) {
+        const int64_t each = (c.blocks + p - 1) / p, parts = (c.blocks + each - 1) / each;
+        const double us = (double)((tiles * parts + at_once - 1) / at_once) * (each * block_us + 5.0) +
+                          (parts > 1 ? parts * part_us + 5.0 : 0.0);
+        if (us < best) best = us, c.each = each, c.parts = parts;
+    }
+}
+
+bool fits(const rocket_sequence_shape *s, const View &dy) {
+    const bool one = s->n == 1 || s->steps == 1 || dy.series == s->steps * dy.step;
+    const int64_t step = s->steps == 1 ? dy.series : dy.step;
+    return one && s->dtype != ROCKET_FLOAT32 && s->channels % 2 == 0 && step % 4 == 0 && (uintptr_t)dy.data % 4 == 0 &&
+           step <= (1 << 24);
+}
+
+// How a call is cut.
+Cut cut_of(const rocket_sequence_shape *s, int64_t channels, const View &dy) {
+    Cut c = {};
+    const int64_t rows = s->n * s->steps, m = s->channels;
+    c.blocks = (rows + kKeepRows - 1) / kKeepRows;
+    c.each = c.parts = 1;
+    c.staged = rows > 256;
+    const int64_t planes = s->dtype == ROCKET_FLOAT32 ? 3 : 1;
+    if (c.staged) {
+        c.tiles_m = (m + 255) / 256, c.tiles_c = (channels + 255) / 256;
+        cut_parts(c, c.tiles_m * c.tiles_c, kCus, 2.2 * planes, (double)m * channels * 8 / 4e6);
+        c.stride = (m + 7) / 8 * 16;
+        c.at_bias = c.parts > 1 ? c.parts * m * channels * 4 : 0;
+        c.at_live = (c.at_bias + c.parts * c.tiles_c * m * 4 + 15) / 16 * 16;
+        c.at_dy = c.at_live + (c.blocks * 16 + 15) / 16 * 16;
+        c.lay = !fits(s, dy);
+        c.bytes = c.at_dy + (c.lay ? planes * rows * c.stride : 0);
+    } else {
+        const int64_t tiles = ((m + kTile - 1) / kTile) * ((channels + kTile - 1) / kTile);
+        c.parts = std::max<int64_t>(1, std::min<int64_t>(c.blocks, kCus / tiles));
+        c.each = std::max<int64_t>(1, (c.blocks + c.parts - 1) / c.parts);
+        c.parts = std::max<int64_t>(1, (c.blocks + c.each - 1) / c.each);
+        c.at_bias = c.parts * m * channels * 4;
+        c.bytes = c.parts > 1 ? c.at_bias + c.parts * m * 4 : 0;
+    }
+    c.bytes = (c.bytes + 7) / 8 * 8;
     return c;
+}
+
+template <bool HALF, int PLANES>
+void staged_launch(const StagedArgs &a, int64_t parts, hipStream_t s) {
+    staged_kernel<HALF, PLANES, 4, 2, 2, 4><<<(uint32_t)(parts * a.tiles_m * a.tiles_c), 512, 0, s>>>(a);
 }
 
 bool sizes_ok(const rocket_sequence_shape *s, int64_t channels) {
@@ -172,10 +524,10 @@ bool sizes_ok(const rocket_sequence_shape *s, int64_t channels) {
 }  // namespace
 
 extern "C" rocket_status rocket_linear_weight_gradient_workspace(const rocket_sequence_shape *shape, int64_t channels,
-                                                                 int64_t *bytes) {
-    if (!bytes || !sizes_ok(shape, channels)) return ROCKET_ERR_INVALID_ARG;
-    const Cut cut = cut_of(shape, channels);
-    *bytes = cut.parts > 1 ? (cut.parts * shape->channels * (channels + 1) * 4 + 7) / 8 * 8 : 0;
+                                                                 const rocket_sequence *dy, int64_t *bytes) {
+    if (!bytes || !sizes_ok(shape, channels) || !rocket::view_ok(dy, shape)) return ROCKET_ERR_INVALID_ARG;
+    View view = rocket::view_of(dy, shape->dtype);
+    *bytes = cut_of(shape, channels, view).bytes;
     return ROCKET_OK;
 }
 
@@ -187,31 +539,68 @@ extern "C" rocket_status rocket_linear_weight_gradient(const rocket_sequence_sha
         (dbias && !rocket::floats_ok(dbias)))
         return ROCKET_ERR_INVALID_ARG;
     if (!rocket::empty(shape) && (!rocket::bytes_ok(q) || !rocket::floats_ok(scale))) return ROCKET_ERR_INVALID_ARG;
-    int64_t need = 0;
-    rocket_linear_weight_gradient_workspace(shape, channels, &need);
-    if (need && (!workspace || (uintptr_t)workspace % 8 != 0 || workspace_bytes < need)) return ROCKET_ERR_INVALID_ARG;
-    const Cut cut = cut_of(shape, channels);
-    GradArgs a = {};
-    a.dy = rocket::view_of(dy, shape->dtype);
-    a.q = q, a.scale = scale;
-    a.m = (int32_t)shape->channels, a.c = (int32_t)channels;
-    a.blocks = cut.blocks, a.each = cut.each;
-    const int64_t count = (int64_t)a.m * a.c;
-    a.dweight = cut.parts > 1 ? (float *)workspace : dweight;
-    a.dbias = !dbias ? nullptr : cut.parts > 1 ? (float *)workspace + cut.parts * count : dbias;
-    View *views[] = {&a.dy};
-    a.rows = rocket::rows_of(shape, views, 1);
+    View dy_view = rocket::view_of(dy, shape->dtype);
+    const Cut cut = cut_of(shape, channels, dy_view);
+    if (cut.bytes && (!workspace || (uintptr_t)workspace % 8 != 0 || workspace_bytes < cut.bytes))
+        return ROCKET_ERR_INVALID_ARG;
+    View *views[] = {&dy_view};
+    const Rows rows = rocket::rows_of(shape, views, 1);
+    const int32_t m = (int32_t)shape->channels, c = (int32_t)channels;
+    const int64_t count = (int64_t)m * c;
     hipStream_t s = (hipStream_t)hip_stream;
-    const uint32_t grid = (uint32_t)((a.c + kTile - 1) / kTile * ((a.m + kTile - 1) / kTile) * cut.parts);
-    if (shape->dtype == ROCKET_FLOAT32)
-        gradient_kernel<ROCKET_FLOAT32><<<grid, 256, 0, s>>>(a);
-    else if (shape->dtype == ROCKET_BFLOAT16)
-        gradient_kernel<ROCKET_BFLOAT16><<<grid, 256, 0, s>>>(a);
-    else
-        gradient_kernel<ROCKET_FLOAT16><<<grid, 256, 0, s>>>(a);
-    if (cut.parts > 1) {
-        join_kernel<<<(uint32_t)((count + 255) / 256), 256, 0, s>>>(a.dweight, dweight, count, (int32_t)cut.parts);
-        if (dbias) join_kernel<<<(uint32_t)((a.m + 255) / 256), 256, 0, s>>>(a.dbias, dbias, a.m, (int32_t)cut.parts);
+    char *work = (char *)workspace;
+    float *parts = cut.parts > 1 ? (float *)work : dweight;
+    int64_t biases;
+    if (cut.staged) {
+        StagedArgs a = {};
+        a.q = q, a.scale = scale, a.dweight = parts, a.dbias = dbias ? (float *)(work + cut.at_bias) : nullptr;
+        a.rows = rows.count, a.blocks = cut.blocks, a.each = cut.each;
+        a.m = m, a.c = c, a.tiles_m = (int32_t)cut.tiles_m, a.tiles_c = (int32_t)cut.tiles_c;
+        biases = cut.parts * cut.tiles_c;
+        a.width = cut.lay ? (int32_t)(cut.stride / 2) : m;
+        if (!cut.lay) {
+            a.dy = dy_view.data, a.dy_stride = shape->steps == 1 ? dy_view.series : dy_view.step;
+            if (rows.lengths) {
+                a.live = (const uint64_t *)(work + cut.at_live);
+                const uint32_t grid = (uint32_t)((rows.count + 255) / 256);
+                live_kernel<<<grid, 256, 0, s>>>(rows, (uint64_t *)(work + cut.at_live));
+            }
+        } else {
+            const int64_t pieces = cut.stride / 16, items = rows.count * pieces, most = rocket::most_groups(256) * 256;
+            a.dy = work + cut.at_dy, a.dy_stride = cut.stride, a.dy_plane = rows.count * cut.stride;
+            for (int64_t at = 0; at < items; at += most) {
+                const uint32_t grid = (uint32_t)((std::min(items - at, most) + 255) / 256);
+                uint16_t *to = (uint16_t *)(work + cut.at_dy);
+                if (shape->dtype == ROCKET_FLOAT32)
+                    lay_kernel<ROCKET_FLOAT32><<<grid, 256, 0, s>>>(rows, dy_view, m, pieces, to, a.dy_plane / 2, at);
+                else  // 16-bit values are moved as they are
+                    lay_kernel<ROCKET_BFLOAT16><<<grid, 256, 0, s>>>(rows, dy_view, m, pieces, to, a.dy_plane / 2, at);
+            }
+        }
+        if (shape->dtype == ROCKET_FLOAT32)
+            staged_launch<false, 3>(a, cut.parts, s);
+        else if (shape->dtype == ROCKET_BFLOAT16)
+            staged_launch<false, 1>(a, cut.parts, s);
+        else
+            staged_launch<true, 1>(a, cut.parts, s);
+    } else {
+        GradArgs a = {};
+        a.rows = rows, a.dy = dy_view, a.q = q, a.scale = scale, a.m = m, a.c = c;
+        a.blocks = cut.blocks, a.each = cut.each, a.dweight = parts;
+        a.dbias = !dbias ? nullptr : cut.parts > 1 ? (float *)(work + cut.at_bias) : dbias;
+        biases = cut.parts;
+        const uint32_t grid = (uint32_t)((c + kTile - 1) / kTile * ((m + kTile - 1) / kTile) * cut.parts);
+        if (shape->dtype == ROCKET_FLOAT32)
+            gradient_kernel<ROCKET_FLOAT32><<<grid, 256, 0, s>>>(a);
+        else if (shape->dtype == ROCKET_BFLOAT16)
+            gradient_kernel<ROCKET_BFLOAT16><<<grid, 256, 0, s>>>(a);
+        else
+            gradient_kernel<ROCKET_FLOAT16><<<grid, 256, 0, s>>>(a);
     }
+    if (cut.parts > 1)
+        join_kernel<<<(uint32_t)((count + 255) / 256), 256, 0, s>>>(parts, dweight, count, (int32_t)cut.parts);
+    if (dbias && (cut.staged || cut.parts > 1))
+        join_kernel<<<(uint32_t)((m + 255) / 256), 256, 0, s>>>((const float *)(work + cut.at_bias), dbias, m,
+                                                                (int32_t)biases);
     return rocket::launched();
 }

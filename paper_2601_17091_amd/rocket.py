@@ -200,7 +200,7 @@ def _signatures() -> dict:
         "rocket_checkpoint": ([shp, seq, vp, vp, vp], st),
         "rocket_restore": ([shp, vp, vp, seq, vp], st),
         "rocket_linear_weight_gradient": ([shp, i64, seq, vp, vp, vp, vp, vp, i64, vp], st),
-        "rocket_linear_weight_gradient_workspace": ([shp, i64, out64], st),
+        "rocket_linear_weight_gradient_workspace": ([shp, i64, seq, out64], st),
     }
 
 

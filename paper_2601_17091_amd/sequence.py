@@ -708,13 +708,13 @@ def linear_weight_gradient(dy, q, scale, *, lengths=None, stream=None):
     if q.get_device() != dy.get_device():
         raise ValueError("q must be on dy's GPU")
     _unrecorded(dy, scale)
-    size = ctypes.c_int64()
-    rocket._check(lib.rocket_linear_weight_gradient_workspace(_byref(shape), channels, _byref(size)),
+    size, view = ctypes.c_int64(), _rows_view(dy, "dy")
+    rocket._check(lib.rocket_linear_weight_gradient_workspace(_byref(shape), channels, _byref(view), _byref(size)),
                   "rocket_linear_weight_gradient_workspace")
     dweight = _empty(dy.shape[-1], channels, dtype=_f32, device=dy.device)
     dbias = _empty(dy.shape[-1], dtype=_f32, device=dy.device)
     work, at = _workspace(size.value, dy.device)
-    status = lib.rocket_linear_weight_gradient(_byref(shape), channels, _byref(_rows_view(dy, "dy")), at_q, at_scale,
+    status = lib.rocket_linear_weight_gradient(_byref(shape), channels, _byref(view), at_q, at_scale,
                                                dweight.data_ptr(), dbias.data_ptr(), at, size.value,
                                                _stream(dy.get_device()))
     rocket._check(status, "rocket_linear_weight_gradient")

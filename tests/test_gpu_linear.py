@@ -408,6 +408,27 @@ def test_weight_gradient_strides_and_extremes(env):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_weight_gradient_scales_far_apart(env, dtype):
+    """Blocks whose scales differ by 2^100 and more, scales of 0 over values that are
+    not, a channel's scales all 0, negative ones: each as the formula has it."""
+    torch, seq = env
+    rng = np.random.default_rng(6)
+    blocks, N, C = 12, 70, 90
+    rows = blocks * 128 - 50
+    q = rng.integers(-127, 128, size=(blocks, C, 128)).astype(np.int8)
+    scale = (2.0 ** rng.integers(-60, 60, size=(blocks, C)) * rng.choice([-1, 1], (blocks, C))).astype(np.float32)
+    scale[rng.random((blocks, C)) < 0.3] = 0.0
+    scale[:, 7] = 0.0
+    scale[:, :5] = (0.5 + rng.random((blocks, 5))).astype(np.float32)
+    dy = cuda(torch, rng.standard_normal((rows, N)), dtype)
+    dyv = values(dy)
+    dw, db = seq.linear_weight_gradient(dy, torch.from_numpy(q).cuda(), cuda(torch, scale))
+    want = lo.linear_weight_gradient(dyv, q, scale)
+    close(dw, want["dweight"], want["dweight_tol"], "dweight")
+    assert (dw[:, 7] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_weight_gradient_error_of_many_rows(env, dtype):
     """20,000 rows: off by less than 1e-6 of the whole in the 2-norm (terms add at random
     signs, each partial sum rounds to 2^-24 of what it has come to)."""

@@ -152,7 +152,7 @@ def test_refused_workspace_shapes(lib, over):
     size, s = ctypes.c_int64(), shape(**over)
     assert lib.rocket_rms_norm_workspace(byref(s), byref(size)) == INV
     assert lib.rocket_linear_bytes_workspace(byref(s), 64, byref(size)) == INV
-    assert lib.rocket_linear_weight_gradient_workspace(byref(s), 64, byref(size)) == INV
+    assert lib.rocket_linear_weight_gradient_workspace(byref(s), 64, byref(seq()), byref(size)) == INV
 
 
 @pytest.mark.parametrize("bad", BAD_OUTPUTS)
@@ -196,15 +196,16 @@ def test_refused_workspaces(lib):
     assert lib.rocket_rms_norm_workspace(byref(long), byref(size)) == 0 and size.value > 0 and size.value % 8 == 0
     for ws, n in ((None, size.value), (DUMMY + 4, size.value), (DUMMY, size.value - 1)):
         assert norm_back(lib, long, wide, wide, dx=wide, ws=ws, size=n) == INV
-    assert lib.rocket_linear_weight_gradient_workspace(byref(long), 100, byref(size)) == 0 and size.value > 0
+    assert lib.rocket_linear_weight_gradient_workspace(byref(long), 100, byref(wide), byref(size)) == 0 and size.value > 0
     for ws, n in ((None, size.value), (DUMMY + 4, size.value), (DUMMY, size.value - 1)):
         assert gradient(lib, long, 100, wide, ws=ws, size=n) == INV
     for call in (lambda s, p: lib.rocket_rms_norm_workspace(s, p),
                  lambda s, p: lib.rocket_linear_bytes_workspace(s, 64, p),
-                 lambda s, p: lib.rocket_linear_weight_gradient_workspace(s, 64, p)):
+                 lambda s, p: lib.rocket_linear_weight_gradient_workspace(s, 64, byref(wide), p)):
         assert call(byref(long), None) == INV and call(None, byref(size)) == INV
     assert lib.rocket_linear_bytes_workspace(byref(long), 96, byref(size)) == INV
-    assert lib.rocket_linear_weight_gradient_workspace(byref(long), 0, byref(size)) == INV
+    for channels, view in ((0, byref(wide)), (64, None), (64, byref(seq(data=None)))):
+        assert lib.rocket_linear_weight_gradient_workspace(byref(long), channels, view, byref(size)) == INV
 
 
 @pytest.mark.parametrize("none", [dict(n=0), dict(steps=0)])
