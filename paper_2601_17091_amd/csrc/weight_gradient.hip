@@ -163,29 +163,19 @@ typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
 typedef const __attribute__((address_space(3))) Words4 *SharedWords;
 typedef _Float16 Half2 __attribute__((ext_vector_type(2)));
 
-// 8 signed bytes as 8 values of the operands' type, exactly.
+// Bytes 2 k and 2 k + 1 of four signed ones as two values of the operands' type,
+// exactly.
 template <bool HALF>
-__device__ inline Words4 widen(uint32_t lo, uint32_t hi) {
-    Words4 w;
+__device__ inline uint32_t widen(uint32_t b, int k) {
     if (HALF) {
         // 1024 + (q + 128) has q + 128 as its lowest bits
-        const uint32_t u[2] = {lo ^ 0x80808080u, hi ^ 0x80808080u};
         const Half2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-            const uint32_t pair = __builtin_amdgcn_perm(0x64646464u, u[k / 2], k % 2 ? 0x04030402u : 0x04010400u);
-            w[k] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(Half2, pair) + off);
-        }
-    } else {
-        // whole numbers below 2^8 leave the lower half of an fp32 value empty
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-            const uint32_t b = k / 2 ? hi : lo;
-            const float x = (float)(int8_t)(b >> (16 * (k % 2))), y = (float)(int8_t)(b >> (16 * (k % 2) + 8));
-            w[k] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);
-        }
+        const uint32_t pair = __builtin_amdgcn_perm(0x64646464u, b ^ 0x80808080u, k ? 0x04030402u : 0x04010400u);
+        return __builtin_bit_cast(uint32_t, __builtin_bit_cast(Half2, pair) + off);
     }
-    return w;
+    // whole numbers below 2^8 leave the lower half of an fp32 value empty
+    const float x = (float)(int8_t)(b >> (16 * k)), y = (float)(int8_t)(b >> (16 * k + 8));
+    return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);
 }
 
 template <bool HALF>
@@ -261,7 +251,9 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
                                           row0 < a.rows ? left_a : 0);
         const Int4 q = rocket::buffer_of(a.q + (block * a.c + c0) * kKeepRows + half * 64,
                                          some ? (int64_t)(a.c - c0) * kKeepRows - half * 64 : 0);
-        const Int4 scale = rocket::buffer_of(a.scale + block * a.c + c0, some ? (int64_t)(a.c - c0) * 4 : 0);
+        // the scale of the next stage's block: it is looked at before that begins
+        const int64_t after = first + (stage + 1) / (2 * PLANES);
+        const Int4 scale = rocket::buffer_of(a.scale + after * a.c + c0, after < last ? (int64_t)(a.c - c0) * 4 : 0);
         const uint32_t to = base + stage % 3 * kStage;
         uint64_t live = ~(uint64_t)0;
         if (a.live && some) live = a.live[row0 / 64];
@@ -295,8 +287,6 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
     Float16 sum[MT][NT] = {};
     float unit[NT], bias = 0.0f;
     uint32_t held[NT];
-#pragma unroll
-    for (int k = 0; k < NT; k++) unit[k] = 0.0f, held[k] = 0u;
     const int64_t to0 = ((int64_t)part * a.m + m0 + wm * 32 * MT + 4 * half) * a.c + c0 + wc * 32 * NT + lane % 32;
     bool begun = false;   // whether dweight holds a sum already
     auto put = [&](bool add) {
@@ -316,19 +306,94 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
         }
     };
 
+    float factor[NT];
+#pragma unroll
+    for (int k = 0; k < NT; k++) {
+        const int c = c0 + (wc * NT + k) * 32 + lane % 32;
+        unit[k] = c < a.c ? a.scale[first * a.c + c] : 0.0f;
+        held[k] = unit[k] == 0.0f ? 0u : ~0u;
+        factor[k] = 1.0f;
+    }
     ask(0);
     ask(1);
-    for (int stage = 0; stage < stages; stage++) {
-        rocket::wait_loads<kLoads>();
-        ask(stage + 2);
-        const uint32_t at = base + stage % 3 * kStage;
-        rocket::Shared from[MT];
+    for (int block = 0; block < stages; block += 2 * PLANES) {
 #pragma unroll
-        for (int k = 0; k < MT; k++) from[k] = rocket::shared_at(at + read_a[k]);
-        if (stage % (2 * PLANES) == 0) {
-            float factor[NT];
-            bool far = false;
+        for (int s = 0; s < 2 * PLANES; s++) {
+            const int stage = block + s;
+            rocket::wait_loads<kLoads>();
+            ask(stage + 2);
+            const uint32_t at = base + stage % 3 * kStage;
+            rocket::Shared from[MT];
+#pragma unroll
+            for (int k = 0; k < MT; k++) from[k] = rocket::shared_at(at + read_a[k]);
+            // 4 groups of 16 rows, MT steps each.  A matrix instruction keeps its unit for
+            // 8 others' time, so between a step's two there is done what is wanted later:
+            // the first operand is read two steps ahead, the second widened a group ahead,
+            // the sum of the next step multiplied.
+            constexpr int kSteps = 4 * MT;
+            Words4 bytes[2][NT], fa[kSteps];
+            uint32_t wide[2][NT][4];
+#pragma unroll
+            for (int k = 0; k < NT; k++)
+                bytes[0][k] = *(SharedWords)rocket::shared_at(at + read_c[k] + (half ^ turn_c) * 16);
+            fa[0] = turned<kM * 2>(from[0]);
+            fa[1] = turned<kM * 2>(from[1]);
+#pragma unroll
+            for (int k = 0; k < NT; k++)
+                bytes[1][k] = *(SharedWords)rocket::shared_at(at + read_c[k] + (2 + half ^ turn_c) * 16);
+            const auto widen_word = [&](int group, int k, int w) {
+                wide[group % 2][k][w] = widen<HALF>(bytes[group / 2][k][group % 2 * 2 + w / 2] & held[k], w % 2);
+            };
+            const auto multiply = [&](int x) {
+#pragma unroll
+                for (int y = 0; y < NT; y++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) sum[x][y][i] *= factor[y];
+            };
+            if (s == 0) multiply(0);
+#pragma unroll
+            for (int k = 0; k < NT; k++)
+#pragma unroll
+                for (int w = 0; w < 4; w++) widen_word(0, k, w);
+#pragma unroll
+            for (int step = 0; step < kSteps; step++) {
+                const int group = step / MT, x = step % MT;
+                __builtin_amdgcn_sched_barrier(0);
+                if (step + 2 < kSteps) {
+                    const int g = (step + 2) / MT;
+                    fa[step + 2] = turned<kM * 2>(from[(step + 2) % MT] + (32 * (g / 2) + 8 * (g % 2)) * (kM * 2));
+                }
+#pragma unroll
+                for (int y = 0; y < NT; y++) {
+                    const uint32_t *w = wide[group % 2][y];
+                    const Words4 fb = {w[0], w[1], w[2], w[3]};
+                    if constexpr (HALF)
+                        sum[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                            __builtin_bit_cast(Half8, fa[step]), __builtin_bit_cast(Half8, fb), sum[x][y], 0, 0, 0);
+                    else
+                        sum[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            __builtin_bit_cast(Bf8, fa[step]), __builtin_bit_cast(Bf8, fb), sum[x][y], 0, 0, 0);
+                    if (group < 3)
+#pragma unroll
+                        for (int w4 = x * 4 / MT; w4 < (x + 1) * 4 / MT; w4++) widen_word(group + 1, y, w4);
+                }
+                if (s == 0 && step + 1 < MT) multiply(step + 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            // dy's own sums: the tiles along c take the stages in turn, a wavefront one
+            // matrix' rows
+            if (a.dbias && stage / PLANES % a.tiles_c == tile_c && wc < MT)
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    const Words4 fa =
+                        turned<kM * 2>(rocket::shared_at(at + read_b) + (32 * (k / 2) + 8 * (k % 2)) * (kM * 2));
+#pragma unroll
+                    for (int e = 0; e < 8; e++) bias += value16<HALF>(fa[e / 2], e % 2);
+                }
+            if (s < 2 * PLANES - 1) continue;
+            // the next block's scale
             float next[NT];
+            bool far = false;
 #pragma unroll
             for (int k = 0; k < NT; k++) {
                 next[k] = *(const __attribute__((address_space(3))) float *)(rocket::shared_at(at + read_s) + k * 128);
@@ -345,54 +410,8 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
                 for (int k = 0; k < NT; k++) factor[k] = 0.0f;
             }
 #pragma unroll
-            for (int x = 0; x < MT; x++)
-#pragma unroll
-                for (int y = 0; y < NT; y++)
-#pragma unroll
-                    for (int i = 0; i < 16; i++) sum[x][y][i] *= factor[y];
-#pragma unroll
             for (int k = 0; k < NT; k++) unit[k] = next[k];
         }
-#pragma unroll
-        for (int pair = 0; pair < 2; pair++) {
-            Words4 bytes[NT], wide[2][NT];
-#pragma unroll
-            for (int k = 0; k < NT; k++)
-                bytes[k] =
-                    *(SharedWords)rocket::shared_at(at + read_c[k] + ((2 * pair + half) ^ turn_c) * 16) & held[k];
-#pragma unroll
-            for (int k = 0; k < NT; k++) {
-                wide[0][k] = widen<HALF>(bytes[k][0], bytes[k][1]);
-                wide[1][k] = widen<HALF>(bytes[k][2], bytes[k][3]);
-            }
-#pragma unroll
-            for (int u = 0; u < 2; u++)
-#pragma unroll
-                for (int x = 0; x < MT; x++) {
-                    const int t = 32 * pair + 8 * u;
-                    const Words4 fa = turned<kM * 2>(from[x] + t * (kM * 2));
-#pragma unroll
-                    for (int y = 0; y < NT; y++) {
-                        const Words4 fb = wide[u][y];
-                        if constexpr (HALF)
-                            sum[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                                __builtin_bit_cast(Half8, fa), __builtin_bit_cast(Half8, fb), sum[x][y], 0, 0, 0);
-                        else
-                            sum[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                                __builtin_bit_cast(Bf8, fa), __builtin_bit_cast(Bf8, fb), sum[x][y], 0, 0, 0);
-                    }
-                }
-        }
-        // dy's own sums: the tiles along c take the stages in turn, a wavefront one
-        // matrix' rows
-        if (a.dbias && stage / PLANES % a.tiles_c == tile_c && wc < MT)
-#pragma unroll
-            for (int k = 0; k < 4; k++) {
-                const Words4 fa =
-                    turned<kM * 2>(rocket::shared_at(at + read_b) + (32 * (k / 2) + 8 * (k % 2)) * (kM * 2));
-#pragma unroll
-                for (int e = 0; e < 8; e++) bias += value16<HALF>(fa[e / 2], e % 2);
-            }
     }
     rocket::wait_loads<0>();
     put(begun);
