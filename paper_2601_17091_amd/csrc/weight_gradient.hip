@@ -206,7 +206,7 @@ __device__ inline Words4 turned(rocket::Shared p) {
 // and begins anew.
 //
 // PLANES: parts of dy's values, the smallest first.
-template <bool HALF, int PLANES, int MT, int NT, int WM, int WC>
+template <bool HALF, int PLANES, bool LIVE, int MT, int NT, int WM, int WC>
 __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
     constexpr int kWaves = WM * WC, kM = 32 * MT * WM, kC = 32 * NT * WC;
     constexpr int kPieces = kM / 8, kRowsA = 64 / kPieces;           // of a row; rows of a load
@@ -242,31 +242,46 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
         const int ch = (wave * kLoadsC + k) * 16 + lane / 4;
         from_c[k] = ch * kKeepRows + (lane % 4 ^ (ch >> 1 & 3)) * 16;
     }
-    auto ask = [&](int stage) {
-        const int step = stage / PLANES, plane = PLANES - 1 - stage % PLANES, half = step & 1;
-        const int64_t block = first + step / 2, row0 = block * kKeepRows + half * 64;
-        const bool some = stage < stages;
-        const int64_t left_a = some ? (a.rows - 1 - row0) * a.dy_stride + (a.width - m0) * 2 : 0;
-        const Int4 dy = rocket::buffer_of(a.dy + plane * a.dy_plane + row0 * a.dy_stride + m0 * 2,
-                                          row0 < a.rows ? left_a : 0);
-        const Int4 q = rocket::buffer_of(a.q + (block * a.c + c0) * kKeepRows + half * 64,
-                                         some ? (int64_t)(a.c - c0) * kKeepRows - half * 64 : 0);
+    // The stage that is asked for next: its buffers, and then its loads one by one, so
+    // that they find room between other work.
+    const char *ask_dy = a.dy + first * kKeepRows * a.dy_stride + m0 * 2;
+    const int8_t *ask_q = a.q + (first * a.c + c0) * kKeepRows;
+    const float *ask_scale = a.scale + first * a.c + c0;
+    int64_t ask_rows = a.rows - first * kKeepRows;
+    int asked = 0, ask_place = 0;
+    uint32_t ask_to = base;
+    Int4 dy_buffer, q_buffer, scale_buffer;
+    uint64_t live = 0;
+    const int has_c = a.c - c0 < kC ? a.c - c0 : kC, row_bytes = (a.width - m0) * 2;
+    auto open_stage = [&]() {
+        const bool some = asked < stages;
+        const int s = asked % (2 * PLANES), half = s / PLANES;
+        const int rows = !some || ask_rows <= 0 ? 0 : ask_rows < 64 ? (int)ask_rows : 64;
+        const int bytes = rows ? (rows - 1) * (int)a.dy_stride + row_bytes : 0;
+        dy_buffer = rocket::buffer_of(ask_dy + (PLANES - 1 - s % PLANES) * a.dy_plane, bytes);
+        q_buffer = rocket::buffer_of(ask_q + half * 64, some ? has_c * kKeepRows - half * 64 : 0);
         // the scale of the next stage's block: it is looked at before that begins
-        const int64_t after = first + (stage + 1) / (2 * PLANES);
-        const Int4 scale = rocket::buffer_of(a.scale + after * a.c + c0, after < last ? (int64_t)(a.c - c0) * 4 : 0);
-        const uint32_t to = base + stage % 3 * kStage;
-        uint64_t live = ~(uint64_t)0;
-        if (a.live && some) live = a.live[row0 / 64];
-#pragma unroll
-        for (int k = 0; k < kLoadsA; k++) {
-            const uint32_t at = live >> row_a[k] & 1 ? from_a[k] : rocket::kNowhere;
-            rocket::load_stage16(dy, to + (wave * kLoadsA + k) * 1024, at);
+        const bool after = s == 2 * PLANES - 1;
+        scale_buffer = rocket::buffer_of(ask_scale + (after ? a.c : 0), asked + (after ? 1 : 0) < stages ? has_c * 4 : 0);
+        ask_to = base + ask_place * kStage;
+        ask_place = ask_place == 2 ? 0 : ask_place + 1;
+        if (LIVE) live = some ? a.live[(a.rows - ask_rows) / 64] : 0;
+        if (s % PLANES == PLANES - 1) ask_dy += 64 * a.dy_stride, ask_rows -= 64;
+        if (after) ask_q += (int64_t)a.c * kKeepRows, ask_scale += a.c;
+        asked++;
+    };
+    auto ask = [&](int k) {
+        if (k < kLoadsA) {
+            uint32_t at = from_a[k];
+            if (LIVE) at = live >> row_a[k] & 1 ? at : rocket::kNowhere;
+            rocket::load_stage16(dy_buffer, ask_to + (wave * kLoadsA + k) * 1024, at);
+        } else if (k < kLoadsA + kLoadsC) {
+            const int l = k - kLoadsA;
+            rocket::load_stage16(q_buffer, ask_to + kBytesA + (wave * kLoadsC + l) * 1024, from_c[l]);
+        } else {
+            rocket::load_stage4(scale_buffer, ask_to + kBytesA + kBytesC + wave * 256,
+                                lane < 32 * NT ? (wc * 32 * NT + lane) * 4 : rocket::kNowhere);
         }
-#pragma unroll
-        for (int k = 0; k < kLoadsC; k++)
-            rocket::load_stage16(q, to + kBytesA + (wave * kLoadsC + k) * 1024, from_c[k]);
-        rocket::load_stage4(scale, to + kBytesA + kBytesC + wave * 256,
-                            lane < 32 * NT ? (wc * 32 * NT + lane) * 4 : rocket::kNowhere);
     };
 
     // where it reads a stage: groups of 16 lanes turn 4 rows of 16 values about
@@ -314,15 +329,18 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
         held[k] = unit[k] == 0.0f ? 0u : ~0u;
         factor[k] = 1.0f;
     }
-    ask(0);
-    ask(1);
+#pragma unroll
+    for (int early = 0; early < 2; early++) {
+        open_stage();
+#pragma unroll
+        for (int k = 0; k < kLoads; k++) ask(k);
+    }
+    uint32_t at = base;
     for (int block = 0; block < stages; block += 2 * PLANES) {
 #pragma unroll
         for (int s = 0; s < 2 * PLANES; s++) {
             const int stage = block + s;
             rocket::wait_loads<kLoads>();
-            ask(stage + 2);
-            const uint32_t at = base + stage % 3 * kStage;
             rocket::Shared from[MT];
 #pragma unroll
             for (int k = 0; k < MT; k++) from[k] = rocket::shared_at(at + read_a[k]);
@@ -341,6 +359,7 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
 #pragma unroll
             for (int k = 0; k < NT; k++)
                 bytes[1][k] = *(SharedWords)rocket::shared_at(at + read_c[k] + (2 + half ^ turn_c) * 16);
+            open_stage();
             const auto widen_word = [&](int group, int k, int w) {
                 wide[group % 2][k][w] = widen<HALF>(bytes[group / 2][k][group % 2 * 2 + w / 2] & held[k], w % 2);
             };
@@ -378,6 +397,8 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
                         for (int w4 = x * 4 / MT; w4 < (x + 1) * 4 / MT; w4++) widen_word(group + 1, y, w4);
                 }
                 if (s == 0 && step + 1 < MT) multiply(step + 1);
+#pragma unroll
+                for (int k = step * kLoads / kSteps; k < (step + 1) * kLoads / kSteps; k++) ask(k);
             }
             __builtin_amdgcn_sched_barrier(0);
             // dy's own sums: the tiles along c take the stages in turn, a wavefront one
@@ -390,13 +411,15 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
 #pragma unroll
                     for (int e = 0; e < 8; e++) bias += value16<HALF>(fa[e / 2], e % 2);
                 }
+            const uint32_t was = at;
+            at = at == base + 2 * kStage ? base : at + kStage;
             if (s < 2 * PLANES - 1) continue;
             // the next block's scale
             float next[NT];
             bool far = false;
 #pragma unroll
             for (int k = 0; k < NT; k++) {
-                next[k] = *(const __attribute__((address_space(3))) float *)(rocket::shared_at(at + read_s) + k * 128);
+                next[k] = *(const __attribute__((address_space(3))) float *)(rocket::shared_at(was + read_s) + k * 128);
                 held[k] = next[k] == 0.0f ? 0u : ~0u;   // a scale of 0: whatever q holds counts nothing
                 if (next[k] == 0.0f) next[k] = unit[k];
                 factor[k] = unit[k] == 0.0f ? 1.0f : unit[k] / next[k];
@@ -533,7 +556,11 @@ Cut cut_of(const rocket_sequence_shape *s, int64_t channels, const View &dy) {
 
 template <bool HALF, int PLANES>
 void staged_launch(const StagedArgs &a, int64_t parts, hipStream_t s) {
-    staged_kernel<HALF, PLANES, 4, 2, 2, 4><<<(uint32_t)(parts * a.tiles_m * a.tiles_c), 512, 0, s>>>(a);
+    const uint32_t grid = (uint32_t)(parts * a.tiles_m * a.tiles_c);
+    if (a.live)
+        staged_kernel<HALF, PLANES, PLANES == 1, 4, 2, 2, 4><<<grid, 512, 0, s>>>(a);
+    else
+        staged_kernel<HALF, PLANES, false, 4, 2, 2, 4><<<grid, 512, 0, s>>>(a);
 }
 
 bool sizes_ok(const rocket_sequence_shape *s, int64_t channels) {
