@@ -240,7 +240,7 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
 #pragma unroll
     for (int k = 0; k < kLoadsC; k++) {
         const int ch = (wave * kLoadsC + k) * 16 + lane / 4;
-        from_c[k] = ch * kKeepRows + (lane % 4 ^ (ch >> 1 & 3)) * 16;
+        from_c[k] = ch * kKeepRows + (lane % 4 ^ (ch >> 2 & 3)) * 16;
     }
     // The stage that is asked for next: its buffers, and then its loads one by one, so
     // that they find room between other work.
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
     const uint32_t read_b = place_a(wm * MT + (wc < MT ? wc : 0));
 #pragma unroll
     for (int k = 0; k < NT; k++) read_c[k] = kBytesA + ((wc * NT + k) * 32 + lane % 32) * 64;
-    const int turn_c = lane % 32 >> 1 & 3;
+    const int turn_c = lane % 32 >> 2 & 3;
     const uint32_t read_s = kBytesA + kBytesC + wave * 256 + lane % 32 * 4;
 
     Float16 sum[MT][NT] = {};
