@@ -28,140 +28,230 @@ struct ProductArgs {
     int32_t columns;   // of q and p: a multiple of 64
     int32_t channels;  // of y
     int32_t tiles;     // along the channels
-    int64_t first;     // the launch's first item
+    int32_t parts, each;   // of the columns' stages, and stages of a part
+    int32_t *sums;         // [parts, rows, channels]
 };
+
+// Few rows: what bounds them is reading the weights, so a workgroup takes 16 channels
+// and up to 64 rows, and its 16 wavefronts share the columns: each reads 64 columns
+// at once straight into the operands' registers (16 lines of 64 bytes), several
+// ahead; their sums meet in shared memory.  64 rows of 2,048 by 1,536 channels: 96
+// workgroups.
+//
+// Matrix instruction 16 x 16 x 64: the first operand's lane holds 16 bytes of row
+// lane % 16, the second's of column lane % 16, both the quarter lane / 16 of the 64;
+// result i of a lane is row 4 (lane / 16) + i of column lane % 16.  The first operand
+// is the weights.
+constexpr int kFewRows = 64, kFewChannels = 16, kFewWaves = 16;
+
+template <int DT, int NT>
+__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(ProductArgs a) {
+    __shared__ int sums[kFewWaves][NT][kFewChannels][17];
+    const int lane = threadIdx.x % 64, wave = rocket::uniform(threadIdx.x / 64);
+    const int m0 = blockIdx.x * kFewChannels, m = m0 + lane % 16;
+    // lines that are not there are read as the last one, and not written
+    const int8_t *p = a.p + (int64_t)(m < a.channels ? m : a.channels - 1) * a.columns + lane / 16 * 16;
+    const int8_t *q[NT];
+#pragma unroll
+    for (int y = 0; y < NT; y++) {
+        const int64_t r = y * 16 + lane % 16;
+        q[y] = a.q + (r < a.rows.count ? r : a.rows.count - 1) * a.columns + lane / 16 * 16;
+    }
+    Int4 sum[NT] = {};
+    constexpr int kAhead = 4;
+    const int stages = a.columns / 64;
+    for (int k0 = wave; k0 < stages; k0 += kAhead * kFewWaves) {
+        Int4 fm[kAhead], ft[kAhead][NT];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            const int k = k0 + u * kFewWaves;
+            if (k >= stages) continue;
+            fm[u] = *(const Int4 *)(p + k * 64);
+#pragma unroll
+            for (int y = 0; y < NT; y++) ft[u][y] = *(const Int4 *)(q[y] + k * 64);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            if (k0 + u * kFewWaves >= stages) continue;
+#pragma unroll
+            for (int y = 0; y < NT; y++)
+                sum[y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fm[u], ft[u][y], sum[y], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int y = 0; y < NT; y++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) sums[wave][y][4 * (lane / 16) + i][lane % 16] = sum[y][i];
+    __syncthreads();
+    const int c = threadIdx.x % 16, t = threadIdx.x / 16;
+    if (t >= 16 * NT || t >= a.rows.count || m0 + c >= a.channels) return;
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; w++) total += sums[w][t / 16][c][t % 16];
+    const Place place = rocket::place_of(a.rows, t);
+    const float bias = a.bias ? a.bias[m0 + c] : 0.0f;
+    const float v = place.live ? __builtin_fmaf((float)total, a.scale[t] * a.wscale[m0 + c], bias) : 0.0f;
+    using raw = typename Elem<DT>::raw;
+    ((raw *)rocket::row_at(a.y, place))[m0 + c] = Elem<DT>::round(v);
+}
 
 // Matrix instruction 32 x 32 x 32: the first operand's lane holds 16 bytes of row
 // lane % 32, the second's of column lane % 32, both the half lane / 32 of the 32;
 // result i of a lane is row 8 (i / 4) + 4 (lane / 32) + i % 4 of column lane % 32.
-constexpr int kTile = 64, kStep = 64;
-constexpr int kLine = kStep + 16;  // bytes of a row in shared memory
+// The first operand is the weights, so that a lane has four channels in a row of one
+// y row.
 
-// The first operand is the weights, so that a lane has four channels in a row of
-// one y row.
-template <int DT>
-__global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
-    __shared__ __attribute__((aligned(16))) int8_t rows[kTile * kLine], weights[kTile * kLine];
-    const int64_t item = a.first + rocket::item_of_block();
-    const int64_t t0 = item / a.tiles * kTile;
-    const int m0 = (int)(item % a.tiles) * kTile;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wm = wave % 2 * 32, wt = wave / 2 * 32;
-    const int line = threadIdx.x / 4, part = threadIdx.x % 4 * 16;
-    const int64_t t = t0 + line;
-    const bool has_t = t < a.rows.count, has_m = m0 + line < a.channels;
-    Int16 sum = {};
-    for (int k = 0; k < a.columns; k += kStep) {
-        Int4 x = {}, w = {};
-        if (has_t) x = *(const Int4 *)(a.q + t * a.columns + k + part);
-        if (has_m) w = *(const Int4 *)(a.p + (int64_t)(m0 + line) * a.columns + k + part);
-        __syncthreads();
-        *(Int4 *)(rows + line * kLine + part) = x;
-        *(Int4 *)(weights + line * kLine + part) = w;
-        __syncthreads();
-#pragma unroll
-        for (int h = 0; h < kStep; h += 32) {
-            const Int4 fa = *(const Int4 *)(weights + (wm + lane % 32) * kLine + h + lane / 32 * 16);
-            const Int4 fb = *(const Int4 *)(rows + (wt + lane % 32) * kLine + h + lane / 32 * 16);
-            sum = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa, fb, sum, 0, 0, 0);
-        }
-    }
-    const int64_t r = t0 + wt + lane % 32;
-    if (r >= a.rows.count) return;
-    const Place p = rocket::place_of(a.rows, r);
-    using raw = typename Elem<DT>::raw;
-    raw *y = (raw *)rocket::row_at(a.y, p);
-    const float scale = p.live ? a.scale[r] : 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; i++) {
-        const int m = m0 + wm + 8 * (i / 4) + 4 * (lane / 32) + i % 4;
-        if (m >= a.channels) continue;
-        const float v = __builtin_fmaf((float)sum[i], scale * a.wscale[m], a.bias ? a.bias[m] : 0.0f);
-        y[m] = Elem<DT>::round(p.live ? v : 0.0f);
-    }
+// A sum from an accumulation register, just where it is used: left to itself the
+// compiler copies all of them at once and has to spill.
+template <bool ACC>
+__device__ inline int taken(int sum) {
+    if (!ACC) return sum;
+    int v;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(sum));
+    return v;
 }
 
-// A tile of y by WM x WT wavefronts, each MT x NT matrices of 32 channels x 32 rows.
+// Tiles of y by WM x WT wavefronts, each MT x NT matrices of 32 channels x 32 rows.
 //
 // A stage is 64 columns of the tile's weights and rows, 64 bytes a line in shared
 // memory, a line's four pieces of 16 bytes moved by its number so that the reads of
-// 32 lines meet every bank alike.  Four stages are there or on their way.  A stage
+// 32 lines meet every bank alike.  Three or four stages are there or on their way.  A stage
 // is two steps of 32 columns; while the matrix unit works on one step's operands,
 // the next step's are read into other registers, over the borders of stages too:
 // what a barrier says is that the next stage has arrived and that this one has
 // been read, and it stands where the matrix unit still has work.
-template <int DT, int MT, int NT, int WM, int WT, int SLOTS>
-__global__ __launch_bounds__(64 * WM * WT) void tile_kernel(ProductArgs a) {
-    constexpr int kWaves = WM * WT, kM = 32 * MT * WM, kT = 32 * NT * WT, kSlots = SLOTS;
-    constexpr int kLoadsM = kM / 16 / kWaves, kLoadsT = kT / 16 / kWaves, kLoads = kLoadsM + kLoadsT;
-    constexpr int kStage = (kM + kT) * 64, kSteps = MT * NT, kReads = MT + NT;
+//
+// A workgroup goes from tile to tile, and the stages go on over their borders: while
+// a tile's results are written, the next one's first stages arrive.
+//
+// SPLIT (of DT fp32): few tiles of many columns; a workgroup takes some of one tile's
+// stages and leaves their sums, whole numbers, to finish_kernel.
+template <int DT, bool SPLIT, int MT, int NT, int WM, int WT, int COLS, int SLOTS, int AT_ONCE>
+__global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs a) {
+    constexpr int kWaves = WM * WT, kThreads = 64 * kWaves, kM = 32 * MT * WM, kT = 32 * NT * WT, kSlots = SLOTS;
+    constexpr int kPieces = COLS / 16, kLines = 64 / kPieces;   // of a line; lines of a load
+    constexpr int kLoadsM = kM / kLines / kWaves, kLoadsT = kT / kLines / kWaves, kLoads = kLoadsM + kLoadsT;
+    constexpr int kStage = (kM + kT) * COLS, kSteps = COLS / 32, kProducts = MT * NT, kReads = MT + NT;
     constexpr int kSize = Elem<DT>::kSize;
+    // results on their way: 32 rows of 128 bytes (64 where there are no more) a wavefront
+    constexpr int kAcross = kSize == 2 && MT > 1 ? 2 : 1, kRowBytes = 32 * kAcross * kSize, kLine = kRowBytes + 16;
+    constexpr int kTable = 8 * kM + 12 * kT, kOut = kSlots * kStage, kTables = kOut + kWaves * 32 * kLine;
     typedef float Float4 __attribute__((ext_vector_type(4)));
     typedef uint32_t Words __attribute__((ext_vector_type(kSize)));   // four values
-    static_assert(kLoadsM * kWaves * 16 == kM && kLoadsT * kWaves * 16 == kT, "whole loads");
-    __shared__ __attribute__((aligned(1024))) char shared[kSlots * kStage + 8 * kM + 12 * kT];
+    static_assert(kLoadsM * kWaves * kLines == kM && kLoadsT * kWaves * kLines == kT, "whole loads");
+    static_assert(kM <= kThreads && kT <= kThreads, "a thread for each line of a table");
+    __shared__ __attribute__((aligned(1024))) char shared[kTables + 2 * kTable];
     const uint32_t base = rocket::shared_address(shared);
     const int lane = threadIdx.x % 64, wave = rocket::uniform(threadIdx.x / 64);
     const int wm = wave % WM, wt = wave / WM, half = lane / 32;
-    const int64_t item = a.first + rocket::item_of_block();
-    const int64_t t0 = item / a.tiles * kT;
-    const int m0 = (int)(item % a.tiles) * kM;
-    const int stages = a.columns / 64;
+    const int all_stages = (a.columns + COLS - 1) / COLS;
+    const uint32_t group = rocket::item_of_block();
+    const int part = SPLIT ? (int)(group % a.parts) : 0, stage0 = part * a.each;
+    const int stages = SPLIT ? (all_stages - stage0 < a.each ? all_stages - stage0 : a.each) : all_stages;
 
-    // where this lane's pieces of a stage come from
-    const int64_t left_t = a.rows.count - t0;
-    const int left_m = a.channels - m0;
-    const Int4 weights = rocket::buffer_of(a.p + (int64_t)m0 * a.columns,
-                                           (int64_t)(left_m < kM ? left_m : kM) * a.columns);
-    const Int4 rows = rocket::buffer_of(a.q + t0 * a.columns, (left_t < kT ? left_t : kT) * a.columns);
-    uint32_t from[kLoads];
+    // tiles: this workgroup's first one, and the way to its next
+    const int64_t first = SPLIT ? group / a.parts : group;
+    const int64_t step_t = SPLIT ? INT32_MAX : (int64_t)gridDim.x / a.tiles;
+    const int step_m = (int)(gridDim.x % a.tiles);
+    struct Tile {
+        int64_t t;
+        int m;
+    };
+    Tile tile = {first / a.tiles, (int)(first % a.tiles)};
+    const int64_t tiles_t = (a.rows.count + kT - 1) / kT;
+    const auto next_of = [&](Tile x) {
+        x.t += step_t, x.m += step_m;
+        if (x.m >= a.tiles) x.m -= a.tiles, x.t++;
+        return x;
+    };
+
+    // a line's pieces are moved by its number, so that 16 lines in a row meet every bank alike
+    const auto turn_of = [](int line) { return COLS == 64 ? line >> 2 & 3 : line >> 1 & 7; };
+    // the stage that is asked for next
+    uint32_t from[kLoads];   // where this lane's pieces of a stage come from
 #pragma unroll
     for (int k = 0; k < kLoads; k++) {
-        const int line = (k < kLoadsM ? wave * kLoadsM + k : wave * kLoadsT + k - kLoadsM) * 16 + lane / 4;
-        from[k] = line * a.columns + (lane % 4 ^ (line >> 2 & 3)) * 16;
+        const int line = (k < kLoadsM ? wave * kLoadsM + k : wave * kLoadsT + k - kLoadsM) * kLines + lane / kPieces;
+        from[k] = line * a.columns + (lane % kPieces ^ turn_of(line)) * 16;
     }
-    // the tile's scales and bias, and where its rows lie, before the stages' loads: a
-    // row that holds no data has its address's lowest bit set, one that is not there 0
-    float *factors = (float *)(shared + kSlots * kStage), *row_scale = factors + 2 * kM;
-    uint64_t *row_at = (uint64_t *)(row_scale + kT);
-    for (int k = threadIdx.x; k < kM; k += 64 * kWaves) {
-        factors[k] = k < left_m ? a.wscale[m0 + k] : 0.0f;
-        factors[kM + k] = k < left_m && a.bias ? a.bias[m0 + k] : 0.0f;
-    }
-    for (int k = threadIdx.x; k < kT; k += 64 * kWaves) {
-        const Place p = rocket::place_of(a.rows, t0 + (k < left_t ? k : 0));
-        const uint64_t to = (uint64_t)(rocket::row_at(a.y, p) + (int64_t)m0 * kSize);
-        row_scale[k] = k < left_t ? a.scale[t0 + k] : 0.0f;
-        row_at[k] = k < left_t ? to | (p.live ? 0 : 1) : 0;
-    }
-
-    int asked = 0;
+    // 128 columns: the last stage may have 64, and the pieces past them read nothing
+    uint32_t rest[2] = {0, 0}, past[2] = {0, 0};
+    if (COLS == 128 && a.columns % COLS)
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+            rest[k] = (lane % kPieces ^ turn_of(k * kLines + lane / kPieces)) >= kPieces / 2 ? rocket::kNowhere : 0;
+    Tile ask_tile = tile;
+    int ask_stage = 0, ask_slot = 0;
     uint32_t ask_at = 0, ask_to = base;
-    auto open_stage = [&]() {
-        ask_at = asked < stages ? asked * 64 : rocket::kNowhere;
-        ask_to = base + asked % kSlots * kStage;
-        asked++;
+    Int4 weights, rows;
+    const auto open_tile = [&]() {
+        const int64_t left_t = a.rows.count - ask_tile.t * kT;   // 0 or less: past the last tile
+        const int left_m = a.channels - ask_tile.m * kM;
+        weights = rocket::buffer_of(a.p + (int64_t)ask_tile.m * kM * a.columns,
+                                    left_t > 0 ? (int64_t)(left_m < kM ? left_m : kM) * a.columns : 0);
+        rows = rocket::buffer_of(a.q + ask_tile.t * kT * a.columns, (left_t < kT ? left_t : kT) * a.columns);
     };
-    auto ask = [&](int k) {
+    const auto open_stage = [&]() {
+        if (ask_stage == stages) {
+            ask_tile = next_of(ask_tile), ask_stage = 0;
+            open_tile();
+        }
+        ask_at = (stage0 + ask_stage++) * COLS;
+        if (COLS == 128)
+            for (int k = 0; k < 2; k++) past[k] = stage0 + ask_stage == all_stages ? rest[k] : 0;
+        ask_to = base + ask_slot * kStage;
+        ask_slot = (ask_slot + 1) % kSlots;
+    };
+    const auto ask = [&](int k) {
         if (k < kLoadsM)
-            rocket::load_stage16(weights, ask_to + (wave * kLoadsM + k) * 1024, from[k], ask_at);
+            rocket::load_stage16(weights, ask_to + (wave * kLoadsM + k) * 1024, from[k] | past[k % 2], ask_at);
         else
-            rocket::load_stage16(rows, ask_to + kM * 64 + (wave * kLoadsT + k - kLoadsM) * 1024, from[k], ask_at);
+            rocket::load_stage16(rows, ask_to + kM * COLS + (wave * kLoadsT + k - kLoadsM) * 1024,
+                                 from[k] | past[k % 2], ask_at);
     };
 
-    // where it reads a stage: the second step's piece is the first one's with bit 1 turned
+    // a tile's scales, bias and where its rows lie: a row that holds no data has its
+    // address's lowest bit set, one that is not there is 0
+    struct Table {
+        float wscale, bias, scale;
+        uint64_t at;
+    };
+    const auto look_up = [&](Tile x) {
+        Table v = {};
+        const int k = threadIdx.x, m = x.m * kM + k;
+        const int64_t r = x.t * kT + k;
+        if (!SPLIT && k < kM && m < a.channels) v.wscale = a.wscale[m], v.bias = a.bias ? a.bias[m] : 0.0f;
+        if (k < kT && r < a.rows.count) {
+            const Place p = rocket::place_of(a.rows, r);
+            v.scale = SPLIT ? 0.0f : a.scale[r];
+            char *to = SPLIT ? (char *)(a.sums + (part * a.rows.count + r) * a.channels) : rocket::row_at(a.y, p);
+            v.at = (uint64_t)(to + (int64_t)x.m * kM * kSize) | (SPLIT || p.live ? 0 : 1);
+        }
+        return v;
+    };
+    const auto write_table = [&](const Table &v, int turn) {
+        float *to = (float *)(shared + kTables + turn * kTable);
+        const int k = threadIdx.x;
+        if (k < kM) to[k] = v.wscale, to[kM + k] = v.bias;
+        if (k < kT) to[2 * kM + k] = v.scale, ((uint64_t *)(to + 2 * kM + kT))[k] = v.at;
+    };
+    write_table(look_up(tile), 0);
+
+    // where it reads a stage: a step's pieces are the first one's with the higher bits turned
     typedef const __attribute__((address_space(3))) Int4 *SharedInt4;
-    const uint32_t piece = (half ^ (lane >> 2 & 3)) * 16 + lane % 32 * 64;
-    const uint32_t read_m = wm * MT * 2048 + piece, read_t = kM * 64 + wt * NT * 2048 + piece;
-    Int16 sum[MT][NT] = {};
+    const uint32_t piece = (half ^ turn_of(lane % 32)) * 16 + lane % 32 * COLS;
+    const uint32_t read_m = wm * MT * 32 * COLS + piece, read_t = (kM + wt * NT * 32) * COLS + piece;
+    Int16 sum[MT][NT];
     Int4 fm[2][MT], ft[2][NT];
-    auto read = [&](int step, uint32_t at, int k) {
+    const auto read = [&](int step, uint32_t at, int k) {
         if (k < MT)
-            fm[step][k] = *(SharedInt4)(rocket::shared_at((at + read_m) ^ step * 32) + k * 2048);
+            fm[step % 2][k] = *(SharedInt4)(rocket::shared_at((at + read_m) ^ step * 32) + k * 32 * COLS);
         else
-            ft[step][k - MT] = *(SharedInt4)(rocket::shared_at((at + read_t) ^ step * 32) + (k - MT) * 2048);
+            ft[step % 2][k - MT] = *(SharedInt4)(rocket::shared_at((at + read_t) ^ step * 32) + (k - MT) * 32 * COLS);
     };
     // the k-th operand of a step in the order in which its products need them
     const auto order = [](int k) { return k == 0 ? 0 : k <= NT ? MT + k - 1 : k - NT; };
+    open_tile();
 #pragma unroll
     for (int early = 0; early < kSlots; early++) {
         open_stage();
@@ -171,108 +261,200 @@ __global__ __launch_bounds__(64 * WM * WT) void tile_kernel(ProductArgs a) {
     rocket::wait_loads<(kSlots - 1) * kLoads>();
 #pragma unroll
     for (int k = 0; k < kReads; k++) read(0, base, order(k));
-    constexpr int kMeet = kSteps - 1 - kSteps / 4;   // the product after which the wavefronts meet
-    for (int stage = 0; stage < stages; stage++) {
-        const uint32_t at = base + stage % kSlots * kStage, next = base + (stage + 1) % kSlots * kStage;
-#pragma unroll
-        for (int k = 0; k < kSteps; k++) {
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int r = k * kReads / (kMeet + 1); r < (k + 1) * kReads / (kMeet + 1) && r < kReads; r++)
-                read(1, at, order(r));
-            sum[k / NT][k % NT] =
-                __builtin_amdgcn_mfma_i32_32x32x32_i8(fm[0][k / NT], ft[0][k % NT], sum[k / NT][k % NT], 0, 0, 0);
-            if (k == kMeet) {
-                __builtin_amdgcn_sched_barrier(0);
-                rocket::wait_loads<(kSlots - 2) * kLoads>();
-            }
-        }
-        open_stage();
-#pragma unroll
-        for (int k = 0; k < kSteps; k++) {
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int r = k * kReads / kSteps; r < (k + 1) * kReads / kSteps; r++) read(0, next, order(r));
-            sum[k / NT][k % NT] =
-                __builtin_amdgcn_mfma_i32_32x32x32_i8(fm[1][k / NT], ft[1][k % NT], sum[k / NT][k % NT], 0, 0, 0);
-#pragma unroll
-            for (int l = k * kLoads / kSteps; l < (k + 1) * kLoads / kSteps; l++) ask(l);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    rocket::wait_loads<0>();
-
-    // A lane has four channels in a row, eight apart, of one row of y.  32 rows at a
-    // time go through shared memory, each wavefront's its own, so that a row's channels
-    // are written side by side.
-    constexpr int kRowBytes = 32 * MT * kSize, kLine = kRowBytes + 16, kLanes = kRowBytes / 16;
-    static_assert(kWaves * 32 * kLine <= kSlots * kStage, "room for the rows");
-    char *mine = shared + wave * 32 * kLine;
-    const int part = lane % kLanes * 16, c = wm * 32 * MT + part / kSize;   // what it writes of a row
-    constexpr int kEach = 16 / kSize;
-#pragma unroll
-    for (int y = 0; y < NT; y++) {
-        const int t = (wt * NT + y) * 32;
-        const float scale = row_scale[t + lane % 32];
-        const uint32_t held = row_at[t + lane % 32] & 1 ? 0u : ~0u;
+    constexpr int kMeet = kProducts - 1 - kProducts / 4;   // the product after which the wavefronts meet
+    int slot = 0;
+    for (int turn = 0; tile.t < tiles_t; turn ^= 1) {
 #pragma unroll
         for (int x = 0; x < MT; x++)
 #pragma unroll
-            for (int g = 0; g < 4; g++) {
-                const int m = x * 32 + 8 * g + 4 * half;
-                const Float4 s = *(const Float4 *)(factors + wm * 32 * MT + m);
-                const Float4 b = *(const Float4 *)(factors + kM + wm * 32 * MT + m);
-                float v[4];
+            for (int y = 0; y < NT; y++) sum[x][y] = Int16{};
+        for (int stage = 0; stage < stages; stage++) {
+            const uint32_t at = base + slot * kStage;
+            slot = (slot + 1) % kSlots;
+            const uint32_t next = base + slot * kStage;
 #pragma unroll
-                for (int e = 0; e < 4; e++) v[e] = __builtin_fmaf((float)sum[x][y][4 * g + e], scale * s[e], b[e]);
-                Words w;
+            for (int step = 0; step < kSteps; step++) {
+                // the wavefronts meet in the last step but one, which reads the last one's operands
+                const bool meets = step == kSteps - 2, ends = step == kSteps - 1;
+                const int within = meets ? kMeet + 1 : kProducts;
+                if (ends) open_stage();
 #pragma unroll
-                for (int e = 0; e < kSize; e++) w[e] = Elem<DT>::put(v + e * Elem<DT>::kPerWord) & held;
-                *(Words *)(mine + lane % 32 * kLine + m * kSize) = w;
+                for (int k = 0; k < kProducts; k++) {
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int r = k * kReads / within; r < (k + 1) * kReads / within && r < kReads; r++)
+                        read(ends ? 0 : step + 1, ends ? next : at, order(r));
+                    sum[k / NT][k % NT] = __builtin_amdgcn_mfma_i32_32x32x32_i8(
+                        fm[step % 2][k / NT], ft[step % 2][k % NT], sum[k / NT][k % NT], 0, 0, 0);
+                    if (meets && k == kMeet) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        rocket::wait_loads<(kSlots - 2) * kLoads>();
+                    }
+                    if (ends)
+#pragma unroll
+                        for (int l = k * kLoads / kProducts; l < (k + 1) * kLoads / kProducts; l++) ask(l);
+                }
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+
+        // A lane has four channels in a row, eight apart, of one row of y.  They go through
+        // shared memory, each wavefront's its own, so that a row's channels are written side
+        // by side.
+        // (the matrix unit's last results reach their registers 18 cycles after they are asked
+        // for, which the compiler does not see that `taken` reads)
+        asm volatile("s_nop 15\n\ts_nop 15");
+        const Tile following = next_of(tile);
+        const Table table = look_up(following);
+        const float *factors = (const float *)(shared + kTables + turn * kTable), *row_scale = factors + 2 * kM;
+        const uint64_t *row_at = (const uint64_t *)(row_scale + kT);
+        const int left_m = a.channels - tile.m * kM;
+        constexpr int kLanes = kRowBytes / 16, kEach = 16 / kSize;   // lanes that write a row; values of a lane
+        char *mine = shared + kOut + wave * 32 * kLine;
 #pragma unroll
-        for (int k = 0; k < kLanes / 2; k++) {
-            const int row = k * (64 / kLanes) + lane / kLanes;
-            const uint32_t *from = (const uint32_t *)(mine + row * kLine + part);
-            const Int4 v = *(const Int4 *)from;
-            char *to = (char *)(row_at[t + row] & ~(uint64_t)1);
-            if (!to || c >= left_m) continue;
-            to += c * kSize;
-            if (c + kEach <= left_m) {
-                rocket::store_at(to, v);
-            } else {
-                using bits = typename Elem<DT>::bits;
-                for (int e = 0; e < kEach && c + e < left_m; e++) ((bits *)to)[e] = ((const bits *)from)[e];
+        for (int x0 = 0; x0 < MT; x0 += kAcross) {
+            const int m0 = (wm * MT + x0) * 32, c = m0 + lane % kLanes * kEach;
+            Float4 wscale[kAcross][4], bias[kAcross][4];
+#pragma unroll
+            for (int x = 0; x < kAcross; x++)
+#pragma unroll
+                for (int g = 0; g < 4; g++) {
+                    wscale[x][g] = *(const Float4 *)(factors + m0 + x * 32 + 8 * g + 4 * half);
+                    bias[x][g] = *(const Float4 *)(factors + kM + m0 + x * 32 + 8 * g + 4 * half);
+                }
+#pragma unroll
+            for (int y = 0; y < NT; y++) {
+                const int t = (wt * NT + y) * 32;
+                const float scale = row_scale[t + lane % 32];
+                const uint32_t held = row_at[t + lane % 32] & 1 ? 0u : ~0u;
+#pragma unroll
+                for (int x = 0; x < kAcross; x++)
+#pragma unroll
+                    for (int g = 0; g < 4; g++) {
+                        float v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            v[e] = __builtin_fmaf((float)taken<kProducts >= 16>(sum[x0 + x][y][4 * g + e]),
+                                                  scale * wscale[x][g][e], bias[x][g][e]);
+                        Words w;
+#pragma unroll
+                        for (int e = 0; e < kSize; e++)
+                            w[e] = SPLIT ? (uint32_t)taken<kProducts >= 16>(sum[x0 + x][y][4 * g + e])
+                                         : Elem<DT>::put(v + e * Elem<DT>::kPerWord) & held;
+                        *(Words *)(mine + lane % 32 * kLine + (x * 32 + 8 * g + 4 * half) * kSize) = w;
+                    }
+#pragma unroll
+                for (int k = 0; k < kLanes / 2; k++) {
+                    const int row = k * (64 / kLanes) + lane / kLanes;
+                    const uint32_t *own = (const uint32_t *)(mine + row * kLine + lane % kLanes * 16);
+                    const Int4 v = *(const Int4 *)own;
+                    char *to = (char *)(row_at[t + row] & ~(uint64_t)1);
+                    if (!to || c >= left_m) continue;
+                    to += c * kSize;
+                    if (c + kEach <= left_m) {
+                        rocket::store_at(to, v);
+                    } else {
+                        using bits = typename Elem<DT>::bits;
+                        for (int e = 0; e < kEach && c + e < left_m; e++) ((bits *)to)[e] = ((const bits *)own)[e];
+                    }
+                }
             }
         }
+        write_table(table, turn ^ 1);
+        tile = following;
     }
+    rocket::wait_loads<0>();
 }
 
-// The tile: the largest of which there are enough to fill the chip.
-template <int DT, int MT, int NT, int WM, int WT, int SLOTS = 4>
+// The results of split tiles: a thread an element, in the order of the sums.
+template <int DT>
+__global__ __launch_bounds__(256) void finish_kernel(ProductArgs a) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, r = i / a.channels, count = a.rows.count * a.channels;
+    if (r >= a.rows.count) return;
+    const int m = (int)(i - r * a.channels);
+    int total = 0;
+    for (int k = 0; k < a.parts; k++) total += a.sums[k * count + i];
+    const Place place = rocket::place_of(a.rows, r);
+    const float bias = a.bias ? a.bias[m] : 0.0f;
+    const float v = place.live ? __builtin_fmaf((float)total, a.scale[r] * a.wscale[m], bias) : 0.0f;
+    using raw = typename Elem<DT>::raw;
+    ((raw *)rocket::row_at(a.y, place))[m] = Elem<DT>::round(v);
+}
+
+constexpr int64_t kCus = 256;
+
+// How a call is cut, by what each way costs: rounds of workgroups, each with its
+// stages of 64 columns and the writing of its results (microseconds as measured with
+// 2,048 columns and 1,536 channels on 1,000 to 64,000 rows).
+enum Way { kFew, kBig, kTall, kMiddle, kMiddleTwice, kSmall, kSplit };
+
+struct Cut {
+    Way way;
+    int32_t parts, each;
+    int64_t bytes;
+};
+
+Cut cut_of(int64_t rows, int64_t channels, int64_t columns) {
+    Cut c = {kFew, 1, 0, 0};
+    if (rows <= kFewRows) return c;
+    struct Cost {
+        Way way;
+        int m, t, at_once;
+        double stage, end;
+    };
+    constexpr Cost kCosts[] = {{kBig, 256, 256, 1, 0.85, 6.0},   {kTall, 256, 128, 1, 0.52, 4.0},
+                               {kMiddle, 128, 128, 1, 0.28, 2.0}, {kMiddleTwice, 128, 128, 2, 0.58, 3.0},
+                               {kSmall, 64, 64, 2, 0.25, 1.0}};
+    const double stages = (double)(columns / 64);
+    double best = 1e300;
+    for (const Cost &k : kCosts) {
+        const int64_t tiles = (rows + k.t - 1) / k.t * ((channels + k.m - 1) / k.m), all = k.at_once * kCus;
+        const double us = (double)((tiles + all - 1) / all) * (stages * k.stage + k.end);
+        if (us < best) best = us, c.way = k.way;
+    }
+    const int64_t tiles = (rows + 127) / 128 * ((channels + 127) / 128), lines = (columns + 127) / 128;
+    for (int64_t p = 2; p <= lines / 2 && tiles * p <= 4 * kCus; p += 1 + p / 8) {
+        const int64_t each = (lines + p - 1) / p, parts = (lines + each - 1) / each;
+        const double us = (double)((tiles * parts + kCus - 1) / kCus) * (each * 0.56 + 2.0) + 6.0 +
+                          (double)(parts * rows * channels) * 8e-6 / 4.0;
+        if (us < best) best = us, c = Cut{kSplit, (int32_t)parts, (int32_t)each, parts * rows * channels * 4};
+    }
+    return c;
+}
+
+template <int DT, bool SPLIT, int MT, int NT, int WM, int WT, int COLS, int SLOTS, int AT_ONCE>
 void tiles(ProductArgs a, hipStream_t s) {
     constexpr int kM = 32 * MT * WM, kT = 32 * NT * WT;
     a.tiles = (a.channels + kM - 1) / kM;
     const int64_t items = (a.rows.count + kT - 1) / kT * a.tiles;
-    const int64_t most = rocket::most_groups(64 * WM * WT);
-    for (a.first = 0; a.first < items; a.first += most)
-        tile_kernel<DT, MT, NT, WM, WT, SLOTS><<<(uint32_t)std::min(items - a.first, most), 64 * WM * WT, 0, s>>>(a);
+    const int64_t groups = SPLIT ? items * a.parts : std::min(items, AT_ONCE * kCus);
+    tile_kernel<DT, SPLIT, MT, NT, WM, WT, COLS, SLOTS, AT_ONCE><<<(uint32_t)groups, 64 * WM * WT, 0, s>>>(a);
 }
 
 template <int DT>
-void launch(ProductArgs a, hipStream_t s) {
-    const int64_t big = (a.rows.count + 255) / 256 * ((a.channels + 255) / 256);
-    const int64_t middle = (a.rows.count + 127) / 128 * ((a.channels + 127) / 128);
-    if (big >= 200)
-        tiles<DT, 4, 4, 2, 2>(a, s);
-    else if (middle >= 200)
-        tiles<DT, 2, 2, 2, 2>(a, s);
-    else if (a.rows.count > 64)
-        tiles<DT, 1, 1, 2, 2>(a, s);
-    else {
-        a.tiles = (a.channels + kTile - 1) / kTile;
-        const int64_t items = (a.rows.count + kTile - 1) / kTile * a.tiles;
-        product_kernel<DT><<<(uint32_t)items, 256, 0, s>>>(a);
+void launch(ProductArgs a, const Cut &cut, hipStream_t s) {
+    a.parts = cut.parts, a.each = cut.each;
+    switch (cut.way) {
+    case kFew: {
+        const uint32_t groups = (uint32_t)((a.channels + kFewChannels - 1) / kFewChannels);
+        if (a.rows.count <= 16)
+            few_kernel<DT, 1><<<groups, 64 * kFewWaves, 0, s>>>(a);
+        else if (a.rows.count <= 32)
+            few_kernel<DT, 2><<<groups, 64 * kFewWaves, 0, s>>>(a);
+        else
+            few_kernel<DT, 4><<<groups, 64 * kFewWaves, 0, s>>>(a);
+        break;
+    }
+    case kBig: tiles<DT, false, 4, 4, 2, 2, 128, 2, 1>(a, s); break;
+    case kTall: tiles<DT, false, 4, 2, 2, 2, 128, 2, 1>(a, s); break;
+    case kMiddle: tiles<DT, false, 2, 2, 2, 2, 128, 3, 1>(a, s); break;
+    case kMiddleTwice: tiles<DT, false, 2, 2, 2, 2, 64, 3, 2>(a, s); break;
+    case kSmall: tiles<DT, false, 1, 1, 2, 2, 64, 4, 2>(a, s); break;
+    case kSplit: {
+        tiles<ROCKET_FLOAT32, true, 2, 2, 2, 2, 128, 3, 1>(a, s);
+        finish_kernel<DT><<<(uint32_t)((a.rows.count * a.channels + 255) / 256), 256, 0, s>>>(a);
+        break;
+    }
     }
 }
 
@@ -283,7 +465,7 @@ bool columns_ok(int64_t columns) { return columns > 0 && columns <= 131072 && co
 extern "C" rocket_status rocket_linear_bytes_workspace(const rocket_sequence_shape *shape, int64_t columns,
                                                   int64_t *bytes) {
     if (!bytes || !rocket::shape_ok(shape) || !columns_ok(columns)) return ROCKET_ERR_INVALID_ARG;
-    *bytes = 0;
+    *bytes = rocket::empty(shape) ? 0 : (cut_of(shape->n * shape->steps, shape->channels, columns).bytes + 7) / 8 * 8;
     return ROCKET_OK;
 }
 
@@ -296,7 +478,11 @@ extern "C" rocket_status rocket_linear_bytes(const rocket_sequence_shape *shape,
     if (!rocket::bytes_ok(q) || !rocket::floats_ok(scale) || !rocket::bytes_ok(weight) ||
         !rocket::floats_ok(weight_scale) || (bias && !rocket::floats_ok(bias)))
         return ROCKET_ERR_INVALID_ARG;
+    const Cut cut = cut_of(shape->n * shape->steps, shape->channels, columns);
+    if (cut.bytes && (!workspace || (uintptr_t)workspace % 8 != 0 || workspace_bytes < cut.bytes))
+        return ROCKET_ERR_INVALID_ARG;
     ProductArgs a = {};
+    a.sums = (int32_t *)workspace;
     a.q = q, a.p = weight, a.scale = scale, a.wscale = weight_scale, a.bias = bias;
     a.y = rocket::view_of(y, shape->dtype);
     a.columns = (int32_t)columns, a.channels = (int32_t)shape->channels;
@@ -304,10 +490,10 @@ extern "C" rocket_status rocket_linear_bytes(const rocket_sequence_shape *shape,
     a.rows = rocket::rows_of(shape, views, 1);
     hipStream_t s = (hipStream_t)hip_stream;
     if (shape->dtype == ROCKET_FLOAT32)
-        launch<ROCKET_FLOAT32>(a, s);
+        launch<ROCKET_FLOAT32>(a, cut, s);
     else if (shape->dtype == ROCKET_BFLOAT16)
-        launch<ROCKET_BFLOAT16>(a, s);
+        launch<ROCKET_BFLOAT16>(a, cut, s);
     else
-        launch<ROCKET_FLOAT16>(a, s);
+        launch<ROCKET_FLOAT16>(a, cut, s);
     return rocket::launched();
 }

@@ -260,6 +260,40 @@ def test_linear8(env, n, L, columns, N, with_lengths, dtype):
     assert torch.equal(again, y)
 
 
+# rows, columns, channels where each size of tile, and tiles whose columns are shared out,
+# cost least; last stages of 64 and of 128 columns, one stage, more tiles than run at once
+WAYS = [(20000, 192, 1100), (70001, 64, 513), (70000, 2048, 250), (6000, 2048, 1530), (9000, 320, 1000),
+        (1000, 1984, 1536), (30000, 256, 768), (100000, 128, 60), (1000, 20032, 190), (130, 20032, 70),
+        (65, 4096, 2000), (300, 8192, 33), (16100, 2048, 1536)]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("with_lengths", [False, True])
+@pytest.mark.parametrize("rows,columns,N", WAYS)
+def test_linear8_large(env, rows, columns, N, with_lengths, dtype):
+    """Against 64-bit products on the GPU, of the roundings that the oracle counts."""
+    torch, seq = env
+    g = torch.Generator(device="cuda").manual_seed(rows + columns + N)
+    rand8 = lambda *s: torch.randint(-127, 128, s, generator=g, device="cuda", dtype=torch.int8)  # noqa: E731
+    rand = lambda *s: torch.rand(*s, generator=g, device="cuda")  # noqa: E731
+    n = next(k for k in (7, 5, 4, 3, 2, 1) if rows % k == 0)
+    L = rows // n
+    q, p, scale, ws, b = rand8(n, L, columns), rand8(N, columns), 0.5 + rand(n, L), 0.01 + rand(N), rand(N) - 0.5
+    lengths, live = None, torch.ones(n, L, 1, dtype=torch.bool, device="cuda")
+    if with_lengths:
+        lengths = torch.randint(0, L + 1, (n,), generator=g, device="cuda", dtype=torch.int32)
+        live = (torch.arange(L, device="cuda")[None, :] < lengths[:, None])[:, :, None]
+        scale = scale.masked_fill(~live[:, :, 0], float("nan"))
+    y = seq.linear8(q, scale, p, ws, b, dtype=getattr(torch, dtype), lengths=lengths)
+    product = (q.view(rows, columns).double() @ p.double().t().contiguous()).view(n, L, N)
+    product = product * scale.double()[:, :, None] * ws.double()
+    want = product + b
+    tol = (3 * product.abs() + want.abs()) * lo.U
+    tol = tol * 1.01 + want.abs() * (2.0 ** -8 if dtype == "bfloat16" else lo.U) * 1.001 + 1e-30
+    ok = ((y.double() - want).abs() <= tol) & live | (y == 0) & ~live
+    assert ok.all(), torch.nonzero(~ok)[:4]
+
+
 def test_linear8_is_exact(env):
     """Whole numbers below 2^24 come out as they are: no rounding anywhere."""
     torch, seq = env
