@@ -36,7 +36,7 @@ struct GradArgs {
     int32_t m, c;
 };
 
-constexpr int kTile = 64, kSteps = 64;
+constexpr int kTile = 64, kRows = 64;
 
 // Parts of a value that 16-bit operands hold: fp32 is the sum of three bf16.
 template <int DT>
@@ -57,106 +57,6 @@ __device__ inline void split(typename Elem<DT>::raw x, uint16_t (&p)[kPlanes<DT>
         p[0] = x;
     }
 }
-
-// Matrix instruction 32 x 32 x 16: a lane holds 8 values of row (column) lane % 32,
-// those of the half lane / 32; the result as in linear8.hip.
-template <int DT>
-__global__ __launch_bounds__(256) void gradient_kernel(GradArgs a) {
-    using raw = typename Elem<DT>::raw;
-    constexpr int kP = kPlanes<DT>;
-    constexpr bool kHalf = DT == ROCKET_FLOAT16;
-    __shared__ uint16_t dy[kP][kSteps][kTile];
-    __shared__ __attribute__((aligned(8))) int8_t q[kTile][kSteps + 8];
-    const uint32_t across = (a.c + kTile - 1) / kTile, down = (a.m + kTile - 1) / kTile;
-    const uint32_t part_of = blockIdx.x / (across * down), tile = blockIdx.x % (across * down);
-    const int m0 = tile / across * kTile, c0 = tile % across * kTile;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wm = wave % 2 * 32, wc = wave / 2 * 32;
-    const int line = threadIdx.x / 4, part = threadIdx.x % 4 * 16;
-    const int c = c0 + wc + lane % 32;
-    Float16 total = {};
-    float bias = 0.0f;   // of channel m0 + threadIdx.x
-    const int64_t begin = part_of * a.each, end = begin + a.each < a.blocks ? begin + a.each : a.blocks;
-    for (int64_t b = begin; b < end; b++) {
-        Float16 sum = {};
-        for (int h = 0; h < kKeepRows; h += kSteps) {
-            const int64_t r = b * kKeepRows + h + line;
-            Place p = {};
-            if (r < a.rows.count) p = rocket::place_of(a.rows, r);
-            const raw *row = (const raw *)rocket::row_at(a.dy, p);
-            __syncthreads();
-            for (int e = 0; e < 16; e++) {
-                const int m = m0 + part + e;
-                uint16_t v[kP] = {};
-                if (p.live && m < a.m) split<DT>(row[m], v);
-#pragma unroll
-                for (int k = 0; k < kP; k++) dy[k][line][part + e] = v[k];
-            }
-            for (int e = 0; e < 16; e += 8) {
-                uint64_t v = 0;
-                if (c0 + line < a.c) v = *(const uint64_t *)(a.q + (b * a.c + c0 + line) * kKeepRows + h + part + e);
-                *(uint64_t *)&q[line][part + e] = v;
-            }
-            __syncthreads();
-            if (threadIdx.x < kTile && c0 == 0)
-                for (int t = 0; t < kSteps; t++)
-#pragma unroll
-                    for (int k = kP - 1; k >= 0; k--)
-                        bias += kHalf ? Elem<ROCKET_FLOAT16>::one(dy[k][t][threadIdx.x])
-                                      : Elem<ROCKET_BFLOAT16>::one(dy[k][t][threadIdx.x]);
-            for (int t = 0; t < kSteps; t += 16) {
-                const int t0 = t + lane / 32 * 8;
-                float f[8];
-#pragma unroll
-                for (int e = 0; e < 8; e++) f[e] = (float)q[wc + lane % 32][t0 + e];
-                if constexpr (kHalf) {
-                    Half8 fa, fb;
-#pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        fa[e] = __builtin_bit_cast(_Float16, dy[0][t0 + e][wm + lane % 32]);
-                        fb[e] = (_Float16)f[e];
-                    }
-                    sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa, fb, sum, 0, 0, 0);
-                } else {
-#pragma unroll
-                    for (int k = kP - 1; k >= 0; k--) {
-                        Bf8 fa, fb;
-#pragma unroll
-                        for (int e = 0; e < 8; e++) {
-                            fa[e] = __builtin_bit_cast(__bf16, dy[k][t0 + e][wm + lane % 32]);
-                            fb[e] = (__bf16)f[e];
-                        }
-                        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb, sum, 0, 0, 0);
-                    }
-                }
-            }
-        }
-        const float scale = c < a.c ? a.scale[b * a.c + c] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < 16; i++) total[i] = __builtin_fmaf(sum[i], scale, total[i]);
-    }
-    if (c < a.c)
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            const int m = m0 + wm + 8 * (i / 4) + 4 * (lane / 32) + i % 4;
-            if (m < a.m) a.dweight[((int64_t)part_of * a.m + m) * a.c + c] = total[i];
-        }
-    if (a.dbias && c0 == 0 && threadIdx.x < kTile && m0 + (int)threadIdx.x < a.m)
-        a.dbias[(int64_t)part_of * a.m + m0 + threadIdx.x] = bias;
-}
-
-// ------------------------------------------------------- many rows: staged tiles
-struct StagedArgs {
-    const char *dy;       // rows of 16-bit values at one distance, 4-byte aligned
-    int64_t dy_stride;    // bytes
-    int64_t dy_plane;     // bytes between the parts of fp32 values
-    const uint64_t *live; // a bit for each row, or null: all of them
-    const int8_t *q;
-    const float *scale;
-    float *dweight, *dbias;  // the parts' sums, [parts, m, c] and [parts, tiles along c, m]
-    int64_t rows, blocks, each;
-    int32_t m, c, tiles_m, tiles_c;
-    int32_t width;  // values of a row of dy: m, or m rounded up where it was laid out anew
-};
 
 typedef short Short4 __attribute__((ext_vector_type(4)));
 typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
@@ -193,6 +93,124 @@ __device__ inline Words4 turned(rocket::Shared p) {
     const uint64_t w0 = __builtin_bit_cast(uint64_t, v0), w1 = __builtin_bit_cast(uint64_t, v1);
     return Words4{(uint32_t)w0, (uint32_t)(w0 >> 32), (uint32_t)w1, (uint32_t)(w1 >> 32)};
 }
+
+// ------------------------------------------------------------ few rows: direct tiles
+// A tile of 64 x 64 by four wavefronts of one 32 x 32 matrix, 64 rows at a time: dy
+// comes through registers, where it is taken apart, to shared memory as it lies, q to
+// [c][64 rows]; the next rows are on their way meanwhile.  What bounds it is the way of
+// one such step, so everything is one launch.
+//
+// Matrix instruction 32 x 32 x 16: a lane holds 8 values of row (column) lane % 32,
+// those of the half lane / 32; the result as in linear8.hip.
+template <int DT>
+__global__ __launch_bounds__(256) void gradient_kernel(GradArgs a) {
+    using raw = typename Elem<DT>::raw;
+    constexpr int kP = kPlanes<DT>, kLineA = 2 * kTile + 16, kLineC = kRows + 16;
+    constexpr bool kHalf = DT == ROCKET_FLOAT16;
+    __shared__ __attribute__((aligned(16))) char dy[kP][kRows * kLineA], q[kTile * kLineC];
+    const uint32_t across = (a.c + kTile - 1) / kTile, down = (a.m + kTile - 1) / kTile;
+    const uint32_t part = blockIdx.x / (across * down), tile = blockIdx.x % (across * down);
+    const int m0 = tile / across * kTile, c0 = tile % across * kTile;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wm = wave % 2 * 32, wc = wave / 2 * 32;
+    const int line = threadIdx.x / 4, piece = threadIdx.x % 4 * 16;
+    const int group = lane / 16, in = lane % 16, half = lane / 32;
+    const int c = c0 + wc + lane % 32;
+    const int64_t begin = part * a.each, end = begin + a.each < a.blocks ? begin + a.each : a.blocks;
+    const int64_t last = end * kKeepRows < a.rows.count ? end * kKeepRows : a.rows.count;
+    raw x[16];
+    Words4 b;
+    const auto load = [&](int64_t row0) {
+        const int64_t r = row0 + line;
+        const int m = m0 + piece;
+        Place p = {};
+        if (r < a.rows.count) p = rocket::place_of(a.rows, r);
+        const raw *row = (const raw *)rocket::row_at(a.dy, p) + m;
+        if (p.live && m + 16 <= a.m) {
+            __builtin_memcpy(x, row, sizeof(x));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; e++) x[e] = p.live && m + e < a.m ? row[e] : raw(0);
+        }
+        b = Words4{0, 0, 0, 0};
+        if (c0 + line < a.c)
+            b = *(const Words4 *)(a.q + (row0 / kKeepRows * a.c + c0 + line) * kKeepRows + row0 % kKeepRows + piece);
+    };
+    const rocket::Shared from_a = rocket::shared_at(rocket::shared_address(dy) + (8 * half + in / 4) * kLineA +
+                                                    2 * (wm + 16 * (group & 1)) + in % 4 * 8);
+    const char *from_c = q + (wc + lane % 32) * kLineC + 8 * half;
+    Float16 total = {}, sum = {};
+    float bias = 0.0f;
+    if (begin * kKeepRows < last) load(begin * kKeepRows);
+    for (int64_t row0 = begin * kKeepRows; row0 < last; row0 += kRows) {
+        __syncthreads();
+        uint32_t v[kP][8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            uint16_t lo[kP], hi[kP];
+            split<DT>(x[2 * e], lo);
+            split<DT>(x[2 * e + 1], hi);
+#pragma unroll
+            for (int k = 0; k < kP; k++) v[k][e] = lo[k] | (uint32_t)hi[k] << 16;
+        }
+#pragma unroll
+        for (int k = 0; k < kP; k++)
+#pragma unroll
+            for (int e = 0; e < 8; e += 4)
+                *(Words4 *)(dy[k] + line * kLineA + 2 * piece + 4 * e) =
+                    Words4{v[k][e], v[k][e + 1], v[k][e + 2], v[k][e + 3]};
+        *(Words4 *)(q + line * kLineC + piece) = b;
+        __syncthreads();
+        if (row0 + kRows < last) load(row0 + kRows);
+#pragma unroll
+        for (int t = 0; t < kRows; t += 16) {
+            const uint64_t bytes = *(const uint64_t *)(from_c + t);
+            Words4 fb;
+#pragma unroll
+            for (int k = 0; k < 4; k++) fb[k] = widen<kHalf>((uint32_t)(bytes >> (32 * (k / 2))), k % 2);
+#pragma unroll
+            for (int k = kP - 1; k >= 0; k--) {
+                const Words4 fa = turned<kLineA>(from_a + k * kRows * kLineA + t * kLineA);
+                if (a.dbias && c0 == 0 && wc == 0)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) bias += value16<kHalf>(fa[e / 2], e % 2);
+                if constexpr (kHalf)
+                    sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(Half8, fa),
+                                                                 __builtin_bit_cast(Half8, fb), sum, 0, 0, 0);
+                else
+                    sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Bf8, fa),
+                                                                  __builtin_bit_cast(Bf8, fb), sum, 0, 0, 0);
+            }
+        }
+        if (row0 % kKeepRows == 0 && row0 + kRows < last) continue;
+        const float scale = c < a.c ? a.scale[row0 / kKeepRows * a.c + c] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; i++) total[i] = __builtin_fmaf(sum[i], scale, total[i]);
+        sum = Float16{};
+    }
+    if (c < a.c)
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const int m = m0 + wm + 8 * (i / 4) + 4 * half + i % 4;
+            if (m < a.m) a.dweight[((int64_t)part * a.m + m) * a.c + c] = total[i];
+        }
+    bias += __shfl_xor(bias, 32);
+    const int m = m0 + wm + lane;
+    if (a.dbias && c0 == 0 && wc == 0 && lane < 32 && m < a.m) a.dbias[(int64_t)part * a.m + m] = bias;
+}
+
+// ------------------------------------------------------- many rows: staged tiles
+struct StagedArgs {
+    const char *dy;       // rows of 16-bit values at one distance, 4-byte aligned
+    int64_t dy_stride;    // bytes
+    int64_t dy_plane;     // bytes between the parts of fp32 values
+    const uint64_t *live; // a bit for each row, or null: all of them
+    const int8_t *q;
+    const float *scale;
+    float *dweight, *dbias;  // the parts' sums, [parts, m, c] and [parts, tiles along c, m]
+    int64_t rows, blocks, each;
+    int32_t m, c, tiles_m, tiles_c;
+    int32_t width;  // values of a row of dy: m, or m rounded up where it was laid out anew
+};
 
 // A tile of dW: WM x WC wavefronts, each MT x NT matrices of 32 x 32.  A stage is
 // 64 rows: dy as it lies ([row][m], a row's 16-byte pieces moved by its number so
@@ -262,7 +280,8 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
         q_buffer = rocket::buffer_of(ask_q + half * 64, some ? has_c * kKeepRows - half * 64 : 0);
         // the scale of the next stage's block: it is looked at before that begins
         const bool after = s == 2 * PLANES - 1;
-        scale_buffer = rocket::buffer_of(ask_scale + (after ? a.c : 0), asked + (after ? 1 : 0) < stages ? has_c * 4 : 0);
+        scale_buffer =
+            rocket::buffer_of(ask_scale + (after ? a.c : 0), asked + (after ? 1 : 0) < stages ? has_c * 4 : 0);
         ask_to = base + ask_place * kStage;
         ask_place = ask_place == 2 ? 0 : ask_place + 1;
         if (LIVE) live = some ? a.live[(a.rows - ask_rows) / 64] : 0;
@@ -336,8 +355,9 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
         for (int k = 0; k < kLoads; k++) ask(k);
     }
     uint32_t at = base;
+    constexpr int kTogether = PLANES == 1 ? 2 : 1;   // stages written out one after the other
     for (int block = 0; block < stages; block += 2 * PLANES) {
-#pragma unroll
+#pragma unroll kTogether
         for (int s = 0; s < 2 * PLANES; s++) {
             const int stage = block + s;
             rocket::wait_loads<kLoads>();
@@ -354,8 +374,12 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
 #pragma unroll
             for (int k = 0; k < NT; k++)
                 bytes[0][k] = *(SharedWords)rocket::shared_at(at + read_c[k] + (half ^ turn_c) * 16);
-            fa[0] = turned<kM * 2>(from[0]);
-            fa[1] = turned<kM * 2>(from[1]);
+            const auto read_step = [&](int step) {
+                const int g = step / MT;
+                fa[step] = turned<kM * 2>(from[step % MT] + (32 * (g / 2) + 8 * (g % 2)) * (kM * 2));
+            };
+            read_step(0);
+            read_step(1);
 #pragma unroll
             for (int k = 0; k < NT; k++)
                 bytes[1][k] = *(SharedWords)rocket::shared_at(at + read_c[k] + (2 + half ^ turn_c) * 16);
@@ -378,10 +402,7 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
             for (int step = 0; step < kSteps; step++) {
                 const int group = step / MT, x = step % MT;
                 __builtin_amdgcn_sched_barrier(0);
-                if (step + 2 < kSteps) {
-                    const int g = (step + 2) / MT;
-                    fa[step + 2] = turned<kM * 2>(from[(step + 2) % MT] + (32 * (g / 2) + 8 * (g % 2)) * (kM * 2));
-                }
+                if (step + 2 < kSteps) read_step(step + 2);
 #pragma unroll
                 for (int y = 0; y < NT; y++) {
                     const uint32_t *w = wide[group % 2][y];
@@ -490,14 +511,49 @@ __global__ __launch_bounds__(256) void join_kernel(const float *parts, float *su
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= count) return;
     float v = 0.0f;
-    for (int k = 0; k < n; k++) v += parts[k * count + i];
+    int k = 0;
+    for (; k + 8 <= n; k += 8) {   // eight loads on their way
+        float x[8];
+#pragma unroll
+        for (int u = 0; u < 8; u++) x[u] = parts[(k + u) * count + i];
+#pragma unroll
+        for (int u = 0; u < 8; u++) v += x[u];
+    }
+    for (; k < n; k++) v += parts[k * count + i];
     sum[i] = v;
+}
+
+// The same of many short parts: 16 columns a workgroup, 16 parts at once.
+__global__ __launch_bounds__(256) void join_many_kernel(const float *parts, float *sum, int64_t m, int32_t n) {
+    __shared__ float shared[16][17];
+    const int col = threadIdx.x % 16, row = threadIdx.x / 16;
+    const int64_t c = (int64_t)blockIdx.x * 16 + col;
+    float v = 0.0f;
+    if (c < m)
+#pragma unroll 4
+        for (int k = row; k < n; k += 16) v += parts[k * m + c];
+    shared[row][col] = v;
+    __syncthreads();
+    if (threadIdx.x >= 16 || c >= m) return;
+    float t = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; k++) t += shared[k][col];
+    sum[c] = t;
+}
+
+// Many parts are of few sums, and those of few parts many (cut_parts).
+void join(const float *parts, float *sum, int64_t count, int32_t n, hipStream_t s) {
+    if (n > 32)
+        join_many_kernel<<<(uint32_t)((count + 15) / 16), 256, 0, s>>>(parts, sum, count, n);
+    else
+        join_kernel<<<(uint32_t)((count + 255) / 256), 256, 0, s>>>(parts, sum, count, n);
 }
 
 struct Cut {
     bool staged;
     bool lay;                // dy is laid out anew first
     int64_t blocks, each, parts;
+    int32_t tile_m;          // channels of dy in a tile; 256 of the checkpoint
     int64_t tiles_m, tiles_c;
     int64_t stride;          // bytes of a laid row
     int64_t at_live, at_bias, at_dy, bytes;   // places in the workspace: after the parts of dW
@@ -505,17 +561,18 @@ struct Cut {
 
 constexpr int64_t kCus = 256;
 
-// Parts of the rows, so that the workgroups fill the chip (`at_once` run at a
-// time) in rounds of which the last is not nearly empty; each part costs its
-// sums' way through memory.
-void cut_parts(Cut &c, int64_t tiles, int64_t at_once, double block_us, double part_us) {
+// The parts of the rows that cost least: workgroups in rounds of `at_once`, a block's
+// time in each, and the parts' sums' way through memory.  Times in microseconds.
+template <class Time>
+double cut_parts(Cut &c, Time time, double part_us) {
     double best = 1e300;
-    for (int64_t p = 1; p <= std::min<int64_t>(c.blocks, 64); p++) {
-        const int64_t each = (c.blocks + p - 1) / p, parts = (c.blocks + each - 1) / each;
-        const double us = (double)((tiles * parts + at_once - 1) / at_once) * (each * block_us + 5.0) +
-                          (parts > 1 ? parts * part_us + 5.0 : 0.0);
+    for (int64_t p = 1; p <= std::min<int64_t>(std::max<int64_t>(c.blocks, 1), 1024); p += 1 + p / 8) {
+        const int64_t each = std::max<int64_t>(1, (c.blocks + p - 1) / p);
+        const int64_t parts = std::max<int64_t>(1, (c.blocks + each - 1) / each);
+        const double us = time(each, parts) + (parts > 1 ? parts * (part_us + 0.02) + 6.0 : 0.0);
         if (us < best) best = us, c.each = each, c.parts = parts;
     }
+    return best;
 }
 
 bool fits(const rocket_sequence_shape *s, const View &dy) {
@@ -530,23 +587,35 @@ Cut cut_of(const rocket_sequence_shape *s, int64_t channels, const View &dy) {
     Cut c = {};
     const int64_t rows = s->n * s->steps, m = s->channels;
     c.blocks = (rows + kKeepRows - 1) / kKeepRows;
-    c.each = c.parts = 1;
-    c.staged = rows > 256;
     const int64_t planes = s->dtype == ROCKET_FLOAT32 ? 3 : 1;
-    if (c.staged) {
-        c.tiles_m = (m + 255) / 256, c.tiles_c = (channels + 255) / 256;
-        cut_parts(c, c.tiles_m * c.tiles_c, kCus, 2.2 * planes, (double)m * channels * 8 / 4e6);
+    const double part_us = (double)m * channels * 8 / 4e6;
+    // direct tiles: a block takes 1.7 us, or 1.05 us for each tile of a CU (1,000 rows of
+    // 192 by 2,000 and of 1,536 by 2,000), of fp32 1.9 times that
+    const int64_t tiles = ((m + kTile - 1) / kTile) * ((channels + kTile - 1) / kTile);
+    const auto direct = [&](int64_t each, int64_t parts) {
+        return 4.0 + each * (planes > 1 ? 1.9 : 1.0) * std::max(1.7, 1.05 * (double)(tiles * parts) / kCus);
+    };
+    const double direct_us = cut_parts(c, direct, part_us);
+    // staged tiles: two workgroups of the smaller ones run beside each other on a CU
+    Cut d = c;
+    d.tile_m = m <= 32 ? 32 : m <= 64 ? 64 : m <= 128 ? 128 : 256;
+    d.tiles_m = (m + d.tile_m - 1) / d.tile_m, d.tiles_c = (channels + 255) / 256;
+    d.lay = !fits(s, dy);
+    const int64_t at_once = d.tile_m <= 64 ? 2 * kCus : kCus;
+    const double block_us = d.tile_m == 256 ? 4.2 : d.tile_m == 128 ? 2.2 : d.tile_m == 64 ? 2.4 : 2.0;
+    const auto staged = [&](int64_t each, int64_t parts) {
+        return (double)((d.tiles_m * d.tiles_c * parts + at_once - 1) / at_once) * (each * block_us * planes + 5.0);
+    };
+    const double staged_us = cut_parts(d, staged, part_us) + (d.lay ? 9.0 : 6.0);
+    if (staged_us < direct_us) {
+        c = d;
+        c.staged = true;
         c.stride = (m + 7) / 8 * 16;
         c.at_bias = c.parts > 1 ? c.parts * m * channels * 4 : 0;
         c.at_live = (c.at_bias + c.parts * c.tiles_c * m * 4 + 15) / 16 * 16;
         c.at_dy = c.at_live + (c.blocks * 16 + 15) / 16 * 16;
-        c.lay = !fits(s, dy);
         c.bytes = c.at_dy + (c.lay ? planes * rows * c.stride : 0);
     } else {
-        const int64_t tiles = ((m + kTile - 1) / kTile) * ((channels + kTile - 1) / kTile);
-        c.parts = std::max<int64_t>(1, std::min<int64_t>(c.blocks, kCus / tiles));
-        c.each = std::max<int64_t>(1, (c.blocks + c.parts - 1) / c.parts);
-        c.parts = std::max<int64_t>(1, (c.blocks + c.each - 1) / c.each);
         c.at_bias = c.parts * m * channels * 4;
         c.bytes = c.parts > 1 ? c.at_bias + c.parts * m * 4 : 0;
     }
@@ -554,13 +623,25 @@ Cut cut_of(const rocket_sequence_shape *s, int64_t channels, const View &dy) {
     return c;
 }
 
-template <bool HALF, int PLANES>
-void staged_launch(const StagedArgs &a, int64_t parts, hipStream_t s) {
-    const uint32_t grid = (uint32_t)(parts * a.tiles_m * a.tiles_c);
+template <bool HALF, int PLANES, int MT, int WM>
+void staged_tiles(const StagedArgs &a, int64_t parts, hipStream_t s) {
+    const uint32_t grid = (uint32_t)(parts * a.tiles_m * a.tiles_c), threads = 64 * WM * 4;
     if (a.live)
-        staged_kernel<HALF, PLANES, PLANES == 1, 4, 2, 2, 4><<<grid, 512, 0, s>>>(a);
+        staged_kernel<HALF, PLANES, PLANES == 1, MT, 2, WM, 4><<<grid, threads, 0, s>>>(a);
     else
-        staged_kernel<HALF, PLANES, false, 4, 2, 2, 4><<<grid, 512, 0, s>>>(a);
+        staged_kernel<HALF, PLANES, false, MT, 2, WM, 4><<<grid, threads, 0, s>>>(a);
+}
+
+template <bool HALF, int PLANES>
+void staged_launch(const StagedArgs &a, const Cut &cut, hipStream_t s) {
+    if (cut.tile_m == 32)
+        staged_tiles<HALF, PLANES, 1, 1>(a, cut.parts, s);
+    else if (cut.tile_m == 64)
+        staged_tiles<HALF, PLANES, 2, 1>(a, cut.parts, s);
+    else if (cut.tile_m == 128)
+        staged_tiles<HALF, PLANES, 4, 1>(a, cut.parts, s);
+    else
+        staged_tiles<HALF, PLANES, 4, 2>(a, cut.parts, s);
 }
 
 bool sizes_ok(const rocket_sequence_shape *s, int64_t channels) {
@@ -624,11 +705,11 @@ extern "C" rocket_status rocket_linear_weight_gradient(const rocket_sequence_sha
             }
         }
         if (shape->dtype == ROCKET_FLOAT32)
-            staged_launch<false, 3>(a, cut.parts, s);
+            staged_launch<false, 3>(a, cut, s);
         else if (shape->dtype == ROCKET_BFLOAT16)
-            staged_launch<false, 1>(a, cut.parts, s);
+            staged_launch<false, 1>(a, cut, s);
         else
-            staged_launch<true, 1>(a, cut.parts, s);
+            staged_launch<true, 1>(a, cut, s);
     } else {
         GradArgs a = {};
         a.rows = rows, a.dy = dy_view, a.q = q, a.scale = scale, a.m = m, a.c = c;
@@ -643,10 +724,8 @@ extern "C" rocket_status rocket_linear_weight_gradient(const rocket_sequence_sha
         else
             gradient_kernel<ROCKET_FLOAT16><<<grid, 256, 0, s>>>(a);
     }
-    if (cut.parts > 1)
-        join_kernel<<<(uint32_t)((count + 255) / 256), 256, 0, s>>>(parts, dweight, count, (int32_t)cut.parts);
+    if (cut.parts > 1) join(parts, dweight, count, (int32_t)cut.parts, s);
     if (dbias && (cut.staged || cut.parts > 1))
-        join_kernel<<<(uint32_t)((m + 255) / 256), 256, 0, s>>>((const float *)(work + cut.at_bias), dbias, m,
-                                                                (int32_t)biases);
+        join((const float *)(work + cut.at_bias), dbias, m, (int32_t)biases, s);
     return rocket::launched();
 }
