@@ -477,6 +477,66 @@ def test_weight_gradient_error_of_many_rows(env, dtype):
     assert float((db.double() - want).norm() / want.norm()) < 1e-6
 
 
+# many rows: staged tiles of 32, 64, 128 and 256 channels of dy, whole and cut off; dy laid
+# out anew (odd channels, fp32)
+MANY = [(40000, 20, 3000), (40000, 50, 3000), (30000, 128, 2000), (30000, 300, 1000), (30011, 301, 999),
+        (40003, 17, 3001)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kind", ["plain", "ragged", "far"])
+@pytest.mark.parametrize("rows,N,C", MANY)
+def test_weight_gradient_many_rows(env, rows, N, C, kind, dtype):
+    """Against 64-bit products on the GPU, within the oracle's bound.  far: blocks whose
+    scales differ by 2^60 and more, scales of 0 over values that are not."""
+    torch, seq = env
+    g = torch.Generator(device="cuda").manual_seed(rows + N + C)
+    n = next(k for k in (8, 7, 3, 1) if rows % k == 0) if kind == "ragged" else 1
+    L, blocks = rows // n, -(-rows // 128)
+    q = torch.randint(-127, 128, (blocks, C, 128), generator=g, device="cuda", dtype=torch.int8)
+    scale = torch.rand(blocks, C, generator=g, device="cuda") + 0.5
+    if kind == "far":
+        scale *= 2.0 ** torch.randint(-40, 40, (blocks, C), generator=g, device="cuda").float()
+        scale[torch.rand(blocks, C, generator=g, device="cuda") < 0.2] = 0.0
+        scale[:, C // 2:] = 1.0 + scale[:, C // 2:].clamp(max=1.0)
+    dy = torch.randn(n, L, N, generator=g, device="cuda").to(getattr(torch, dtype))
+    lengths, live = None, torch.ones(n, L, 1, dtype=torch.bool, device="cuda")
+    if kind == "ragged":
+        lengths = torch.randint(0, L + 1, (n,), generator=g, device="cuda", dtype=torch.int32)
+        live = (torch.arange(L, device="cuda")[None, :] < lengths[:, None])[:, :, None]
+        dy.masked_fill_(~live, float("nan"))
+    dw, db = seq.linear_weight_gradient(dy, q, scale, lengths=lengths)
+    d = torch.where(live, dy.double(), 0.0).view(rows, N)
+    x = (q.double() * scale.double()[:, :, None]).transpose(1, 2).reshape(-1, C)[:rows]
+    want = d.t().contiguous() @ x
+    # a product enters a block's sum of at most 384, rounded or cut off, then at most
+    # `blocks` sums and multiplications and as many joins
+    units = 2 * 384 + 4 * blocks
+    tol = (d.abs().t().contiguous() @ x.abs()) * units * lo.U
+    assert ((dw.double() - want).abs() <= tol).all()
+    if kind != "far":   # and by far less as a whole: each rounding at random
+        assert float((dw.double() - want).norm() / want.norm()) < 1e-6
+    want = d.sum(0)
+    assert ((db.double() - want).abs() <= d.abs().sum(0) * 3 * rows * lo.U).all()
+    assert float((db.double() - want).norm() / want.norm()) < 1e-6
+    again = seq.linear_weight_gradient(dy, q, scale, lengths=lengths)
+    assert torch.equal(dw, again[0]) and torch.equal(db, again[1])
+
+
+def test_weight_gradient_many_rows_nothing_finite(env):
+    """NaN scales and infinite dy reach their column and row, and no others."""
+    torch, seq = env
+    dy = torch.randn(30000, 256, device="cuda").bfloat16()
+    q, scale = seq.checkpoint(torch.randn(30000, 512, device="cuda"))
+    want = seq.linear_weight_gradient(dy, q, scale)
+    scale[100, 11], scale[0, 12], scale[234, 13] = float("nan"), float("nan"), float("nan")
+    dy[20000, 9] = float("inf")
+    dw, db = seq.linear_weight_gradient(dy, q, scale)
+    assert dw[:, 11:14].isnan().all() and torch.isinf(db[9]) and not torch.isfinite(dw[9]).any()
+    rest_m, rest_c = [m for m in range(256) if m != 9], [c for c in range(512) if not 11 <= c <= 13]
+    assert torch.equal(dw[rest_m][:, rest_c], want[0][rest_m][:, rest_c]) and torch.equal(db[rest_m], want[1][rest_m])
+
+
 # -------------------------------------------------------------- all of them
 def block(seq, x, r, w, wq, ws, b, lengths=None, dtype=None):
     """Norm in 8 bits, product, checkpoint of the sum: a layer's forward pass."""
