@@ -70,11 +70,27 @@ __device__ inline void store4(char *row, int c, int channels, const float (&f)[4
         if (c + e < channels) ((raw *)row)[c + e] = Elem<DT>::round(f[e]);
 }
 
+// Where the rows of a block lie: 0 where there is none, the lowest bit set where it holds
+// no data.  A row's place takes a division, so a thread finds one for all.
+__device__ inline void look_up(const KeepArgs &a, int64_t block, uint64_t *rows) {
+    if (threadIdx.x < kKeepRows) {
+        const int64_t r = block * kKeepRows + threadIdx.x;
+        uint64_t at = 0;
+        if (r < a.rows.count) {
+            const Place p = rocket::place_of(a.rows, r);
+            at = (uint64_t)rocket::row_at(a.x, p) | (p.live ? 0 : 1);
+        }
+        rows[threadIdx.x] = at;
+    }
+    __syncthreads();
+}
+
 // Item: a tile of 64 channels of a block.  Thread: quad (4 channels) and band
 // (rows 4 band .. 4 band + 3 of both halves of the block).
 template <int DT>
 __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a) {
     __shared__ uint32_t tops[kBands][kChannels];
+    __shared__ uint64_t rows[kKeepRows];
     __shared__ __attribute__((aligned(16))) uint8_t turned[kChannels * kRow];
     const int64_t item = a.first + rocket::item_of_block();
     const int64_t block = item / a.tiles;
@@ -82,13 +98,12 @@ __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a) {
     const int c = c0 + 4 * quad;
     float f[8][4];
     uint32_t top[4] = {0, 0, 0, 0};
+    look_up(a, block, rows);
 #pragma unroll
     for (int k = 0; k < 8; k++) {
-        const int64_t r = block * kKeepRows + (k / 4) * 64 + 4 * band + k % 4;
-        Place p = {};
-        if (r < a.rows.count) p = rocket::place_of(a.rows, r);
-        if (p.live && c < a.channels) {
-            load4<DT>(rocket::row_at(a.x, p), c, a.channels, f[k]);
+        const uint64_t at = rows[(k / 4) * 64 + 4 * band + k % 4];
+        if (at != 0 && !(at & 1) && c < a.channels) {
+            load4<DT>((const char *)at, c, a.channels, f[k]);
         } else {
 #pragma unroll
             for (int e = 0; e < 4; e++) f[k][e] = 0.0f;
@@ -133,6 +148,7 @@ __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a) {
 template <int DT>
 __global__ __launch_bounds__(kThreads) void restore_kernel(KeepArgs a) {
     __shared__ __attribute__((aligned(16))) uint8_t turned[kChannels * kRow];
+    __shared__ uint64_t rows[kKeepRows];
     const int64_t item = a.first + rocket::item_of_block();
     const int64_t block = item / a.tiles;
     const int c0 = (int)(item - block * a.tiles) * kChannels, quad = threadIdx.x % kQuads, band = threadIdx.x / kQuads;
@@ -150,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void restore_kernel(KeepArgs a) {
     float scale[4];
 #pragma unroll
     for (int e = 0; e < 4; e++) scale[e] = c + e < a.channels ? a.scale[block * a.channels + c + e] : 0.0f;
-    __syncthreads();
+    look_up(a, block, rows);
     if (c >= a.channels) return;
 #pragma unroll
     for (int h = 0; h < 2; h++) {
@@ -160,18 +176,17 @@ __global__ __launch_bounds__(kThreads) void restore_kernel(KeepArgs a) {
             w[e] = c + e < a.channels ? *(const uint32_t *)(turned + (4 * quad + e) * kRow + h * 64 + 4 * band) : 0u;
 #pragma unroll
         for (int k = 0; k < 4; k++) {
-            const int64_t r = block * kKeepRows + h * 64 + 4 * band + k;
-            if (r >= a.rows.count) continue;
-            const Place p = rocket::place_of(a.rows, r);
+            const uint64_t at = rows[h * 64 + 4 * band + k];
+            if (at == 0) continue;
             float f[4];
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                f[e] = p.live ? (float)(int8_t)(w[e] >> 8 * k) * scale[e] : 0.0f;
+                f[e] = !(at & 1) ? (float)(int8_t)(w[e] >> 8 * k) * scale[e] : 0.0f;
                 // the fp32 product is rounded before the type's rounding: fp16 is what
                 // fp32's result rounds to (the compiler would make one instruction of both)
                 if (DT == ROCKET_FLOAT16) asm("" : "+v"(f[e]));
             }
-            store4<DT>(rocket::row_at(a.x, p), c, a.channels, f);
+            store4<DT>((char *)(at & ~(uint64_t)1), c, a.channels, f);
         }
     }
 }

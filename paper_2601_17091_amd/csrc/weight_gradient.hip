@@ -470,9 +470,11 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
 
 // A bit for each row: whether it holds data.
 __global__ __launch_bounds__(256) void live_kernel(Rows rows, uint64_t *live) {
-    const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint64_t bits = __ballot(r < rows.count && rocket::place_of(rows, r).live);
-    if (threadIdx.x % 64 == 0 && r < rows.count) live[r / 64] = bits;
+    for (int64_t first = (int64_t)blockIdx.x * 256; first < rows.count; first += (int64_t)gridDim.x * 256) {
+        const int64_t r = first + threadIdx.x;
+        const uint64_t bits = __ballot(r < rows.count && rocket::place_of(rows, r).live);
+        if (threadIdx.x % 64 == 0 && r < rows.count) live[r / 64] = bits;
+    }
 }
 
 // dy's rows laid out for the staged kernel: 16-bit parts, 16-byte aligned rows,
@@ -689,7 +691,7 @@ extern "C" rocket_status rocket_linear_weight_gradient(const rocket_sequence_sha
             a.dy = dy_view.data, a.dy_stride = shape->steps == 1 ? dy_view.series : dy_view.step;
             if (rows.lengths) {
                 a.live = (const uint64_t *)(work + cut.at_live);
-                const uint32_t grid = (uint32_t)((rows.count + 255) / 256);
+                const uint32_t grid = (uint32_t)std::min<int64_t>((rows.count + 255) / 256, 8 * kCus);
                 live_kernel<<<grid, 256, 0, s>>>(rows, (uint64_t *)(work + cut.at_live));
             }
         } else {
