@@ -577,11 +577,13 @@ double cut_parts(Cut &c, Time time, double part_us) {
     return best;
 }
 
+// Whether dy's rows are read as they lie: at one distance that lets no row reach into
+// the next (those past the last one are told by where they would lie), 4-byte aligned.
 bool fits(const rocket_sequence_shape *s, const View &dy) {
     const bool one = s->n == 1 || s->steps == 1 || dy.series == s->steps * dy.step;
     const int64_t step = s->steps == 1 ? dy.series : dy.step;
-    return one && s->dtype != ROCKET_FLOAT32 && s->channels % 2 == 0 && step % 4 == 0 && (uintptr_t)dy.data % 4 == 0 &&
-           step <= (1 << 24);
+    return one && s->dtype != ROCKET_FLOAT32 && s->channels % 2 == 0 && step % 4 == 0 && step >= s->channels * 2 &&
+           (uintptr_t)dy.data % 4 == 0 && step <= (1 << 24);
 }
 
 // How a call is cut.
@@ -608,7 +610,10 @@ Cut cut_of(const rocket_sequence_shape *s, int64_t channels, const View &dy) {
     const auto staged = [&](int64_t each, int64_t parts) {
         return (double)((d.tiles_m * d.tiles_c * parts + at_once - 1) / at_once) * (each * block_us * planes + 5.0);
     };
-    const double staged_us = cut_parts(d, staged, part_us) + (d.lay ? 9.0 : 6.0);
+    // by the shape alone, not by whether these rows have to be laid out anew: results do
+    // not change with strides and alignment
+    const bool anew = planes > 1 || m % 2 != 0;
+    const double staged_us = cut_parts(d, staged, part_us) + (anew ? 9.0 : 6.0);
     if (staged_us < direct_us) {
         c = d;
         c.staged = true;

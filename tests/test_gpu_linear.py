@@ -264,7 +264,7 @@ def test_linear8(env, n, L, columns, N, with_lengths, dtype):
 # cost least; last stages of 64 and of 128 columns, one stage, more tiles than run at once
 WAYS = [(20000, 192, 1100), (70001, 64, 513), (70000, 2048, 250), (6000, 2048, 1530), (9000, 320, 1000),
         (1000, 1984, 1536), (30000, 256, 768), (100000, 128, 60), (1000, 20032, 190), (130, 20032, 70),
-        (65, 4096, 2000), (300, 8192, 33), (16100, 2048, 1536)]
+        (65, 4096, 2000), (300, 8192, 33), (16100, 1984, 1536), (33000, 1984, 1030), (65000, 64, 2000)]
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
@@ -521,6 +521,30 @@ def test_weight_gradient_many_rows(env, rows, N, C, kind, dtype):
     assert float((db.double() - want).norm() / want.norm()) < 1e-6
     again = seq.linear_weight_gradient(dy, q, scale, lengths=lengths)
     assert torch.equal(dw, again[0]) and torch.equal(db, again[1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("first,N", [(0, 300), (1, 300), (2, 301), (7, 299)])
+def test_weight_gradient_many_rows_of_wider_ones(env, first, N, dtype):
+    """dy as columns of a wider matrix, rows turned about: aligned to a value only, as they
+    stand or laid out anew; NaN beside them does not reach the result."""
+    torch, seq = env
+    wide = torch.full((200, 150, 312), float("nan"), device="cuda").to(getattr(torch, dtype))
+    dy = wide[:, :, first:first + N]
+    dy.copy_(torch.randn(200, 150, N, device="cuda"))
+    q, scale = seq.checkpoint(torch.randn(30000, 520, device="cuda"))
+    want = seq.linear_weight_gradient(dy.contiguous(), q, scale)
+    for a, b in zip(want, seq.linear_weight_gradient(dy, q, scale)):
+        assert torch.equal(a, b)
+    turned = dy.transpose(0, 1)
+    want = seq.linear_weight_gradient(turned.contiguous(), q, scale)
+    for a, b in zip(want, seq.linear_weight_gradient(turned, q, scale)):
+        assert torch.equal(a, b)
+    # one row for all of them
+    same_row = dy[3, 4].expand(200, 150, N)
+    for a, b in zip(seq.linear_weight_gradient(same_row.contiguous(), q, scale),
+                    seq.linear_weight_gradient(same_row, q, scale)):
+        assert torch.equal(a, b)
 
 
 def test_weight_gradient_many_rows_nothing_finite(env):
