@@ -43,6 +43,7 @@ stream is the caller's to order and to keep alive (Tensor.record_stream).
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -447,6 +448,33 @@ def _bytes8(t, like, name: str, shape=None):
     return t.data_ptr()
 
 
+# Workspaces' sizes, which go by sizes, types, strides and alignment alone.
+@functools.lru_cache(4096)
+def _rms_norm_size(n: int, steps: int, channels: int, dtype: int) -> int:
+    size, shape = ctypes.c_int64(), CSequenceShape(n, steps, channels, dtype, None)
+    rocket._check(rocket.library().rocket_rms_norm_workspace(_byref(shape), _byref(size)), "rocket_rms_norm_workspace")
+    return size.value
+
+
+@functools.lru_cache(4096)
+def _linear8_size(n: int, steps: int, channels: int, dtype: int, columns: int) -> int:
+    size, shape = ctypes.c_int64(), CSequenceShape(n, steps, channels, dtype, None)
+    rocket._check(rocket.library().rocket_linear_bytes_workspace(_byref(shape), columns, _byref(size)),
+                  "rocket_linear_bytes_workspace")
+    return size.value
+
+
+@functools.lru_cache(4096)
+def _weight_gradient_size(n: int, steps: int, channels: int, dtype: int, kept: int, series: int, step: int,
+                          aligned: int) -> int:
+    size, shape = ctypes.c_int64(), CSequenceShape(n, steps, channels, dtype, None)
+    view = CSequence(4096 + aligned, series, step)   # an address of that alignment: nothing is read
+    rocket._check(rocket.library().rocket_linear_weight_gradient_workspace(_byref(shape), kept, _byref(view),
+                                                                           _byref(size)),
+                  "rocket_linear_weight_gradient_workspace")
+    return size.value
+
+
 def _pad8(channels: int) -> int:
     return -(-channels // ROWS8_PAD) * ROWS8_PAD
 
@@ -481,7 +509,7 @@ def rms_norm(x, weight=None, *, residual=None, eps: float = 1e-5, lengths=None, 
     if out is None:
         out = _dense(x)
     total = x if residual is None else _dense(x) if total_out is None else total_out
-    rstd = _empty(x.shape[:-1], dtype=_f32, device=x.device)
+    rstd = _empty(*x.shape[:-1], dtype=_f32, device=x.device)
     status = lib.rocket_rms_norm_forward(
         _byref(shape), _byref(_rows_view(x, "x")), _optional_rows(residual, "residual"), w, eps,
         _byref(_rows_view(out, "out")), None if residual is None else _byref(_rows_view(total, "total_out")),
@@ -504,7 +532,7 @@ def rms_norm8(x, weight=None, *, residual=None, eps: float = 1e-5, lengths=None,
     total = x if residual is None else _dense(x) if total_out is None else total_out
     rows = x.shape[:-1]
     q = _empty(*rows, _pad8(x.shape[-1]), dtype=torch.int8, device=x.device)
-    scale = _empty(rows, dtype=_f32, device=x.device)
+    scale = _empty(*rows, dtype=_f32, device=x.device)
     rstd = _dense(scale)
     status = lib.rocket_rms_norm_bytes_forward(
         _byref(shape), _byref(_rows_view(x, "x")), _optional_rows(residual, "residual"), w, eps, q.data_ptr(),
@@ -537,13 +565,12 @@ def rms_norm_backward(dy, total, rstd, weight=None, *, dtotal=None, lengths=None
     given = out
     if out is None:
         out = _dense(total)
-    size = ctypes.c_int64()
-    rocket._check(lib.rocket_rms_norm_workspace(_byref(shape), _byref(size)), "rocket_rms_norm_workspace")
+    size = _rms_norm_size(shape.n, shape.steps, shape.channels, shape.dtype)
     dweight = _empty(total.shape[-1], dtype=_f32, device=total.device)
-    work, at = _workspace(size.value, total.device)
+    work, at = _workspace(size, total.device)
     status = lib.rocket_rms_norm_backward(
         _byref(shape), _byref(_rows_view(dy, "dy")), _byref(_rows_view(total, "total")), w, r,
-        _optional_rows(dtotal, "dtotal"), _byref(_rows_view(out, "out")), dweight.data_ptr(), at, size.value,
+        _optional_rows(dtotal, "dtotal"), _byref(_rows_view(out, "out")), dweight.data_ptr(), at, size,
         _stream(total.get_device()))
     rocket._check(status, "rocket_rms_norm_backward")
     if given is not None:
@@ -561,7 +588,7 @@ def quantize_rows(x, *, lengths=None, stream=None):
     shape = _rows_shape(x, lengths, "x")
     _unrecorded(x)
     q = _empty(*x.shape[:-1], _pad8(x.shape[-1]), dtype=torch.int8, device=x.device)
-    scale = _empty(x.shape[:-1], dtype=_f32, device=x.device)
+    scale = _empty(*x.shape[:-1], dtype=_f32, device=x.device)
     status = lib.rocket_quantize_rows(_byref(shape), _byref(_rows_view(x, "x")), q.data_ptr(), scale.data_ptr(),
                                       _stream(x.get_device()))
     rocket._check(status, "rocket_quantize_rows")
@@ -592,7 +619,7 @@ def _steps_pointer(lengths, leading, like):
 def _result(out, shape, dtype, like):
     """`out` checked, or a new tensor."""
     if out is None:
-        return _empty(shape, dtype=dtype, device=like.device)
+        return _empty(*shape, dtype=dtype, device=like.device)
     if not isinstance(out, torch.Tensor) or not out.is_cuda:
         raise TypeError("out must be a torch tensor on the GPU")
     if out.shape != shape or out.dtype != dtype or out.get_device() != like.get_device():
@@ -628,12 +655,10 @@ def linear8(q, scale, wq, wscale, bias=None, *, dtype=None, lengths=None, out=No
     out = _result(out, (*leading, channels), dtype, q)
     n, rows = leading if len(leading) == 2 else (1, leading[0])
     shape = CSequenceShape(n, rows, channels, code, steps)
-    size = ctypes.c_int64()
-    rocket._check(lib.rocket_linear_bytes_workspace(_byref(shape), columns, _byref(size)),
-                  "rocket_linear_bytes_workspace")
-    work, at = _workspace(size.value, q.device)
+    size = _linear8_size(n, rows, channels, code, columns)
+    work, at = _workspace(size, q.device)
     status = lib.rocket_linear_bytes(_byref(shape), columns, at_q, at_scale, at_w, at_wscale, at_bias,
-                                _byref(_rows_view(out, "out")), at, size.value, _stream(q.get_device()))
+                                _byref(_rows_view(out, "out")), at, size, _stream(q.get_device()))
     rocket._check(status, "rocket_linear_bytes")
     if given is not None:
         _written(given)
@@ -708,14 +733,14 @@ def linear_weight_gradient(dy, q, scale, *, lengths=None, stream=None):
     if q.get_device() != dy.get_device():
         raise ValueError("q must be on dy's GPU")
     _unrecorded(dy, scale)
-    size, view = ctypes.c_int64(), _rows_view(dy, "dy")
-    rocket._check(lib.rocket_linear_weight_gradient_workspace(_byref(shape), channels, _byref(view), _byref(size)),
-                  "rocket_linear_weight_gradient_workspace")
+    view = _rows_view(dy, "dy")
+    size = _weight_gradient_size(shape.n, shape.steps, shape.channels, shape.dtype, channels, view.series_stride,
+                                 view.step_stride, (view.data or 0) % 16)
     dweight = _empty(dy.shape[-1], channels, dtype=_f32, device=dy.device)
     dbias = _empty(dy.shape[-1], dtype=_f32, device=dy.device)
-    work, at = _workspace(size.value, dy.device)
+    work, at = _workspace(size, dy.device)
     status = lib.rocket_linear_weight_gradient(_byref(shape), channels, _byref(view), at_q, at_scale,
-                                               dweight.data_ptr(), dbias.data_ptr(), at, size.value,
+                                               dweight.data_ptr(), dbias.data_ptr(), at, size,
                                                _stream(dy.get_device()))
     rocket._check(status, "rocket_linear_weight_gradient")
     return dweight, dbias
