@@ -508,47 +508,58 @@ __global__ __launch_bounds__(256) void lay_kernel(Rows rows, View dy, int32_t m,
     for (int k = 0; k < kPlanes<DT>; k++) rocket::store_at(to + k * plane + i * 8, __builtin_bit_cast(Words4, v[k]));
 }
 
-// Sums of the parts, in their order.
-__global__ __launch_bounds__(256) void join_kernel(const float *parts, float *sum, int64_t count, int32_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= count) return;
-    float v = 0.0f;
-    int k = 0;
-    for (; k + 8 <= n; k += 8) {   // eight loads on their way
-        float x[8];
-#pragma unroll
-        for (int u = 0; u < 8; u++) x[u] = parts[(k + u) * count + i];
-#pragma unroll
-        for (int u = 0; u < 8; u++) v += x[u];
-    }
-    for (; k < n; k++) v += parts[k * count + i];
-    sum[i] = v;
+// Sums of `n` parts of `count` values, in an order of their own: few parts by a thread
+// a value, many parts (which are of few values: cut_parts) by 16 threads a value.
+struct Sums {
+    const float *parts;
+    float *sum;
+    int64_t count;
+    int32_t n;
+    uint32_t groups;   // workgroups that it takes
+};
+
+constexpr int kMany = 32;
+
+Sums sums_of(const float *parts, float *sum, int64_t count, int64_t n) {
+    const int64_t each = n > kMany ? 16 : 256;
+    return Sums{parts, sum, count, (int32_t)n, n > 1 || parts != sum ? (uint32_t)((count + each - 1) / each) : 0};
 }
 
-// The same of many short parts: 16 columns a workgroup, 16 parts at once.
-__global__ __launch_bounds__(256) void join_many_kernel(const float *parts, float *sum, int64_t m, int32_t n) {
+// Two of them in one launch.
+__global__ __launch_bounds__(256) void join_kernel(Sums a, Sums b) {
     __shared__ float shared[16][17];
+    const bool second = blockIdx.x >= a.groups;
+    const Sums s = second ? b : a;
+    const int64_t group = second ? blockIdx.x - a.groups : blockIdx.x;
+    if (s.n <= kMany) {
+        const int64_t i = group * 256 + threadIdx.x;
+        if (i >= s.count) return;
+        float v = 0.0f;
+        int k = 0;
+        for (; k + 8 <= s.n; k += 8) {   // eight loads on their way
+            float x[8];
+#pragma unroll
+            for (int u = 0; u < 8; u++) x[u] = s.parts[(k + u) * s.count + i];
+#pragma unroll
+            for (int u = 0; u < 8; u++) v += x[u];
+        }
+        for (; k < s.n; k++) v += s.parts[k * s.count + i];
+        s.sum[i] = v;
+        return;
+    }
     const int col = threadIdx.x % 16, row = threadIdx.x / 16;
-    const int64_t c = (int64_t)blockIdx.x * 16 + col;
+    const int64_t c = group * 16 + col;
     float v = 0.0f;
-    if (c < m)
+    if (c < s.count)
 #pragma unroll 4
-        for (int k = row; k < n; k += 16) v += parts[k * m + c];
+        for (int k = row; k < s.n; k += 16) v += s.parts[k * s.count + c];
     shared[row][col] = v;
     __syncthreads();
-    if (threadIdx.x >= 16 || c >= m) return;
+    if (threadIdx.x >= 16 || c >= s.count) return;
     float t = 0.0f;
 #pragma unroll
     for (int k = 0; k < 16; k++) t += shared[k][col];
-    sum[c] = t;
-}
-
-// Many parts are of few sums, and those of few parts many (cut_parts).
-void join(const float *parts, float *sum, int64_t count, int32_t n, hipStream_t s) {
-    if (n > 32)
-        join_many_kernel<<<(uint32_t)((count + 15) / 16), 256, 0, s>>>(parts, sum, count, n);
-    else
-        join_kernel<<<(uint32_t)((count + 255) / 256), 256, 0, s>>>(parts, sum, count, n);
+    s.sum[c] = t;
 }
 
 struct Cut {
@@ -731,8 +742,10 @@ extern "C" rocket_status rocket_linear_weight_gradient(const rocket_sequence_sha
         else
             gradient_kernel<ROCKET_FLOAT16><<<grid, 256, 0, s>>>(a);
     }
-    if (cut.parts > 1) join(parts, dweight, count, (int32_t)cut.parts, s);
+    const Sums first = sums_of(parts, dweight, count, cut.parts);
+    Sums second = {};
     if (dbias && (cut.staged || cut.parts > 1))
-        join((const float *)(work + cut.at_bias), dbias, m, (int32_t)biases, s);
+        second = sums_of((const float *)(work + cut.at_bias), dbias, m, biases);
+    if (first.groups + second.groups > 0) join_kernel<<<first.groups + second.groups, 256, 0, s>>>(first, second);
     return rocket::launched();
 }
