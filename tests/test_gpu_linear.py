@@ -479,8 +479,8 @@ def test_weight_gradient_error_of_many_rows(env, dtype):
 
 # many rows: staged tiles of 32, 64, 128 and 256 channels of dy, whole and cut off; dy laid
 # out anew (odd channels, fp32)
-MANY = [(40000, 20, 3000), (40000, 50, 3000), (30000, 128, 2000), (30000, 300, 1000), (30011, 301, 999),
-        (40003, 17, 3001)]
+MANY = [(40000, 20, 3000), (40000, 50, 3000), (30000, 128, 2000), (30000, 300, 1000), (30009, 301, 999),
+        (40005, 17, 3001), (50001, 63, 2000), (20001, 129, 2500)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
