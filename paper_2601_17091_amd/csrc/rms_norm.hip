@@ -8,11 +8,16 @@
 //   gradient: g = dy w,  dx = k (g - s k mean(g s k)) + dtotal,  dw = sum over rows of dy s k
 //
 // Bound: HBM; a value takes some ten operations.  So a row is read once and
-// stays in the registers of G threads (16 of them to a workgroup), 16 bytes a
-// thread and load, up to 24,576 channels; a workgroup goes from row to row with
-// the weights in registers.  Wider rows are read twice.  The backward pass sums
-// dw over its rows in registers, a second kernel joins the workgroups' sums in
-// a fixed order.
+// stays in the registers of G threads (at least 16), 16 bytes a thread and load,
+// up to 24,576 channels; wider rows are read twice.  The backward pass sums dw
+// over a workgroup's rows in registers, a second kernel joins the workgroups'
+// sums in a fixed order.
+// Measured, bf16 where nothing else is said (a sum of two 256 MB tensors runs at
+// 5.9 TB/s, a smaller set comes from the 256 MB cache):
+//   s and y of x and a residual, 500 x 1000 x 256   178 us, 5.75 TB/s
+//   y of x, 2048 x 20000 fp32                        65 us, 5.0 TB/s
+//   dx and dw of dy, s and ds, 1000 x 1000 x 256    386 us, 5.3 TB/s
+//   the same without ds, 100 x 1000 x 2000          240 us, 5.0 TB/s
 #include <algorithm>
 
 #include "rows.h"
@@ -181,7 +186,7 @@ __device__ inline void join_row(float &s, uint32_t &top, float *shared, int turn
     }
 }
 
-constexpr int threads_of(int G) { return G > 256 ? G : 256; }
+constexpr int threads_of(int G) { return G > 64 ? G : 256; }
 
 __device__ inline float rstd_of(float squares, const NormArgs &a) {
     return 1.0f / __builtin_sqrtf(squares / (float)a.channels + a.eps);
@@ -332,9 +337,9 @@ __global__ __launch_bounds__(threads_of(G)) void norm_kernel(NormArgs a) {
     }
 }
 
-// WEIGHTS: dw is summed too (else CHUNKS is 0 and a kernel of its own sums it).
-// Rows of more than 16 elements a thread take the weights anew for every row:
-// the registers hold s, dy and the sums.
+// dw is summed too, in registers (CHUNKS 0: a kernel of its own sums it).  Rows of
+// more than 16 elements a thread take the weights anew for every row: the registers
+// hold s, dy and the sums.
 template <int DT, int G, int CHUNKS>
 __global__ __launch_bounds__(threads_of(G)) void back_kernel(BackArgs a) {
     constexpr int V = kVec<DT>, kThreads = threads_of(G), kRows = kThreads / G, kHeld = CHUNKS ? CHUNKS : 1;
@@ -404,6 +409,15 @@ __global__ __launch_bounds__(threads_of(G)) void back_kernel(BackArgs a) {
             }
             join_row<G, false>(inner, none, shared, turn);
             const float mean = inner * inv_c;
+            // what was computed of the words is computed again, not held over the barrier
+#pragma unroll
+            for (int q = 0; kHold && q < kHeld; q++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    uint32_t ws = s[q][e], wd = d[q][e];
+                    asm volatile("" : "+v"(ws), "+v"(wd));
+                    s[q][e] = ws, d[q][e] = wd;
+                }
 #pragma unroll
             for (int q = 0; q < kHeld; q++) {
                 const int c = (q * G + j) * V;
@@ -486,16 +500,19 @@ __global__ __launch_bounds__(1024) void join_kernel(const float *partial, float 
 
 constexpr int kCus = 256;
 
-// Workgroups of a call: as many as run at once, each with more rows than one.
-inline uint32_t grid_of(int64_t rows, int threads, int rows_each) {
-    const int64_t most = (int64_t)kCus * (2048 / threads);
+// Workgroups of a call.  Of rows that a workgroup shares or holds in two loads each, as
+// many as there are (500 x 1000 x 256 bf16 with a residual: 178 us; 211 us where only
+// those that run at once go from row to row); of wider rows those that run at once,
+// which keep the weights (20 x 1000 x 6000 bf16: 94 us against 114 us).
+inline uint32_t grid_of(int64_t rows, int threads, int rows_each, int chunks) {
+    const int64_t most = threads == 256 && chunks <= 2 ? 1 << 22 : (int64_t)kCus * (2048 / threads);
     return (uint32_t)std::min((rows + rows_each - 1) / rows_each, most);
 }
 
 template <int DT, int G, int CHUNKS, int KIND>
 void norm_one(const NormArgs &a, hipStream_t s) {
     constexpr int kThreads = threads_of(G);
-    norm_kernel<DT, G, CHUNKS, KIND><<<grid_of(a.rows.count, kThreads, kThreads / G), kThreads, 0, s>>>(a);
+    norm_kernel<DT, G, CHUNKS, KIND><<<grid_of(a.rows.count, kThreads, kThreads / G, CHUNKS), kThreads, 0, s>>>(a);
 }
 
 // The threads and chunks that hold a row: as few threads as take at most 4
@@ -529,7 +546,6 @@ rocket_status norm_launch(const NormArgs &a, int32_t dtype, void *stream) {
 }
 
 // ------------------------------------------------------------ backward pass
-constexpr int kMostParts = 1024;   // workgroups whose sums of dw are joined
 constexpr int kWideParts = 64;     // the same of rows too wide for registers
 
 int64_t chunks_of(const rocket_sequence_shape *s) {
@@ -539,15 +555,40 @@ int64_t chunks_of(const rocket_sequence_shape *s) {
 
 bool too_wide(const rocket_sequence_shape *s) { return s->channels > 24576; }
 
-int threads_for(int64_t chunks) {
-    return chunks <= 16 ? 16 : chunks <= 32 ? 32 : chunks <= 256 ? 64 : chunks <= 1024 ? 256 : 1024;
+// Threads and loads of a row in the backward pass: at most 16 elements a thread, so
+// that s, dy, the weights and their sums stay in registers (20 x 1000 x 6000 bf16: 210
+// us, and 414 with 32 elements, where the weights are read for each row and a SIMD holds
+// one wave; 2000 channels, 100 x 1000: 240 and 344).  The last kind, 24, reads them
+// (8 x 1000 x 20000 fp32: 681 us; nothing wider than a workgroup holds a row).
+// The workgroups are those that run at once, each with a sum of dw in registers; more
+// make waves of unlike length and more sums to join (100 x 1000 x 2000 bf16: 240 us, 274
+// with two thirds of them, 308 with four thirds).
+struct Row {
+    int threads, chunks;
+};
+
+Row row_of(int64_t chunks, int vec) {
+    const int most = 16 / vec;   // loads of a thread
+    if (chunks <= 16) return {16, 1};
+    if (chunks <= 32) return {32, 1};
+    if (chunks <= 64) return {64, 1};
+    if (chunks <= 128) return {64, 2};
+    if (chunks <= 64 * most) return {64, most};
+    for (int g = 128; g <= 1024; g *= 2)
+        if (chunks <= g * most) return {g, most};
+    return {1024, 24 / vec};
 }
 
 int64_t back_parts(const rocket_sequence_shape *s) {
     const int64_t rows = s->n * s->steps;
     if (too_wide(s)) return std::min<int64_t>(rows, kWideParts);
-    const int G = threads_for(chunks_of(s)), each = threads_of(G) / G;
-    return std::min<int64_t>((rows + each - 1) / each, G == 1024 ? kCus : kMostParts);
+    const int vec = s->dtype == ROCKET_FLOAT32 ? 4 : 8;
+    const Row row = row_of(chunks_of(s), vec);
+    const int each = threads_of(row.threads) / row.threads;
+    // three waves of a SIMD's registers, but four of the 128 chunks of a wave in 16 bits
+    const int waves = row.threads == 64 && row.chunks == 2 && vec == 8 ? 4 : 3;
+    const int most = row.threads < 512 ? kCus * waves * 256 / threads_of(row.threads) : kCus;
+    return std::min<int64_t>((rows + each - 1) / each, most);
 }
 
 template <int DT, int G, int CHUNKS>
@@ -558,20 +599,35 @@ void back_one(const BackArgs &a, int64_t parts, hipStream_t s) {
 
 template <int DT>
 void back_type(const BackArgs &a, int64_t parts, hipStream_t s) {
-    const int64_t chunks = (a.channels + kVec<DT> - 1) / kVec<DT>;
+    constexpr int V = kVec<DT>, kMost = 16 / V;
+    const int64_t chunks = (a.channels + V - 1) / V;
     if (a.channels > 24576) {
         if (a.partial)  // first: dx may be written over dy or s
             weight_kernel<DT><<<dim3((uint32_t)((a.channels + 255) / 256), (uint32_t)parts), 256, 0, s>>>(a);
         back_one<DT, 1024, 0>(a, std::min<int64_t>(a.rows.count, 2 * kCus), s);
-    } else if (chunks <= 16) back_one<DT, 16, 1>(a, parts, s);
-    else if (chunks <= 32) back_one<DT, 32, 1>(a, parts, s);
-    else if (chunks <= 64) back_one<DT, 64, 1>(a, parts, s);
-    else if (chunks <= 128) back_one<DT, 64, 2>(a, parts, s);
-    else if (chunks <= 256) back_one<DT, 64, 4>(a, parts, s);
-    else if (chunks <= 512) back_one<DT, 256, 2>(a, parts, s);
-    else if (chunks <= 1024) back_one<DT, 256, 4>(a, parts, s);
-    else if (chunks <= 2048) back_one<DT, 1024, 2>(a, parts, s);
-    else back_one<DT, 1024, 24 / kVec<DT>>(a, parts, s);
+        return;
+    }
+    const Row row = row_of(chunks, V);
+    switch (row.threads) {
+    case 16: back_one<DT, 16, 1>(a, parts, s); break;
+    case 32: back_one<DT, 32, 1>(a, parts, s); break;
+    case 64:
+        if (row.chunks == 1)
+            back_one<DT, 64, 1>(a, parts, s);
+        else if (row.chunks == 2)
+            back_one<DT, 64, 2>(a, parts, s);
+        else
+            back_one<DT, 64, kMost>(a, parts, s);
+        break;
+    case 128: back_one<DT, 128, kMost>(a, parts, s); break;
+    case 256: back_one<DT, 256, kMost>(a, parts, s); break;
+    case 512: back_one<DT, 512, kMost>(a, parts, s); break;
+    default:
+        if (row.chunks == kMost)
+            back_one<DT, 1024, kMost>(a, parts, s);
+        else
+            back_one<DT, 1024, 24 / V>(a, parts, s);
+    }
 }
 
 bool eps_ok(float eps) { return eps >= 0.0f && eps <= 3.4028234e38f; }

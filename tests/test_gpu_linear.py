@@ -104,6 +104,14 @@ def test_rms_norm_lengths(env, n, L, C, residual, dtype):
     check_norm(*env, n, L, C, residual, dtype, True)
 
 
+# of each width more rows than the workgroups of a launch, with empty rows between
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,L,C", [(4500, 1, 900), (400, 5, 1400), (401, 5, 2047), (330, 3, 2049), (270, 3, 4001),
+                                   (150, 2, 7001), (140, 2, 8193), (140, 2, 12001), (130, 2, 16400)])
+def test_rms_norm_many_wide_rows(env, n, L, C, dtype):
+    check_norm(*env, n, L, C, True, dtype, True)
+
+
 @pytest.mark.parametrize("C", [40, 30000])
 def test_rms_norm_without_weights(env, C):
     check_norm(*env, 3, 5, C, True, "float32", True, weighted=False)
