@@ -30,6 +30,7 @@ struct ProductArgs {
     int32_t tiles;     // along the channels
     int32_t parts, each;   // of the columns' stages, and stages of a part
     int32_t *sums;         // [parts, rows, channels]
+    const int32_t *order;  // [rows + 1]: order_kernel's
 };
 
 // Few rows: what bounds them is reading the weights, so a workgroup takes 16 channels
@@ -126,7 +127,15 @@ __device__ inline int taken(int sum) {
 //
 // SPLIT (of DT fp32): few tiles of many columns; a workgroup takes some of one tile's
 // stages and leaves their sums, whole numbers, to finish_kernel.
-template <int DT, bool SPLIT, int MT, int NT, int WM, int WT, int COLS, int SLOTS, int AT_ONCE>
+//
+// LIVE: the tiles are of the rows that hold data, one behind the other as order_kernel
+// lists them; the others are zeroed at the end, most of them by the workgroups that have
+// a tile less.  A row's place in q is looked up two tiles ahead, since the next tile's
+// stages are on their way when this one's results are written; so a tile must have as
+// many stages as there are slots.  777 series of up to 129 steps, half of the rows, of
+// 960 columns by 993 channels: 111 us, and 172 where empty rows are multiplied like the
+// others; where all rows hold data the list costs 6 us.
+template <int DT, bool SPLIT, bool LIVE, int MT, int NT, int WM, int WT, int COLS, int SLOTS, int AT_ONCE>
 __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs a) {
     constexpr int kWaves = WM * WT, kThreads = 64 * kWaves, kM = 32 * MT * WM, kT = 32 * NT * WT, kSlots = SLOTS;
     constexpr int kPieces = COLS / 16, kLines = 64 / kPieces;   // of a line; lines of a load
@@ -140,7 +149,8 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
     typedef uint32_t Words __attribute__((ext_vector_type(kSize)));   // four values
     static_assert(kLoadsM * kWaves * kLines == kM && kLoadsT * kWaves * kLines == kT, "whole loads");
     static_assert(kM <= kThreads && kT <= kThreads, "a thread for each line of a table");
-    __shared__ __attribute__((aligned(1024))) char shared[kTables + 2 * kTable];
+    constexpr int kSources = kTables + 2 * kTable;   // LIVE: where the lines of two tiles' rows lie in q
+    __shared__ __attribute__((aligned(1024))) char shared[kSources + (LIVE ? 8 * kT : 0)];
     const uint32_t base = rocket::shared_address(shared);
     const int lane = threadIdx.x % 64, wave = rocket::uniform(threadIdx.x / 64);
     const int wm = wave % WM, wt = wave / WM, half = lane / 32;
@@ -158,7 +168,7 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
         int m;
     };
     Tile tile = {first / a.tiles, (int)(first % a.tiles)};
-    const int64_t tiles_t = (a.rows.count + kT - 1) / kT;
+    const int64_t count = LIVE ? a.order[a.rows.count] : a.rows.count, tiles_t = (count + kT - 1) / kT;
     const auto next_of = [&](Tile x) {
         x.t += step_t, x.m += step_m;
         if (x.m >= a.tiles) x.m -= a.tiles, x.t++;
@@ -181,15 +191,26 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
         for (int k = 0; k < 2; k++)
             rest[k] = (lane % kPieces ^ turn_of(k * kLines + lane / kPieces)) >= kPieces / 2 ? rocket::kNowhere : 0;
     Tile ask_tile = tile;
-    int ask_stage = 0, ask_slot = 0;
+    int ask_stage = 0, ask_slot = 0, ask_turn = 0;
     uint32_t ask_at = 0, ask_to = base;
     Int4 weights, rows;
     const auto open_tile = [&]() {
-        const int64_t left_t = a.rows.count - ask_tile.t * kT;   // 0 or less: past the last tile
+        const int64_t left_t = count - ask_tile.t * kT;   // 0 or less: past the last tile
         const int left_m = a.channels - ask_tile.m * kM;
         weights = rocket::buffer_of(a.p + (int64_t)ask_tile.m * kM * a.columns,
                                     left_t > 0 ? (int64_t)(left_m < kM ? left_m : kM) * a.columns : 0);
-        rows = rocket::buffer_of(a.q + ask_tile.t * kT * a.columns, (left_t < kT ? left_t : kT) * a.columns);
+        if (LIVE) {
+            rows = rocket::buffer_of(a.q, a.rows.count * a.columns);
+            const uint32_t *sources = (const uint32_t *)(shared + kSources) + ask_turn * kT;
+            ask_turn ^= 1;
+#pragma unroll
+            for (int k = 0; k < kLoadsT; k++) {
+                const int line = (wave * kLoadsT + k) * kLines + lane / kPieces;
+                from[kLoadsM + k] = sources[line] + (lane % kPieces ^ turn_of(line)) * 16;
+            }
+        } else {
+            rows = rocket::buffer_of(a.q + ask_tile.t * kT * a.columns, (left_t < kT ? left_t : kT) * a.columns);
+        }
     };
     const auto open_stage = [&]() {
         if (ask_stage == stages) {
@@ -216,16 +237,19 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
         float wscale, bias, scale;
         uint64_t at;
     };
-    const auto look_up = [&](Tile x) {
+    const auto row_of = [&](Tile x) -> int64_t {   // -1: not there
+        const int64_t r = x.t * kT + threadIdx.x;
+        return threadIdx.x >= kT || r >= count ? -1 : LIVE ? a.order[r] : r;
+    };
+    const auto look_up = [&](Tile x, int64_t r) {
         Table v = {};
         const int k = threadIdx.x, m = x.m * kM + k;
-        const int64_t r = x.t * kT + k;
         if (!SPLIT && k < kM && m < a.channels) v.wscale = a.wscale[m], v.bias = a.bias ? a.bias[m] : 0.0f;
-        if (k < kT && r < a.rows.count) {
+        if (r >= 0) {
             const Place p = rocket::place_of(a.rows, r);
             v.scale = SPLIT ? 0.0f : a.scale[r];
             char *to = SPLIT ? (char *)(a.sums + (part * a.rows.count + r) * a.channels) : rocket::row_at(a.y, p);
-            v.at = (uint64_t)(to + (int64_t)x.m * kM * kSize) | (SPLIT || p.live ? 0 : 1);
+            v.at = (uint64_t)(to + (int64_t)x.m * kM * kSize) | (SPLIT || LIVE || p.live ? 0 : 1);
         }
         return v;
     };
@@ -235,7 +259,19 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
         if (k < kM) to[k] = v.wscale, to[kM + k] = v.bias;
         if (k < kT) to[2 * kM + k] = v.scale, ((uint64_t *)(to + 2 * kM + kT))[k] = v.at;
     };
-    write_table(look_up(tile), 0);
+    const auto write_sources = [&](int64_t r, int turn) {
+        if (threadIdx.x < kT)
+            ((uint32_t *)(shared + kSources))[turn * kT + threadIdx.x] =
+                r < 0 ? rocket::kNowhere : (uint32_t)r * (uint32_t)a.columns;
+    };
+    int64_t coming = row_of(tile);
+    write_table(look_up(tile, coming), 0);
+    if (LIVE) {
+        write_sources(coming, 0);
+        coming = row_of(next_of(tile));
+        write_sources(coming, 1);
+        __syncthreads();
+    }
 
     // where it reads a stage: a step's pieces are the first one's with the higher bits turned
     typedef const __attribute__((address_space(3))) Int4 *SharedInt4;
@@ -305,7 +341,8 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
         // for, which the compiler does not see that `taken` reads)
         asm volatile("s_nop 15\n\ts_nop 15");
         const Tile following = next_of(tile);
-        const Table table = look_up(following);
+        const Table table = look_up(following, LIVE ? coming : row_of(following));
+        if (LIVE) coming = row_of(next_of(following));
         const float *factors = (const float *)(shared + kTables + turn * kTable), *row_scale = factors + 2 * kM;
         const uint64_t *row_at = (const uint64_t *)(row_scale + kT);
         const int left_m = a.channels - tile.m * kM;
@@ -361,9 +398,63 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
             }
         }
         write_table(table, turn ^ 1);
+        if (LIVE) write_sources(coming, turn);
         tile = following;
     }
+    if (LIVE) {
+        // a wavefront takes some rows at a time, whose places its lanes look up at once
+        constexpr int kSome = 16, kEach = 16 / kSize;
+        const Int4 zero = {0, 0, 0, 0};
+        const int64_t some = (a.rows.count - count + kSome - 1) / kSome;
+        // workgroups with a tile more, and what a tile is worth in zeros at 25 GB/s
+        const int64_t more = tiles_t * a.tiles % gridDim.x, fewer = gridDim.x - more;
+        const int64_t worth = more ? (stages * 21250 + 150000) / (kSome * kSize * a.channels) : 0;
+        const int64_t each = some > fewer * worth ? (some - fewer * worth) / gridDim.x : 0;   // of those with more
+        const int64_t rest = some - more * each, mine = (rest + fewer - 1) / fewer;
+        const int64_t from_some = group < more ? rest + group * each : (group - more) * mine;
+        const int64_t to_some = group < more ? from_some + each : std::min(from_some + mine, rest);
+        for (int64_t u = from_some + wave; u < to_some; u += kWaves) {
+            const int64_t d = count + u * kSome;
+            const int places = (int)std::min<int64_t>(kSome, a.rows.count - d);
+            const int32_t r = a.order[d + std::min(lane, places - 1)];
+            for (int k = 0; k < places; k++) {
+                char *to = rocket::row_at(a.y, rocket::place_of(a.rows, __builtin_amdgcn_readlane(r, k)));
+                for (int c = lane * kEach; c < a.channels; c += 64 * kEach) {
+                    if (c + kEach <= a.channels) {
+                        rocket::store_at(to + (int64_t)c * kSize, zero);
+                    } else {
+                        using bits = typename Elem<DT>::bits;
+                        for (int e = c; e < a.channels; e++) ((bits *)to)[e] = 0;
+                    }
+                }
+            }
+        }
+    }
     rocket::wait_loads<0>();
+}
+
+// Rows that hold data, then those that do not, each in their order, and how many do: a
+// workgroup a series, which counts the rows before it.
+__global__ __launch_bounds__(256) void order_kernel(Rows rows, int32_t *order) {
+    __shared__ int32_t counts[2][4];
+    int32_t all = 0, before = 0;
+    for (int i = threadIdx.x; i < rows.n; i += 256) {
+        const int32_t length = rows.lengths[i], here = length < 0 ? 0 : length > rows.steps ? rows.steps : length;
+        all += here;
+        if (i < (int)blockIdx.x) before += here;
+    }
+#pragma unroll
+    for (int k = 32; k; k /= 2) all += __shfl_xor(all, k), before += __shfl_xor(before, k);
+    if (threadIdx.x % 64 == 0) counts[0][threadIdx.x / 64] = all, counts[1][threadIdx.x / 64] = before;
+    __syncthreads();
+    all = counts[0][0] + counts[0][1] + counts[0][2] + counts[0][3];
+    before = counts[1][0] + counts[1][1] + counts[1][2] + counts[1][3];
+    const int32_t first = blockIdx.x * rows.steps, dead = all + first - before;
+    const int32_t length = rows.lengths[blockIdx.x];
+    const int32_t here = length < 0 ? 0 : length > rows.steps ? rows.steps : length;
+    for (int t = threadIdx.x; t < rows.steps; t += 256)
+        order[t < here ? before + t : dead + t - here] = first + t;
+    if (blockIdx.x == 0 && threadIdx.x == 0) order[rows.count] = all;
 }
 
 // The results of split tiles: a thread an element, in the order of the sums.
@@ -392,10 +483,14 @@ struct Cut {
     Way way;
     int32_t parts, each;
     int64_t bytes;
+    bool live;   // where lengths are given, the rows that hold data are listed first
 };
 
-Cut cut_of(int64_t rows, int64_t channels, int64_t columns) {
-    Cut c = {kFew, 1, 0, 0};
+constexpr int64_t kMostSeries = 4096;   // that order_kernel's workgroups count, each for itself
+
+Cut cut_of(const rocket_sequence_shape *s, int64_t columns) {
+    const int64_t rows = s->n * s->steps, channels = s->channels, steps = s->steps;
+    Cut c = {kFew, 1, 0, 0, false};
     if (rows <= kFewRows) return c;
     struct Cost {
         Way way;
@@ -412,23 +507,27 @@ Cut cut_of(int64_t rows, int64_t channels, int64_t columns) {
         const double us = (double)((tiles + all - 1) / all) * (stages * k.stage + k.end);
         if (us < best) best = us, c.way = k.way;
     }
+    const int64_t series = rows / steps;
+    c.live = c.way == kBig && series > 1 && series <= kMostSeries && steps > 1 && columns >= 256 &&
+             rows * columns <= INT32_MAX;
+    if (c.live) c.bytes = (rows + 1) * 4;
     const int64_t tiles = (rows + 127) / 128 * ((channels + 127) / 128), lines = (columns + 127) / 128;
     for (int64_t p = 2; p <= lines / 2 && tiles * p <= 4 * kCus; p += 1 + p / 8) {
         const int64_t each = (lines + p - 1) / p, parts = (lines + each - 1) / each;
         const double us = (double)((tiles * parts + kCus - 1) / kCus) * (each * 0.56 + 2.0) + 6.0 +
                           (double)(parts * rows * channels) * 8e-6 / 4.0;
-        if (us < best) best = us, c = Cut{kSplit, (int32_t)parts, (int32_t)each, parts * rows * channels * 4};
+        if (us < best) best = us, c = Cut{kSplit, (int32_t)parts, (int32_t)each, parts * rows * channels * 4, false};
     }
     return c;
 }
 
-template <int DT, bool SPLIT, int MT, int NT, int WM, int WT, int COLS, int SLOTS, int AT_ONCE>
+template <int DT, bool SPLIT, bool LIVE, int MT, int NT, int WM, int WT, int COLS, int SLOTS, int AT_ONCE>
 void tiles(ProductArgs a, hipStream_t s) {
     constexpr int kM = 32 * MT * WM, kT = 32 * NT * WT;
     a.tiles = (a.channels + kM - 1) / kM;
     const int64_t items = (a.rows.count + kT - 1) / kT * a.tiles;
     const int64_t groups = SPLIT ? items * a.parts : std::min(items, AT_ONCE * kCus);
-    tile_kernel<DT, SPLIT, MT, NT, WM, WT, COLS, SLOTS, AT_ONCE><<<(uint32_t)groups, 64 * WM * WT, 0, s>>>(a);
+    tile_kernel<DT, SPLIT, LIVE, MT, NT, WM, WT, COLS, SLOTS, AT_ONCE><<<(uint32_t)groups, 64 * WM * WT, 0, s>>>(a);
 }
 
 template <int DT>
@@ -445,13 +544,21 @@ void launch(ProductArgs a, const Cut &cut, hipStream_t s) {
             few_kernel<DT, 4><<<groups, 64 * kFewWaves, 0, s>>>(a);
         break;
     }
-    case kBig: tiles<DT, false, 4, 4, 2, 2, 128, 2, 1>(a, s); break;
-    case kTall: tiles<DT, false, 4, 2, 2, 2, 128, 2, 1>(a, s); break;
-    case kMiddle: tiles<DT, false, 2, 2, 2, 2, 128, 3, 1>(a, s); break;
-    case kMiddleTwice: tiles<DT, false, 2, 2, 2, 2, 64, 3, 2>(a, s); break;
-    case kSmall: tiles<DT, false, 1, 1, 2, 2, 64, 4, 2>(a, s); break;
+    case kBig:
+        if (cut.live && a.rows.lengths) {
+            order_kernel<<<(uint32_t)a.rows.n, 256, 0, s>>>(a.rows, a.sums);
+            a.order = a.sums;
+            tiles<DT, false, true, 4, 4, 2, 2, 128, 2, 1>(a, s);
+        } else {
+            tiles<DT, false, false, 4, 4, 2, 2, 128, 2, 1>(a, s);
+        }
+        break;
+    case kTall: tiles<DT, false, false, 4, 2, 2, 2, 128, 2, 1>(a, s); break;
+    case kMiddle: tiles<DT, false, false, 2, 2, 2, 2, 128, 3, 1>(a, s); break;
+    case kMiddleTwice: tiles<DT, false, false, 2, 2, 2, 2, 64, 3, 2>(a, s); break;
+    case kSmall: tiles<DT, false, false, 1, 1, 2, 2, 64, 4, 2>(a, s); break;
     case kSplit: {
-        tiles<ROCKET_FLOAT32, true, 2, 2, 2, 2, 128, 3, 1>(a, s);
+        tiles<ROCKET_FLOAT32, true, false, 2, 2, 2, 2, 128, 3, 1>(a, s);
         finish_kernel<DT><<<(uint32_t)((a.rows.count * a.channels + 255) / 256), 256, 0, s>>>(a);
         break;
     }
@@ -465,7 +572,7 @@ bool columns_ok(int64_t columns) { return columns > 0 && columns <= 131072 && co
 extern "C" rocket_status rocket_linear_bytes_workspace(const rocket_sequence_shape *shape, int64_t columns,
                                                   int64_t *bytes) {
     if (!bytes || !rocket::shape_ok(shape) || !columns_ok(columns)) return ROCKET_ERR_INVALID_ARG;
-    *bytes = rocket::empty(shape) ? 0 : (cut_of(shape->n * shape->steps, shape->channels, columns).bytes + 7) / 8 * 8;
+    *bytes = rocket::empty(shape) ? 0 : (cut_of(shape, columns).bytes + 7) / 8 * 8;
     return ROCKET_OK;
 }
 
@@ -478,7 +585,7 @@ extern "C" rocket_status rocket_linear_bytes(const rocket_sequence_shape *shape,
     if (!rocket::bytes_ok(q) || !rocket::floats_ok(scale) || !rocket::bytes_ok(weight) ||
         !rocket::floats_ok(weight_scale) || (bias && !rocket::floats_ok(bias)))
         return ROCKET_ERR_INVALID_ARG;
-    const Cut cut = cut_of(shape->n * shape->steps, shape->channels, columns);
+    const Cut cut = cut_of(shape, columns);
     if (cut.bytes && (!workspace || (uintptr_t)workspace % 8 != 0 || workspace_bytes < cut.bytes))
         return ROCKET_ERR_INVALID_ARG;
     ProductArgs a = {};

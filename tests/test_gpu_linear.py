@@ -302,6 +302,78 @@ def test_linear8_large(env, rows, columns, N, with_lengths, dtype):
     assert ok.all(), torch.nonzero(~ok)[:4]
 
 
+def row_lengths(kind, n, L, g):
+    """Lengths [n]: any, none, all, one row of one series, past both ends, all or nothing."""
+    import torch
+    any_ = torch.randint(0, L + 1, (n,), generator=g, device="cuda", dtype=torch.int32)
+    if kind == "none":
+        return torch.zeros_like(any_)
+    if kind == "all":
+        return torch.full_like(any_, L)
+    if kind == "one row":
+        any_.zero_()[n - 2] = 1
+    elif kind == "past both ends":
+        any_[::3], any_[1::3] = -5, L + 7
+    elif kind == "all or nothing":
+        any_ = (any_ > L // 2).int() * L
+    return any_
+
+
+# (series, steps, columns, channels) of large products whose live rows are listed first: the
+# most series, the least columns, last stages of 64 columns, a launch's last tiles of each
+# number; and those past what is listed: more series, more bytes
+LISTED = [(4096, 16, 256, 768), (777, 129, 960, 993), (2, 33000, 256, 1000), (3000, 30, 320, 1000),
+          (64, 1000, 2048, 1536)]
+UNLISTED = [(4097, 16, 256, 768), (2, 33000, 32768, 768)]
+
+
+@pytest.mark.parametrize("kind", ["any", "none", "all", "one row", "past both ends", "all or nothing"])
+@pytest.mark.parametrize("n,L,columns,N", LISTED + UNLISTED)
+def test_linear8_of_listed_rows(env, n, L, columns, N, kind):
+    """Rows that hold data have the very results of a call without lengths, the others are
+    zeros, and nothing is written beside them."""
+    torch, seq = env
+    rows, listed = n * L, (n, L, columns, N) in LISTED
+    assert (seq._linear8_size(n, L, N, 2, columns) == (rows * 4 + 11) // 8 * 8) == listed
+    g = torch.Generator(device="cuda").manual_seed(rows + columns + N)
+    q = torch.randint(-127, 128, (n, L, columns), generator=g, device="cuda", dtype=torch.int8)
+    p = torch.randint(-127, 128, (N, columns), generator=g, device="cuda", dtype=torch.int8)
+    scale, ws, b = (torch.rand(k, generator=g, device="cuda") + 0.5 for k in ((n, L), (N,), (N,)))
+    ws *= 2.0 ** -12   # results that float16 holds
+    lengths = row_lengths(kind, n, L, g)
+    live = (torch.arange(L, device="cuda")[None, :] < lengths[:, None])
+    want = seq.linear8(q, scale, p, ws, b, dtype=torch.float16).masked_fill(~live[:, :, None], 0)
+    scale = scale.masked_fill(~live, float("nan"))
+    wide = torch.full((n, L, N + 5), 7.0, dtype=torch.float16, device="cuda")
+    out = wide[:, :, 3:N + 3]
+    seq.linear8(q, scale, p, ws, b, lengths=lengths, out=out)
+    assert torch.equal(out, want)
+    assert (wide[:, :, :3] == 7).all() and (wide[:, :, N + 3:] == 7).all()
+
+
+def test_linear8_of_listed_rows_in_a_graph(env):
+    """A captured call lists the rows anew in every replay."""
+    torch, seq = env
+    n, L, columns, N = LISTED[1]
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q = torch.randint(-127, 128, (n, L, columns), generator=g, device="cuda", dtype=torch.int8)
+    p = torch.randint(-127, 128, (N, columns), generator=g, device="cuda", dtype=torch.int8)
+    scale, ws = torch.rand(n, L, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda")
+    lengths = row_lengths("any", n, L, g)
+    call = lambda: seq.linear8(q, scale, p, ws, lengths=lengths)  # noqa: E731
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = call()
+    for kind in ("any", "one row", "all", "none", "past both ends"):
+        lengths.copy_(row_lengths(kind, n, L, g))
+        graph.replay()
+        got = y.clone()
+        assert torch.equal(got, call())
+        live = torch.arange(L, device="cuda")[None, :] < lengths[:, None]
+        assert (got[~live] == 0).all()
+
+
 def test_linear8_is_exact(env):
     """Whole numbers below 2^24 come out as they are: no rounding anywhere."""
     torch, seq = env
