@@ -8,7 +8,8 @@ Python-side entry points (argument marshalling over ctypes):
     MiniRocketPlan(params)  .transform(X): PPV features [n, n_features]
     sequence: operators of a trained head over feature sequences [n, steps,
         channels]: group_norm, recurrence, recurrence_step, dropout, and their
-        backward passes
+        backward passes; and of its linear layers: rms_norm (to 8-bit rows too),
+        linear8, checkpoint, restore, linear_weight_gradient
 The seeded synthetic series live in ``paper_2601_17091_amd.workloads``.
 With ROCKET_DEBUG=1 in the environment the checked build is loaded
 (librocket_checked.so: device-side bounds checks, see check_flags).

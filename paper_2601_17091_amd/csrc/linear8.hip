@@ -4,6 +4,15 @@
 //
 // The sum is of whole numbers and exact: 32 bits hold it up to 131,072 columns.
 // Scales and bias are fp32, the result is rounded once.
+//
+// Bound: few rows by reading the weights, many by the matrix unit (2,440 TOP/s in a
+// library's product of 8,192) and its clock, which falls to 2.0 GHz and below under it.
+// Measured, bf16 results where nothing else is said:
+//   64 rows, 2,000 by 1,536 channels           7.5 us (a row by 192 channels: 4.1)
+//   64 x 1000 rows, 2,000 by 1,536             212 us, 1,850 TOP/s (1,900 of the padded
+//                                              columns); without writing results 170
+//   777 x 129 rows, half of them empty, 924 by 993, fp16    98 to 120 us, by whether
+//                                              the tiles take three or four rounds
 #include <algorithm>
 
 #include "rows.h"
@@ -406,9 +415,9 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
         constexpr int kSome = 16, kEach = 16 / kSize;
         const Int4 zero = {0, 0, 0, 0};
         const int64_t some = (a.rows.count - count + kSome - 1) / kSome;
-        // workgroups with a tile more, and what a tile is worth in zeros at 25 GB/s
+        // workgroups with a tile more, and what a tile is worth in zeros
         const int64_t more = tiles_t * a.tiles % gridDim.x, fewer = gridDim.x - more;
-        const int64_t worth = more ? (stages * 21250 + 150000) / (kSome * kSize * a.channels) : 0;
+        const int64_t worth = more ? ((int64_t)stages * COLS * kM * kT / 400 + kM * kT * 2) / (kSome * kSize * a.channels) : 0;
         const int64_t each = some > fewer * worth ? (some - fewer * worth) / gridDim.x : 0;   // of those with more
         const int64_t rest = some - more * each, mine = (rest + fewer - 1) / fewer;
         const int64_t from_some = group < more ? rest + group * each : (group - more) * mine;
@@ -434,14 +443,16 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
 }
 
 // Rows that hold data, then those that do not, each in their order, and how many do: a
-// workgroup a series, which counts the rows before it.
-__global__ __launch_bounds__(256) void order_kernel(Rows rows, int32_t *order) {
+// workgroup some series, after it has counted the rows before them.
+__global__ __launch_bounds__(256) void order_kernel(Rows rows, int32_t each, int32_t *order) {
     __shared__ int32_t counts[2][4];
+    const int first = blockIdx.x * each, end = std::min(first + each, rows.n);
+    const auto held = [&](int i) { return std::max(0, std::min(rows.lengths[i], rows.steps)); };
     int32_t all = 0, before = 0;
     for (int i = threadIdx.x; i < rows.n; i += 256) {
-        const int32_t length = rows.lengths[i], here = length < 0 ? 0 : length > rows.steps ? rows.steps : length;
+        const int32_t here = held(i);
         all += here;
-        if (i < (int)blockIdx.x) before += here;
+        if (i < first) before += here;
     }
 #pragma unroll
     for (int k = 32; k; k /= 2) all += __shfl_xor(all, k), before += __shfl_xor(before, k);
@@ -449,11 +460,12 @@ __global__ __launch_bounds__(256) void order_kernel(Rows rows, int32_t *order) {
     __syncthreads();
     all = counts[0][0] + counts[0][1] + counts[0][2] + counts[0][3];
     before = counts[1][0] + counts[1][1] + counts[1][2] + counts[1][3];
-    const int32_t first = blockIdx.x * rows.steps, dead = all + first - before;
-    const int32_t length = rows.lengths[blockIdx.x];
-    const int32_t here = length < 0 ? 0 : length > rows.steps ? rows.steps : length;
-    for (int t = threadIdx.x; t < rows.steps; t += 256)
-        order[t < here ? before + t : dead + t - here] = first + t;
+    for (int i = first; i < end; i++) {
+        const int32_t here = held(i), row = i * rows.steps, dead = all + row - before;
+        for (int t = threadIdx.x; t < rows.steps; t += 256)
+            order[t < here ? before + t : dead + t - here] = row + t;
+        before += here;
+    }
     if (blockIdx.x == 0 && threadIdx.x == 0) order[rows.count] = all;
 }
 
@@ -476,7 +488,7 @@ constexpr int64_t kCus = 256;
 
 // How a call is cut, by what each way costs: rounds of workgroups, each with its
 // stages of 64 columns and the writing of its results (microseconds as measured with
-// 2,048 columns and 1,536 channels on 1,000 to 64,000 rows).
+// 128 to 2,048 columns and 256 to 1,536 channels on 1,000 to 300,000 rows).
 enum Way { kFew, kBig, kTall, kMiddle, kMiddleTwice, kSmall, kSplit };
 
 struct Cut {
@@ -486,7 +498,7 @@ struct Cut {
     bool live;   // where lengths are given, the rows that hold data are listed first
 };
 
-constexpr int64_t kMostSeries = 4096;   // that order_kernel's workgroups count, each for itself
+constexpr int64_t kMostSeries = 4096;   // that order_kernel's workgroups count, each all of them
 
 Cut cut_of(const rocket_sequence_shape *s, int64_t columns) {
     const int64_t rows = s->n * s->steps, channels = s->channels, steps = s->steps;
@@ -497,18 +509,28 @@ Cut cut_of(const rocket_sequence_shape *s, int64_t columns) {
         int m, t, at_once;
         double stage, end;
     };
-    constexpr Cost kCosts[] = {{kBig, 256, 256, 1, 0.85, 6.0},   {kTall, 256, 128, 1, 0.52, 4.0},
-                               {kMiddle, 128, 128, 1, 0.28, 2.0}, {kMiddleTwice, 128, 128, 2, 0.58, 3.0},
-                               {kSmall, 64, 64, 2, 0.25, 1.0}};
+    constexpr Cost kCosts[] = {{kBig, 256, 256, 1, 0.80, 8.0},   {kTall, 256, 128, 1, 0.52, 3.8},
+                               {kMiddle, 128, 128, 1, 0.285, 2.3}, {kMiddleTwice, 128, 128, 2, 0.56, 3.2},
+                               {kSmall, 64, 64, 2, 0.26, 1.1}};
     const double stages = (double)(columns / 64);
     double best = 1e300;
+    int64_t rounds = 0;
     for (const Cost &k : kCosts) {
         const int64_t tiles = (rows + k.t - 1) / k.t * ((channels + k.m - 1) / k.m), all = k.at_once * kCus;
-        const double us = (double)((tiles + all - 1) / all) * (stages * k.stage + k.end);
-        if (us < best) best = us, c.way = k.way;
+        // two on a CU: a last round of few tiles goes faster
+        const double rest = (double)(tiles % all) / (double)all;
+        const double last = k.at_once == 1 ? 1.0 : std::min(1.0, 0.4 + 2.0 * rest);
+        const double us = ((double)(tiles / all) + (rest > 0.0 ? last : 0.0)) * (stages * k.stage + k.end);
+        if (us < best) best = us, c.way = k.way, rounds = (tiles + all - 1) / all;
     }
     const int64_t series = rows / steps;
-    c.live = c.way == kBig && series > 1 && series <= kMostSeries && steps > 1 && columns >= 256 &&
+    // rows that hold data are listed where that takes less than what empty rows would cost,
+    // were they half of them: a round and the product's share, which falls with the columns
+    // (100 x 1000 by 512 columns and 192 channels 31.7 us, else 50.1; 4000 x 50 by 256
+    // columns and channels 47, else 38)
+    const int64_t least = c.way == kMiddleTwice ? 3 * 64 : 2 * 128;   // columns of a way's slots
+    c.live = (c.way == kBig || c.way == kTall || c.way == kMiddleTwice) && rounds > 1 && columns >= least &&
+             best * std::min(1.0, stages / 8.0) > 20.0 && series > 1 && series <= kMostSeries && steps > 1 &&
              rows * columns <= INT32_MAX;
     if (c.live) c.bytes = (rows + 1) * 4;
     const int64_t tiles = (rows + 127) / 128 * ((channels + 127) / 128), lines = (columns + 127) / 128;
@@ -530,6 +552,18 @@ void tiles(ProductArgs a, hipStream_t s) {
     tile_kernel<DT, SPLIT, LIVE, MT, NT, WM, WT, COLS, SLOTS, AT_ONCE><<<(uint32_t)groups, 64 * WM * WT, 0, s>>>(a);
 }
 
+template <int DT, int MT, int NT, int COLS, int SLOTS, int AT_ONCE>
+void listed(ProductArgs a, const Cut &cut, hipStream_t s) {
+    if (cut.live && a.rows.lengths) {
+        const int32_t each = (int32_t)((a.rows.n + kCus - 1) / kCus);
+        order_kernel<<<(uint32_t)((a.rows.n + each - 1) / each), 256, 0, s>>>(a.rows, each, a.sums);
+        a.order = a.sums;
+        tiles<DT, false, true, MT, NT, 2, 2, COLS, SLOTS, AT_ONCE>(a, s);
+    } else {
+        tiles<DT, false, false, MT, NT, 2, 2, COLS, SLOTS, AT_ONCE>(a, s);
+    }
+}
+
 template <int DT>
 void launch(ProductArgs a, const Cut &cut, hipStream_t s) {
     a.parts = cut.parts, a.each = cut.each;
@@ -544,18 +578,10 @@ void launch(ProductArgs a, const Cut &cut, hipStream_t s) {
             few_kernel<DT, 4><<<groups, 64 * kFewWaves, 0, s>>>(a);
         break;
     }
-    case kBig:
-        if (cut.live && a.rows.lengths) {
-            order_kernel<<<(uint32_t)a.rows.n, 256, 0, s>>>(a.rows, a.sums);
-            a.order = a.sums;
-            tiles<DT, false, true, 4, 4, 2, 2, 128, 2, 1>(a, s);
-        } else {
-            tiles<DT, false, false, 4, 4, 2, 2, 128, 2, 1>(a, s);
-        }
-        break;
-    case kTall: tiles<DT, false, false, 4, 2, 2, 2, 128, 2, 1>(a, s); break;
+    case kBig: listed<DT, 4, 4, 128, 2, 1>(a, cut, s); break;
+    case kTall: listed<DT, 4, 2, 128, 2, 1>(a, cut, s); break;
     case kMiddle: tiles<DT, false, false, 2, 2, 2, 2, 128, 3, 1>(a, s); break;
-    case kMiddleTwice: tiles<DT, false, false, 2, 2, 2, 2, 64, 3, 2>(a, s); break;
+    case kMiddleTwice: listed<DT, 2, 2, 64, 3, 2>(a, cut, s); break;
     case kSmall: tiles<DT, false, false, 1, 1, 2, 2, 64, 4, 2>(a, s); break;
     case kSplit: {
         tiles<ROCKET_FLOAT32, true, false, 2, 2, 2, 2, 128, 3, 1>(a, s);

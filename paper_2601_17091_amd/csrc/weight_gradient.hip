@@ -6,6 +6,18 @@
 // A channel's scale is a factor of its block's sum, so nothing is rounded before
 // the sums: q is exact in bf16 and fp16, dy is taken as it is (fp32 as the exact
 // sum of three bf16 parts), and the matrix unit sums their products in fp32.
+//
+// Bound: the matrix unit, 2 rows m c operations.  Many rows: tiles of 256 x 256 whose
+// stages are on their way while others are read (staged_kernel); what is left is its
+// clock: with the unit 47 % busy it falls to 2.0 to 2.1 GHz, and a whole version that
+// does not widen q takes 394 of 440 us, one that loads nothing 337.  Few rows: tiles of
+// 64 x 64 straight from registers (gradient_kernel).  The rows are shared out where the
+// tiles do not fill the chip, and the parts' sums joined in a fixed order.
+// Measured:
+//   64 x 1000 rows bf16, 1,536 by 2,000     410 us, 960 TFLOP/s
+//   777 x 129 rows fp16, 993 by 924         262 us: 66 to lay out dy, whose rows have odd
+//                                           places, 190 the product, 6 the join
+//   64 rows fp32, 192 by 2,000              5.3 us
 #include <algorithm>
 
 #include "rows.h"

@@ -321,10 +321,11 @@ def row_lengths(kind, n, L, g):
 
 # (series, steps, columns, channels) of large products whose live rows are listed first: the
 # most series, the least columns, last stages of 64 columns, a launch's last tiles of each
-# number; and those past what is listed: more series, more bytes
-LISTED = [(4096, 16, 256, 768), (777, 129, 960, 993), (2, 33000, 256, 1000), (3000, 30, 320, 1000),
-          (64, 1000, 2048, 1536)]
-UNLISTED = [(4097, 16, 256, 768), (2, 33000, 32768, 768)]
+# number, of each size; and those past what is listed: more series, more bytes, fewer
+# stages, less work
+LISTED = [(4096, 20, 256, 768), (777, 129, 960, 993), (2, 33000, 256, 1000), (3000, 30, 320, 1000),
+          (64, 1000, 2048, 1536), (333, 50, 2048, 1536), (200, 1000, 192, 512), (300, 1000, 256, 130)]
+UNLISTED = [(4097, 30, 256, 768), (2, 33000, 32768, 768), (50, 1000, 128, 1024), (777, 129, 192, 200)]
 
 
 @pytest.mark.parametrize("kind", ["any", "none", "all", "one row", "past both ends", "all or nothing"])
