@@ -560,8 +560,8 @@ bool too_wide(const rocket_sequence_shape *s) { return s->channels > 24576; }
 // us, and 414 with 32 elements, where the weights are read for each row and a SIMD holds
 // one wave; 2000 channels, 100 x 1000: 240 and 344).  The last kind, 24, reads them
 // (8 x 1000 x 20000 fp32: 681 us; nothing wider than a workgroup holds a row).
-// The workgroups are those that run at once, each with a sum of dw in registers; more
-// make waves of unlike length and more sums to join (100 x 1000 x 2000 bf16: 240 us, 274
+// The workgroups are at most those that run at once, each with a sum of dw in registers;
+// more make waves of unlike length and more sums to join (100 x 1000 x 2000 bf16: 240 us, 274
 // with two thirds of them, 308 with four thirds).
 struct Row {
     int threads, chunks;
@@ -585,8 +585,14 @@ int64_t back_parts(const rocket_sequence_shape *s) {
     const int vec = s->dtype == ROCKET_FLOAT32 ? 4 : 8;
     const Row row = row_of(chunks_of(s), vec);
     const int each = threads_of(row.threads) / row.threads;
-    // three waves of a SIMD's registers, but four of the 128 chunks of a wave in 16 bits
-    const int waves = row.threads == 64 && row.chunks == 2 && vec == 8 ? 4 : 3;
+    // waves of a SIMD: three, which is what rows of 16 elements a thread leave room for and
+    // what feeds it where every thread's loads are whole; of 16-bit rows in two loads of a
+    // wave four; of narrower rows that leave threads idle or end inside a load six
+    // (1,000,000 x 64 bf16 157 us with three, 103 with six; 500,000 x 250 232 and 181;
+    // 1,000,000 x 256 386 and 423)
+    const bool whole = s->channels % (row.threads * row.chunks * vec) == 0;
+    const bool narrow = row.threads <= 64 && row.chunks * vec <= 8, two = row.threads == 64 && row.chunks * vec == 16;
+    const int waves = narrow && !whole ? 6 : two && vec == 8 ? 4 : 3;
     const int most = row.threads < 512 ? kCus * waves * 256 / threads_of(row.threads) : kCus;
     return std::min<int64_t>((rows + each - 1) / each, most);
 }

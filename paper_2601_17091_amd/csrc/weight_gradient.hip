@@ -9,7 +9,7 @@
 //
 // Bound: the matrix unit, 2 rows m c operations.  Many rows: tiles of 256 x 256 whose
 // stages are on their way while others are read (staged_kernel); what is left is its
-// clock: with the unit 47 % busy it falls to 2.0 to 2.1 GHz, and a whole version that
+// clock: with the unit 46 % busy it falls to 2.0 to 2.1 GHz, and a whole version that
 // does not widen q takes 394 of 440 us, one that loads nothing 337.  Few rows: tiles of
 // 64 x 64 straight from registers (gradient_kernel).  The rows are shared out where the
 // tiles do not fill the chip, and the parts' sums joined in a fixed order.

@@ -106,7 +106,7 @@ def test_rms_norm_lengths(env, n, L, C, residual, dtype):
 
 # of each width more rows than the workgroups of a launch, with empty rows between
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("n,L,C", [(4500, 1, 900), (400, 5, 1400), (401, 5, 2047), (330, 3, 2049), (270, 3, 4001),
+@pytest.mark.parametrize("n,L,C", [(4500, 1, 900), (9000, 3, 33), (13000, 1, 200), (4000, 2, 256), (400, 5, 1400), (401, 5, 2047), (330, 3, 2049), (270, 3, 4001),
                                    (150, 2, 7001), (140, 2, 8193), (140, 2, 12001), (130, 2, 16400)])
 def test_rms_norm_many_wide_rows(env, n, L, C, dtype):
     check_norm(*env, n, L, C, True, dtype, True)
