@@ -60,11 +60,29 @@ __device__ inline float float_of(uint32_t w) { return __builtin_bit_cast(float, 
 template <int DT>
 constexpr int kVec = 4 * Elem<DT>::kPerWord;  // elements of 16 bytes
 
-// 16 bytes of a row from column c on; zeros past the row's end.
+// 16 bytes of a row from column c on; zeros past the row's end.  A row's last piece of
+// 16-bit values is read as the row's last 16 bytes and moved down: by elements it would
+// be up to seven loads that the whole wavefront waits for (300 x 1000 x 331 fp16 with a
+// residual 215 us, else 281; its gradient 149, else 226).  Of fp32, up to three loads,
+// it only costs registers (236 us, moved down 288).
 template <int DT>
 __device__ inline Words load_chunk(const char *row, int c, int channels) {
-    constexpr int V = kVec<DT>;
-    if (c + V <= channels) return rocket::load_at<Words>(row + (int64_t)c * Elem<DT>::kSize);
+    constexpr int V = kVec<DT>, kSize = Elem<DT>::kSize;
+    if (kSize == 2 && channels >= V) {
+        const int over = c + V - channels;
+        Words w = rocket::load_at<Words>(row + (int64_t)(over > 0 ? channels - V : c) * kSize);
+        if (over > 0) {
+            typedef uint64_t Two __attribute__((ext_vector_type(2)));
+            Two t = __builtin_bit_cast(Two, w);
+            const int bits = over * kSize * 8, less = bits & 63;
+            const uint64_t carried = less ? t[1] << (64 - less) : 0;
+            t[0] = bits < 64 ? t[0] >> less | carried : bits < 128 ? t[1] >> less : 0;
+            t[1] = bits < 64 ? t[1] >> less : 0;
+            w = __builtin_bit_cast(Words, t);
+        }
+        return w;
+    }
+    if (c + V <= channels) return rocket::load_at<Words>(row + (int64_t)c * kSize);
     Words w = {0, 0, 0, 0};
     using bits = typename Elem<DT>::bits;
 #pragma unroll
@@ -586,13 +604,11 @@ int64_t back_parts(const rocket_sequence_shape *s) {
     const Row row = row_of(chunks_of(s), vec);
     const int each = threads_of(row.threads) / row.threads;
     // waves of a SIMD: three, which is what rows of 16 elements a thread leave room for and
-    // what feeds it where every thread's loads are whole; of 16-bit rows in two loads of a
-    // wave four; of narrower rows that leave threads idle or end inside a load six
-    // (1,000,000 x 64 bf16 157 us with three, 103 with six; 500,000 x 250 232 and 181;
-    // 1,000,000 x 256 386 and 423)
+    // what feeds it where every thread's loads are whole; of narrower rows that leave
+    // threads idle or end inside a load six (1,000,000 x 64 bf16 157 us with three, 103
+    // with six; 1,000,000 x 256 386 and 423)
     const bool whole = s->channels % (row.threads * row.chunks * vec) == 0;
-    const bool narrow = row.threads <= 64 && row.chunks * vec <= 8, two = row.threads == 64 && row.chunks * vec == 16;
-    const int waves = narrow && !whole ? 6 : two && vec == 8 ? 4 : 3;
+    const int waves = row.threads <= 64 && row.chunks * vec <= 8 && !whole ? 6 : 3;
     const int most = row.threads < 512 ? kCus * waves * 256 / threads_of(row.threads) : kCus;
     return std::min<int64_t>((rows + each - 1) / each, most);
 }
