@@ -64,11 +64,12 @@ constexpr int kVec = 4 * Elem<DT>::kPerWord;  // elements of 16 bytes
 // 16-bit values is read as the row's last 16 bytes and moved down: by elements it would
 // be up to seven loads that the whole wavefront waits for (300 x 1000 x 331 fp16 with a
 // residual 215 us, else 281; its gradient 149, else 226).  Of fp32, up to three loads,
-// it only costs registers (236 us, moved down 288).
-template <int DT>
+// it only costs registers (236 us, moved down 288), as in gradients that spill (8 x 1000
+// x 20000 bf16 446 us, moved down 525).
+template <int DT, bool MOVE = true>
 __device__ inline Words load_chunk(const char *row, int c, int channels) {
     constexpr int V = kVec<DT>, kSize = Elem<DT>::kSize;
-    if (kSize == 2 && channels >= V) {
+    if (MOVE && kSize == 2 && channels >= V) {
         const int over = c + V - channels;
         Words w = rocket::load_at<Words>(row + (int64_t)(over > 0 ? channels - V : c) * kSize);
         if (over > 0) {
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(threads_of(G)) void norm_kernel(NormArgs a) {
 template <int DT, int G, int CHUNKS>
 __global__ __launch_bounds__(threads_of(G)) void back_kernel(BackArgs a) {
     constexpr int V = kVec<DT>, kThreads = threads_of(G), kRows = kThreads / G, kHeld = CHUNKS ? CHUNKS : 1;
-    constexpr bool kHold = CHUNKS > 0 && kHeld * V <= 16;
+    constexpr bool kHold = CHUNKS > 0 && kHeld * V <= 16, kMove = G < 1024;
     __shared__ float shared[G > 64 ? 4 * (G / 64) : CHUNKS ? kThreads * V : 1];
     const int j = threadIdx.x % G, C = a.channels;
     const int64_t stride = (int64_t)gridDim.x * kRows;
@@ -411,9 +412,9 @@ __global__ __launch_bounds__(threads_of(G)) void back_kernel(BackArgs a) {
             Words s[kHeld], d[kHeld], t[kHeld];
 #pragma unroll
             for (int q = 0; q < kHeld; q++) {
-                s[q] = load_chunk<DT>(from_s, (q * G + j) * V, C);
-                d[q] = load_chunk<DT>(from_dy, (q * G + j) * V, C);
-                t[q] = kHold && from_dt ? load_chunk<DT>(from_dt, (q * G + j) * V, C) : zero;
+                s[q] = load_chunk<DT, kMove>(from_s, (q * G + j) * V, C);
+                d[q] = load_chunk<DT, kMove>(from_dy, (q * G + j) * V, C);
+                t[q] = kHold && from_dt ? load_chunk<DT, kMove>(from_dt, (q * G + j) * V, C) : zero;
             }
 #pragma unroll
             for (int q = 0; q < kHeld; q++) {
@@ -440,20 +441,20 @@ __global__ __launch_bounds__(threads_of(G)) void back_kernel(BackArgs a) {
             for (int q = 0; q < kHeld; q++) {
                 const int c = (q * G + j) * V;
                 if (!kHold) load_weights<V>(a.weight, c, C, w[q]);
-                if (!kHold && from_dt) t[q] = load_chunk<DT>(from_dt, c, C);
+                if (!kHold && from_dt) t[q] = load_chunk<DT, kMove>(from_dt, c, C);
                 if (c < C) give(s[q], d[q], t[q], c, w[q], mean);
             }
         } else {
             for (int c = j * V; c < C; c += G * V) {
                 load_weights<V>(a.weight, c, C, w[0]);
-                take(load_chunk<DT>(from_s, c, C), load_chunk<DT>(from_dy, c, C), w[0]);
+                take(load_chunk<DT, kMove>(from_s, c, C), load_chunk<DT, kMove>(from_dy, c, C), w[0]);
             }
             join_row<G, false>(inner, none, shared, turn);
             const float mean = inner * inv_c;
             for (int c = j * V; c < C; c += G * V) {
                 load_weights<V>(a.weight, c, C, w[0]);
-                give(load_chunk<DT>(from_s, c, C), load_chunk<DT>(from_dy, c, C),
-                     from_dt ? load_chunk<DT>(from_dt, c, C) : zero, c, w[0], mean);
+                give(load_chunk<DT, kMove>(from_s, c, C), load_chunk<DT, kMove>(from_dy, c, C),
+                     from_dt ? load_chunk<DT, kMove>(from_dt, c, C) : zero, c, w[0], mean);
             }
         }
     }
