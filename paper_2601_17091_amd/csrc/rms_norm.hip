@@ -10,8 +10,8 @@
 // Bound: HBM; a value takes some ten operations.  So a row is read once and
 // stays in the registers of G threads (at least 16), 16 bytes a thread and load,
 // up to 24,576 channels; wider rows are read twice.  The backward pass sums dw
-// over a workgroup's rows in registers, a second kernel joins the workgroups'
-// sums in a fixed order.
+// over a workgroup's rows in registers (of 1,024 threads in shared memory), a second
+// kernel joins the workgroups' sums in a fixed order.
 // Measured, bf16 where nothing else is said (a sum of two 256 MB tensors runs at
 // 5.9 TB/s, a smaller set comes from the 256 MB cache):
 //   s and y of x and a residual, 500 x 1000 x 256   178 us, 5.75 TB/s
@@ -64,8 +64,7 @@ constexpr int kVec = 4 * Elem<DT>::kPerWord;  // elements of 16 bytes
 // 16-bit values is read as the row's last 16 bytes and moved down: by elements it would
 // be up to seven loads that the whole wavefront waits for (300 x 1000 x 331 fp16 with a
 // residual 215 us, else 281; its gradient 149, else 226).  Of fp32, up to three loads,
-// it only costs registers (236 us, moved down 288), as in gradients that spill (8 x 1000
-// x 20000 bf16 446 us, moved down 525).
+// it only costs registers (236 us, moved down 288), as in gradients of 1,024 threads.
 template <int DT, bool MOVE = true>
 __device__ inline Words load_chunk(const char *row, int c, int channels) {
     constexpr int V = kVec<DT>, kSize = Elem<DT>::kSize;
@@ -363,11 +362,19 @@ template <int DT, int G, int CHUNKS>
 __global__ __launch_bounds__(threads_of(G)) void back_kernel(BackArgs a) {
     constexpr int V = kVec<DT>, kThreads = threads_of(G), kRows = kThreads / G, kHeld = CHUNKS ? CHUNKS : 1;
     constexpr bool kHold = CHUNKS > 0 && kHeld * V <= 16, kMove = G < 1024;
+    // 1,024 threads have 128 registers each: dw's sums lie in shared memory, four values of
+    // a thread side by side (8 x 1000 x 20000: fp32 681 us in registers, of which 86 were
+    // spilled, 414 so, bf16 446 and 257; x 12001 fp32 327 and 227)
+    constexpr bool kAside = CHUNKS > 0 && G == 1024;
+    typedef float Four __attribute__((ext_vector_type(4)));
     __shared__ float shared[G > 64 ? 4 * (G / 64) : CHUNKS ? kThreads * V : 1];
+    __shared__ Four aside[kAside ? kThreads * kHeld * V / 4 : 1];
     const int j = threadIdx.x % G, C = a.channels;
     const int64_t stride = (int64_t)gridDim.x * kRows;
     const float inv_c = 1.0f / (float)C;
     float w[kHeld][V], dw[kHeld][V];
+    if (kAside)
+        for (int k = 0; k < kHeld * V / 4; k++) aside[k * kThreads + threadIdx.x] = Four{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < kHeld; k++) {
         if (kHold) load_weights<V>(a.weight, (k * G + j) * V, C, w[k]);
@@ -423,14 +430,25 @@ __global__ __launch_bounds__(threads_of(G)) void back_kernel(BackArgs a) {
                 float fs[V], fd[V];
                 values_of<DT>(s[q], fs);
                 values_of<DT>(d[q], fd);
+                if (kAside) {
 #pragma unroll
-                for (int e = 0; e < V; e++) dw[q][e] = __builtin_fmaf(fd[e], fs[e] * k, dw[q][e]);
+                    for (int h = 0; h < V / 4; h++) {
+                        Four &sum = aside[(q * (V / 4) + h) * kThreads + threadIdx.x];
+                        Four v = sum;
+#pragma unroll
+                        for (int e = 0; e < 4; e++) v[e] = __builtin_fmaf(fd[4 * h + e], fs[4 * h + e] * k, v[e]);
+                        sum = v;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; e++) dw[q][e] = __builtin_fmaf(fd[e], fs[e] * k, dw[q][e]);
+                }
             }
             join_row<G, false>(inner, none, shared, turn);
             const float mean = inner * inv_c;
             // what was computed of the words is computed again, not held over the barrier
 #pragma unroll
-            for (int q = 0; kHold && q < kHeld; q++)
+            for (int q = 0; q < kHeld; q++)
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     uint32_t ws = s[q][e], wd = d[q][e];
@@ -476,8 +494,10 @@ __global__ __launch_bounds__(threads_of(G)) void back_kernel(BackArgs a) {
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < V; e++)
-                if (c + e < C) to[c + e] = dw[q][e];
+            for (int e = 0; e < V; e++) {
+                const float sum = kAside ? aside[(q * (V / 4) + e / 4) * kThreads + threadIdx.x][e % 4] : dw[q][e];
+                if (c + e < C) to[c + e] = sum;
+            }
         }
     }
 }
@@ -577,8 +597,7 @@ bool too_wide(const rocket_sequence_shape *s) { return s->channels > 24576; }
 // Threads and loads of a row in the backward pass: at most 16 elements a thread, so
 // that s, dy, the weights and their sums stay in registers (20 x 1000 x 6000 bf16: 210
 // us, and 414 with 32 elements, where the weights are read for each row and a SIMD holds
-// one wave; 2000 channels, 100 x 1000: 240 and 344).  The last kind, 24, reads them
-// (8 x 1000 x 20000 fp32: 681 us; nothing wider than a workgroup holds a row).
+// one wave; 2000 channels, 100 x 1000: 240 and 344).  The last kind, 24, reads them.
 // The workgroups are at most those that run at once, each with a sum of dw in registers;
 // more make waves of unlike length and more sums to join (100 x 1000 x 2000 bf16: 240 us, 274
 // with two thirds of them, 308 with four thirds).
