@@ -727,8 +727,11 @@ rocket_status rocket_rms_norm_forward(const rocket_sequence_shape *shape, const 
 
 /*
  * 8-bit rows, what rocket_linear_bytes reads: row (i, t) of a sequence as
- *     a = max |v_c|,  q_c = v_c 127 / a to the nearest whole number (ties to even),
+ *     a = max |v_c|,  q_c = v_c (127 / a) to the nearest whole number,
  *     scale = a / 127,  v_c stands for q_c scale
+ * The quotient and the product are fp32 operations that round once each, and then
+ * ties go to even.  A value halfway between two whole numbers may so go to either
+ * (of 16-bit values only such, of fp32 those within 2^-16 of halfway).
  *   q      DEVICE int8 [n, steps, P], P = channels rounded up to a multiple of
  *          ROCKET_ROWS8_PAD, the columns past the channels 0; 16-byte aligned
  *   scale  DEVICE fp32 [n, steps]
@@ -799,7 +802,8 @@ rocket_status rocket_linear_bytes_workspace(const rocket_sequence_shape *shape, 
  * (R = ROCKET_CHECKPOINT_ROWS), and a channel of a block has a scale of its own,
  * since channels (features) differ in level:
  *     a = max |x_c| over the block's rows,  scale[b, c] = a / 127
- *     q[b, c, r - R b] = x[r, c] 127 / a to the nearest whole number (ties to even)
+ *     q[b, c, r - R b] = x[r, c] (127 / a) to the nearest whole number, rounded as
+ *                        8-bit rows are
  *   q      DEVICE int8 [ceil(n steps / R), channels, R], 16-byte aligned
  *   scale  DEVICE fp32 [ceil(n steps / R), channels]
  * Rows past the last, and steps past a series' length, are zeros.  A channel of

@@ -94,8 +94,11 @@ __device__ inline float step8(uint32_t top) {
 __device__ inline uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
 __device__ inline uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// A value to the nearest whole number, ties to even, as a byte; inverse 0 gives
-// 0 whatever the value.
+// A value to the nearest whole number as a byte; inverse 0 gives 0 whatever the value.
+// The inverse and the product are rounded, then ties go to even: off by less than
+// 127 * 2 * 2^-24 before the last rounding, so that a value halfway between two whole
+// numbers may go to either (777 x 129 x 331 fp16: 9,457 of 33 million are, and 1,101 of
+// them go the other way than the quotient itself would).
 __device__ inline uint32_t byte8(float x, float inverse) {
     return inverse == 0.0f ? 0u : (uint32_t)(int)__builtin_rintf(x * inverse) & 255u;
 }

@@ -1,0 +1,29 @@
+"""Operators around linear layers, without a GPU: limits of what their definitions
+promise, and rules of the code that no run can show."""
+import numpy as np
+import pytest
+
+from oracle import linear_oracle as lo
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_8_bit_values_of_16_bit_ones_are_nearest(dtype):
+    """|127 v - q a| <= a / 2 in whole numbers: never the farther neighbour.  Of values that
+    lie exactly halfway some go to the odd one, which is what the header says."""
+    rng = np.random.default_rng(11)
+    bits = 8 if dtype == "bfloat16" else 11
+    # 254 v = a (2 k + 1) asks for 127 in a (halves are common then, but bfloat16 holds
+    # no such a but 127 2^e, whose quotient is exact) or in 2 k + 1: v = a / 2, 63.5 steps
+    top = np.concatenate([rng.integers(1, 2 ** bits // 127 + 1, size=2000) * 127, rng.integers(1, 2 ** bits, size=2000)])
+    twice = rng.integers(-2 * top[:, None], 2 * top[:, None] + 1, size=(4000, 60))   # of v
+    # v = twice / 2 as the type holds it
+    v = lo.to_type(twice.astype(np.float32) / 2, dtype)
+    v = np.concatenate([np.clip(v, -top[:, None], top[:, None])[:, :59], top[:, None] / 2, top[:, None]], 1)
+    v = v.astype(np.float32)
+    assert np.array_equal(lo.to_type(v, dtype), v)
+    q, scale = lo.quantize_rows(v)
+    q, v2 = q[:, :61].astype(np.int64), np.rint(2 * v).astype(np.int64)
+    apart = np.abs(127 * v2 - 2 * q * top[:, None])   # twice the distance, in units of a
+    assert (apart <= top[:, None]).all()
+    halfway = apart == top[:, None]
+    assert halfway.any() and (q[halfway] % 2 != 0).any() and (q[halfway] % 2 == 0).any()
