@@ -18,11 +18,17 @@ typedef int Int4 __attribute__((ext_vector_type(4)));
 
 // A buffer of `bytes` (clamped into [0, 2^31 - 1]) at an address that is the
 // same for the whole wavefront; offsets past it read zeros.
+//
+// A load may read a scalar register only 5 wait states after a vector instruction
+// (readfirstlane is one) has written it.  The compiler does not see the loads below, so
+// the wait stands here: nothing reads the buffer before it.
 __device__ inline Int4 buffer_of(const void *p, int64_t bytes) {
     const uint64_t at = (uint64_t)p;
     const int n = bytes < 0 ? 0 : bytes > INT32_MAX ? INT32_MAX : (int)bytes;
-    return Int4{__builtin_amdgcn_readfirstlane((int)at), __builtin_amdgcn_readfirstlane((int)(at >> 32) & 0xffff),
-                __builtin_amdgcn_readfirstlane(n), 0x00020000};
+    Int4 buffer = {__builtin_amdgcn_readfirstlane((int)at), __builtin_amdgcn_readfirstlane((int)(at >> 32) & 0xffff),
+                   __builtin_amdgcn_readfirstlane(n), 0x00020000};
+    asm volatile("s_nop 4" : "+s"(buffer));
+    return buffer;
 }
 
 // An offset that is past every buffer.
