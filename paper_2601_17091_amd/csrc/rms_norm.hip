@@ -21,6 +21,7 @@
 #include <algorithm>
 
 #include "rows.h"
+#include "join.h"
 
 namespace {
 
@@ -152,10 +153,9 @@ __device__ inline uint32_t moved(uint32_t x) {
 // The sum of s and the largest top over a row's G threads, to all of them.
 // Lanes of a wavefront meet within rows of 16 (exchange of neighbours, of
 // pairs, mirrored halves, mirrored rows), then by exchanges of rows and halves;
-// wavefronts meet in shared memory, whose two halves take turns so that one
-// barrier a row is enough.
+// wavefronts meet in shared memory.
 template <int G, bool TOP>
-__device__ inline void join_row(float &s, uint32_t &top, float *shared, int turn) {
+__device__ inline void join_row(float &s, uint32_t &top, float *shared, int &turn) {
     s += moved<0xB1>(s);
     s += moved<0x4E>(s);
     s += moved<0x141>(s);
@@ -184,24 +184,7 @@ __device__ inline void join_row(float &s, uint32_t &top, float *shared, int turn
             top = rocket::larger(t[0], t[1]);
         }
     }
-    if (G > 64) {
-        constexpr int kWaves = G / 64;
-        float *at = shared + turn * 2 * kWaves;
-        const int wave = threadIdx.x / 64;
-        if (threadIdx.x % 64 == 0) {
-            at[wave] = s;
-            if (TOP) at[kWaves + wave] = __builtin_bit_cast(float, top);
-        }
-        __syncthreads();
-        s = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kWaves; k++) s += at[k];
-        if (TOP) {
-            top = 0;
-#pragma unroll
-            for (int k = 0; k < kWaves; k++) top = rocket::larger(top, __builtin_bit_cast(uint32_t, at[kWaves + k]));
-        }
-    }
+    if constexpr (G > 64) rocket::join_waves<G / 64, TOP>(s, top, shared, turn);
 }
 
 constexpr int threads_of(int G) { return G > 64 ? G : 256; }
@@ -252,10 +235,10 @@ __global__ __launch_bounds__(threads_of(G)) void norm_kernel(NormArgs a) {
 #pragma unroll
         for (int k = 0; k < kHeld; k++) load_weights<V>(a.weight, (k * G + j) * V, C, w[k]);
     int turn = 0;
-    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G; r < a.rows.count; r += stride, turn ^= 1) {
+    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G; r < a.rows.count; r += stride) {
         const Place p = rocket::place_of(a.rows, r);
         if (!p.live) {
-            // nothing is read; a row's threads all come here, so no barrier is missed
+            // nothing is read; a row's threads all come here, and none of them joins
             const Words zero = {0, 0, 0, 0};
             for (int c = j * V; c < end; c += G * V) {
                 if (KIND == kSequence)
@@ -382,7 +365,7 @@ __global__ __launch_bounds__(threads_of(G)) void back_kernel(BackArgs a) {
         for (int e = 0; e < V; e++) dw[k][e] = 0.0f;
     }
     int turn = 0;
-    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G; r < a.rows.count; r += stride, turn ^= 1) {
+    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G; r < a.rows.count; r += stride) {
         const Place p = rocket::place_of(a.rows, r);
         char *dx = rocket::row_at(a.dx, p);
         if (!p.live) {

@@ -38,3 +38,38 @@ def test_8_bit_values_halfway_between_two(env, dtype):
     assert np.array_equal(kq.cpu().numpy(), want) and np.array_equal(ks.cpu().numpy(), wscale)
     q = q.cpu().numpy()[:, :128].astype(np.int64)
     assert (np.abs(127 * np.rint(2 * v).astype(np.int64) - 2 * q * top) <= top).all()
+
+
+# threads of a row from 128 to 1,024, held in registers, summed aside, and read twice
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("C", [1500, 2500, 5000, 10000, 20000, 25000])
+def test_rms_norm_rows_without_data_between_others(env, C, dtype):
+    """Workgroups that go from row to row, with any number of rows without data between two
+    that hold some: each row's results are those of a call without such rows."""
+    torch, seq = env
+    g = torch.Generator(device="cuda").manual_seed(C)
+    rows = 2500
+    lengths = torch.randint(0, 2, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    live = lengths.bool()
+    rand = lambda: torch.randn(rows, 1, C, generator=g, device="cuda").to(getattr(torch, dtype))  # noqa: E731
+    x, r, dy, dt = rand(), rand(), rand(), rand()
+    x *= 1 + torch.rand(rows, 1, 1, generator=g, device="cuda").to(x.dtype) * 9   # no row's sum is another's
+    w = 1 + 0.2 * torch.randn(C, generator=g, device="cuda")
+    own = [t[live].clone() for t in (x, r, dy, dt)]
+    for t in (x, r, dy, dt):
+        t[~live] = float("nan")
+    for _ in range(3):
+        y, total, rstd = seq.rms_norm(x, w, residual=r, lengths=lengths)
+        q, scale, _, rstd8 = seq.rms_norm8(x, w, residual=r, lengths=lengths)
+        qx, sx = seq.quantize_rows(x, lengths=lengths)
+        dx, dw = seq.rms_norm_backward(dy, total, rstd, w, dtotal=dt, lengths=lengths)
+        y1, total1, rstd1 = seq.rms_norm(own[0], w, residual=own[1])
+        q1, scale1, _, _ = seq.rms_norm8(own[0], w, residual=own[1])
+        qx1, sx1 = seq.quantize_rows(own[0])
+        dx1, dw1 = seq.rms_norm_backward(own[2], total1, rstd1, w, dtotal=own[3])
+        for got, want in ((y, y1), (total, total1), (rstd, rstd1), (q, q1), (scale, scale1), (rstd8, rstd1), (qx, qx1),
+                          (sx, sx1), (dx, dx1)):
+            assert torch.equal(got[live], want) and (got[~live] == 0).all()
+        # sums of at most 2,500 terms in two orders, 2^-24 of the terms for each
+        terms = (own[2].double() * total1.double() * rstd1.double()[:, :, None]).abs().sum((0, 1))
+        assert ((dw.double() - dw1.double()).abs() <= 2 * (rows + 2) * lo.U * terms).all()
