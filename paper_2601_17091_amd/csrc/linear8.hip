@@ -17,6 +17,7 @@
 
 #include "rows.h"
 #include "stage.h"
+#include "walk.h"
 
 namespace {
 
@@ -25,6 +26,7 @@ using rocket::Int4;
 using rocket::Elem;
 using rocket::Place;
 using rocket::Rows;
+using rocket::Tile;
 using rocket::View;
 
 typedef int Int16 __attribute__((ext_vector_type(16)));
@@ -170,19 +172,9 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
 
     // tiles: this workgroup's first one, and the way to its next
     const int64_t first = SPLIT ? group / a.parts : group;
-    const int64_t step_t = SPLIT ? INT32_MAX : (int64_t)gridDim.x / a.tiles;
-    const int step_m = (int)(gridDim.x % a.tiles);
-    struct Tile {
-        int64_t t;
-        int m;
-    };
+    const rocket::Steps steps = {SPLIT ? INT32_MAX : (int64_t)gridDim.x / a.tiles, (int)(gridDim.x % a.tiles), a.tiles};
     Tile tile = {first / a.tiles, (int)(first % a.tiles)};
     const int64_t count = LIVE ? a.order[a.rows.count] : a.rows.count, tiles_t = (count + kT - 1) / kT;
-    const auto next_of = [&](Tile x) {
-        x.t += step_t, x.m += step_m;
-        if (x.m >= a.tiles) x.m -= a.tiles, x.t++;
-        return x;
-    };
 
     // a line's pieces are moved by its number, so that 16 lines in a row meet every bank alike
     const auto turn_of = [](int line) { return COLS == 64 ? line >> 2 & 3 : line >> 1 & 7; };
@@ -199,15 +191,15 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
 #pragma unroll
         for (int k = 0; k < 2; k++)
             rest[k] = (lane % kPieces ^ turn_of(k * kLines + lane / kPieces)) >= kPieces / 2 ? rocket::kNowhere : 0;
-    Tile ask_tile = tile;
-    int ask_stage = 0, ask_slot = 0, ask_turn = 0;
+    rocket::Asked asked = {tile, 0, true};
+    int ask_slot = 0, ask_turn = 0;
     uint32_t ask_at = 0, ask_to = base;
     Int4 weights, rows;
     const auto open_tile = [&]() {
-        const int64_t left_t = count - ask_tile.t * kT;   // 0 or less: past the last tile
-        const int left_m = a.channels - ask_tile.m * kM;
-        weights = rocket::buffer_of(a.p + (int64_t)ask_tile.m * kM * a.columns,
-                                    left_t > 0 ? (int64_t)(left_m < kM ? left_m : kM) * a.columns : 0);
+        const int64_t first_t = asked.tile.t * kT, first_m = (int64_t)asked.tile.m * kM;
+        asked.there = first_t < count;
+        weights = rocket::buffer_of(a.p + first_m * a.columns,
+                                    asked.there ? rocket::bytes_of_lines(a.channels, first_m, kM, a.columns) : 0);
         if (LIVE) {
             rows = rocket::buffer_of(a.q, a.rows.count * a.columns);
             const uint32_t *sources = (const uint32_t *)(shared + kSources) + ask_turn * kT;
@@ -218,17 +210,14 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
                 from[kLoadsM + k] = sources[line] + (lane % kPieces ^ turn_of(line)) * 16;
             }
         } else {
-            rows = rocket::buffer_of(a.q + ask_tile.t * kT * a.columns, (left_t < kT ? left_t : kT) * a.columns);
+            rows = rocket::buffer_of(a.q + first_t * a.columns, rocket::bytes_of_lines(count, first_t, kT, a.columns));
         }
     };
     const auto open_stage = [&]() {
-        if (ask_stage == stages) {
-            ask_tile = next_of(ask_tile), ask_stage = 0;
-            open_tile();
-        }
-        ask_at = (stage0 + ask_stage++) * COLS;
+        if (asked.crosses(stages, steps)) open_tile();
+        ask_at = asked.next(stage0, COLS);
         if (COLS == 128)
-            for (int k = 0; k < 2; k++) past[k] = stage0 + ask_stage == all_stages ? rest[k] : 0;
+            for (int k = 0; k < 2; k++) past[k] = stage0 + asked.stage == all_stages ? rest[k] : 0;
         ask_to = base + ask_slot * kStage;
         ask_slot = (ask_slot + 1) % kSlots;
     };
@@ -277,7 +266,7 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
     write_table(look_up(tile, coming), 0);
     if (LIVE) {
         write_sources(coming, 0);
-        coming = row_of(next_of(tile));
+        coming = row_of(steps.after(tile));
         write_sources(coming, 1);
         __syncthreads();
     }
@@ -349,9 +338,9 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
         // (the matrix unit's last results reach their registers 18 cycles after they are asked
         // for, which the compiler does not see that `taken` reads)
         asm volatile("s_nop 15\n\ts_nop 15");
-        const Tile following = next_of(tile);
+        const Tile following = steps.after(tile);
         const Table table = look_up(following, LIVE ? coming : row_of(following));
-        if (LIVE) coming = row_of(next_of(following));
+        if (LIVE) coming = row_of(steps.after(following));
         const float *factors = (const float *)(shared + kTables + turn * kTable), *row_scale = factors + 2 * kM;
         const uint64_t *row_at = (const uint64_t *)(row_scale + kT);
         const int left_m = a.channels - tile.m * kM;

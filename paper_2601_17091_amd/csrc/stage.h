@@ -43,9 +43,9 @@ typedef __attribute__((address_space(3))) char *Shared;
 __device__ inline Shared shared_at(uint32_t at) { return (Shared)(uintptr_t)at; }
 
 // 64 pieces of 16 bytes to shared memory from `to` on, a lane's from `offset` and
-// `more`, which is the same for all.  Written in assembly since
-// the compiler would wait for every load before the next read of shared memory;
-// it has no result, and M0, which it sets, holds nothing of the compiler's here.
+// `more`, which is the same for all and at most the buffer's bytes (walk.h).  Written in
+// assembly since the compiler would wait for every load before the next read of shared
+// memory; it has no result, and M0, which it sets, holds nothing of the compiler's here.
 __device__ inline void load_stage16(const Int4 &buffer, uint32_t to, uint32_t offset, uint32_t more = 0) {
     asm volatile(
         "s_mov_b32 m0, %0\n\t"
