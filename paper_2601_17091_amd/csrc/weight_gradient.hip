@@ -637,7 +637,9 @@ Cut cut_of(const rocket_sequence_shape *s, int64_t channels, const View &dy) {
     // not change with strides and alignment
     const bool anew = planes > 1 || m % 2 != 0;
     const double staged_us = cut_parts(d, staged, part_us) + (anew ? 9.0 : 6.0);
-    if (staged_us < direct_us) {
+    // no rows: the staged kernel would read the first block's scales, which is not there;
+    // the direct one reads nothing and writes zeros
+    if (rows > 0 && staged_us < direct_us) {
         c = d;
         c.staged = true;
         c.stride = (m + 7) / 8 * 16;

@@ -73,3 +73,17 @@ def test_rms_norm_rows_without_data_between_others(env, C, dtype):
         # sums of at most 2,500 terms in two orders, 2^-24 of the terms for each
         terms = (own[2].double() * total1.double() * rstd1.double()[:, :, None]).abs().sum((0, 1))
         assert ((dw.double() - dw1.double()).abs() <= 2 * (rows + 2) * lo.U * terms).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("N,C", [(2000, 6000), (4096, 4096), (1536, 20000)])
+def test_weight_gradient_of_no_rows_of_a_large_layer(env, N, C, dtype):
+    """Zeros, and nothing is read: the checkpoint of no rows has no memory."""
+    torch, seq = env
+    q, scale = torch.empty(0, C, 128, dtype=torch.int8, device="cuda"), torch.empty(0, C, device="cuda")
+    for leading in ((0, 5), (5, 0), (0,)):
+        dy = torch.empty(*leading, N, dtype=getattr(torch, dtype), device="cuda")
+        ways = [None] if len(leading) == 1 else [None, torch.zeros(leading[0], dtype=torch.int32, device="cuda")]
+        for lengths in ways:
+            dw, db = seq.linear_weight_gradient(dy, q, scale, lengths=lengths)
+            assert dw.shape == (N, C) and (dw == 0).all() and (db == 0).all()

@@ -27,3 +27,41 @@ def test_8_bit_values_of_16_bit_ones_are_nearest(dtype):
     assert (apart <= top[:, None]).all()
     halfway = apart == top[:, None]
     assert halfway.any() and (q[halfway] % 2 != 0).any() and (q[halfway] % 2 == 0).any()
+
+
+# ---------------------------------------------------------------- the C ABI
+@pytest.fixture(scope="module")
+def lib():
+    import os
+
+    from paper_2601_17091_amd import rocket as rb
+    if not os.path.exists(rb.LIB_PATH):
+        from paper_2601_17091_amd import build_lib
+        build_lib.build()
+    return rb.library()
+
+
+def gradient_workspace(lib, n, steps, m, c, dtype, lengths=None, data=0x10000, step=None):
+    """Bytes that rocket_linear_weight_gradient asks for; rows at a distance of `step` values (m)."""
+    import ctypes
+
+    from paper_2601_17091_amd import rocket as rb
+    shape = rb.CSequenceShape(n, steps, m, dtype, lengths)
+    view = rb.CSequence(data, steps * (step or m), step or m)
+    size = ctypes.c_int64(-1)
+    assert lib.rocket_linear_weight_gradient_workspace(ctypes.byref(shape), c, ctypes.byref(view), ctypes.byref(size)) == 0
+    return size.value
+
+
+LARGE_LAYERS = [(1536, 20000), (2000, 6000), (1000, 12000), (600, 20000), (4096, 4096)]
+
+
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("m,c", LARGE_LAYERS)
+def test_a_gradient_of_no_rows_stages_nothing(lib, m, c, dtype):
+    """The staged kernel reads its first block's scales at once: without a block it must not
+    be the one chosen, which its workspace (the biases' sums at least) tells."""
+    assert gradient_workspace(lib, 8, 1000, m, c, dtype) > 0   # with rows it is
+    for n, steps in ((0, 5), (5, 0), (0, 0)):
+        for lengths in (None, 0x10000):
+            assert gradient_workspace(lib, n, steps, m, c, dtype, lengths, data=None) == 0
