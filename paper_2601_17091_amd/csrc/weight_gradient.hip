@@ -232,8 +232,10 @@ struct StagedArgs {
 //
 // The sum is kept in units of the current block's scale: at a block's first stage
 // it is multiplied by (last scale / this scale), so that one set of registers
-// holds it.  Where that quotient leaves 2^-40 .. 2^40 the sum is added to `dweight`
-// and begins anew.
+// holds it.  Where a scale is 2^20 or more from the one at which the sum began, the sum
+// is added to `dweight` and begins anew: any two scales of a sum are so less than 2^40
+// apart, and no term leaves fp32's range on its way (quotients of neighbours alone may
+// be small and yet multiply to anything, as a channel fades).
 //
 // PLANES: parts of dy's values, the smallest first.
 template <bool HALF, int PLANES, bool LIVE, int MT, int NT, int WM, int WC>
@@ -331,7 +333,7 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
     const uint32_t read_s = kBytesA + kBytesC + wave * 256 + lane % 32 * 4;
 
     Float16 sum[MT][NT] = {};
-    float unit[NT], bias = 0.0f;
+    float unit[NT], began[NT], bias = 0.0f;   // the block's scale, and the one at which the sum began
     uint32_t held[NT];
     const int64_t to0 = ((int64_t)part * a.m + m0 + wm * 32 * MT + 4 * half) * a.c + c0 + wc * 32 * NT + lane % 32;
     bool begun = false;   // whether dweight holds a sum already
@@ -356,7 +358,7 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
 #pragma unroll
     for (int k = 0; k < NT; k++) {
         const int c = c0 + (wc * NT + k) * 32 + lane % 32;
-        unit[k] = c < a.c ? a.scale[first * a.c + c] : 0.0f;
+        began[k] = unit[k] = c < a.c ? a.scale[first * a.c + c] : 0.0f;
         held[k] = unit[k] == 0.0f ? 0u : ~0u;
         factor[k] = 1.0f;
     }
@@ -456,14 +458,15 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
                 held[k] = next[k] == 0.0f ? 0u : ~0u;   // a scale of 0: whatever q holds counts nothing
                 if (next[k] == 0.0f) next[k] = unit[k];
                 factor[k] = unit[k] == 0.0f ? 1.0f : unit[k] / next[k];
-                const float size = __builtin_fabsf(factor[k]);
-                far |= size > 0x1p40f || size < 0x1p-40f;
+                if (unit[k] == 0.0f) began[k] = next[k];   // all scales were 0: there is no sum yet
+                const float from = __builtin_fabsf(began[k]), to = __builtin_fabsf(next[k]);
+                far |= from > 0x1p20f * to || to > 0x1p20f * from;
             }
             if (__any(far)) {
                 put(begun);
                 begun = true;
 #pragma unroll
-                for (int k = 0; k < NT; k++) factor[k] = 0.0f;
+                for (int k = 0; k < NT; k++) factor[k] = 0.0f, began[k] = next[k];
             }
 #pragma unroll
             for (int k = 0; k < NT; k++) unit[k] = next[k];

@@ -87,3 +87,42 @@ def test_weight_gradient_of_no_rows_of_a_large_layer(env, N, C, dtype):
         for lengths in ways:
             dw, db = seq.linear_weight_gradient(dy, q, scale, lengths=lengths)
             assert dw.shape == (N, C) and (dw == 0).all() and (db == 0).all()
+
+
+# staged tiles of 32, 64, 128 and 256 channels of dy (as they lie and laid out anew), and the
+# direct way
+DRIFTS = [(40000, 20, 3000), (40000, 50, 3000), (30000, 128, 2000), (30000, 300, 1000), (30009, 301, 999), (1536, 40, 90)]
+
+
+def drifting(torch, kind, blocks):
+    """Scales [blocks, 1] that move by less than 2^40 a block, by 2^117 and more in a few."""
+    b = torch.arange(blocks, device="cuda")
+    turns = {"falls": 60 - 39 * (b % 4), "rises": 39 * (b % 4) - 60, "falls slowly": 100 - 19 * (b % 11),
+             "to and fro": torch.where(b % 8 < 4, 60 - 39 * (b % 4), 39 * (b % 4) - 57)}
+    return (2.0 ** turns[kind].float())[:, None]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("kind", ["falls", "rises", "falls slowly", "to and fro"])
+@pytest.mark.parametrize("rows,N,C", DRIFTS)
+def test_weight_gradient_of_drifting_scales(env, rows, N, C, kind, dtype):
+    """A channel that fades along the rows, or grows: what an early block gave stays, also
+    where no later one adds to it."""
+    torch, seq = env
+    g = torch.Generator(device="cuda").manual_seed(rows + N + C)
+    blocks = -(-rows // 128)
+    q = torch.randint(-127, 128, (blocks, C, 128), generator=g, device="cuda", dtype=torch.int8)
+    scale = (torch.rand(blocks, C, generator=g, device="cuda") * 0.25 + 1) * drifting(torch, kind, blocks)
+    scale[:, C // 2:] = 1.0 + scale[:, C // 2:].clamp(max=1.0)   # ordinary ones beside them
+    dy = torch.randn(rows, N, generator=g, device="cuda").to(getattr(torch, dtype))
+    for m in range(0, N, 3):   # channels that only every 16th block reaches
+        dy[:, m] *= ((torch.arange(rows, device="cuda") // 128 + m // 3) % 16 == 0).to(dy.dtype)
+    dw, db = seq.linear_weight_gradient(dy, q, scale)
+    d = dy.double()
+    x = (q.double() * scale.double()[:, :, None]).transpose(1, 2).reshape(-1, C)[:rows]
+    want = d.t().contiguous() @ x
+    # a product enters a block's sum of at most 384, rounded or cut off, then at most
+    # `blocks` sums and multiplications and as many joins
+    tol = (d.abs().t().contiguous() @ x.abs()) * (2 * 384 + 4 * blocks) * lo.U
+    assert ((dw.double() - want).abs() <= tol).all()
+    assert ((db.double() - d.sum(0)).abs() <= d.abs().sum(0) * 3 * rows * lo.U).all()
