@@ -19,6 +19,7 @@
 //                                           places, 190 the product, 6 the join
 //   64 rows fp32, 192 by 2,000              5.3 us
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.h"
 #include "stage.h"
@@ -337,7 +338,16 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
     uint32_t held[NT];
     const int64_t to0 = ((int64_t)part * a.m + m0 + wm * 32 * MT + 4 * half) * a.c + c0 + wc * 32 * NT + lane % 32;
     bool begun = false;   // whether dweight holds a sum already
-    auto put = [&](bool add) {
+    // A sum that was put aside begins at 0, and not as a product with 0, which would make a
+    // NaN of an infinity.  The zeros are written where the sum lies: as values of the
+    // language they make the compiler keep a second sum (50 registers spilled, 813 us in
+    // place of 420), and chosen where the next block multiplies they take 444 us.  Of fp32's
+    // three parts this here spills 139 registers, and the choice takes 2 % (228 us and 232).
+    const auto zeroed = [](float v) {
+        asm volatile("v_mov_b32 %0, 0" : "+v"(v));
+        return v;
+    };
+    auto put = [&](bool add, auto anew) {
 #pragma unroll
         for (int y = 0; y < NT; y++) {
             float *to = a.dweight + to0 + y * 32;
@@ -347,6 +357,7 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
                     if (left > 0) *to = (add ? *to : 0.0f) + sum[x][y][i] * unit[y];
+                    if constexpr (anew) sum[x][y][i] = zeroed(sum[x][y][i]);
                     to += i % 4 == 3 ? (int64_t)5 * a.c : (int64_t)a.c;
                     left -= i % 4 == 3 ? 5 : 1;
                     asm volatile("" : "+v"(to), "+v"(left)::"memory");   // one after the other: few registers
@@ -355,6 +366,7 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
     };
 
     float factor[NT];
+    bool anew = false;   // the sum was added to dweight and begins at 0
 #pragma unroll
     for (int k = 0; k < NT; k++) {
         const int c = c0 + (wc * NT + k) * 32 + lane % 32;
@@ -405,7 +417,8 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
 #pragma unroll
                 for (int y = 0; y < NT; y++)
 #pragma unroll
-                    for (int i = 0; i < 16; i++) sum[x][y][i] *= factor[y];
+                    for (int i = 0; i < 16; i++)
+                        sum[x][y][i] = PLANES > 1 && anew ? 0.0f : sum[x][y][i] * factor[y];
             };
             if (s == 0) multiply(0);
 #pragma unroll
@@ -462,18 +475,19 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
                 const float from = __builtin_fabsf(began[k]), to = __builtin_fabsf(next[k]);
                 far |= from > 0x1p20f * to || to > 0x1p20f * from;
             }
-            if (__any(far)) {
-                put(begun);
+            anew = __any(far);
+            if (anew) {
+                put(begun, std::bool_constant<PLANES == 1>());
                 begun = true;
 #pragma unroll
-                for (int k = 0; k < NT; k++) factor[k] = 0.0f, began[k] = next[k];
+                for (int k = 0; k < NT; k++) factor[k] = 1.0f, began[k] = next[k];
             }
 #pragma unroll
             for (int k = 0; k < NT; k++) unit[k] = next[k];
         }
     }
     rocket::wait_loads<0>();
-    put(begun);
+    put(begun, std::false_type());
     if (a.dbias) {
         static_assert(MT <= WC, "a wavefront counts at most one matrix' rows");
         bias += __shfl_xor(bias, 32);

@@ -126,3 +126,33 @@ def test_weight_gradient_of_drifting_scales(env, rows, N, C, kind, dtype):
     tol = (d.abs().t().contiguous() @ x.abs()) * (2 * 384 + 4 * blocks) * lo.U
     assert ((dw.double() - want).abs() <= tol).all()
     assert ((db.double() - d.sum(0)).abs() <= d.abs().sum(0) * 3 * rows * lo.U).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("kind", ["even", "far", "falls"])
+def test_weight_gradient_keeps_infinities(env, kind, dtype):
+    """An infinite dy gives infinities of its products' signs (NaN where it meets a 0), whatever
+    the scales of later blocks are; a finite channel is not touched."""
+    torch, seq = env
+    rows, N, C = 30000, 300, 1000
+    g = torch.Generator(device="cuda").manual_seed(9)
+    blocks = -(-rows // 128)
+    q = torch.randint(-127, 128, (blocks, C, 128), generator=g, device="cuda", dtype=torch.int8)
+    scale = torch.rand(blocks, C, generator=g, device="cuda") + 0.5
+    if kind == "far":
+        scale *= 2.0 ** (60.0 * (torch.arange(blocks, device="cuda") % 2))[:, None]
+    elif kind == "falls":
+        scale *= drifting(torch, kind, blocks)
+    dy = torch.randn(rows, N, generator=g, device="cuda").to(getattr(torch, dtype))
+    want = seq.linear_weight_gradient(dy, q, scale)
+    at = {7: (130, float("inf")), 100: (5 * 128 + 3, float("-inf")), 299: (0, float("inf"))}
+    for m, (row, value) in at.items():
+        dy[row, m] = value
+    dw, db = seq.linear_weight_gradient(dy, q, scale)
+    for m, (row, value) in at.items():
+        met = q[row // 128, :, row % 128].float() * value   # NaN for 0
+        assert torch.equal(dw[m].isnan(), met.isnan()) and torch.equal(dw[m][met != 0].nan_to_num(0.0, 1.0, -1.0),
+                                                                       met[met != 0].nan_to_num(0.0, 1.0, -1.0))
+        assert db[m] == value
+    rest = [m for m in range(N) if m not in at]
+    assert torch.equal(dw[rest], want[0][rest]) and torch.equal(db[rest], want[1][rest])
