@@ -285,7 +285,10 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
     uint32_t ask_to = base;
     Int4 dy_buffer, q_buffer, scale_buffer;
     uint64_t live = 0;
-    const int has_c = a.c - c0 < kC ? a.c - c0 : kC, row_bytes = (a.width - m0) * 2;
+    // of a stage's last row this tile's bytes, not those to the row's end: rows that are laid
+    // out may be 2^25 bytes apart
+    static_assert(63ll * (1 << 25) + kM * 2 <= INT32_MAX, "a stage of the widest rows");
+    const int has_c = a.c - c0 < kC ? a.c - c0 : kC, row_bytes = (a.width - m0 < kM ? a.width - m0 : kM) * 2;
     auto open_stage = [&]() {
         const bool some = asked < stages;
         const int s = asked % (2 * PLANES), half = s / PLANES;

@@ -156,3 +156,20 @@ def test_weight_gradient_keeps_infinities(env, kind, dtype):
         assert db[m] == value
     rest = [m for m in range(N) if m not in at]
     assert torch.equal(dw[rest], want[0][rest]) and torch.equal(db[rest], want[1][rest])
+
+
+@pytest.mark.parametrize("N", [2 ** 24, 2 ** 24 - 7, 2 ** 24 - 8])
+def test_weight_gradient_of_the_widest_rows(env, N):
+    """A stage of rows that are laid out 2^25 bytes apart reaches 2^31."""
+    torch, seq = env
+    rows, C = 130, 256
+    g = torch.Generator(device="cuda").manual_seed(4)
+    dy = torch.randn(rows, N, generator=g, device="cuda", dtype=torch.bfloat16)
+    q, scale = seq.checkpoint(torch.randn(rows, C, generator=g, device="cuda"))
+    dw, db = seq.linear_weight_gradient(dy, q, scale)
+    x = (q.double() * scale.double()[:, :, None]).transpose(1, 2).reshape(-1, C)[:rows]
+    for part in (slice(0, 300), slice(N // 2 - 300, N // 2 + 300), slice(N - 300, N)):
+        d = dy[:, part].double()
+        tol = (d.abs().t().contiguous() @ x.abs()) * (2 * rows + 18) * lo.U
+        assert ((dw[part].double() - d.t().contiguous() @ x).abs() <= tol).all()
+        assert ((db[part].double() - d.sum(0)).abs() <= d.abs().sum(0) * (3 * rows + 2) * lo.U).all()
