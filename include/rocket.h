@@ -778,7 +778,7 @@ rocket_status rocket_rms_norm_workspace(const rocket_sequence_shape *shape, int6
  *     y[i, t, m] = scale[i, t] weight_scale[m] (sum over k of q[i, t, k] weight[m, k]) + bias[m]
  *   shape         that of y; channels: the weights' rows
  *   columns       of q and weight: a positive multiple of ROCKET_ROWS8_PAD, at most
- *                 131,072 (the sum is of whole numbers and exact in 32 bits)
+ *                 131,072 (the sum is of whole numbers and exact, whatever they are)
  *   q, scale      DEVICE int8 [n, steps, columns], fp32 [n, steps]: 8-bit rows
  *   weight, weight_scale  DEVICE int8 [channels, columns], fp32 [channels]:
  *                 8-bit rows of the weights

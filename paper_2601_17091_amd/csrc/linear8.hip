@@ -2,7 +2,8 @@
 //
 //   y[t, m] = scale[t] wscale[m] (sum over k of q[t, k] p[m, k]) + bias[m]
 //
-// The sum is of whole numbers and exact: 32 bits hold it up to 131,072 columns.
+// The sum is of whole numbers and exact: 32 bits hold it up to 131,072 columns (2^31 of
+// -128 by -128 in all of them is told from -2^31, which no sum reaches).
 // Scales and bias are fp32, the result is rounded once.
 //
 // Bound: few rows by reading the weights, many by the matrix unit (2,440 TOP/s in a
@@ -30,6 +31,12 @@ using rocket::Tile;
 using rocket::View;
 
 typedef int Int16 __attribute__((ext_vector_type(16)));
+
+// The most columns: 2^31 / 2^14.  The sum 2^31 arrives as -2^31, which stands for nothing
+// else (128 * 127 * 131,072 is less); as 2^31 - 1 it is 2^31 again once it is fp32.
+constexpr int kMostColumns = 131072;
+
+__device__ inline int held_sum(int sum) { return sum == INT32_MIN ? INT32_MAX : sum; }
 
 struct ProductArgs {
     Rows rows;
@@ -97,9 +104,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(ProductArgs a) {
     __syncthreads();
     const int c = threadIdx.x % 16, t = threadIdx.x / 16;
     if (t >= 16 * NT || t >= a.rows.count || m0 + c >= a.channels) return;
-    int total = 0;
+    uint32_t sum_of_waves = 0;
 #pragma unroll
-    for (int w = 0; w < kFewWaves; w++) total += sums[w][t / 16][c][t % 16];
+    for (int w = 0; w < kFewWaves; w++) sum_of_waves += (uint32_t)sums[w][t / 16][c][t % 16];
+    const int total = held_sum((int)sum_of_waves);
     const Place place = rocket::place_of(a.rows, t);
     const float bias = a.bias ? a.bias[m0 + c] : 0.0f;
     const float v = place.live ? __builtin_fmaf((float)total, a.scale[t] * a.wscale[m0 + c], bias) : 0.0f;
@@ -160,6 +168,10 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
     typedef uint32_t Words __attribute__((ext_vector_type(kSize)));   // four values
     static_assert(kLoadsM * kWaves * kLines == kM && kLoadsT * kWaves * kLines == kT, "whole loads");
     static_assert(kM <= kThreads && kT <= kThreads, "a thread for each line of a table");
+    // Tiles that tell a sum of 2^31 from -2^31; cut_of gives the others no call of that many
+    // columns.  The same in tiles of 256 x 256 spills 150 registers, and in those of 64 x 64
+    // it takes 5 us (1,000 rows of 1,984 columns by 1,536 channels 14 us, 19 so); here nothing.
+    constexpr bool kTellsMost = !SPLIT && !LIVE && kProducts == 4 && COLS == 64;
     constexpr int kSources = kTables + 2 * kTable;   // LIVE: where the lines of two tiles' rows lie in q
     __shared__ __attribute__((aligned(1024))) char shared[kSources + (LIVE ? 8 * kT : 0)];
     const uint32_t base = rocket::shared_address(shared);
@@ -338,6 +350,13 @@ __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs
         // (the matrix unit's last results reach their registers 18 cycles after they are asked
         // for, which the compiler does not see that `taken` reads)
         asm volatile("s_nop 15\n\ts_nop 15");
+        if (kTellsMost && a.columns == kMostColumns)
+#pragma unroll
+            for (int x = 0; x < MT; x++)
+#pragma unroll
+                for (int y = 0; y < NT; y++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) sum[x][y][i] = held_sum(sum[x][y][i]);
         const Tile following = steps.after(tile);
         const Table table = look_up(following, LIVE ? coming : row_of(following));
         if (LIVE) coming = row_of(steps.after(following));
@@ -464,8 +483,9 @@ __global__ __launch_bounds__(256) void finish_kernel(ProductArgs a) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, r = i / a.channels, count = a.rows.count * a.channels;
     if (r >= a.rows.count) return;
     const int m = (int)(i - r * a.channels);
-    int total = 0;
-    for (int k = 0; k < a.parts; k++) total += a.sums[k * count + i];
+    uint32_t sum_of_parts = 0;
+    for (int k = 0; k < a.parts; k++) sum_of_parts += (uint32_t)a.sums[k * count + i];
+    const int total = held_sum((int)sum_of_parts);
     const Place place = rocket::place_of(a.rows, r);
     const float bias = a.bias ? a.bias[m] : 0.0f;
     const float v = place.live ? __builtin_fmaf((float)total, a.scale[r] * a.wscale[m], bias) : 0.0f;
@@ -505,6 +525,7 @@ Cut cut_of(const rocket_sequence_shape *s, int64_t columns) {
     double best = 1e300;
     int64_t rounds = 0;
     for (const Cost &k : kCosts) {
+        if (columns == kMostColumns && k.way != kMiddleTwice) continue;   // kTellsMost
         const int64_t tiles = (rows + k.t - 1) / k.t * ((channels + k.m - 1) / k.m), all = k.at_once * kCus;
         // two on a CU: a last round of few tiles goes faster
         const double rest = (double)(tiles % all) / (double)all;
@@ -520,7 +541,7 @@ Cut cut_of(const rocket_sequence_shape *s, int64_t columns) {
     const int64_t least = c.way == kMiddleTwice ? 3 * 64 : 2 * 128;   // columns of a way's slots
     c.live = (c.way == kBig || c.way == kTall || c.way == kMiddleTwice) && rounds > 1 && columns >= least &&
              best * std::min(1.0, stages / 8.0) > 20.0 && series > 1 && series <= kMostSeries && steps > 1 &&
-             rows * columns <= INT32_MAX;
+             rows * columns <= INT32_MAX && columns != kMostColumns;
     if (c.live) c.bytes = (rows + 1) * 4;
     const int64_t tiles = (rows + 127) / 128 * ((channels + 127) / 128), lines = (columns + 127) / 128;
     for (int64_t p = 2; p <= lines / 2 && tiles * p <= 4 * kCus; p += 1 + p / 8) {
@@ -580,7 +601,7 @@ void launch(ProductArgs a, const Cut &cut, hipStream_t s) {
     }
 }
 
-bool columns_ok(int64_t columns) { return columns > 0 && columns <= 131072 && columns % rocket::kPad8 == 0; }
+bool columns_ok(int64_t columns) { return columns > 0 && columns <= kMostColumns && columns % rocket::kPad8 == 0; }
 
 }  // namespace
 

@@ -173,3 +173,35 @@ def test_weight_gradient_of_the_widest_rows(env, N):
         tol = (d.abs().t().contiguous() @ x.abs()) * (2 * rows + 18) * lo.U
         assert ((dw[part].double() - d.t().contiguous() @ x).abs() <= tol).all()
         assert ((db[part].double() - d.sum(0)).abs() <= d.abs().sum(0) * (3 * rows + 2) * lo.U).all()
+
+
+# rows and channels of each way that takes the most columns: few rows, columns shared out,
+# tiles of 128 and of 64 channels; live rows listed and not
+@pytest.mark.parametrize("n,L,N", [(1, 1, 1), (1, 64, 33), (1, 130, 70), (1, 300, 192), (2, 900, 192), (1, 7000, 513),
+                                   (2, 3500, 1300), (5, 700, 2000), (1, 20000, 17)])
+def test_linear8_of_the_largest_sums(env, n, L, N):
+    """-128 by -128 at 131,072 columns is 2^31, one more than 32 bits hold; with one value
+    less, or at 131,008 columns, it is not."""
+    torch, seq = env
+    most = 131072
+    one = lambda *s: torch.ones(s, device="cuda")  # noqa: E731
+    q = torch.full((n, L, most), -128, dtype=torch.int8, device="cuda")
+    p = torch.full((N, most), -128, dtype=torch.int8, device="cuda")
+    q[:, 1::5] = 127
+    p[1::3] = 127
+    q[:, 2::5, 99] = -127
+    lengths = torch.full((n,), L, dtype=torch.int32, device="cuda")
+    lengths[0] = L // 2 + 1
+    live = (torch.arange(L, device="cuda")[None, :] < lengths[:, None])[:, :, None]
+    for columns in (most, most - 64):
+        # whole numbers below 2^53 whatever their order
+        kinds = q[0, :3, :columns].double() @ p[:2, :columns].double().t().contiguous()
+        row, col = torch.arange(L, device="cuda") % 5, torch.arange(N, device="cuda") % 3
+        row = torch.where(row > 2, torch.zeros_like(row), row)
+        want = kinds[row.clamp(max=kinds.shape[0] - 1)][:, (col == 1).long().clamp(max=kinds.shape[1] - 1)]
+        y = seq.linear8(q[:, :, :columns].contiguous(), one(n, L), p[:, :columns].contiguous(), one(N), dtype=torch.float32)
+        assert torch.equal(y, want.float().expand(n, L, N))
+        y = seq.linear8(q[:, :, :columns].contiguous(), one(n, L), p[:, :columns].contiguous(), one(N),
+                        dtype=torch.bfloat16, lengths=lengths)
+        assert torch.equal(y, torch.where(live, want.float().bfloat16().expand(n, L, N), 0))
+    assert float(seq.linear8(q[:, :1].contiguous(), one(n, 1), p, one(N), dtype=torch.float32)[0, 0, 0]) == 2.0 ** 31
