@@ -716,9 +716,11 @@ rocket_status rocket_dropout(const void *x, const void *residual, void *y, int64
  *   eps     finite, >= 0
  *   rstd    DEVICE fp32 [n, steps]: k, 0 for steps past a series' length
  * The sum of squares has to be finite in fp32 (values below 2^63 / sqrt C are).
- * y may be x or residual, total may be the other one of them.
+ * y may be x or residual, total may be the other one of them; y and total are two.
+ * Where y is x and there is no residual, what the backward pass reads is gone.
  * Errors: ROCKET_ERR_INVALID_ARG (a NULL pointer, a shape, view, stride, type or
- *         eps outside the above, one of residual and total alone); ROCKET_ERR_HIP.
+ *         eps outside the above, one of residual and total alone, y and total at
+ *         one address); ROCKET_ERR_HIP.
  */
 rocket_status rocket_rms_norm_forward(const rocket_sequence_shape *shape, const rocket_sequence *x,
                                       const rocket_sequence *residual, const float *weight, float eps,

@@ -684,6 +684,7 @@ extern "C" rocket_status rocket_rms_norm_forward(const rocket_sequence_shape *sh
     if (!forward_args(shape, x, residual, weight, eps, total, rstd, a) || !rocket::out_ok(y, shape))
         return ROCKET_ERR_INVALID_ARG;
     if (rocket::empty(shape)) return ROCKET_OK;
+    if (total && total->data == y->data) return ROCKET_ERR_INVALID_ARG;   // one of the two would be lost
     a.y = rocket::view_of(y, shape->dtype);
     View *views[] = {&a.x, &a.r, &a.total, &a.y};
     a.rows = rocket::rows_of(shape, views, 4);

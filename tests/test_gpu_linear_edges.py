@@ -205,3 +205,12 @@ def test_linear8_of_the_largest_sums(env, n, L, N):
                         dtype=torch.bfloat16, lengths=lengths)
         assert torch.equal(y, torch.where(live, want.float().bfloat16().expand(n, L, N), 0))
     assert float(seq.linear8(q[:, :1].contiguous(), one(n, 1), p, one(N), dtype=torch.float32)[0, 0, 0]) == 2.0 ** 31
+
+
+def test_a_norm_and_its_sum_in_one_tensor_are_refused(env):
+    from paper_2601_17091_amd.rocket import RocketError
+    torch, seq = env
+    x, r = torch.randn(3, 5, 8, device="cuda"), torch.randn(3, 5, 8, device="cuda")
+    for t in (torch.empty_like(x), x, r):
+        with pytest.raises(RocketError):
+            seq.rms_norm(x, residual=r, out=t, total_out=t)
