@@ -495,8 +495,9 @@ def _norm_operands(x, weight, residual, lengths, total_out):
 
 def rms_norm(x, weight=None, *, residual=None, eps: float = 1e-5, lengths=None, out=None, total_out=None, stream=None):
     """rocket_rms_norm_forward: (y, total, rstd [n, steps] or [rows]); total is
-    x + residual as it was normalised (x itself without a residual).  `out` takes
-    y and `total_out` the sum (they may be x and residual, either way round)."""
+    x + residual as it was normalised (x itself without a residual, None where `out`
+    then takes x's place).  `out` takes y and `total_out` the sum (they may be x and
+    residual, either way round)."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return rms_norm(x, weight, residual=residual, eps=eps, lengths=lengths, out=out, total_out=total_out)
@@ -509,6 +510,8 @@ def rms_norm(x, weight=None, *, residual=None, eps: float = 1e-5, lengths=None, 
     if out is None:
         out = _dense(x)
     total = x if residual is None else _dense(x) if total_out is None else total_out
+    if given and residual is None and out.data_ptr() == x.data_ptr():
+        total = None   # written over: nothing is left for the backward pass
     rstd = _empty(*x.shape[:-1], dtype=_f32, device=x.device)
     status = lib.rocket_rms_norm_forward(
         _byref(shape), _byref(_rows_view(x, "x")), _optional_rows(residual, "residual"), w, eps,

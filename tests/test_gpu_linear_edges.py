@@ -214,3 +214,27 @@ def test_a_norm_and_its_sum_in_one_tensor_are_refused(env):
     for t in (torch.empty_like(x), x, r):
         with pytest.raises(RocketError):
             seq.rms_norm(x, residual=r, out=t, total_out=t)
+
+
+def test_a_norm_in_place_gives_no_sum(env):
+    """x is written over, so that it is not what was normalised; the gradient's call says so."""
+    torch, seq = env
+    x = torch.randn(3, 5, 8, device="cuda")
+    want, total, rstd = seq.rms_norm(x)
+    assert total is x
+    for view in (x.clone(), x.clone().view(15, 8)):
+        for out in (view, view.view(view.shape)):
+            kept = view.clone()
+            y, total, k = seq.rms_norm(view, out=out)
+            assert y is out and total is None and torch.equal(y.view(3, 5, 8), want) and torch.equal(k.view(3, 5), rstd)
+            with pytest.raises(TypeError):
+                seq.rms_norm_backward(y, total, k)
+            view.copy_(kept)
+    # with a residual the sum has a place of its own
+    r = torch.randn(3, 5, 8, device="cuda")
+    y, total, _ = seq.rms_norm(x.clone(), residual=r)
+    z = x.clone()
+    y2, total2, _ = seq.rms_norm(z, residual=r, out=z)
+    assert torch.equal(y, y2) and torch.equal(total, total2)
+    empty = torch.empty(0, 5, 8, device="cuda")
+    assert seq.rms_norm(empty)[1] is empty
