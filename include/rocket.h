@@ -786,7 +786,9 @@ rocket_status rocket_rms_norm_workspace(const rocket_sequence_shape *shape, int6
  *                 8-bit rows of the weights
  *   bias          DEVICE fp32 [channels], or NULL: 0
  * q and weight are 16-byte aligned.  scale of steps past a series' length is not
- * looked at; y there is 0.
+ * looked at; y there is 0.  scale weight_scale is rounded to fp32 before the sum comes
+ * to it: it has to be within fp32's normal range, or 0, or NaN (past the largest value
+ * a sum of 0 would give NaN).
  * Errors: ROCKET_ERR_INVALID_ARG (as above, or a workspace too small); ROCKET_ERR_HIP.
  */
 rocket_status rocket_linear_bytes(const rocket_sequence_shape *shape, int64_t columns, const int8_t *q,
