@@ -796,7 +796,8 @@ rocket_status rocket_linear_bytes(const rocket_sequence_shape *shape, int64_t co
                              const float *bias, const rocket_sequence *y, void *workspace,
                              int64_t workspace_bytes, void *hip_stream);
 
-/* Its workspace for this shape of y and these columns.  Host only.
+/* Its workspace for this shape of y and these columns, with lengths or without (the
+ * same: the list of rows that a large ragged call makes).  Host only.
  * Errors: ROCKET_ERR_INVALID_ARG (bytes NULL, a shape or columns outside the above). */
 rocket_status rocket_linear_bytes_workspace(const rocket_sequence_shape *shape, int64_t columns, int64_t *bytes);
 

@@ -9,11 +9,13 @@
 // Bound: few rows by reading the weights, many by the matrix unit (2,440 TOP/s in a
 // library's product of 8,192) and its clock, which falls to 2.0 GHz and below under it.
 // Measured, bf16 results where nothing else is said:
-//   64 rows, 2,000 by 1,536 channels           7.5 us (a row by 192 channels: 4.1)
-//   64 x 1000 rows, 2,000 by 1,536             212 us, 1,850 TOP/s (1,900 of the padded
-//                                              columns); without writing results 170
-//   777 x 129 rows, half of them empty, 924 by 993, fp16    98 to 120 us, by whether
-//                                              the tiles take three or four rounds
+//   64 rows, 2,000 by 1,536 channels           7.6 us (a row by 192 channels: 3.9)
+//   64 x 1000 rows, 2,000 by 1,536             211 to 225 us by the card, 1,750 to 1,860
+//                                              TOP/s; without writing results 170
+//   777 x 129 rows, half of them empty, 924 by 993, fp16    94 to 117 us, by how far the
+//                                              tiles fill their three or four rounds, where
+//                                              the 199 MB of results are in the last-level
+//                                              cache already; 142 to 150 where they are not
 #include <algorithm>
 
 #include "rows.h"
@@ -152,8 +154,8 @@ __device__ inline int taken(int sum) {
 // a tile less.  A row's place in q is looked up two tiles ahead, since the next tile's
 // stages are on their way when this one's results are written; so a tile must have as
 // many stages as there are slots.  777 series of up to 129 steps, half of the rows, of
-// 960 columns by 993 channels: 111 us, and 172 where empty rows are multiplied like the
-// others; where all rows hold data the list costs 6 us.
+// 960 columns by 993 channels, into one place: 111 us, and 172 where empty rows are
+// multiplied like the others; where all rows hold data the list costs 6 us.
 template <int DT, bool SPLIT, bool LIVE, int MT, int NT, int WM, int WT, int COLS, int SLOTS, int AT_ONCE>
 __global__ __launch_bounds__(64 * WM * WT, AT_ONCE) void tile_kernel(ProductArgs a) {
     constexpr int kWaves = WM * WT, kThreads = 64 * kWaves, kM = 32 * MT * WM, kT = 32 * NT * WT, kSlots = SLOTS;

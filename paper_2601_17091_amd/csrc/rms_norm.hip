@@ -17,7 +17,7 @@
 //   s and y of x and a residual, 500 x 1000 x 256   178 us, 5.75 TB/s
 //   y of x, 2048 x 20000 fp32                        65 us, 5.0 TB/s
 //   dx and dw of dy, s and ds, 1000 x 1000 x 256    386 us, 5.3 TB/s
-//   the same without ds, 100 x 1000 x 2000          240 us, 5.0 TB/s
+//   the same without ds, 100 x 1000 x 2000          240 to 245 us, 5.0 TB/s
 #include <algorithm>
 
 #include "rows.h"

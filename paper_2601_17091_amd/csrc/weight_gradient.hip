@@ -8,16 +8,19 @@
 // sum of three bf16 parts), and the matrix unit sums their products in fp32.
 //
 // Bound: the matrix unit, 2 rows m c operations.  Many rows: tiles of 256 x 256 whose
-// stages are on their way while others are read (staged_kernel); what is left is its
-// clock: with the unit 46 % busy it falls to 2.0 to 2.1 GHz, and a whole version that
-// does not widen q takes 394 of 440 us, one that loads nothing 337.  Few rows: tiles of
+// stages are on their way while others are read (staged_kernel).  The unit is busy for
+// 46 % of the cycles at 2.0 to 2.1 GHz and wavefronts wait for 31 % of theirs; memory is
+// no bound (3.2 GB read from L2, of which 84 % are there).  Whole versions that do not
+// widen q or load nothing took 394 and 337 of 440 us: two wavefronts a SIMD do not cover
+// loads, widening and barriers with the other's products.  Few rows: tiles of
 // 64 x 64 straight from registers (gradient_kernel).  The rows are shared out where the
 // tiles do not fill the chip, and the parts' sums joined in a fixed order.
-// Measured:
-//   64 x 1000 rows bf16, 1,536 by 2,000     410 us, 960 TFLOP/s
-//   777 x 129 rows fp16, 993 by 924         262 us: 66 to lay out dy, whose rows have odd
-//                                           places, 190 the product, 6 the join
-//   64 rows fp32, 192 by 2,000              5.3 us
+// Measured (the same call differs by 6 % between cards):
+//   64 x 1000 rows bf16, 1,536 by 2,000     405 to 430 us, 915 to 970 TFLOP/s
+//   777 x 129 rows fp16, 993 by 924         263 to 275 us: 66 to lay out dy, whose rows have
+//                                           odd places, 190 to 204 the product, 6 the join
+//   20 x 1000 rows fp32, 768 by 2,000       232 to 238 us
+//   64 rows fp32, 192 by 2,000              5.2 us
 #include <algorithm>
 #include <type_traits>
 
