@@ -483,6 +483,9 @@ __global__ __launch_bounds__(64 * WM * WC) void staged_kernel(StagedArgs a) {
             }
             anew = __any(far);
             if (anew) {
+                // the matrix unit's last results are there before `zeroed`, which the compiler
+                // does not see writing their registers, writes them
+                asm volatile("s_nop 15\n\ts_nop 15");
                 put(begun, std::bool_constant<PLANES == 1>());
                 begun = true;
 #pragma unroll
